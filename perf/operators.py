@@ -407,12 +407,11 @@ def _own(s):
             clip_high=0.25, kl_weight=0.04, temperature=case["temperature"])
         return {"loss": loss, "losses": losses, "logp": logp, "d_logits": d_logits}
     if op == "preference":
-        logp, lse = S.sched_token_logprobs(s["logits"], s["tokens"],
-                                           temperature=case["temperature"])
+        logp = S.sched_token_logprobs(s["logits"], s["tokens"], temperature=case["temperature"])
         loss, margins, d_logp = S.sched_preference_loss(logp, s["ref_logp"], s["tokens"],
                                                         s["offsets"], beta=0.1,
                                                         smoothing=case["smoothing"])
-        d_logits = S.sched_token_logprobs_grad(s["logits"], s["tokens"], lse, d_logp,
+        d_logits = S.sched_token_logprobs_grad(s["logits"], s["tokens"], logp, d_logp,
                                                temperature=case["temperature"])
         return {"loss": loss, "margins": margins, "logp": logp, "d_logp": d_logp,
                 "d_logits": d_logits}
