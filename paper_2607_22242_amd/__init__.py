@@ -1,7 +1,9 @@
 """Brute-force device-mapping search on MI355X (HIP for gfx950).
 
 The search itself lives in libsched.so (C ABI declared in
-include/sched_search.h); `binding` marshals arguments to it.
+include/sched_search.h); `binding` marshals arguments to it.  `policy` does the
+same for the operators of an agent that proposes mappings
+(include/sched_policy.h).
 """
 from .binding import (  # noqa: F401
     EXPORTED, INFEASIBLE, NO_INDEX, Monitor, Problem, SchedError, sched_bruteforce_argmin,
@@ -14,3 +16,7 @@ from .binding import (  # noqa: F401
     sched_monitor_observe, sched_problem_destroy, sched_pruned_argmin,
     sched_pruned_workspace_bytes, pruned_workspace, sched_strerror, sched_valu_probe,
     sched_wave_or_probe, sched_workspace_bytes, workspace)
+from .policy import (  # noqa: F401
+    POLICY_EXPORTED, sched_attention, sched_attention_grad, sched_embed, sched_embed_grad,
+    sched_group_advantages, sched_policy_loss, sched_preference_loss, sched_token_logprobs,
+    sched_token_logprobs_grad)

@@ -16,7 +16,8 @@ INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 # the longest to compile first, so that they fill the compiler jobs evenly.
 UNITS = [("inst.hip", [f"-DINST_N={n}"]) for n in range(40, 0, -1)] + [
     ("api.cpp", []), ("monitor.cpp", []), ("dispatch.hip", []), ("probe.hip", []),
-    ("scratch.hip", []), ("closed.hip", [])]
+    ("scratch.hip", []), ("closed.hip", []), ("attend_grad.hip", []), ("attend.hip", []),
+    ("rows.hip", []), ("embed.hip", []), ("policy_api.cpp", [])]
 ARCH = "gfx950"
 
 

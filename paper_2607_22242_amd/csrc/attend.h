@@ -1,0 +1,165 @@
+// attend.h -- what the attention kernels share: products of 32 x 32 tiles,
+// tiles in LDS, and where a block's rows lie in the packed tensors.
+//
+// One product of 16-bit operands takes A (32 x 16) and B (16 x 32) to C (32 x
+// 32): lane l holds row (A) or column (B) l % 32 of the operands, elements
+// 8 (l / 32) .. + 7 along the contraction, and of C column l % 32, rows
+// 8 (i / 4) + 4 (l / 32) + i % 4 for i = 0 .. 15.
+//
+// Scores are computed so that a lane's column is what its statistics belong to
+// and its 16 values run along the axis that the next product contracts.  That
+// product's B is then the lane's own values, eight at a time, if its A lists
+// the contraction in the same order: lane half h has 16 s + 4 h + {0 .. 3} and
+// 16 s + 8 + 4 h + {0 .. 3} in step s.  Nothing moves between lanes.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "sched_policy.h"
+#include "tensors.h"
+
+namespace policy {
+
+typedef float Acc __attribute__((ext_vector_type(16)));
+
+template <class T>
+struct Frag {
+  typedef T type __attribute__((ext_vector_type(8)));
+};
+
+__device__ __forceinline__ Acc product(Frag<bf16>::type a, Frag<bf16>::type b, Acc c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ Acc product(Frag<f16>::type a, Frag<f16>::type b, Acc c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+
+struct HeadsView {
+  char* data;
+  int64_t row, head;  // strides in elements
+};
+
+struct AttendArgs {
+  HeadsView q, k, v, out, d_out, d_q, d_k, d_v;
+  float* lse;
+  float* delta;
+  const int32_t *q_offsets, *k_offsets, *k_lengths;
+  int32_t n_seqs, q_rows, k_rows, q_heads, group, dim, causal;
+  float scale;
+};
+
+template <class T>
+__device__ __forceinline__ T* head_row(const HeadsView& x, int64_t row, int head) {
+  return reinterpret_cast<T*>(x.data) + row * x.row + int64_t(head) * x.head;
+}
+
+// A sequence: where its queries and keys begin, and how many there are; slot
+// counts the key rows that it owns, keys those in use.
+struct Seq {
+  int q0, k0, queries, keys, slot;
+};
+__device__ __forceinline__ Seq sequence(const AttendArgs& a, int b) {
+  Seq s;
+  s.q0 = offset_at(a.q_offsets, b, a.q_rows);
+  s.k0 = offset_at(a.k_offsets, b, a.k_rows);
+  s.queries = max(0, offset_at(a.q_offsets, b + 1, a.q_rows) - s.q0);
+  s.slot = max(0, offset_at(a.k_offsets, b + 1, a.k_rows) - s.k0);
+  s.keys = a.k_lengths ? min(s.slot, max(0, a.k_lengths[b])) : s.slot;
+  return s;
+}
+
+// Tiles of `tile` rows without a list of them: sequence b begins at tile
+// number offset / tile + b, which leaves it as many numbers as it has tiles or
+// one more.  Returns the sequence of a number and the tile within it, which may
+// lie behind the sequence's last or, before the first sequence, be negative.
+struct Tile {
+  int seq, index;
+};
+__device__ __forceinline__ Tile tile_of(const int32_t* offsets, int n_seqs, int rows, int group,
+                                        int tile, int number) {
+  int lo = 0, hi = n_seqs;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (offset_at(offsets, mid, rows) * group / tile + mid <= number) lo = mid;
+    else hi = mid;
+  }
+  return {lo, number - (offset_at(offsets, lo, rows) * group / tile + lo)};
+}
+
+inline int64_t tile_count(int64_t rows, int n_seqs, int tile) { return rows / tile + n_seqs; }
+
+// Query rows of a block: the heads that share a key head are rows of their own,
+// row r being query r / group and head r % group of the key head's.
+struct QueryRow {
+  int query, head;
+};
+__device__ __forceinline__ QueryRow query_row(const AttendArgs& a, int kv_head, int r) {
+  return {r / a.group, kv_head * a.group + r % a.group};
+}
+
+// 16 bytes of a row, zeros behind the head's last element.
+template <class T>
+__device__ __forceinline__ typename Frag<T>::type piece(const T* row, int d, int dim, bool on) {
+  typename Frag<T>::type v = T(0);
+  if (on && d < dim) v = *reinterpret_cast<const typename Frag<T>::type*>(row + d);
+  return v;
+}
+
+// A tile in LDS: rows of D elements and 16 bytes, which spreads the rows'
+// pieces over the banks.
+template <class T, int D>
+struct Rows {
+  static constexpr int kStride = D + 8;
+  T* at;
+
+  // A or B along the rows: lane l has row l % 32 of the 32 from `row`, elements
+  // 16 k + 8 (l / 32) .. + 7.
+  __device__ __forceinline__ typename Frag<T>::type along(int row, int k) const {
+    const int l = int(threadIdx.x) % kWave;
+    return *reinterpret_cast<const typename Frag<T>::type*>(at + (row + l % 32) * kStride + 16 * k +
+                                                            8 * (l / 32));
+  }
+  // A across the rows: lane l has column 32 c + l % 32 of the rows row + 4 h +
+  // {0..3} and row + 8 + 4 h + {0..3}, h = l / 32.
+  __device__ __forceinline__ typename Frag<T>::type across(int row, int c) const {
+    const int l = int(threadIdx.x) % kWave;
+    typename Frag<T>::type v;
+    const T* p = at + (row + 4 * (l / 32)) * kStride + 32 * c + l % 32;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = p[(e / 4 * 8 + e % 4) * kStride];
+    return v;
+  }
+};
+
+template <class T>
+__device__ __forceinline__ typename Frag<T>::type narrow(const Acc& x, int s) {
+  typename Frag<T>::type v;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = T(x[8 * s + e]);
+  return v;
+}
+
+// Row of C that element i of lane l holds.
+__device__ __forceinline__ int c_row(int i) {
+  return 8 * (i / 4) + 4 * (int(threadIdx.x) % kWave / 32) + i % 4;
+}
+
+// A lane's column of C tiles (D / 32 of them, rows being the head's elements)
+// times f, to a row in memory.
+template <class T, int D>
+__device__ __forceinline__ void store_column(T* row, const Acc (&x)[D / 32], int dim, float f) {
+  typedef T four __attribute__((ext_vector_type(4)));
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      const int d = 32 * c + c_row(i);
+      if (d < dim) {
+        four v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = T(x[c][i + e] * f);
+        *reinterpret_cast<four*>(row + d) = v;
+      }
+    }
+}
+
+}  // namespace policy

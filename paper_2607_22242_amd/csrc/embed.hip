@@ -1,0 +1,499 @@
+// embed.hip -- embedding lookup with scaling, and its gradient by sorted tokens.
+//
+// Lookup: out[i] = scale * table[t_i], a copy of rows.  Gradient: row v of the
+// table gets scale * the sum of d_rows[i] over the i with t_i = v.  The pairs
+// (t_i, i) are sorted by token, stable, so that every row's sum runs over one
+// run of the list in the order of i: no atomics on values, one order.  A run
+// may hold one token or all of them; whole chunks of a run are summed first by
+// waves of their own and the row adds their sums.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "policy_launch.h"
+#include "tensors.h"
+
+namespace policy {
+namespace {
+
+constexpr int kBlock = 256;
+constexpr int kDigit = 9;                // bits of a digit at most
+constexpr int kBins = 1 << kDigit;
+constexpr int kSmall = 8192;             // tokens that one block sorts in LDS
+constexpr int kSmallThreads = 1024;
+constexpr int kTile = 4096;              // tokens of a block otherwise
+constexpr int kTileThreads = 512;
+constexpr int kRowsPerBlock = 16;
+
+__device__ __forceinline__ uint64_t below(int lane) { return (1ull << lane) - 1; }
+
+// --- lookup ---------------------------------------------------------------
+
+// `lanes` threads (a power of two up to 256) take a row, in 16-byte pieces.
+template <class T>
+__global__ __launch_bounds__(kBlock) void embed_kernel(const T* table, int64_t vocab, int64_t dim,
+                                                       int64_t stride, Tokens tokens, int64_t n,
+                                                       float scale, T* out, int64_t out_stride,
+                                                       int lanes, int64_t first) {
+  constexpr int N = Vec<T>::kN;
+  const int64_t i = first + int64_t(blockIdx.x) * (kBlock / lanes) + int(threadIdx.x) / lanes;
+  if (i >= n) return;
+  const int64_t t = token_in(tokens, i, vocab);
+  const T* row = table + (t < 0 ? 0 : t) * stride;
+  T* to = out + i * out_stride;
+  for (int64_t j = int64_t(int(threadIdx.x) % lanes) * N; j < dim; j += int64_t(lanes) * N) {
+    if (j + N <= dim) {
+      typename Vec<T>::type v = T(0);
+      if (t >= 0) {
+        v = load16(row + j);
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = T(float(v[k]) * scale);
+      }
+      store16(to + j, v);
+    } else {
+      for (int64_t k = j; k < dim; ++k) to[k] = t < 0 ? T(0) : T(float(row[k]) * scale);
+    }
+  }
+}
+
+// --- sort by token ----------------------------------------------------------
+
+// One digit of a stable sort of the keys of a block, `kRounds` per lane: wave w
+// holds keys w * 64 * kRounds .. in order, round r the r-th 64 of them.  counts
+// (waves x kBins in LDS) ends as each wave's running count per digit; place()
+// is called for every key with its number among the block's keys of its digit.
+template <int kRounds, int kThreads>
+__device__ __forceinline__ void count_digits(const uint32_t (&key)[kRounds], const bool (&on)[kRounds],
+                                             int shift, int bins, uint32_t* counts) {
+  for (int i = int(threadIdx.x); i < bins * (kThreads / kWave); i += kThreads) counts[i] = 0;
+  __syncthreads();
+  uint32_t* mine = counts + int(threadIdx.x) / kWave * bins;
+#pragma unroll
+  for (int r = 0; r < kRounds; ++r)
+    if (on[r]) atomicAdd(&mine[(key[r] >> shift) & (bins - 1)], 1u);
+  __syncthreads();
+}
+
+// Lanes of the wave with this lane's digit, of those taking part.
+__device__ __forceinline__ uint64_t peers_of(uint32_t digit, bool on, int bits) {
+  uint64_t peers = __ballot(on);
+  for (int b = 0; b < bits; ++b) {
+    const uint64_t set = __ballot((digit >> b) & 1);
+    peers &= (digit >> b) & 1 ? set : ~set;
+  }
+  return peers;
+}
+
+// Exclusive sum over 512 or 1024 threads' values.
+template <int kThreads>
+__device__ __forceinline__ uint32_t block_before(uint32_t x, uint32_t* part) {
+  const int lane = int(threadIdx.x) % kWave, wave = int(threadIdx.x) / kWave;
+  uint32_t s = x;
+#pragma unroll
+  for (int d = 1; d < kWave; d <<= 1) {
+    const uint32_t up = __shfl_up(s, d);
+    if (lane >= d) s += up;
+  }
+  if (lane == kWave - 1) part[wave] = s;
+  __syncthreads();
+  uint32_t before = s - x;
+  for (int w = 0; w < wave; ++w) before += part[w];
+  return before;
+}
+
+struct SortArgs {
+  Tokens tokens;
+  uint32_t n, vocab;
+  int bits, passes;  // of a digit, and digits
+  uint32_t *key[2], *at[2];
+  uint32_t* hist;    // blocks x bins
+};
+
+__device__ __forceinline__ uint32_t key_of(const SortArgs& a, uint32_t i) {
+  const int64_t t = token_in(a.tokens, i, a.vocab);
+  return t < 0 ? a.vocab : uint32_t(t);  // padding comes last
+}
+
+// All of n <= kSmall tokens in one block, in LDS.
+__global__ __launch_bounds__(kSmallThreads) void sort_small_kernel(SortArgs a) {
+  constexpr int kRounds = kSmall / kSmallThreads, kWaves = kSmallThreads / kWave;
+  __shared__ uint2 list[kSmall];
+  __shared__ uint32_t counts[kWaves * kBins];
+  __shared__ uint32_t part[kWaves];
+  const int lane = int(threadIdx.x) % kWave, wave = int(threadIdx.x) / kWave, bins = 1 << a.bits;
+  // Waves share the tokens evenly, in whole rounds.
+  const uint32_t span = (a.n + kSmallThreads - 1) / kSmallThreads * kWave;
+  uint32_t key[kRounds], at[kRounds];
+  bool on[kRounds];
+#pragma unroll
+  for (int r = 0; r < kRounds; ++r) {
+    const uint32_t i = uint32_t(wave) * span + uint32_t(r * kWave + lane);
+    on[r] = uint32_t(r * kWave) < span && i < a.n;
+    key[r] = on[r] ? key_of(a, i) : 0;
+    at[r] = i;
+  }
+  for (int p = 0; p < a.passes; ++p) {
+    const int shift = p * a.bits;
+    count_digits<kRounds, kSmallThreads>(key, on, shift, bins, counts);
+    uint32_t total = 0;
+    if (int(threadIdx.x) < bins)
+      for (int w = 0; w < kWaves; ++w) {
+        const uint32_t c = counts[w * bins + threadIdx.x];
+        counts[w * bins + threadIdx.x] = total;
+        total += c;
+      }
+    const uint32_t before = block_before<kSmallThreads>(total, part);
+    if (int(threadIdx.x) < bins)
+      for (int w = 0; w < kWaves; ++w) counts[w * bins + threadIdx.x] += before;
+    __syncthreads();
+    volatile uint32_t* mine = counts + wave * bins;
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+      const uint32_t digit = (key[r] >> shift) & uint32_t(bins - 1);
+      const uint64_t peers = peers_of(digit, on[r], a.bits);
+      uint32_t base = 0;
+      if (on[r]) base = mine[digit];
+      __builtin_amdgcn_wave_barrier();
+      if (on[r]) {
+        list[base + uint32_t(__popcll(peers & below(lane)))] = {key[r], at[r]};
+        if ((peers >> lane) == 1) mine[digit] = base + uint32_t(__popcll(peers));
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r)
+      if (on[r]) {
+        const uint2 e = list[uint32_t(wave) * span + uint32_t(r * kWave + lane)];
+        key[r] = e.x;
+        at[r] = e.y;
+      }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int r = 0; r < kRounds; ++r)
+    if (on[r]) {
+      const uint32_t i = uint32_t(wave) * span + uint32_t(r * kWave + lane);
+      a.key[0][i] = key[r];
+      a.at[0][i] = at[r];
+    }
+}
+
+// Longer lists, a digit at a time: every block's count of each digit, then
+// each block's keys to their places.
+__global__ __launch_bounds__(kTileThreads) void sort_count_kernel(SortArgs a, int p) {
+  __shared__ uint32_t counts[kBins];
+  const int bins = 1 << a.bits;
+  for (int i = int(threadIdx.x); i < bins; i += kTileThreads) counts[i] = 0;
+  __syncthreads();
+  const uint32_t first = blockIdx.x * uint32_t(kTile);
+  for (uint32_t i = first + threadIdx.x; i < first + kTile && i < a.n; i += kTileThreads) {
+    const uint32_t key = p == 0 ? key_of(a, i) : a.key[(p - 1) & 1][i];
+    atomicAdd(&counts[(key >> (p * a.bits)) & uint32_t(bins - 1)], 1u);
+  }
+  __syncthreads();
+  for (int i = int(threadIdx.x); i < bins; i += kTileThreads)
+    a.hist[blockIdx.x * uint32_t(bins) + i] = counts[i];
+}
+
+__global__ __launch_bounds__(kTileThreads) void sort_place_kernel(SortArgs a, int p) {
+  constexpr int kRounds = kTile / kTileThreads, kWaves = kTileThreads / kWave;
+  static_assert(kBins <= kTileThreads, "a thread per digit");
+  __shared__ uint32_t counts[kWaves * kBins];
+  __shared__ uint32_t part[kWaves];
+  const int lane = int(threadIdx.x) % kWave, wave = int(threadIdx.x) / kWave, bins = 1 << a.bits;
+  const int shift = p * a.bits;
+  uint32_t key[kRounds], at[kRounds];
+  bool on[kRounds];
+#pragma unroll
+  for (int r = 0; r < kRounds; ++r) {
+    const uint32_t i = blockIdx.x * uint32_t(kTile) + uint32_t((wave * kRounds + r) * kWave + lane);
+    on[r] = i < a.n;
+    key[r] = !on[r] ? 0 : p == 0 ? key_of(a, i) : a.key[(p - 1) & 1][i];
+    at[r] = !on[r] ? 0 : p == 0 ? i : a.at[(p - 1) & 1][i];
+  }
+  count_digits<kRounds, kTileThreads>(key, on, shift, bins, counts);
+  // This block's first place of each digit: keys of lower digits, and of the
+  // same digit in earlier blocks.
+  uint32_t total = 0, earlier = 0;
+  if (int(threadIdx.x) < bins)
+    for (uint32_t b = 0; b < gridDim.x; ++b) {
+      const uint32_t c = a.hist[b * uint32_t(bins) + threadIdx.x];
+      total += c;
+      earlier += b < blockIdx.x ? c : 0;
+    }
+  uint32_t before = block_before<kTileThreads>(total, part) + earlier;
+  if (int(threadIdx.x) < bins)
+    for (int w = 0; w < kWaves; ++w) {
+      const uint32_t c = counts[w * bins + threadIdx.x];
+      counts[w * bins + threadIdx.x] = before;
+      before += c;
+    }
+  __syncthreads();
+  volatile uint32_t* mine = counts + wave * bins;
+  uint32_t *to_key = a.key[p & 1], *to_at = a.at[p & 1];
+#pragma unroll
+  for (int r = 0; r < kRounds; ++r) {
+    const uint32_t digit = (key[r] >> shift) & uint32_t(bins - 1);
+    const uint64_t peers = peers_of(digit, on[r], a.bits);
+    uint32_t base = 0;
+    if (on[r]) base = mine[digit];
+    __builtin_amdgcn_wave_barrier();
+    if (on[r]) {
+      const uint32_t to = base + uint32_t(__popcll(peers & below(lane)));
+      to_key[to] = key[r];
+      to_at[to] = at[r];
+      if ((peers >> lane) == 1) mine[digit] = base + uint32_t(__popcll(peers));
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// --- sums over runs ---------------------------------------------------------
+
+struct SumArgs {
+  const void* d_rows;
+  int64_t row_stride, dim, vocab;
+  const uint32_t *key, *at;  // sorted
+  uint32_t n, chunk;
+  float* partial;            // n / chunk rows of dim
+  float scale;
+  void* table;
+  int64_t table_stride;
+  int lanes;                 // of a row's piece: a power of two up to 64
+  int64_t first;             // row of the table that the launch starts with
+};
+
+// Sum of rows in the order of the list, by a wave: 64 / lanes entries at once,
+// 16-byte pieces; the groups' sums are added in one order at the end.
+template <class T>
+__device__ __forceinline__ void add_rows(const SumArgs& a, uint32_t b, uint32_t e, int64_t j,
+                                         float (&acc)[Vec<T>::kN]) {
+  constexpr int N = Vec<T>::kN;
+  const int lane = int(threadIdx.x) % kWave, groups = kWave / a.lanes;
+  const T* rows = static_cast<const T*>(a.d_rows);
+  for (uint32_t i = b + uint32_t(lane / a.lanes); i < e; i += uint32_t(groups)) {
+    const T* row = rows + int64_t(a.at[i]) * a.row_stride + j;
+    if (j + N <= a.dim) {
+      const typename Vec<T>::type v = load16(row);
+#pragma unroll
+      for (int k = 0; k < N; ++k) acc[k] += float(v[k]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < N; ++k)
+        if (j + k < a.dim) acc[k] += float(row[k]);
+    }
+  }
+}
+
+template <int N>
+__device__ __forceinline__ void join_groups(const SumArgs& a, float (&acc)[N]) {
+  for (int d = a.lanes; d < kWave; d <<= 1)
+#pragma unroll
+    for (int k = 0; k < N; ++k) acc[k] += __shfl_xor(acc[k], d);
+}
+
+// Chunks of the list that hold one token only (parts of long runs).
+template <class T>
+__global__ __launch_bounds__(kBlock) void chunk_kernel(SumArgs a) {
+  constexpr int N = Vec<T>::kN;
+  const uint32_t c = blockIdx.x * (kBlock / kWave) + threadIdx.x / kWave;
+  if (c >= a.n / a.chunk) return;
+  const uint32_t b = c * a.chunk, e = b + a.chunk, v = a.key[b];
+  if (v != a.key[e - 1] || v >= uint32_t(a.vocab)) return;
+  const int lane = int(threadIdx.x) % kWave;
+  const int64_t j = (int64_t(blockIdx.y) * a.lanes + lane % a.lanes) * N;
+  float acc[N] = {};
+  if (j < a.dim) add_rows<T>(a, b, e, j, acc);
+  join_groups(a, acc);
+  if (lane < a.lanes)
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if (j + k < a.dim) a.partial[int64_t(c) * a.dim + j + k] = acc[k];
+}
+
+// First place of the sorted list whose token is at least v.
+__device__ __forceinline__ uint32_t place_of(const uint32_t* key, uint32_t n, uint32_t v) {
+  uint32_t lo = 0, hi = n;
+  while (lo < hi) {
+    const uint32_t mid = lo + (hi - lo) / 2;
+    if (key[mid] < v) lo = mid + 1;
+    else hi = mid;
+  }
+  return lo;
+}
+
+// Rows of the table, one wave each in turn: the entries before the first whole
+// chunk of the run, the chunks' sums, the entries behind the last.
+template <class T, class O, bool kAdd>
+__global__ __launch_bounds__(kBlock) void table_kernel(SumArgs a) {
+  constexpr int N = Vec<T>::kN;
+  constexpr int kPer = kRowsPerBlock / (kBlock / kWave);
+  const int lane = int(threadIdx.x) % kWave;
+  const int64_t v0 = a.first + int64_t(blockIdx.x) * kRowsPerBlock + int(threadIdx.x) / kWave * kPer;
+  const uint32_t mine = place_of(a.key, a.n, uint32_t(v0 + (lane < kPer ? lane : kPer)));
+  const int64_t j = (int64_t(blockIdx.y) * a.lanes + lane % a.lanes) * N;
+  const int group = lane / a.lanes, groups = kWave / a.lanes;
+  for (int r = 0; r < kPer && v0 + r < a.vocab; ++r) {
+    const uint32_t s = __shfl(mine, r), e = __shfl(mine, r + 1);
+    if (kAdd && s == e) continue;
+    float acc[N] = {};
+    const uint32_t c0 = (s + a.chunk - 1) / a.chunk, c1 = e / a.chunk;
+    if (j < a.dim) {
+      if (c1 > c0) {
+        add_rows<T>(a, s, c0 * a.chunk, j, acc);
+        for (uint32_t c = c0 + uint32_t(group); c < c1; c += uint32_t(groups))
+#pragma unroll
+          for (int k = 0; k < N; ++k)
+            if (j + k < a.dim) acc[k] += a.partial[int64_t(c) * a.dim + j + k];
+        add_rows<T>(a, c1 * a.chunk, e, j, acc);
+      } else {
+        add_rows<T>(a, s, e, j, acc);
+      }
+    }
+    join_groups(a, acc);
+    O* to = static_cast<O*>(a.table) + (v0 + r) * a.table_stride + j;
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if (lane < a.lanes && j + k < a.dim)
+        to[k] = O((kAdd ? float(to[k]) : 0.f) + acc[k] * a.scale);
+  }
+}
+
+int lanes_for(int64_t pieces, int most) {
+  int l = 1;
+  while (l < most && l < pieces) l *= 2;
+  return l;
+}
+
+uint32_t chunk_for(int64_t n) {
+  uint32_t c = 64;
+  while (n / c > 4096) c *= 2;
+  return c;
+}
+
+size_t up(size_t x) { return (x + 255) & ~size_t(255); }
+
+uint32_t tiles_for(int64_t n) { return uint32_t((n + kTile - 1) / kTile); }
+
+template <class T>
+hipError_t embed_of(const sched_matrix& table, const sched_tokens& tokens, float scale,
+                    const sched_matrix& out, hipStream_t s) {
+  const int lanes = lanes_for((table.cols + Vec<T>::kN - 1) / Vec<T>::kN, kBlock);
+  const int64_t blocks = (tokens.n + kBlock / lanes - 1) / (kBlock / lanes);
+  hipError_t e = hipSuccess;
+  for (int64_t b = 0; b < blocks && e == hipSuccess; b += kMostBlocks) {
+    hipLaunchKernelGGL(embed_kernel<T>, dim3(unsigned(std::min(blocks - b, kMostBlocks))),
+                       dim3(kBlock), 0, s, static_cast<const T*>(table.data), table.rows,
+                       table.cols, table.stride, Tokens{tokens.data, tokens.bits == 64}, tokens.n,
+                       scale, static_cast<T*>(out.data), out.stride, lanes, b * (kBlock / lanes));
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+template <class T, class O>
+hipError_t sums_of(const SumArgs& in, bool accumulate, hipStream_t s) {
+  SumArgs a = in;
+  const int64_t pieces = (a.dim + Vec<T>::kN - 1) / Vec<T>::kN;
+  a.lanes = lanes_for(pieces, kWave);
+  const unsigned tiles = unsigned((pieces + a.lanes - 1) / a.lanes);
+  if (const uint32_t chunks = a.n / a.chunk) {
+    hipLaunchKernelGGL(chunk_kernel<T>, dim3((chunks + 3) / 4, tiles), dim3(kBlock), 0, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  const int64_t blocks = (a.vocab + kRowsPerBlock - 1) / kRowsPerBlock;
+  hipError_t e = hipSuccess;
+  for (int64_t b = 0; b < blocks && e == hipSuccess; b += kMostBlocks) {
+    a.first = b * kRowsPerBlock;
+    const dim3 grid(unsigned(std::min(blocks - b, kMostBlocks)), tiles);
+    if (accumulate)
+      hipLaunchKernelGGL((table_kernel<T, O, true>), grid, dim3(kBlock), 0, s, a);
+    else
+      hipLaunchKernelGGL((table_kernel<T, O, false>), grid, dim3(kBlock), 0, s, a);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+template <class T>
+hipError_t sums_to(const SumArgs& a, bool same, bool accumulate, hipStream_t s) {
+  return same ? sums_of<T, T>(a, accumulate, s) : sums_of<T, float>(a, accumulate, s);
+}
+
+}  // namespace
+
+hipError_t launch_embed(const sched_matrix& table, const sched_tokens& tokens, float scale,
+                        const sched_matrix& out, hipStream_t s) {
+  if (tokens.n == 0 || table.cols == 0) return hipSuccess;
+  return table.dtype == SCHED_F32   ? embed_of<float>(table, tokens, scale, out, s)
+         : table.dtype == SCHED_F16 ? embed_of<f16>(table, tokens, scale, out, s)
+                                    : embed_of<bf16>(table, tokens, scale, out, s);
+}
+
+size_t embed_grad_bytes(int64_t n, int64_t dim) {
+  const size_t lists = n <= kSmall ? 2 : 4;
+  return lists * up(size_t(n) * 4) + (n <= kSmall ? 0 : up(size_t(tiles_for(n)) * kBins * 4)) +
+         up(size_t(n / chunk_for(n)) * size_t(dim) * 4);
+}
+
+hipError_t launch_embed_grad(const sched_matrix& d_rows, const sched_tokens& tokens, float scale,
+                             bool accumulate, const sched_matrix& d_table, void* ws,
+                             hipStream_t s) {
+  if (d_table.rows == 0 || d_table.cols == 0) return hipSuccess;
+  SortArgs a = {};
+  a.tokens = {tokens.data, tokens.bits == 64};
+  a.n = uint32_t(tokens.n);
+  a.vocab = uint32_t(d_table.rows);
+  const int width = 32 - __builtin_clz(a.vocab);  // keys are 0 .. vocab
+  a.passes = (width + kDigit - 1) / kDigit;
+  a.bits = (width + a.passes - 1) / a.passes;
+  char* at = static_cast<char*>(ws);
+  auto take = [&](size_t bytes) {
+    char* p = at;
+    at += up(bytes);
+    return p;
+  };
+  int last = 0;
+  a.key[0] = reinterpret_cast<uint32_t*>(take(size_t(a.n) * 4));
+  a.at[0] = reinterpret_cast<uint32_t*>(take(size_t(a.n) * 4));
+  hipError_t e = hipSuccess;
+  if (a.n > uint32_t(kSmall)) {
+    a.key[1] = reinterpret_cast<uint32_t*>(take(size_t(a.n) * 4));
+    a.at[1] = reinterpret_cast<uint32_t*>(take(size_t(a.n) * 4));
+    const uint32_t tiles = tiles_for(a.n);
+    a.hist = reinterpret_cast<uint32_t*>(take(size_t(tiles) * kBins * 4));
+    for (int p = 0; p < a.passes && e == hipSuccess; ++p) {
+      hipLaunchKernelGGL(sort_count_kernel, dim3(tiles), dim3(kTileThreads), 0, s, a, p);
+      e = hipGetLastError();
+      if (e != hipSuccess) break;
+      hipLaunchKernelGGL(sort_place_kernel, dim3(tiles), dim3(kTileThreads), 0, s, a, p);
+      e = hipGetLastError();
+    }
+    last = (a.passes - 1) & 1;
+  } else if (a.n > 0) {
+    hipLaunchKernelGGL(sort_small_kernel, dim3(1), dim3(kSmallThreads), 0, s, a);
+    e = hipGetLastError();
+  }
+  if (e != hipSuccess) return e;
+  SumArgs b = {};
+  b.d_rows = d_rows.data;
+  b.row_stride = d_rows.stride;
+  b.dim = d_table.cols;
+  b.vocab = d_table.rows;
+  b.key = a.key[last];
+  b.at = a.at[last];
+  b.n = a.n;
+  b.chunk = chunk_for(a.n);
+  b.partial = reinterpret_cast<float*>(at);
+  b.scale = scale;
+  b.table = d_table.data;
+  b.table_stride = d_table.stride;
+  const bool same = d_table.dtype == d_rows.dtype;
+  return d_rows.dtype == SCHED_F32   ? sums_to<float>(b, same, accumulate, s)
+         : d_rows.dtype == SCHED_F16 ? sums_to<f16>(b, same, accumulate, s)
+                                     : sums_to<bf16>(b, same, accumulate, s);
+}
+
+}  // namespace policy

@@ -1,0 +1,560 @@
+"""The operators of include/sched_policy.h against plain 64-bit forms
+(policy64), element by element within the bounds that their roundings give."""
+import math
+import os
+import sys
+
+import pytest
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
+import policy64 as R  # noqa: E402
+
+import paper_2607_22242_amd as S  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+TYPES = [torch.float32, torch.float16, torch.bfloat16]
+HALVES = [torch.float16, torch.bfloat16]
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def randn(g, *shape, dtype=torch.float32):
+    return torch.randn(shape, generator=g).to(dtype)
+
+
+def offsets(lengths):
+    at = [0]
+    for x in lengths:
+        at.append(at[-1] + x)
+    return at
+
+
+def i32(values):
+    return torch.tensor(values, dtype=torch.int32, device="cuda")
+
+
+# --- embedding ---------------------------------------------------------------
+
+
+def draw_tokens(g, n, vocab, dtype=torch.int64):
+    t = torch.randint(0, vocab, (n,), generator=g)
+    t[::7] = t[:1].clone()  # one token in a seventh of the places
+    if n > 5:
+        t[3], t[5] = -1, vocab  # padding
+    return t.to(dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,vocab,dim", [(1, 1, 1), (1, 3, 8), (5, 7, 3), (63, 40, 65), (300, 2, 24),
+                                         (257, 1000, 129), (40, 50021, 512), (130, 9, 1030)])
+def test_embed(dtype, n, vocab, dim):
+    g = gen(n * 7 + vocab + dim)
+    table, tokens = randn(g, vocab, dim, dtype=dtype), draw_tokens(g, n, vocab)
+    out = S.sched_embed(table.cuda(), tokens.cuda(), scale=1.75)
+    want = R.embed(table, tokens, 1.75)
+    R.close(out, want, (R.U[dtype] + 2 * R.F) * want.abs() + R.TINY[dtype])
+    assert out.dtype == dtype
+    same = S.sched_embed(table.cuda(), tokens.to(torch.int32).cuda(), scale=1.75)
+    assert torch.equal(out, same)
+
+
+def check_embed_grad(d_rows, tokens, vocab, scale, out_type=None, acc=None, **kw):
+    want, size, count = R.embed_grad(d_rows, tokens, vocab, scale)
+    out = None
+    if out_type is not None:
+        out = torch.full((vocab, d_rows.shape[1]), float("nan"), dtype=out_type, device="cuda")
+    if acc is not None:
+        out, want = acc.cuda(), want + acc.double()
+    got = S.sched_embed_grad(d_rows.cuda(), tokens.cuda(), vocab, scale=scale, out=out,
+                             accumulate=acc is not None, **kw)
+    steps = 2 * R.F * (count[:, None] + 4)
+    R.close(got, want, steps * size + (R.U[got.dtype] + 2 * R.F) * want.abs() + R.TINY[got.dtype])
+    return got
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,vocab,dim", [(0, 5, 8), (1, 1, 1), (1, 70, 8), (5, 7, 3), (200, 3, 65),
+                                         (1000, 2, 24), (257, 1000, 129), (700, 33, 520),
+                                         (64, 64, 64), (130, 5000, 16)])
+def test_embed_grad(dtype, n, vocab, dim):
+    g = gen(n + 3 * vocab + dim)
+    d_rows, tokens = randn(g, n, dim, dtype=dtype), draw_tokens(g, n, vocab)
+    first = check_embed_grad(d_rows, tokens, vocab, 0.5, out_type=dtype)
+    again = check_embed_grad(d_rows, tokens.to(torch.int32), vocab, 0.5)
+    assert torch.equal(first, again)  # one order of sums
+    check_embed_grad(d_rows, tokens, vocab, 0.5, out_type=torch.float32)
+    check_embed_grad(d_rows, tokens, vocab, 0.5, acc=randn(g, vocab, dim))
+
+
+@pytest.mark.parametrize("n,vocab", [(8191, 600), (8192, 3), (8193, 70000), (20000, 1), (12289, 515),
+                                     (70001, 300000), (9000, 511), (9000, 512)])
+def test_embed_grad_of_long_lists(n, vocab):
+    """One block's sort and the sort in parts, on both sides of the bound; runs
+    of thousands of rows."""
+    g = gen(n)
+    d_rows, tokens = randn(g, n, 4), draw_tokens(g, n, vocab)
+    check_embed_grad(d_rows, tokens, vocab, 1.0)
+
+
+def test_embed_grad_against_differences():
+    g = gen(5)
+    table, tokens = randn(g, 11, 24), draw_tokens(g, 60, 11)
+    w, d = randn(g, 60, 24), randn(g, 11, 24)
+    grad = S.sched_embed_grad(w.cuda(), tokens.cuda(), 11, scale=3.0).cpu().double()
+    f = lambda h: float((R.embed(table.double() + h * d.double(), tokens, 3.0) * w).sum())  # noqa: E731
+    # Linear: what is left is the gradient's rounding in 32 bits, of sums of order 100.
+    assert abs(float((grad * d).sum()) - (f(0.125) - f(-0.125)) * 4) < 1e-3
+
+
+def test_embed_strides_and_empty():
+    g = gen(1)
+    wide = randn(g, 50, 40, dtype=torch.bfloat16).cuda()
+    table = wide[:, 3:36]  # rows apart, 2-byte alignment
+    tokens = draw_tokens(g, 33, 50).cuda()
+    assert torch.equal(S.sched_embed(table, tokens, 2.0), S.sched_embed(table.contiguous(), tokens, 2.0))
+    out = torch.zeros((33, 64), dtype=torch.bfloat16, device="cuda")
+    S.sched_embed(table, tokens, 2.0, out=out[:, 5:38])
+    assert torch.equal(out[:, 5:38], S.sched_embed(table, tokens, 2.0))
+    assert not out[:, :5].any() and not out[:, 38:].any()
+    d = S.sched_embed_grad(out[:, 5:38], tokens, 50)
+    assert torch.equal(d, S.sched_embed_grad(out[:, 5:38].contiguous(), tokens, 50))
+    big = torch.full((50, 40), 7.0, device="cuda")
+    S.sched_embed_grad(out[:, 5:38], tokens, 50, out=big[:, 2:35])
+    assert bool((big[:, :2] == 7).all()) and bool((big[:, 35:] == 7).all())
+    assert S.sched_embed(table, tokens[:0]).shape == (0, 33)
+    assert S.sched_embed(table, tokens[:6].view(2, 3)).shape == (2, 3, 33)
+    none = torch.full((4,), -1, device="cuda")
+    assert not S.sched_embed(table, none).any()
+    assert not S.sched_embed_grad(out[:4], none, 9).any()
+
+
+# --- rows of logits ----------------------------------------------------------
+
+ROWS = [(1, 1), (3, 2), (70, 3), (5, 4), (9, 17), (33, 64), (7, 65), (5, 257), (4, 1000), (3, 4099),
+        (2, 32003), (2, 70001), (1, 131072), (1, 200003)]
+
+
+def draw_rows(g, n, vocab, dtype, wide=4.0):
+    x = (randn(g, n, vocab) * wide).to(dtype)
+    t = torch.randint(0, vocab, (n,), generator=g)
+    if n > 2:
+        t[1] = -1
+    return x, t
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,vocab", ROWS)
+@pytest.mark.parametrize("temperature", [1.0, 0.6])
+def test_logprobs_and_gradient(dtype, n, vocab, temperature):
+    g = gen(n + vocab)
+    x, t = draw_rows(g, n, vocab, dtype)
+    d_logp = randn(g, n)
+    logp, p, on = R.logprobs(x, t, temperature)
+    got = S.sched_token_logprobs(x.cuda(), t.cuda(), temperature=temperature)
+    R.close(got, logp, R.logits_error(x, temperature) + 4 * R.F * logp.abs(), "logp")
+    want, bound = R.d_logits(x, t, p, on, logp, d_logp, temperature)
+    grad = S.sched_token_logprobs_grad(x.cuda(), t.cuda(), got, d_logp.cuda(), temperature=temperature)
+    R.close(grad, want, bound, "d_logits")
+    y = x.cuda()  # in place
+    same = S.sched_token_logprobs_grad(y, t.to(torch.int32).cuda(), got, d_logp.cuda(),
+                                       temperature=temperature, d_logits=y)
+    assert same is y and torch.equal(grad, y)
+
+
+def test_logprobs_gradient_against_differences():
+    g = gen(3)
+    x, t = draw_rows(g, 6, 29, torch.float32)
+    d_logp, d = randn(g, 6), randn(g, 6, 29)
+    logp = S.sched_token_logprobs(x.cuda(), t.cuda(), temperature=0.8)
+    grad = S.sched_token_logprobs_grad(x.cuda(), t.cuda(), logp, d_logp.cuda(), temperature=0.8)
+    f = lambda h: float((R.logprobs(x.double() + h * d.double(), t, 0.8)[0] * d_logp).sum())  # noqa: E731
+    step = 2.0 ** -14  # the third derivative is of order 100: step^2 leaves 1e-6
+    assert abs(float((grad.cpu().double() * d).sum()) - (f(step) - f(-step)) / (2 * step)) < 2e-5
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab", [3, 64, 300, 5003, 66003])
+def test_masked_logits(dtype, vocab):
+    """Masks of -inf and of the type's lowest value, rows that leave nothing,
+    masked tokens, and NaN."""
+    g = gen(vocab)
+    x, _ = draw_rows(g, 8, vocab, dtype)
+    t = torch.zeros(8, dtype=torch.int64)
+    low = torch.finfo(dtype).min
+    x[0, 1:], x[1, 1:] = -math.inf, low   # one entry left
+    x[2], x[3] = -math.inf, low           # nothing left; all the lowest
+    x[4, 0] = -math.inf                   # the token itself is masked
+    x[5, vocab // 2:] = -math.inf
+    x[6, vocab - 1] = math.nan
+    t[5] = vocab // 2 - 1 if vocab > 3 else 0
+    d_logp = torch.ones(8)
+    logp, p, on = R.logprobs(x, t, 1.0)
+    got = S.sched_token_logprobs(x.cuda(), t.cuda())
+    assert float(got[0]) == 0 and float(got[2]) == float(got[4]) == -math.inf
+    assert math.isnan(float(got[6]))
+    R.close(got, logp, R.logits_error(x.nan_to_num(0, 0, 0), 1.0) + 4 * R.F * logp.abs())
+    grad = S.sched_token_logprobs_grad(x.cuda(), t.cuda(), got, d_logp.cuda())
+    keep = [0, 1, 2, 3, 4, 5, 7]
+    want, bound = R.d_logits(x[keep], t[keep], p[keep], on[keep], logp[keep], d_logp[keep], 1.0)
+    R.close(grad[keep], want, bound)
+    assert not grad[2].any() and not grad[4].any()
+    assert bool((grad[5, vocab // 2:] == 0).all())
+    loss, losses, lp, d = S.sched_policy_loss(
+        x.cuda(), t.cuda(), torch.zeros(8).cuda(), torch.zeros(8).cuda(), torch.ones(8).cuda(),
+        torch.ones(8).cuda(), kl_weight=0.1)
+    assert torch.equal(lp[keep], got[keep]) and math.isnan(float(lp[6]))
+    assert not d[2].any() and not d[4].any()
+    assert bool((d[5, vocab // 2:] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,vocab", ROWS)
+@pytest.mark.parametrize("kl", [0.0, 0.05])
+def test_policy_loss(dtype, n, vocab, kl):
+    g = gen(n * 3 + vocab)
+    x, t = draw_rows(g, n, vocab, dtype, 2.0)
+    logp, p, on = R.logprobs(x, t, 1.3)
+    shift = (torch.rand(n, generator=g) - 0.5) * 0.9
+    near = ((torch.exp(shift) - 0.8).abs() < 1e-2) | ((torch.exp(shift) - 1.3).abs() < 1e-2)
+    shift[near] = 0.05  # the gradient jumps at the clip bounds
+    old, ref = (logp - shift).float(), (logp + randn(g, n) * 0.3).float()
+    adv, w = randn(g, n), torch.rand(n, generator=g)
+    args = (t.cuda(), old.cuda(), ref.cuda() if kl else None, adv.cuda(), w.cuda())
+    kw = dict(clip_low=0.2, clip_high=0.3, kl_weight=kl, temperature=1.3, loss_scale=2.5)
+    loss, losses, got, grad = S.sched_policy_loss(x.cuda(), *args, **kw)
+    err = R.logits_error(x, 1.3) + 4 * R.F * logp.abs() + 2 * R.F * (old.abs() + ref.abs())
+    R.close(got, logp, err, "logp")
+    want, slope = R.policy(logp, on, old, ref, adv, w, 0.2, 0.3, kl)
+    # Both loss and slope move by at most (|A| r + kl exp(e)) times the log-probability's error.
+    factor = w * (adv.abs() * 2 + kl * 4)
+    bound = (4 * (err + 8 * R.F) * factor + 4 * R.F * want.abs()).double()
+    R.close(losses, want, bound, "losses")
+    R.close(loss, want.sum().view(1), bound.sum() + 2 * R.F * want.sum().abs(), "loss")
+    d, d_bound = R.d_logits(x, t, p, on, logp, slope * 2.5, 1.3)
+    R.close(grad, d, d_bound + (2.5 * bound / 1.3)[:, None] * torch.where(d == 0, 0.0, 1.0), "d_logits")
+    y = x.cuda()
+    again = S.sched_policy_loss(y, *args, d_logits=y, **kw)
+    assert torch.equal(y, grad) and torch.equal(again[0], loss)
+
+
+def test_logits_with_strides_and_one_value_of_many():
+    g = gen(9)
+    wide = randn(g, 12, 700, dtype=torch.bfloat16).cuda()
+    t = torch.randint(0, 301, (12,), generator=g).cuda()
+    d_logp = torch.ones(12, device="cuda")
+    for x in (wide[:, 5:306], wide[:, 8:309], wide[:1, 3:304].expand(12, 301)):
+        y = x.contiguous()
+        logp = S.sched_token_logprobs(x, t)
+        assert torch.equal(logp, S.sched_token_logprobs(y, t))
+        out = torch.zeros((12, 333), dtype=torch.bfloat16, device="cuda")
+        S.sched_token_logprobs_grad(x, t, logp, d_logp, d_logits=out[:, 7:308])
+        assert torch.equal(out[:, 7:308], S.sched_token_logprobs_grad(y, t, logp, d_logp))
+        assert not out[:, :7].any() and not out[:, 308:].any()
+    none = wide[:0, :300]
+    assert S.sched_token_logprobs(none, t[:0]).shape == (0,)
+    loss = S.sched_policy_loss(none, t[:0], *[d_logp[:0]] * 4)[0]
+    assert float(loss) == 0
+
+
+# --- advantages and pairs ----------------------------------------------------
+
+
+@pytest.mark.parametrize("mean", ["tokens", "sequences"])
+@pytest.mark.parametrize("sizes", [[1], [2, 1, 3], [64] * 5, [70, 1, 130]])
+def test_group_advantages(mean, sizes):
+    g = gen(sum(sizes))
+    n = sum(sizes)
+    lengths = [int(x) for x in torch.randint(0, 90, (n,), generator=g)]
+    lengths[0] = 5
+    off, groups = offsets(lengths), offsets(sizes)
+    tokens = torch.randint(-2, 9, (off[-1],), generator=g)
+    m = torch.randint(1, 1 << 29, (n,), generator=g)
+    m[torch.rand(n, generator=g) < 0.2] = (1 << 63) - 1
+    m[groups[-2]:] = (1 << 63) - 1  # a group without a feasible mapping
+    limits = torch.full((len(sizes),), 1 << 28)
+    adv, w = S.sched_group_advantages(m.cuda(), limits.cuda(), i32(groups), i32(off), tokens.cuda(),
+                                      mean=mean)
+    want, weight = R.advantages(m, limits, groups, off, tokens, mean)
+    R.close(adv, want, 2 * R.F * want.abs() + 1e-12)
+    R.close(w, weight, 2 * R.F * weight)
+
+
+@pytest.mark.parametrize("pairs", [1, 3, 70, 1100])
+@pytest.mark.parametrize("eps", [0.0, 0.2])
+def test_preference_loss(pairs, eps):
+    g = gen(pairs)
+    lengths = [int(x) for x in torch.randint(0, 40, (2 * pairs,), generator=g)]
+    lengths[0], lengths[-1] = 0, 600
+    off = offsets(lengths)
+    n = off[-1]
+    tokens = torch.randint(-1, 9, (n,), generator=g)
+    logp, ref = -torch.rand(n, generator=g) * 5, -torch.rand(n, generator=g) * 5
+    ref[tokens < 0] = math.nan  # padding is not read
+    loss, margins, d = S.sched_preference_loss(logp.cuda(), ref.cuda(), tokens.cuda(), i32(off),
+                                               beta=0.7, smoothing=eps, loss_scale=2.0)
+    want, m, slope = R.preference(logp, ref, tokens, off, 0.7, eps)
+    R.close(margins, m, 2 * R.F * m.abs() + 1e-12)
+    R.close(loss, (2 * want).view(1), 4 * R.F * (want + 1))
+    R.close(d, 2 * slope, 4 * R.F * slope.abs() * (1 + m.abs().max()) + 1e-30)
+    step, dx = 2.0 ** -10, randn(g, n)
+    f = lambda h: float(R.preference(logp.double() + h * dx.double(), ref, tokens, off, 0.7, eps)[0])  # noqa: E731
+    slope_d = float((d.cpu().double() * dx).sum()) / 2
+    # beta^3 times the cube of a pair's sum, up to 30: step^2 leaves 1e-2 of it
+    assert abs(slope_d - (f(step) - f(-step)) / (2 * step)) < 2e-3 * (1 + abs(slope_d))
+
+
+# --- attention ---------------------------------------------------------------
+
+LAYOUTS = [
+    # queries, keys (None: as queries), heads, key heads, dim, causal
+    ([1], None, 1, 1, 8, True),
+    ([5, 0, 1, 33], None, 2, 1, 16, True),
+    ([64, 31, 129], None, 4, 4, 64, True),
+    ([130, 7], None, 6, 2, 40, False),
+    ([200, 3, 70], None, 8, 1, 128, True),
+    ([300], None, 3, 3, 96, True),
+    ([257, 64], None, 4, 2, 120, False),
+    ([10, 40, 5], [0, 7, 90], 4, 2, 80, True),       # fewer keys than queries: rows that see nothing
+    ([10, 40, 5], [0, 7, 300], 2, 2, 128, False),
+    ([1, 1, 1], [1, 700, 33], 8, 2, 128, True),
+    ([2, 3], [513, 1000], 16, 4, 64, True),
+    ([1, 4], [2049, 65], 5, 1, 128, False),
+]
+
+
+def attention_case(dtype, q_len, k_len, heads, kv, dim, seed, spread=1.0):
+    g = gen(seed)
+    k_len = q_len if k_len is None else k_len
+    q = randn(g, sum(q_len), heads, dim, dtype=dtype) * spread
+    k, v = randn(g, sum(k_len), kv, dim, dtype=dtype) * spread, randn(g, sum(k_len), kv, dim, dtype=dtype)
+    return q, k, v, randn(g, sum(q_len), heads, dim, dtype=dtype), offsets(q_len), offsets(k_len)
+
+
+def check_attention(q, k, v, d_out, qo, ko, causal, k_len=None, scale=None, grads=True, views=None):
+    want = R.Attention(q, k, v, qo, ko, k_len, causal, scale or q.shape[2] ** -0.5, d_out)
+    a = views or [t.cuda() for t in (q, k, v)]
+    lens = None if k_len is None else i32(k_len)
+    kw = dict(k_lengths=lens, causal=causal, scale=scale)
+    out, lse = S.sched_attention(*a, i32(qo), i32(ko), **kw)
+    R.close(out, want.out, want.out_b, "out")
+    R.close(lse, want.lse, want.lse_b, "lse")
+    again, _ = S.sched_attention(*a, i32(qo), i32(ko), **kw)
+    assert torch.equal(out, again)
+    if grads:
+        got = S.sched_attention_grad(*a, out, lse, d_out.cuda(), i32(qo), i32(ko), **kw)
+        for name, x, y, b in (("dq", got[0], want.dq, want.dq_b), ("dk", got[1], want.dk, want.dk_b),
+                              ("dv", got[2], want.dv, want.dv_b)):
+            R.close(x, y, b, name)
+        return out, lse, got
+    return out, lse
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("layout", LAYOUTS, ids=lambda x: f"{x[0]}-{x[1]}-{x[2]}-{x[3]}-{x[4]}-{x[5]}")
+def test_attention(dtype, layout):
+    q_len, k_len, heads, kv, dim, causal = layout
+    q, k, v, do, qo, ko = attention_case(dtype, q_len, k_len, heads, kv, dim, sum(q_len) + dim)
+    check_attention(q, k, v, do, qo, ko, causal)
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+def test_attention_of_large_scores(dtype):
+    """Scores of hundreds: one key takes all, others' powers vanish."""
+    q, k, v, do, qo, ko = attention_case(dtype, [90, 70], None, 2, 1, 64, 4, spread=6.0)
+    check_attention(q, k, v, do, qo, ko, True, scale=0.9)
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("lengths,slot,heads,kv,dim", [
+    ([1, 0, 17, 40], 40, 4, 2, 64), ([0, 0], 9, 2, 2, 128), ([700, 33, 64, 65, 1], 700, 8, 1, 128),
+    ([3000], 5000, 16, 8, 96), ([2000, 4097], 4100, 20, 4, 128)])
+def test_attention_over_a_cache(dtype, lengths, slot, heads, kv, dim):
+    """Single tokens over slots whose other rows hold NaN and infinities."""
+    b = len(lengths)
+    q, k, v, do, qo, ko = attention_case(dtype, [1] * b, [slot] * b, heads, kv, dim, slot)
+    for i, n in enumerate(lengths):
+        k[i * slot + n:(i + 1) * slot] = math.nan
+        v[i * slot + n:(i + 1) * slot] = math.inf
+    out, lse = check_attention(q, k, v, None, qo, ko, True, k_len=lengths, grads=False)
+    flat, lse2 = check_attention(q, k, v, None, qo, ko, False, k_len=lengths, grads=False)
+    assert torch.equal(out, flat) and torch.equal(lse, lse2)
+
+
+def test_attention_gradient_over_slots():
+    lengths, slot = [5, 0, 64, 33], 70
+    q, k, v, do, qo, ko = attention_case(torch.bfloat16, [4, 3, 64, 40], [slot] * 4, 4, 2, 64, 8)
+    for i, n in enumerate(lengths):
+        k[i * slot + n:(i + 1) * slot], v[i * slot + n:(i + 1) * slot] = math.nan, math.nan
+    _, _, (dq, dk, dv) = check_attention(q, k, v, do, qo, ko, True, k_len=lengths)
+    for i, n in enumerate(lengths):
+        assert not dk[i * slot + n:(i + 1) * slot].any() and not dv[i * slot + n:(i + 1) * slot].any()
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+def test_attention_of_one_projection(dtype):
+    """Slices of one tensor, gradients into slices of one tensor, and heads
+    before rows."""
+    g = gen(2)
+    x = randn(g, 170, 8, 64, dtype=dtype)
+    q, k, v, do = x[:, :4], x[:, 4:6], x[:, 6:], randn(g, 170, 4, 64, dtype=dtype)
+    qo = [0, 100, 170]
+    y = x.cuda()
+    a = [y[:, :4], y[:, 4:6], y[:, 6:]]
+    out, lse, grads = check_attention(q, k, v, do, qo, qo, True, views=a)
+    d = torch.zeros_like(y)
+    S.sched_attention_grad(*a, out, lse, do.cuda(), i32(qo), i32(qo), d_q=d[:, :4], d_k=d[:, 4:6],
+                           d_v=d[:, 6:])
+    assert torch.equal(d, torch.cat(grads, 1))
+    first = [t.transpose(0, 1).contiguous().transpose(0, 1) for t in a]
+    assert torch.equal(S.sched_attention(*first, i32(qo), i32(qo))[0], out)
+
+
+def test_attention_gradient_against_differences():
+    q, k, v, do, qo, ko = attention_case(torch.float16, [20, 9], None, 4, 2, 32, 6)
+    _, _, grads = check_attention(q, k, v, do, qo, ko, True)
+    g = gen(7)
+    dirs = [torch.randn(t.shape, generator=g, dtype=torch.float64) for t in (q, k, v)]
+
+    def f(h):
+        x = [t.double() + h * d for t, d in zip((q, k, v), dirs)]
+        group = 2
+        total = 0.0
+        for a, b in zip(qo, qo[1:]):
+            for head in range(4):
+                s = x[0][a:b, head] @ x[1][a:b, head // group].T * 32 ** -0.5
+                s = s.masked_fill(torch.triu(torch.ones(b - a, b - a, dtype=torch.bool), 1), -math.inf)
+                total += float((torch.softmax(s, 1) @ x[2][a:b, head // group] * do[a:b, head]).sum())
+        return total
+    step = 2.0 ** -12
+    slope = sum(float((x.cpu().double() * d).sum()) for x, d in zip(grads, dirs))
+    # fp16 results: a relative error of 2^-10 of terms that add up like a random walk
+    size = math.sqrt(sum(float((x.cpu().double() * d).square().sum()) for x, d in zip(grads, dirs)))
+    assert abs(slope - (f(step) - f(-step)) / (2 * step)) < 2.0 ** -8 * size
+
+
+# --- streams, graphs, refusals -----------------------------------------------
+
+
+def test_another_stream():
+    g = gen(0)
+    x = randn(g, 64, 5000).cuda()
+    t = torch.randint(0, 5000, (64,), generator=g).cuda()
+    d = randn(g, 64, 48).cuda()
+    want = S.sched_token_logprobs(x, t)
+    want_d = S.sched_embed_grad(d, t, 5000)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    for _ in range(3):
+        got = S.sched_token_logprobs(x, t, stream=s)
+        got_d = S.sched_embed_grad(d, t, 5000, stream=s)
+        s.synchronize()
+        assert torch.equal(got, want) and torch.equal(got_d, want_d)
+
+
+def test_graph():
+    """Captured once, replayed on new inputs: nothing of the first call stays."""
+    g = gen(4)
+    n, vocab, off = 60, 301, [0, 20, 25, 40, 60]
+    x = randn(g, n, vocab, dtype=torch.bfloat16).cuda()
+    t = torch.randint(0, vocab, (n,), generator=g).cuda()
+    ref = -torch.rand(n, generator=g).cuda() * 6
+    q = randn(g, n, 6, 64, dtype=torch.bfloat16).cuda()
+    do = randn(g, n, 2, 64, dtype=torch.bfloat16).cuda()
+    m = torch.randint(1, 1 << 20, (4,), generator=g).cuda()
+    lim, groups, o = torch.full((2,), 1 << 19).cuda(), i32([0, 2, 4]), i32(off)
+
+    def step():
+        adv, w = S.sched_group_advantages(m, lim, groups, o, t)
+        a = S.sched_policy_loss(x, t, ref, ref, adv, w, kl_weight=0.1)
+        logp = S.sched_token_logprobs(x, t)
+        b = S.sched_preference_loss(logp, ref, t, o)
+        c = S.sched_token_logprobs_grad(x, t, logp, b[2])
+        rows = S.sched_embed(q.view(n * 6, 64), t)
+        d = S.sched_embed_grad(rows, t, vocab)
+        out, lse = S.sched_attention(q[:, :2], q[:, 2:4], q[:, 4:], o, o)
+        e = S.sched_attention_grad(q[:, :2], q[:, 2:4], q[:, 4:], out, lse, do, o, o)
+        return [*a, *b, c, rows, d, out, lse, *e]
+
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for seed in range(3):
+        h = gen(seed + 50)
+        x.copy_(randn(h, n, vocab)), q.copy_(randn(h, n, 6, 64)), do.copy_(randn(h, n, 2, 64))
+        t.copy_(torch.randint(-1, vocab, (n,), generator=h))
+        m.copy_(torch.randint(1, 1 << 20, (4,), generator=h))
+        want = [y.clone() for y in step()]
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for y, z in zip(held, want):
+            assert torch.equal(y, z)
+
+
+def refused(name, fn, *a, **kw):
+    with pytest.raises(S.SchedError) as e:
+        fn(*a, **kw)
+    assert e.value.name == name, e.value
+
+
+def test_refusals():
+    x = torch.zeros((4, 10), device="cuda")
+    t = torch.zeros(4, dtype=torch.int64, device="cuda")
+    f = torch.zeros(4, device="cuda")
+    refused("SCHED_E_VALUE", S.sched_embed, x.cpu(), t)
+    refused("SCHED_E_VALUE", S.sched_embed, x.double(), t)
+    refused("SCHED_E_VALUE", S.sched_embed, x, t.float())
+    refused("SCHED_E_VALUE", S.sched_embed, x, t, scale=math.nan)
+    refused("SCHED_E_VALUE", S.sched_embed, x.t(), t)
+    refused("SCHED_E_SIZE", S.sched_embed, x, t, out=x[:3])
+    refused("SCHED_E_VALUE", S.sched_embed, x, t, out=x[:1].expand(4, 10))
+    refused("SCHED_E_NULL", S.sched_embed_grad, x, t, 5, accumulate=True)
+    refused("SCHED_E_VALUE", S.sched_embed_grad, x, t, 5, out=torch.zeros((5, 10), device="cuda").half())
+    refused("SCHED_E_SIZE", S.sched_embed_grad, x, t, 5, out=x)
+    ws = torch.empty(4096, dtype=torch.uint8, device="cuda")
+    refused("SCHED_E_WORKSPACE", S.sched_embed_grad, x, t, 5, workspace=ws[:8])
+    refused("SCHED_E_WORKSPACE", S.sched_embed_grad, x, t, 5, workspace=ws[16:])
+    refused("SCHED_E_SIZE", S.sched_token_logprobs, x, t[:3])
+    refused("SCHED_E_VALUE", S.sched_token_logprobs, x, t, temperature=0.0)
+    refused("SCHED_E_VALUE", S.sched_token_logprobs, x, t, temperature=-1.0)
+    refused("SCHED_E_SIZE", S.sched_token_logprobs, x[:, :0], t)
+    refused("SCHED_E_SIZE", S.sched_token_logprobs, x, t, logp=f[:2])
+    refused("SCHED_E_VALUE", S.sched_token_logprobs_grad, x, t, f, f, d_logits=x.half())
+    refused("SCHED_E_SIZE", S.sched_token_logprobs_grad, x, t, f, f, d_logits=x[:, :9])
+    refused("SCHED_E_NULL", S.sched_policy_loss, x, t, f, None, f, f, kl_weight=0.1)
+    refused("SCHED_E_VALUE", S.sched_policy_loss, x, t, f, f, f, f, clip_low=-0.1)
+    refused("SCHED_E_VALUE", S.sched_policy_loss, x, t, f, f, f, f, clip_high=math.inf)
+    refused("SCHED_E_SIZE", S.sched_preference_loss, f, f, t, i32([0, 2, 3, 4]))
+    refused("SCHED_E_SIZE", S.sched_preference_loss, f, f, t, i32([0]))
+    refused("SCHED_E_VALUE", S.sched_preference_loss, f, f, t, i32([0, 2, 4]), smoothing=1.5)
+    refused("SCHED_E_VALUE", S.sched_group_advantages, t, t, i32([0, 1, 2, 3, 4]), i32([0] * 5), t,
+            mean="all")
+    q = torch.zeros((6, 4, 64), device="cuda", dtype=torch.bfloat16)
+    o = i32([0, 6])
+    refused("SCHED_E_VALUE", S.sched_attention, q.float(), q.float(), q.float(), o, o)
+    refused("SCHED_E_SIZE", S.sched_attention, q[:, :3], q[:, :2], q[:, :2], o, o)
+    refused("SCHED_E_SIZE", S.sched_attention, q[..., :20], q[..., :20], q[..., :20], o, o)
+    wide = torch.zeros((6, 4, 136), device="cuda", dtype=torch.bfloat16)
+    refused("SCHED_E_SIZE", S.sched_attention, wide, wide, wide, o, o)
+    refused("SCHED_E_VALUE", S.sched_attention, wide[..., 4:68], q, q, o, o)  # 8-byte alignment
+    refused("SCHED_E_VALUE", S.sched_attention, q, q, q, o, o, scale=-1.0)
+    refused("SCHED_E_SIZE", S.sched_attention, q, q, q, o, i32([0, 3, 6]))
+    refused("SCHED_E_SIZE", S.sched_attention, q, q, q, o, o, k_lengths=i32([1, 2]))
+
+
+def test_offsets_that_leave_the_tensor_are_cut():
+    """Wrong offsets read and write nothing outside the tensors."""
+    q = torch.randn((40, 2, 64), device="cuda").half()
+    want, _ = S.sched_attention(q, q, q, i32([0, 40]), i32([0, 40]), causal=False)
+    got, _ = S.sched_attention(q, q, q, i32([-5, 1000]), i32([-100, 70000]), causal=False)
+    assert torch.equal(got, want)
+    got, _ = S.sched_attention(q, q, q, i32([0, 40]), i32([0, 40]), k_lengths=i32([90]), causal=False)
+    assert torch.equal(got, want)
