@@ -104,29 +104,44 @@ __device__ __forceinline__ typename Frag<T>::type piece(const T* row, int d, int
   return v;
 }
 
-// A tile in LDS: rows of D elements and 16 bytes, which spreads the rows'
-// pieces over the banks.
+// A tile in LDS: rows of D elements in pieces of 16 bytes, the pieces of a row
+// permuted so that neither way of reading meets a bank twice: 16 rows at one
+// piece (along), and 4 rows at 4 pieces next to each other (across).
 template <class T, int D>
 struct Rows {
-  static constexpr int kStride = D + 8;
   T* at;
 
+  // Where piece c (elements 8 c .. + 7) of a row lies.
+  static __device__ __forceinline__ int place(int row, int c) {
+    const int f = D == 128 ? row % 4 * 4 + row / 4 % 4 : row / 2 % 2 * 4 + row / 4 % 4;
+    return row * D + (c ^ f) * 8;
+  }
+  __device__ __forceinline__ void put(int row, int c, typename Frag<T>::type v) const {
+    *reinterpret_cast<typename Frag<T>::type*>(at + place(row, c)) = v;
+  }
   // A or B along the rows: lane l has row l % 32 of the 32 from `row`, elements
   // 16 k + 8 (l / 32) .. + 7.
   __device__ __forceinline__ typename Frag<T>::type along(int row, int k) const {
     const int l = int(threadIdx.x) % kWave;
-    return *reinterpret_cast<const typename Frag<T>::type*>(at + (row + l % 32) * kStride + 16 * k +
-                                                            8 * (l / 32));
+    return *reinterpret_cast<const typename Frag<T>::type*>(at + place(row + l % 32, 2 * k + l / 32));
   }
   // A across the rows: lane l has column 32 c + l % 32 of the rows row + 4 h +
-  // {0..3} and row + 8 + 4 h + {0..3}, h = l / 32.
+  // {0..3} and row + 8 + 4 h + {0..3}, h = l / 32.  Sixteen lanes read four rows
+  // of sixteen columns, four elements each, and get a column of four.
   __device__ __forceinline__ typename Frag<T>::type across(int row, int c) const {
     const int l = int(threadIdx.x) % kWave;
-    typename Frag<T>::type v;
-    const T* p = at + (row + 4 * (l / 32)) * kStride + 32 * c + l % 32;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = p[(e / 4 * 8 + e % 4) * kStride];
-    return v;
+    const int r = row + 4 * (l / 32) + l % 16 / 4, col = 4 * c + l % 32 / 16 * 2 + l % 4 / 2;
+    const auto lo = turned(at + place(r, col) + l % 2 * 4);
+    const auto hi = turned(at + place(r + 8, col) + l % 2 * 4);
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+
+ private:
+  typedef T Four __attribute__((ext_vector_type(4)));
+  static __device__ __forceinline__ Four turned(const T* p) {
+    typedef short Raw __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) Raw Lds;
+    return __builtin_bit_cast(Four, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(p)));
   }
 };
 

@@ -17,9 +17,9 @@ constexpr int kRowsOfBlock = 128;  // 32 of each wave
 constexpr int kKeys = 64;          // of a tile
 
 template <class T, int D>
-__global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
-  __shared__ T k_tile[kKeys * Rows<T, D>::kStride];
-  __shared__ T v_tile[kKeys * Rows<T, D>::kStride];
+__global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendArgs a) {
+  __shared__ __attribute__((aligned(16))) T k_tile[kKeys * D];
+  __shared__ __attribute__((aligned(16))) T v_tile[kKeys * D];
   const Tile tile = tile_of(a.q_offsets, a.n_seqs, a.q_rows, a.group, kRowsOfBlock, int(blockIdx.x));
   const Seq s = sequence(a, tile.seq);
   const int first = tile.index * kRowsOfBlock, rows = s.queries * a.group;
@@ -51,8 +51,8 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
       const int64_t at = int64_t(s.k0) + (in ? j0 + row : 0);
       const auto kp = piece(head_row<T>(a.k, at, kv), d, a.dim, in);
       const auto vp = piece(head_row<T>(a.v, at, kv), d, a.dim, in);
-      *reinterpret_cast<typename Frag<T>::type*>(k_tile + row * Rows<T, D>::kStride + d) = kp;
-      *reinterpret_cast<typename Frag<T>::type*>(v_tile + row * Rows<T, D>::kStride + d) = vp;
+      ks.put(row, d / 8, kp);
+      vs.put(row, d / 8, vp);
     }
     __syncthreads();
     Acc x[kKeys / 32] = {};

@@ -42,9 +42,9 @@ __global__ __launch_bounds__(kThreads) void delta_kernel(AttendArgs a, int64_t f
 // Keys 32 wave + lane % 32 of the block's tile; lanes' columns are keys, their
 // values run along the query rows.
 template <class T, int D>
-__global__ __launch_bounds__(kThreads) void keys_kernel(AttendArgs a) {
-  __shared__ T q_tile[kQueries * Rows<T, D>::kStride];
-  __shared__ T o_tile[kQueries * Rows<T, D>::kStride];
+__global__ __launch_bounds__(kThreads, 2) void keys_kernel(AttendArgs a) {
+  __shared__ __attribute__((aligned(16))) T q_tile[kQueries * D];
+  __shared__ __attribute__((aligned(16))) T o_tile[kQueries * D];
   __shared__ float lse2[kQueries], delta[kQueries];
   const Tile tile = tile_of(a.k_offsets, a.n_seqs, a.k_rows, 1, kTileOfBlock, int(blockIdx.x));
   const Seq s = sequence(a, tile.seq);
@@ -75,8 +75,8 @@ __global__ __launch_bounds__(kThreads) void keys_kernel(AttendArgs a) {
       const QueryRow at = query_row(a, kv, in ? r0 + row : 0);
       const auto qp = piece(head_row<T>(a.q, s.q0 + at.query, at.head), d, a.dim, in);
       const auto op = piece(head_row<T>(a.d_out, s.q0 + at.query, at.head), d, a.dim, in);
-      *reinterpret_cast<typename Frag<T>::type*>(q_tile + row * Rows<T, D>::kStride + d) = qp;
-      *reinterpret_cast<typename Frag<T>::type*>(o_tile + row * Rows<T, D>::kStride + d) = op;
+      qs.put(row, d / 8, qp);
+      os.put(row, d / 8, op);
       if (d == 0) {
         const int64_t n = int64_t(at.head) * a.q_rows + s.q0 + at.query;
         lse2[row] = in ? a.lse[n] * kLog2e : INFINITY;  // powers of rows that are not there are 0
@@ -115,9 +115,9 @@ __global__ __launch_bounds__(kThreads) void keys_kernel(AttendArgs a) {
 // Query rows 32 wave + lane % 32 of the block's tile; lanes' columns are query
 // rows, their values run along the keys.
 template <class T, int D>
-__global__ __launch_bounds__(kThreads) void queries_kernel(AttendArgs a) {
-  __shared__ T k_tile[kKeys * Rows<T, D>::kStride];
-  __shared__ T v_tile[kKeys * Rows<T, D>::kStride];
+__global__ __launch_bounds__(kThreads, 2) void queries_kernel(AttendArgs a) {
+  __shared__ __attribute__((aligned(16))) T k_tile[kKeys * D];
+  __shared__ __attribute__((aligned(16))) T v_tile[kKeys * D];
   const Tile tile = tile_of(a.q_offsets, a.n_seqs, a.q_rows, a.group, kTileOfBlock, int(blockIdx.x));
   const Seq s = sequence(a, tile.seq);
   const int first = tile.index * kTileOfBlock, rows = s.queries * a.group;
@@ -150,8 +150,8 @@ __global__ __launch_bounds__(kThreads) void queries_kernel(AttendArgs a) {
       const int64_t at = int64_t(s.k0) + (in ? j0 + row : 0);
       const auto kp = piece(head_row<T>(a.k, at, kv), d, a.dim, in);
       const auto vp = piece(head_row<T>(a.v, at, kv), d, a.dim, in);
-      *reinterpret_cast<typename Frag<T>::type*>(k_tile + row * Rows<T, D>::kStride + d) = kp;
-      *reinterpret_cast<typename Frag<T>::type*>(v_tile + row * Rows<T, D>::kStride + d) = vp;
+      ks.put(row, d / 8, kp);
+      vs.put(row, d / 8, vp);
     }
     __syncthreads();
     Acc x = {}, y = {};
