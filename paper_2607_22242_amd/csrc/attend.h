@@ -96,6 +96,26 @@ __device__ __forceinline__ QueryRow query_row(const AttendArgs& a, int kv_head, 
   return {r / a.group, kv_head * a.group + r % a.group};
 }
 
+// Which tile and key head a block takes.  Blocks go to the card's 8 dies in
+// turn, each with a cache of its own: a die works on one key head at a time (or
+// shares it with few others), whose keys and values its cache then holds.
+struct Work {
+  int tile, kv;
+};
+__device__ __forceinline__ Work work_of(int block, int tiles, int kv_heads) {
+  const int die = block % 8, i = block / 8;
+  if (kv_heads % 8 == 0) return {i % tiles, die + 8 * (i / tiles)};
+  if (8 % kv_heads == 0) return {i * (8 / kv_heads) + die / kv_heads, die % kv_heads};
+  return {block / kv_heads, block % kv_heads};
+}
+inline int64_t work_blocks(int64_t tiles, int kv_heads) {
+  if (kv_heads % 8 != 0 && 8 % kv_heads == 0) {
+    const int share = 8 / kv_heads;
+    return (tiles + share - 1) / share * 8;
+  }
+  return tiles * kv_heads;
+}
+
 // 16 bytes of a row, zeros behind the head's last element.
 template <class T>
 __device__ __forceinline__ typename Frag<T>::type piece(const T* row, int d, int dim, bool on) {
@@ -142,6 +162,33 @@ struct Rows {
     typedef short Raw __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) Raw Lds;
     return __builtin_bit_cast(Four, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(p)));
+  }
+};
+
+// A tile's 16 bytes per thread from memory to LDS without a register between:
+// a wave fills 1024 bytes in a row, so the permutation is in what a lane reads.
+// Nothing waits for it until the next barrier.
+template <class T>
+__device__ __forceinline__ void to_lds(const T* from, T* wave_at) {
+  typedef __attribute__((address_space(1))) const void Global;
+  typedef __attribute__((address_space(3))) void Lds;
+  __builtin_amdgcn_global_load_lds((Global*)from, (Lds*)wave_at, 16, 0, 0);
+}
+
+// Threads of a block over a tile of kRows rows: round p of a thread brings one
+// piece of row p * kStep + row, always the same piece of its row.
+template <class T, int D, int kRows, int kThreads>
+struct Fill {
+  static constexpr int kStep = kThreads / (D / 8), kRounds = kRows / kStep;
+  int row, d;  // of this thread
+
+  __device__ __forceinline__ Fill(int dim) {
+    row = int(threadIdx.x) / (D / 8);
+    const int c = Rows<T, D>::place(row, int(threadIdx.x) % (D / 8)) % D / 8;
+    d = min(8 * c, dim - 8);  // behind the head's last element: what is there twice is not used
+  }
+  __device__ __forceinline__ static T* at(T* tile, int p) {
+    return tile + (p * kThreads + int(threadIdx.x) / kWave * kWave) * 8;
   }
 };
 

@@ -15,63 +15,67 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kRowsOfBlock = 128;  // 32 of each wave
 constexpr int kKeys = 64;          // of a tile
+// How far scores may pass the reference of a row's powers (2^8) before the
+// reference moves: the sums stay in 32 bits, and rescaling is rare.
+constexpr float kSlack = 8.f;
 
+// Keys and values of a tile to LDS; rows behind the last key repeat it, their
+// probabilities are zero.
 template <class T, int D>
-__global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendArgs a) {
-  __shared__ __attribute__((aligned(16))) T k_tile[kKeys * D];
-  __shared__ __attribute__((aligned(16))) T v_tile[kKeys * D];
-  const Tile tile = tile_of(a.q_offsets, a.n_seqs, a.q_rows, a.group, kRowsOfBlock, int(blockIdx.x));
-  const Seq s = sequence(a, tile.seq);
-  const int first = tile.index * kRowsOfBlock, rows = s.queries * a.group;
-  if (tile.index < 0 || first >= rows) return;
-  const int lane = int(threadIdx.x) % kWave, wave = int(threadIdx.x) / kWave;
-  const int kv = int(blockIdx.y), r = first + 32 * wave + lane % 32;
-  const bool on = r < rows;
-  const QueryRow me = query_row(a, kv, on ? r : 0);
-  // Keys that a row sees: j <= last.
-  const int ahead = s.keys - s.queries;
-  const int last = !on ? -1 : a.causal ? min(s.keys - 1, me.query + ahead) : s.keys - 1;
-  const int last_row = min(first + kRowsOfBlock, rows) - 1;
-  const int end = a.causal ? min(s.keys, last_row / a.group + ahead + 1) : s.keys;
-
-  typename Frag<T>::type q[D / 16];
-  const T* q_row = head_row<T>(a.q, s.q0 + me.query, me.head);
+__device__ __forceinline__ void fetch(const AttendArgs& a, const Seq& s, int kv, int j0,
+                                      const Fill<T, D, kKeys, kThreads>& fill, T* k_tile,
+                                      T* v_tile) {
+  typedef Fill<T, D, kKeys, kThreads> F;
 #pragma unroll
-  for (int k = 0; k < D / 16; ++k) q[k] = piece(q_row, 16 * k + 8 * (lane / 32), a.dim, on);
+  for (int p = 0; p < F::kRounds; ++p) {
+    const int64_t row = int64_t(s.k0) + min(j0 + fill.row + p * F::kStep, s.keys - 1);
+    to_lds(head_row<T>(a.k, row, kv) + fill.d, F::at(k_tile, p));
+    to_lds(head_row<T>(a.v, row, kv) + fill.d, F::at(v_tile, p));
+  }
+}
 
-  const float c = a.scale * kLog2e;
-  const Rows<T, D> ks = {k_tile}, vs = {v_tile};
-  Acc o[D / 32] = {};
-  float most = -INFINITY, sum = 0.f;
-  for (int j0 = 0; j0 < end; j0 += kKeys) {
-    __syncthreads();
-    for (int i = int(threadIdx.x); i < kKeys * (D / 8); i += kThreads) {
-      const int row = i / (D / 8), d = i % (D / 8) * 8;
-      const bool in = j0 + row < s.keys;
-      const int64_t at = int64_t(s.k0) + (in ? j0 + row : 0);
-      const auto kp = piece(head_row<T>(a.k, at, kv), d, a.dim, in);
-      const auto vp = piece(head_row<T>(a.v, at, kv), d, a.dim, in);
-      ks.put(row, d / 8, kp);
-      vs.put(row, d / 8, vp);
-    }
-    __syncthreads();
-    Acc x[kKeys / 32] = {};
-    float m = most;
+// A wave's 32 query rows (lane l has row l % 32) and what has been added up
+// over the keys so far.
+template <class T, int D>
+struct Sweep {
+  typename Frag<T>::type q[D / 16];
+  Acc o[D / 32];
+  float most, sum;  // reference of the powers; their sum over this lane's half of the keys
+
+  // Adds a tile of keys, of which the lane's row sees those up to `last`
+  // (`whole`: all rows of the wave see all).
+  __device__ __forceinline__ void add(const T* k_tile, const T* v_tile, int j0, int last,
+                                      bool whole, float c) {
+    const Rows<T, D> ks = {const_cast<T*>(k_tile)}, vs = {const_cast<T*>(v_tile)};
+    Acc x[kKeys / 32];
 #pragma unroll
     for (int t = 0; t < kKeys / 32; ++t) {
+      x[t] = Acc(0.f);
 #pragma unroll
       for (int k = 0; k < D / 16; ++k) x[t] = product(ks.along(32 * t, k), q[k], x[t]);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        if (j0 + 32 * t + c_row(i) > last) x[t][i] = -INFINITY;
-        m = fmaxf(m, x[t][i]);
-      }
     }
+    if (!whole) {
+#pragma unroll
+      for (int t = 0; t < kKeys / 32; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (j0 + 32 * t + c_row(i) > last) x[t][i] = -INFINITY;
+    }
+    float m = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < kKeys / 32; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) m = fmaxf(m, x[t][i]);
     m = fmaxf(m, __shfl_xor(m, 32));
-    const float f = m == -INFINITY ? 0.f : m, fc = f * c;
-    const float keep = pow2((most - f) * c);
-    most = m;
-    sum *= keep;
+    if (__any(m * c > most * c + kSlack)) {
+      const float up = fmaxf(m, most), f = up == -INFINITY ? 0.f : up;
+      const float keep = pow2((most - f) * c);
+      most = up;
+      sum *= keep;
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d) o[d] *= keep;
+    }
+    const float fc = (most == -INFINITY ? 0.f : most) * c;
 #pragma unroll
     for (int t = 0; t < kKeys / 32; ++t)
 #pragma unroll
@@ -80,29 +84,77 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendArgs a) {
         sum += x[t][i];
       }
 #pragma unroll
-    for (int d = 0; d < D / 32; ++d) {
-      o[d] *= keep;
+    for (int t = 0; t < kKeys / 32; ++t)
 #pragma unroll
-      for (int t = 0; t < kKeys / 32; ++t)
+      for (int p = 0; p < 2; ++p) {
+        const auto b = narrow<T>(x[t], p);
 #pragma unroll
-        for (int p = 0; p < 2; ++p)
-          o[d] = product(vs.across(32 * t + 16 * p, d), narrow<T>(x[t], p), o[d]);
-    }
+        for (int d = 0; d < D / 32; ++d)
+          o[d] = product(vs.across(32 * t + 16 * p, d), b, o[d]);
+      }
   }
-  sum += __shfl_xor(sum, 32);
+};
+
+template <class T, int D>
+__global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendArgs a, int tiles) {
+  __shared__ __attribute__((aligned(16))) T k_even[kKeys * D], v_even[kKeys * D];
+  __shared__ __attribute__((aligned(16))) T k_odd[kKeys * D], v_odd[kKeys * D];
+  const Work work = work_of(int(blockIdx.x), tiles, a.q_heads / a.group);
+  if (work.tile >= tiles) return;
+  // The last tiles of a sequence see the most keys: they go first.
+  const Tile tile = tile_of(a.q_offsets, a.n_seqs, a.q_rows, a.group, kRowsOfBlock,
+                            tiles - 1 - work.tile);
+  const Seq s = sequence(a, tile.seq);
+  const int first = tile.index * kRowsOfBlock, rows = s.queries * a.group;
+  if (tile.index < 0 || first >= rows) return;
+  const int lane = int(threadIdx.x) % kWave, wave = int(threadIdx.x) / kWave;
+  const int kv = work.kv, r = first + 32 * wave + lane % 32;
+  const bool on = r < rows;
+  const QueryRow me = query_row(a, kv, on ? r : 0);
+  // Keys that a row sees: j <= last; those that all or any rows of the wave see.
+  const int ahead = s.keys - s.queries;
+  const int last = !on || !a.causal ? s.keys - 1 : min(s.keys - 1, me.query + ahead);
+  const int last_row = min(first + kRowsOfBlock, rows) - 1;
+  const int end = a.causal ? min(s.keys, last_row / a.group + ahead + 1) : s.keys;
+  const int wave_first = min(first + 32 * wave, rows - 1);
+  const int wave_last = min(wave_first + 31, rows - 1);
+  const int all = !a.causal ? s.keys - 1 : min(s.keys - 1, wave_first / a.group + ahead);
+  const int any = !a.causal ? s.keys - 1 : min(s.keys - 1, wave_last / a.group + ahead);
+
+  Sweep<T, D> w;
+  const T* q_row = head_row<T>(a.q, s.q0 + me.query, me.head);
+#pragma unroll
+  for (int k = 0; k < D / 16; ++k) w.q[k] = piece(q_row, 16 * k + 8 * (lane / 32), a.dim, on);
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d) w.o[d] = Acc(0.f);
+  w.most = -INFINITY;
+  w.sum = 0.f;
+  const float c = a.scale * kLog2e;
+  const Fill<T, D, kKeys, kThreads> fill(a.dim);
+  if (end > 0) fetch<T, D>(a, s, kv, 0, fill, k_even, v_even);
+  for (int j0 = 0; j0 < end; j0 += 2 * kKeys) {
+    __syncthreads();  // the tile is there, and nobody reads the other buffer any more
+    if (j0 + kKeys < end) fetch<T, D>(a, s, kv, j0 + kKeys, fill, k_odd, v_odd);
+    if (j0 <= any) w.add(k_even, v_even, j0, last, j0 + kKeys - 1 <= all, c);
+    if (j0 + kKeys >= end) break;
+    __syncthreads();
+    if (j0 + 2 * kKeys < end) fetch<T, D>(a, s, kv, j0 + 2 * kKeys, fill, k_even, v_even);
+    if (j0 + kKeys <= any) w.add(k_odd, v_odd, j0 + kKeys, last, j0 + 2 * kKeys - 1 <= all, c);
+  }
+  const float sum = w.sum + __shfl_xor(w.sum, 32);
   if (!on) return;
-  store_column<T, D>(head_row<T>(a.out, s.q0 + me.query, me.head), o, a.dim,
+  store_column<T, D>(head_row<T>(a.out, s.q0 + me.query, me.head), w.o, a.dim,
                      sum > 0.f ? 1.f / sum : 0.f);
   if (lane < 32)
     a.lse[int64_t(me.head) * a.q_rows + s.q0 + me.query] =
-        sum > 0.f ? (most * c + log_2(sum)) * kLn2 : -INFINITY;
+        sum > 0.f ? (w.most * c + log_2(sum)) * kLn2 : -INFINITY;
 }
 
 template <class T, int D>
 hipError_t attend(const AttendArgs& a, int kv_heads, hipStream_t s) {
   const int64_t tiles = tile_count(int64_t(a.q_rows) * a.group, a.n_seqs, kRowsOfBlock);
-  hipLaunchKernelGGL((attend_kernel<T, D>), dim3(unsigned(tiles), unsigned(kv_heads)),
-                     dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL((attend_kernel<T, D>), dim3(unsigned(work_blocks(tiles, kv_heads))),
+                     dim3(kThreads), 0, s, a, int(tiles));
   return hipGetLastError();
 }
 
