@@ -41,9 +41,10 @@ struct HeadsView {
 struct AttendArgs {
   HeadsView q, k, v, out, d_out, d_q, d_k, d_v;
   float* lse;
-  float* delta;
+  float *lse2, *delta;  // q_heads x q_rows each: lse log2(e) (+inf in place of -inf), -rowsum(dO o O)
   const int32_t *q_offsets, *k_offsets, *k_lengths;
   int32_t n_seqs, q_rows, k_rows, q_heads, group, dim, causal;
+  uint32_t per_group;  // ceil(2^32 / group): quotients of small numbers
   float scale;
 };
 

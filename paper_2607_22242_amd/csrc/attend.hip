@@ -179,6 +179,7 @@ AttendArgs attend_args(const sched_attention_desc& d) {
   a.k_rows = int32_t(d.k_rows);
   a.q_heads = d.q_heads;
   a.group = d.q_heads / d.kv_heads;
+  a.per_group = uint32_t(((uint64_t(1) << 32) + a.group - 1) / a.group);
   a.dim = d.head_dim;
   a.causal = d.causal;
   a.scale = d.scale;

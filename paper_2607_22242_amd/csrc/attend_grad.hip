@@ -8,6 +8,8 @@
 // one order and no atomics: 14 D operations per pair in place of 10 D.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "attend.h"
 #include "policy_launch.h"
 
@@ -18,11 +20,11 @@ AttendArgs attend_args(const sched_attention_desc& d);
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kTileOfBlock = 128;  // keys or query rows that a block holds, 32 of each wave
-constexpr int kQueries = 32;       // rows of a tile that the kernel of dK and dV walks over
-constexpr int kKeys = 32;          // keys of a tile that the kernel of dQ walks over
+constexpr int kTile = 64;          // rows of a tile that is walked over
+constexpr int kKeysOfBlock = 64;   // keys that a block holds for dK and dV
+constexpr int kRowsOfBlock = 128;  // query rows that a block holds for dQ, 32 of each wave
 
-// delta of every query row and head; 16 lanes a row.
+// lse2 and delta of every query row and head; 16 lanes a row.
 template <class T>
 __global__ __launch_bounds__(kThreads) void delta_kernel(AttendArgs a, int64_t first) {
   const int64_t i = first + int64_t(blockIdx.x) * (kThreads / 16) + int(threadIdx.x) / 16;
@@ -36,143 +38,301 @@ __global__ __launch_bounds__(kThreads) void delta_kernel(AttendArgs a, int64_t f
   for (int e = 0; e < 8; ++e) sum += float(x[e]) * float(y[e]);
 #pragma unroll
   for (int k = 8; k; k >>= 1) sum += __shfl_xor(sum, k);
-  if (threadIdx.x % 16 == 0) a.delta[int64_t(head) * a.q_rows + row] = sum;
+  if (threadIdx.x % 16 == 0) {
+    const int64_t n = int64_t(head) * a.q_rows + row;
+    const float lse = a.lse[n];
+    a.delta[n] = -sum;
+    a.lse2[n] = lse == -INFINITY ? INFINITY : lse * kLog2e;
+  }
 }
 
-// Keys 32 wave + lane % 32 of the block's tile; lanes' columns are keys, their
-// values run along the query rows.
-template <class T, int D>
-__global__ __launch_bounds__(kThreads, 2) void keys_kernel(AttendArgs a) {
-  __shared__ __attribute__((aligned(16))) T q_tile[kQueries * D];
-  __shared__ __attribute__((aligned(16))) T o_tile[kQueries * D];
-  __shared__ float lse2[kQueries], delta[kQueries];
-  const Tile tile = tile_of(a.k_offsets, a.n_seqs, a.k_rows, 1, kTileOfBlock, int(blockIdx.x));
-  const Seq s = sequence(a, tile.seq);
-  const int first = tile.index * kTileOfBlock;
-  if (tile.index < 0 || first >= s.slot) return;
-  const int lane = int(threadIdx.x) % kWave, wave = int(threadIdx.x) / kWave;
-  const int kv = int(blockIdx.y), j = first + 32 * wave + lane % 32;
-  const bool on = j < s.keys;
-  const int64_t key = int64_t(s.k0) + (on ? j : 0);
-  typename Frag<T>::type k[D / 16], v[D / 16];
-#pragma unroll
-  for (int i = 0; i < D / 16; ++i) {
-    k[i] = piece(head_row<T>(a.k, key, kv), 16 * i + 8 * (lane / 32), a.dim, on);
-    v[i] = piece(head_row<T>(a.v, key, kv), 16 * i + 8 * (lane / 32), a.dim, on);
+// --- dK and dV ----------------------------------------------------------------
+
+// A tile of query rows: where row 0 of it lies, counted in queries and in rows
+// behind the query's first head.
+struct RowTile {
+  int r0, query, rest;
+};
+__device__ __forceinline__ RowTile row_tile(const AttendArgs& a, int r0) {
+  return {r0, r0 / a.group, r0 % a.group};
+}
+__device__ __forceinline__ void advance(const AttendArgs& a, RowTile& t) {
+  t.r0 += kTile;
+  t.query += kTile / a.group;
+  t.rest += kTile % a.group;
+  if (t.rest >= a.group) {
+    t.rest -= a.group;
+    ++t.query;
   }
-  const float c = a.scale * kLog2e;
-  const Rows<T, D> qs = {q_tile}, os = {o_tile};
-  Acc dk[D / 32] = {}, dv[D / 32] = {};
-  const int rows = first < s.keys ? s.queries * a.group : 0, ahead = s.keys - s.queries;
-  // The first query that sees the block's first key.
-  const int begin =
-      a.causal && rows > 0 ? max(0, first - ahead) * a.group / kQueries * kQueries : 0;
-  for (int r0 = begin; r0 < rows; r0 += kQueries) {
-    __syncthreads();
-    for (int i = int(threadIdx.x); i < kQueries * (D / 8); i += kThreads) {
-      const int row = i / (D / 8), d = i % (D / 8) * 8;
-      const bool in = r0 + row < rows;
-      const QueryRow at = query_row(a, kv, in ? r0 + row : 0);
-      const auto qp = piece(head_row<T>(a.q, s.q0 + at.query, at.head), d, a.dim, in);
-      const auto op = piece(head_row<T>(a.d_out, s.q0 + at.query, at.head), d, a.dim, in);
-      qs.put(row, d / 8, qp);
-      os.put(row, d / 8, op);
-      if (d == 0) {
-        const int64_t n = int64_t(at.head) * a.q_rows + s.q0 + at.query;
-        lse2[row] = in ? a.lse[n] * kLog2e : INFINITY;  // powers of rows that are not there are 0
-        delta[row] = in ? a.delta[n] : 0.f;
+}
+
+struct Stats {
+  float lse2[kTile], delta[kTile];
+};
+
+// Q, dO and the rows' statistics to LDS; rows behind the last repeat it.
+template <class T, int D>
+__device__ __forceinline__ void fetch_rows(const AttendArgs& a, const Seq& s, int kv, int rows,
+                                           const RowTile& t,
+                                           const Fill<T, D, kTile, kThreads>& fill, T* q_tile,
+                                           T* o_tile, Stats* stats) {
+  typedef Fill<T, D, kTile, kThreads> F;
+  const int most = t.rest + rows - 1 - t.r0;
+  auto row_of = [&](int i) -> QueryRow {
+    const int x = min(t.rest + i, most), q = int(__umulhi(uint32_t(x), a.per_group));
+    return a.group == 1 ? QueryRow{t.query + x, kv}
+                        : QueryRow{t.query + q, kv * a.group + x - q * a.group};
+  };
+#pragma unroll
+  for (int p = 0; p < F::kRounds; ++p) {
+    const QueryRow r = row_of(fill.row + p * F::kStep);
+    to_lds(head_row<T>(a.q, int64_t(s.q0) + r.query, r.head) + fill.d, F::at(q_tile, p));
+    to_lds(head_row<T>(a.d_out, int64_t(s.q0) + r.query, r.head) + fill.d, F::at(o_tile, p));
+  }
+  const int wave = int(threadIdx.x) / kWave;
+  if (wave < 2) {
+    const QueryRow r = row_of(int(threadIdx.x) % kWave);
+    const int64_t n = int64_t(r.head) * a.q_rows + s.q0 + r.query;
+    typedef __attribute__((address_space(1))) const void Global;
+    typedef __attribute__((address_space(3))) void Lds;
+    __builtin_amdgcn_global_load_lds((Global*)((wave ? a.delta : a.lse2) + n),
+                                     (Lds*)(wave ? stats->delta : stats->lse2), 4, 0, 0);
+  }
+}
+
+// 32 keys of a wave (lane l has key l % 32) against the rows it is given: the
+// lanes' columns are keys, their values run along the query rows.
+template <class T, int D>
+struct KeySweep {
+  typename Frag<T>::type k[D / 16], v[D / 16];
+  Acc dk[D / 32], dv[D / 32];
+
+  // Rows half .. half + 31 of a tile; the lane's key is seen by the tile's rows
+  // from `from` to `upto` (`whole`: all of the wave's are by all).
+  __device__ __forceinline__ void add(const T* q_tile, const T* o_tile, const Stats& stats,
+                                      int half, int from, int upto, bool whole, float c) {
+    const Rows<T, D> qs = {const_cast<T*>(q_tile)}, os = {const_cast<T*>(o_tile)};
+    typedef float Four __attribute__((ext_vector_type(4)));
+    const int h4 = int(threadIdx.x) % kWave / 32 * 4;
+    Acc x = Acc(0.f), y;
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      const Four d = *reinterpret_cast<const Four*>(&stats.delta[half + 2 * i + h4]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[i + e] = d[e];
+    }
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) x = product(qs.along(half, i), k[i], x);
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) y = product(os.along(half, i), v[i], y);
+    if (!whole) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int r = half + c_row(i);
+        if (r < from || r > upto) x[i] = -INFINITY;
       }
     }
-    __syncthreads();
-    Acc x = {}, y = {};
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) {
-      x = product(qs.along(0, i), k[i], x);
-      y = product(os.along(0, i), v[i], y);
+    for (int i = 0; i < 16; i += 4) {
+      const Four l = *reinterpret_cast<const Four*>(&stats.lse2[half + 2 * i + h4]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[i + e] = pow2(__builtin_fmaf(x[i + e], c, -l[e]));
     }
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int r = c_row(i);
-      const bool seen = on && (!a.causal || j <= (r0 + r) / a.group + ahead);
-      x[i] = seen ? pow2(__builtin_fmaf(x[i], c, -lse2[r])) : 0.f;
-      y[i] = x[i] * (y[i] - delta[r]);
-    }
+    for (int i = 0; i < 16; ++i) y[i] *= x[i];
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
       const auto pb = narrow<T>(x, p), db = narrow<T>(y, p);
 #pragma unroll
-      for (int d = 0; d < D / 32; ++d) {
-        dv[d] = product(os.across(16 * p, d), pb, dv[d]);
-        dk[d] = product(qs.across(16 * p, d), db, dk[d]);
+      for (int d = 0; d < D / 32; ++d) dv[d] = product(os.across(half + 16 * p, d), pb, dv[d]);
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d) dk[d] = product(qs.across(half + 16 * p, d), db, dk[d]);
+    }
+  }
+};
+
+// A block holds 64 keys; waves 0 and 1 take the even 32 rows of each tile with
+// keys 0 .. 31 and 32 .. 63, waves 2 and 3 the odd 32; their sums meet at the end.
+template <class T, int D>
+__global__ __launch_bounds__(kThreads, 1) void keys_kernel(AttendArgs a, int tiles) {
+  __shared__ __attribute__((aligned(16))) T q_even[kTile * D], o_even[kTile * D];
+  __shared__ __attribute__((aligned(16))) T q_odd[kTile * D], o_odd[kTile * D];
+  __shared__ __attribute__((aligned(16))) Stats s_even, s_odd;
+  const Work work = work_of(int(blockIdx.x), tiles, a.q_heads / a.group);
+  if (work.tile >= tiles) return;
+  const Tile tile = tile_of(a.k_offsets, a.n_seqs, a.k_rows, 1, kKeysOfBlock, work.tile);
+  const Seq s = sequence(a, tile.seq);
+  const int first = tile.index * kKeysOfBlock;
+  if (tile.index < 0 || first >= s.slot) return;
+  const int lane = int(threadIdx.x) % kWave, wave = int(threadIdx.x) / kWave;
+  const int kv = work.kv, half = wave / 2 * 32, wave_key = first + wave % 2 * 32;
+  const int j = wave_key + lane % 32;
+  const bool on = j < s.keys;
+  const int64_t key = int64_t(s.k0) + (on ? j : 0);
+  KeySweep<T, D> w;
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) {
+    w.k[i] = piece(head_row<T>(a.k, key, kv), 16 * i + 8 * (lane / 32), a.dim, on);
+    w.v[i] = piece(head_row<T>(a.v, key, kv), 16 * i + 8 * (lane / 32), a.dim, on);
+  }
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) w.dk[i] = w.dv[i] = Acc(0.f);
+  const float c = a.scale * kLog2e;
+  const int rows = first < s.keys ? s.queries * a.group : 0, ahead = s.keys - s.queries;
+  // The first row that sees a key: the block's first, the lane's, the wave's
+  // last and first.
+  auto seen_from = [&](int key) { return a.causal ? max(0, key - ahead) * a.group : 0; };
+  const int begin = rows > 0 ? seen_from(first) / kTile * kTile : 0;
+  const int from = on ? seen_from(j) : rows;
+  const int all = wave_key + 31 < s.keys ? seen_from(wave_key + 31) : rows;
+  const int any = wave_key < s.keys ? seen_from(wave_key) : rows;
+  const Fill<T, D, kTile, kThreads> fill(a.dim);
+  RowTile t = row_tile(a, begin);
+  auto step = [&](int r0, const T* q_tile, const T* o_tile, const Stats& stats) {
+    if (r0 + half + 31 < any || r0 + half >= rows) return;
+    w.add(q_tile, o_tile, stats, half, from - r0, rows - 1 - r0,
+          r0 + half >= all && r0 + half + 31 < rows, c);
+  };
+  if (begin < rows) fetch_rows<T, D>(a, s, kv, rows, t, fill, q_even, o_even, &s_even);
+  for (int r0 = begin; r0 < rows; r0 += 2 * kTile) {
+    __syncthreads();  // the tile is there, and nobody reads the other buffer any more
+    advance(a, t);
+    if (t.r0 < rows) fetch_rows<T, D>(a, s, kv, rows, t, fill, q_odd, o_odd, &s_odd);
+    step(r0, q_even, o_even, s_even);
+    if (r0 + kTile >= rows) break;
+    __syncthreads();
+    advance(a, t);
+    if (t.r0 < rows) fetch_rows<T, D>(a, s, kv, rows, t, fill, q_even, o_even, &s_even);
+    step(r0 + kTile, q_odd, o_odd, s_odd);
+  }
+  // Waves 2 and 3 hand over their sums, D / 32 tiles of 16 values a lane, in
+  // two turns through one buffer each.
+  static_assert(sizeof(q_even) >= size_t(D) / 32 * 16 * kWave * 2 * sizeof(T), "a wave's sums");
+  float* const hand = reinterpret_cast<float*>(wave % 2 ? o_even : q_even);
+  float* const hand2 = reinterpret_cast<float*>(wave % 2 ? o_odd : q_odd);
+  __syncthreads();
+  if (wave >= 2) {
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        hand[(d * 16 + i) * kWave + lane] = w.dk[d][i];
+        hand2[(d * 16 + i) * kWave + lane] = w.dv[d][i];
+      }
+  }
+  __syncthreads();
+  if (wave >= 2 || j >= s.slot) return;
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      w.dk[d][i] += hand[(d * 16 + i) * kWave + lane];
+      w.dv[d][i] += hand2[(d * 16 + i) * kWave + lane];
+    }
+  store_column<T, D>(head_row<T>(a.d_k, int64_t(s.k0) + j, kv), w.dk, a.dim, a.scale);
+  store_column<T, D>(head_row<T>(a.d_v, int64_t(s.k0) + j, kv), w.dv, a.dim, 1.f);
+}
+
+// --- dQ -----------------------------------------------------------------------
+
+template <class T, int D>
+__device__ __forceinline__ void fetch_keys(const AttendArgs& a, const Seq& s, int kv, int j0,
+                                           const Fill<T, D, kTile, kThreads>& fill, T* k_tile,
+                                           T* v_tile) {
+  typedef Fill<T, D, kTile, kThreads> F;
+#pragma unroll
+  for (int p = 0; p < F::kRounds; ++p) {
+    const int64_t row = int64_t(s.k0) + min(j0 + fill.row + p * F::kStep, s.keys - 1);
+    to_lds(head_row<T>(a.k, row, kv) + fill.d, F::at(k_tile, p));
+    to_lds(head_row<T>(a.v, row, kv) + fill.d, F::at(v_tile, p));
+  }
+}
+
+// 32 query rows of a wave (lane l has row l % 32): the lanes' columns are query
+// rows, their values run along the keys.
+template <class T, int D>
+struct RowSweep {
+  typename Frag<T>::type q[D / 16], o[D / 16];
+  Acc dq[D / 32];
+  float lse2, delta;
+
+  __device__ __forceinline__ void add(const T* k_tile, const T* v_tile, int j0, int last,
+                                      bool whole, float c) {
+    const Rows<T, D> ks = {const_cast<T*>(k_tile)}, vs = {const_cast<T*>(v_tile)};
+#pragma unroll
+    for (int t = 0; t < kTile / 32; ++t) {
+      Acc x = Acc(0.f), y = Acc(delta);
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) x = product(ks.along(32 * t, i), q[i], x);
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) y = product(vs.along(32 * t, i), o[i], y);
+      if (!whole) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (j0 + 32 * t + c_row(i) > last) x[i] = -INFINITY;
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) y[i] *= pow2(__builtin_fmaf(x[i], c, -lse2));
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        const auto b = narrow<T>(y, p);
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d) dq[d] = product(ks.across(32 * t + 16 * p, d), b, dq[d]);
       }
     }
   }
-  if (j >= s.slot) return;
-  store_column<T, D>(head_row<T>(a.d_k, int64_t(s.k0) + j, kv), dk, a.dim, on ? a.scale : 0.f);
-  store_column<T, D>(head_row<T>(a.d_v, int64_t(s.k0) + j, kv), dv, a.dim, on ? 1.f : 0.f);
-}
+};
 
-// Query rows 32 wave + lane % 32 of the block's tile; lanes' columns are query
-// rows, their values run along the keys.
 template <class T, int D>
-__global__ __launch_bounds__(kThreads, 2) void queries_kernel(AttendArgs a) {
-  __shared__ __attribute__((aligned(16))) T k_tile[kKeys * D];
-  __shared__ __attribute__((aligned(16))) T v_tile[kKeys * D];
-  const Tile tile = tile_of(a.q_offsets, a.n_seqs, a.q_rows, a.group, kTileOfBlock, int(blockIdx.x));
+__global__ __launch_bounds__(kThreads, 2) void queries_kernel(AttendArgs a, int tiles) {
+  __shared__ __attribute__((aligned(16))) T k_even[kTile * D], v_even[kTile * D];
+  __shared__ __attribute__((aligned(16))) T k_odd[kTile * D], v_odd[kTile * D];
+  const Work work = work_of(int(blockIdx.x), tiles, a.q_heads / a.group);
+  if (work.tile >= tiles) return;
+  // The last tiles of a sequence see the most keys: they go first.
+  const Tile tile = tile_of(a.q_offsets, a.n_seqs, a.q_rows, a.group, kRowsOfBlock,
+                            tiles - 1 - work.tile);
   const Seq s = sequence(a, tile.seq);
-  const int first = tile.index * kTileOfBlock, rows = s.queries * a.group;
+  const int first = tile.index * kRowsOfBlock, rows = s.queries * a.group;
   if (tile.index < 0 || first >= rows) return;
   const int lane = int(threadIdx.x) % kWave, wave = int(threadIdx.x) / kWave;
-  const int kv = int(blockIdx.y), r = first + 32 * wave + lane % 32;
+  const int kv = work.kv, r = first + 32 * wave + lane % 32;
   const bool on = r < rows;
   const QueryRow me = query_row(a, kv, on ? r : 0);
   const int ahead = s.keys - s.queries;
-  const int last = !on ? -1 : a.causal ? min(s.keys - 1, me.query + ahead) : s.keys - 1;
-  const int last_row = min(first + kTileOfBlock, rows) - 1;
+  const int last = !on || !a.causal ? s.keys - 1 : min(s.keys - 1, me.query + ahead);
+  const int last_row = min(first + kRowsOfBlock, rows) - 1;
   const int end = a.causal ? min(s.keys, last_row / a.group + ahead + 1) : s.keys;
-  typename Frag<T>::type q[D / 16], o[D / 16];
+  const int wave_first = min(first + 32 * wave, rows - 1);
+  const int wave_last = min(wave_first + 31, rows - 1);
+  const int all = !a.causal ? s.keys - 1 : min(s.keys - 1, wave_first / a.group + ahead);
+  const int any = !a.causal ? s.keys - 1 : min(s.keys - 1, wave_last / a.group + ahead);
+
+  RowSweep<T, D> w;
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) {
     const int d = 16 * i + 8 * (lane / 32);
-    q[i] = piece(head_row<T>(a.q, s.q0 + me.query, me.head), d, a.dim, on);
-    o[i] = piece(head_row<T>(a.d_out, s.q0 + me.query, me.head), d, a.dim, on);
+    w.q[i] = piece(head_row<T>(a.q, s.q0 + me.query, me.head), d, a.dim, on);
+    w.o[i] = piece(head_row<T>(a.d_out, s.q0 + me.query, me.head), d, a.dim, on);
   }
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) w.dq[i] = Acc(0.f);
   const int64_t n = int64_t(me.head) * a.q_rows + s.q0 + me.query;
-  const float c = a.scale * kLog2e, lse2 = on ? a.lse[n] * kLog2e : INFINITY;
-  const float delta = on ? a.delta[n] : 0.f;
-  const Rows<T, D> ks = {k_tile}, vs = {v_tile};
-  Acc dq[D / 32] = {};
-  for (int j0 = 0; j0 < end; j0 += kKeys) {
+  w.lse2 = on ? a.lse2[n] : INFINITY;
+  w.delta = on ? a.delta[n] : 0.f;
+  const float c = a.scale * kLog2e;
+  const Fill<T, D, kTile, kThreads> fill(a.dim);
+  if (end > 0) fetch_keys<T, D>(a, s, kv, 0, fill, k_even, v_even);
+  for (int j0 = 0; j0 < end; j0 += 2 * kTile) {
     __syncthreads();
-    for (int i = int(threadIdx.x); i < kKeys * (D / 8); i += kThreads) {
-      const int row = i / (D / 8), d = i % (D / 8) * 8;
-      const bool in = j0 + row < s.keys;
-      const int64_t at = int64_t(s.k0) + (in ? j0 + row : 0);
-      const auto kp = piece(head_row<T>(a.k, at, kv), d, a.dim, in);
-      const auto vp = piece(head_row<T>(a.v, at, kv), d, a.dim, in);
-      ks.put(row, d / 8, kp);
-      vs.put(row, d / 8, vp);
-    }
+    if (j0 + kTile < end) fetch_keys<T, D>(a, s, kv, j0 + kTile, fill, k_odd, v_odd);
+    if (j0 <= any) w.add(k_even, v_even, j0, last, j0 + kTile - 1 <= all, c);
+    if (j0 + kTile >= end) break;
     __syncthreads();
-    Acc x = {}, y = {};
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i) {
-      x = product(ks.along(0, i), q[i], x);
-      y = product(vs.along(0, i), o[i], y);
-    }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const float p = j0 + c_row(i) <= last ? pow2(__builtin_fmaf(x[i], c, -lse2)) : 0.f;
-      y[i] = p * (y[i] - delta);
-    }
-#pragma unroll
-    for (int p = 0; p < 2; ++p) {
-      const auto db = narrow<T>(y, p);
-#pragma unroll
-      for (int d = 0; d < D / 32; ++d) dq[d] = product(ks.across(16 * p, d), db, dq[d]);
-    }
+    if (j0 + 2 * kTile < end) fetch_keys<T, D>(a, s, kv, j0 + 2 * kTile, fill, k_even, v_even);
+    if (j0 + kTile <= any) w.add(k_odd, v_odd, j0 + kTile, last, j0 + 2 * kTile - 1 <= all, c);
   }
-  if (on) store_column<T, D>(head_row<T>(a.d_q, s.q0 + me.query, me.head), dq, a.dim, a.scale);
+  if (on) store_column<T, D>(head_row<T>(a.d_q, s.q0 + me.query, me.head), w.dq, a.dim, a.scale);
 }
 
 template <class T, int D>
@@ -180,22 +340,22 @@ hipError_t attend_grad(const AttendArgs& a, int kv_heads, hipStream_t s) {
   const int64_t rows = int64_t(a.q_rows) * a.q_heads, blocks = (rows + 15) / 16;
   hipError_t e = hipSuccess;
   for (int64_t b = 0; b < blocks && e == hipSuccess; b += kMostBlocks) {
-    hipLaunchKernelGGL(delta_kernel<T>, dim3(unsigned(blocks - b < kMostBlocks ? blocks - b : kMostBlocks)),
+    hipLaunchKernelGGL(delta_kernel<T>, dim3(unsigned(std::min(blocks - b, kMostBlocks))),
                        dim3(kThreads), 0, s, a, b * 16);
     e = hipGetLastError();
   }
   if (e != hipSuccess) return e;
   if (a.k_rows > 0) {
-    const int64_t tiles = tile_count(a.k_rows, a.n_seqs, kTileOfBlock);
-    hipLaunchKernelGGL((keys_kernel<T, D>), dim3(unsigned(tiles), unsigned(kv_heads)),
-                       dim3(kThreads), 0, s, a);
+    const int64_t tiles = tile_count(a.k_rows, a.n_seqs, kKeysOfBlock);
+    hipLaunchKernelGGL((keys_kernel<T, D>), dim3(unsigned(work_blocks(tiles, kv_heads))),
+                       dim3(kThreads), 0, s, a, int(tiles));
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   if (a.q_rows > 0) {
-    const int64_t tiles = tile_count(int64_t(a.q_rows) * a.group, a.n_seqs, kTileOfBlock);
-    hipLaunchKernelGGL((queries_kernel<T, D>), dim3(unsigned(tiles), unsigned(kv_heads)),
-                       dim3(kThreads), 0, s, a);
+    const int64_t tiles = tile_count(int64_t(a.q_rows) * a.group, a.n_seqs, kRowsOfBlock);
+    hipLaunchKernelGGL((queries_kernel<T, D>), dim3(unsigned(work_blocks(tiles, kv_heads))),
+                       dim3(kThreads), 0, s, a, int(tiles));
     e = hipGetLastError();
   }
   return e;
@@ -208,7 +368,7 @@ HeadsView view(const sched_heads& h) {
 }  // namespace
 
 size_t attention_grad_bytes(const sched_attention_desc& d) {
-  return size_t(d.q_rows) * size_t(d.q_heads) * 4;
+  return size_t(d.q_rows) * size_t(d.q_heads) * 8;
 }
 
 hipError_t launch_attention_grad(const sched_attention_desc& d, const sched_heads& d_out,
@@ -220,7 +380,8 @@ hipError_t launch_attention_grad(const sched_attention_desc& d, const sched_head
   a.d_q = view(d_q);
   a.d_k = view(d_k);
   a.d_v = view(d_v);
-  a.delta = static_cast<float*>(ws);
+  a.lse2 = static_cast<float*>(ws);
+  a.delta = a.lse2 + size_t(d.q_rows) * size_t(d.q_heads);
   const bool wide = d.head_dim > 64;
   if (d.dtype == SCHED_F16)
     return wide ? attend_grad<f16, 128>(a, d.kv_heads, s) : attend_grad<f16, 64>(a, d.kv_heads, s);

@@ -81,7 +81,8 @@ int check_heads(const sched_heads& h, int64_t rows, int32_t heads, int32_t dim, 
 int check_attention_sizes(const sched_attention_desc& d) {
   if (d.dtype != SCHED_F16 && d.dtype != SCHED_BF16) return SCHED_E_VALUE;
   if (d.head_dim < 8 || d.head_dim > 128 || d.head_dim % 8 || d.kv_heads < 1 ||
-      d.kv_heads > 65535 || d.q_heads < 1 || d.q_heads % d.kv_heads || d.n_seqs < 0 ||
+      d.kv_heads > 65535 || d.q_heads < 1 || d.q_heads % d.kv_heads ||
+      d.q_heads / d.kv_heads > 4096 || d.n_seqs < 0 ||
       d.q_rows < 0 || d.k_rows < 0 || d.k_rows > kMostRows - 256 || d.q_rows > kMostRows ||
       d.q_rows * (d.q_heads / d.kv_heads) > kMostRows - 256)
     return SCHED_E_SIZE;
