@@ -44,7 +44,7 @@ struct AttendArgs {
   float *lse2, *delta;  // q_heads x q_rows each: lse log2(e) (+inf in place of -inf), -rowsum(dO o O)
   const int32_t *q_offsets, *k_offsets, *k_lengths;
   int32_t n_seqs, q_rows, k_rows, q_heads, group, dim, causal;
-  uint32_t per_group;  // ceil(2^32 / group): quotients of small numbers
+  uint32_t per_group;  // ceil(2^32 / group), in 32 bits: quotients of small numbers
   float scale;
 };
 
@@ -128,41 +128,58 @@ __device__ __forceinline__ typename Frag<T>::type piece(const T* row, int d, int
 // A tile in LDS: rows of D elements in pieces of 16 bytes, the pieces of a row
 // permuted so that neither way of reading meets a bank twice: 16 rows at one
 // piece (along), and 4 rows at 4 pieces next to each other (across).
+template <int D>
+__device__ __forceinline__ int turn_of(int row) {  // what a row's pieces are permuted by
+  return D == 128 ? row % 4 * 4 + row / 4 % 4 : row / 2 % 2 * 4 + row / 4 % 4;
+}
+
+// Where a lane reads in a tile, in bytes: pieces differ by an exclusive or.
+// fresh() keeps the compiler from holding every one of them in a register.
+template <int D>
+struct Places {
+  int along, across;
+
+  __device__ __forceinline__ Places() {
+    const int l = int(threadIdx.x) % kWave, h = l / 32, row = l % 16 / 4;
+    along = l % 32 * D * 2 + (h ^ turn_of<D>(l % 32)) * 16;
+    const int col = l % 32 / 16 * 2 + l % 4 / 2;
+    across = (4 * h + row) * D * 2 + (col ^ turn_of<D>(4 * h + row)) * 16 + l % 2 * 8;
+  }
+  __device__ __forceinline__ Places fresh() const {
+    Places p = *this;
+    asm volatile("" : "+v"(p.along), "+v"(p.across));
+    return p;
+  }
+};
+
 template <class T, int D>
 struct Rows {
-  T* at;
+  const T* at;
+  Places<D> places;
 
-  // Where piece c (elements 8 c .. + 7) of a row lies.
-  static __device__ __forceinline__ int place(int row, int c) {
-    const int f = D == 128 ? row % 4 * 4 + row / 4 % 4 : row / 2 % 2 * 4 + row / 4 % 4;
-    return row * D + (c ^ f) * 8;
-  }
-  __device__ __forceinline__ void put(int row, int c, typename Frag<T>::type v) const {
-    *reinterpret_cast<typename Frag<T>::type*>(at + place(row, c)) = v;
-  }
   // A or B along the rows: lane l has row l % 32 of the 32 from `row`, elements
   // 16 k + 8 (l / 32) .. + 7.
   __device__ __forceinline__ typename Frag<T>::type along(int row, int k) const {
-    const int l = int(threadIdx.x) % kWave;
-    return *reinterpret_cast<const typename Frag<T>::type*>(at + place(row + l % 32, 2 * k + l / 32));
+    return *reinterpret_cast<const typename Frag<T>::type*>(
+        reinterpret_cast<const char*>(at) + row * D * 2 + (places.along ^ (k << 5)));
   }
   // A across the rows: lane l has column 32 c + l % 32 of the rows row + 4 h +
-  // {0..3} and row + 8 + 4 h + {0..3}, h = l / 32.  Sixteen lanes read four rows
-  // of sixteen columns, four elements each, and get a column of four.
+  // {0..3} and row + 8 + 4 h + {0..3}, h = l / 32; row is a multiple of 16.
+  // Sixteen lanes read four rows of sixteen columns, four elements each, and
+  // get a column of four.
   __device__ __forceinline__ typename Frag<T>::type across(int row, int c) const {
-    const int l = int(threadIdx.x) % kWave;
-    const int r = row + 4 * (l / 32) + l % 16 / 4, col = 4 * c + l % 32 / 16 * 2 + l % 4 / 2;
-    const auto lo = turned(at + place(r, col) + l % 2 * 4);
-    const auto hi = turned(at + place(r + 8, col) + l % 2 * 4);
+    const int at0 = places.across ^ (c << 6);
+    const auto lo = turned(row * D * 2 + at0), hi = turned((row + 8) * D * 2 + (at0 ^ 32));
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   }
 
  private:
   typedef T Four __attribute__((ext_vector_type(4)));
-  static __device__ __forceinline__ Four turned(const T* p) {
+  __device__ __forceinline__ Four turned(int byte) const {
     typedef short Raw __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) Raw Lds;
-    return __builtin_bit_cast(Four, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(p)));
+    return __builtin_bit_cast(Four, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                        (Lds*)(reinterpret_cast<const char*>(at) + byte)));
   }
 };
 
@@ -185,8 +202,13 @@ struct Fill {
 
   __device__ __forceinline__ Fill(int dim) {
     row = int(threadIdx.x) / (D / 8);
-    const int c = Rows<T, D>::place(row, int(threadIdx.x) % (D / 8)) % D / 8;
+    const int c = int(threadIdx.x) % (D / 8) ^ turn_of<D>(row);
     d = min(8 * c, dim - 8);  // behind the head's last element: what is there twice is not used
+  }
+  __device__ __forceinline__ Fill fresh() const {  // as Places::fresh
+    Fill f = *this;
+    asm volatile("" : "+v"(f.row), "+v"(f.d));
+    return f;
   }
   __device__ __forceinline__ static T* at(T* tile, int p) {
     return tile + (p * kThreads + int(threadIdx.x) / kWave * kWave) * 8;

@@ -45,8 +45,8 @@ struct Sweep {
   // Adds a tile of keys, of which the lane's row sees those up to `last`
   // (`whole`: all rows of the wave see all).
   __device__ __forceinline__ void add(const T* k_tile, const T* v_tile, int j0, int last,
-                                      bool whole, float c) {
-    const Rows<T, D> ks = {const_cast<T*>(k_tile)}, vs = {const_cast<T*>(v_tile)};
+                                      bool whole, float c, const Places<D>& places) {
+    const Rows<T, D> ks = {k_tile, places.fresh()}, vs = {v_tile, ks.places};
     Acc x[kKeys / 32];
 #pragma unroll
     for (int t = 0; t < kKeys / 32; ++t) {
@@ -130,16 +130,17 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendArgs a, int t
   w.most = -INFINITY;
   w.sum = 0.f;
   const float c = a.scale * kLog2e;
+  const Places<D> places;
   const Fill<T, D, kKeys, kThreads> fill(a.dim);
   if (end > 0) fetch<T, D>(a, s, kv, 0, fill, k_even, v_even);
   for (int j0 = 0; j0 < end; j0 += 2 * kKeys) {
     __syncthreads();  // the tile is there, and nobody reads the other buffer any more
     if (j0 + kKeys < end) fetch<T, D>(a, s, kv, j0 + kKeys, fill, k_odd, v_odd);
-    if (j0 <= any) w.add(k_even, v_even, j0, last, j0 + kKeys - 1 <= all, c);
+    if (j0 <= any) w.add(k_even, v_even, j0, last, j0 + kKeys - 1 <= all, c, places);
     if (j0 + kKeys >= end) break;
     __syncthreads();
     if (j0 + 2 * kKeys < end) fetch<T, D>(a, s, kv, j0 + 2 * kKeys, fill, k_even, v_even);
-    if (j0 + kKeys <= any) w.add(k_odd, v_odd, j0 + kKeys, last, j0 + 2 * kKeys - 1 <= all, c);
+    if (j0 + kKeys <= any) w.add(k_odd, v_odd, j0 + kKeys, last, j0 + 2 * kKeys - 1 <= all, c, places);
   }
   const float sum = w.sum + __shfl_xor(w.sum, 32);
   if (!on) return;

@@ -56,13 +56,13 @@ struct RowTile {
 __device__ __forceinline__ RowTile row_tile(const AttendArgs& a, int r0) {
   return {r0, r0 / a.group, r0 % a.group};
 }
-__device__ __forceinline__ void advance(const AttendArgs& a, RowTile& t) {
-  t.r0 += kTile;
-  t.query += kTile / a.group;
-  t.rest += kTile % a.group;
-  if (t.rest >= a.group) {
-    t.rest -= a.group;
-    ++t.query;
+__device__ __forceinline__ void retreat(const AttendArgs& a, RowTile& t) {
+  t.r0 -= kTile;
+  t.query -= kTile / a.group;
+  t.rest -= kTile % a.group;
+  if (t.rest < 0) {
+    t.rest += a.group;
+    --t.query;
   }
 }
 
@@ -74,14 +74,15 @@ struct Stats {
 template <class T, int D>
 __device__ __forceinline__ void fetch_rows(const AttendArgs& a, const Seq& s, int kv, int rows,
                                            const RowTile& t,
-                                           const Fill<T, D, kTile, kThreads>& fill, T* q_tile,
+                                           const Fill<T, D, kTile, kThreads>& held, T* q_tile,
                                            T* o_tile, Stats* stats) {
   typedef Fill<T, D, kTile, kThreads> F;
+  const F fill = held.fresh();
   const int most = t.rest + rows - 1 - t.r0;
   auto row_of = [&](int i) -> QueryRow {
-    const int x = min(t.rest + i, most), q = int(__umulhi(uint32_t(x), a.per_group));
-    return a.group == 1 ? QueryRow{t.query + x, kv}
-                        : QueryRow{t.query + q, kv * a.group + x - q * a.group};
+    const int x = min(t.rest + i, most), y = int(__umulhi(uint32_t(x), a.per_group));
+    const int q = a.per_group ? y : x;  // 0: groups of one
+    return {t.query + q, kv * a.group + x - q * a.group};
   };
 #pragma unroll
   for (int p = 0; p < F::kRounds; ++p) {
@@ -90,73 +91,106 @@ __device__ __forceinline__ void fetch_rows(const AttendArgs& a, const Seq& s, in
     to_lds(head_row<T>(a.d_out, int64_t(s.q0) + r.query, r.head) + fill.d, F::at(o_tile, p));
   }
   const int wave = int(threadIdx.x) / kWave;
-  if (wave < 2) {
-    const QueryRow r = row_of(int(threadIdx.x) % kWave);
+  constexpr int kParts = kTile / kWave;  // waves that bring one of the statistics
+  if (wave < 2 * kParts) {
+    const int part = wave % kParts * kWave;
+    const QueryRow r = row_of(part + int(threadIdx.x) % kWave);
     const int64_t n = int64_t(r.head) * a.q_rows + s.q0 + r.query;
+    const bool second = wave >= kParts;
     typedef __attribute__((address_space(1))) const void Global;
     typedef __attribute__((address_space(3))) void Lds;
-    __builtin_amdgcn_global_load_lds((Global*)((wave ? a.delta : a.lse2) + n),
-                                     (Lds*)(wave ? stats->delta : stats->lse2), 4, 0, 0);
+    __builtin_amdgcn_global_load_lds((Global*)((second ? a.delta : a.lse2) + n),
+                                     (Lds*)((second ? stats->delta : stats->lse2) + part), 4, 0, 0);
   }
 }
 
 // 32 keys of a wave (lane l has key l % 32) against the rows it is given: the
-// lanes' columns are keys, their values run along the query rows.
+// lanes' columns are keys, their values run along the query rows.  The sums
+// (D / 32 tiles each) and the keys and values take most of the 256 registers
+// that leave two waves on a unit; of 128 elements the values' upper half stays
+// in LDS for that.
 template <class T, int D>
 struct KeySweep {
-  typename Frag<T>::type k[D / 16], v[D / 16];
+  static constexpr int kHeld = D == 128 ? D / 32 : D / 16;  // pieces of the values in registers
+  typename Frag<T>::type k[D / 16], v[kHeld];
   Acc dk[D / 32], dv[D / 32];
 
-  // Rows half .. half + 31 of a tile; the lane's key is seen by the tile's rows
+  // Rows part .. part + 31 of a tile; the lane's key is seen by the tile's rows
   // from `from` to `upto` (`whole`: all of the wave's are by all).
   __device__ __forceinline__ void add(const T* q_tile, const T* o_tile, const Stats& stats,
-                                      int half, int from, int upto, bool whole, float c) {
-    const Rows<T, D> qs = {const_cast<T*>(q_tile)}, os = {const_cast<T*>(o_tile)};
+                                      const Rows<T, 64>& rest, int wave_row, int part, int from,
+                                      int upto, bool whole, float c, const Places<D>& places) {
+    const Rows<T, D> qs = {q_tile, places.fresh()}, os = {o_tile, qs.places};
     typedef float Four __attribute__((ext_vector_type(4)));
     const int h4 = int(threadIdx.x) % kWave / 32 * 4;
     Acc x = Acc(0.f), y;
 #pragma unroll
     for (int i = 0; i < 16; i += 4) {
-      const Four d = *reinterpret_cast<const Four*>(&stats.delta[half + 2 * i + h4]);
+      const Four d = *reinterpret_cast<const Four*>(&stats.delta[part + 2 * i + h4]);
 #pragma unroll
       for (int e = 0; e < 4; ++e) y[i + e] = d[e];
     }
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) x = product(qs.along(half, i), k[i], x);
+    for (int i = 0; i < D / 16; ++i) x = product(qs.along(part, i), k[i], x);
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) y = product(os.along(half, i), v[i], y);
+    for (int i = 0; i < D / 16; ++i)
+      y = product(os.along(part, i), i < kHeld ? v[i] : rest.along(wave_row, i - kHeld), y);
     if (!whole) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const int r = half + c_row(i);
+        const int r = part + c_row(i);
         if (r < from || r > upto) x[i] = -INFINITY;
       }
     }
 #pragma unroll
     for (int i = 0; i < 16; i += 4) {
-      const Four l = *reinterpret_cast<const Four*>(&stats.lse2[half + 2 * i + h4]);
+      const Four l = *reinterpret_cast<const Four*>(&stats.lse2[part + 2 * i + h4]);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[i + e] = pow2(__builtin_fmaf(x[i + e], c, -l[e]));
+      for (int e = 0; e < 4; ++e) {
+        x[i + e] = pow2(__builtin_fmaf(x[i + e], c, -l[e]));
+        y[i + e] *= x[i + e];
+      }
     }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) y[i] *= x[i];
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
       const auto pb = narrow<T>(x, p), db = narrow<T>(y, p);
 #pragma unroll
-      for (int d = 0; d < D / 32; ++d) dv[d] = product(os.across(half + 16 * p, d), pb, dv[d]);
+      for (int d = 0; d < D / 32; ++d) dv[d] = product(os.across(part + 16 * p, d), pb, dv[d]);
 #pragma unroll
-      for (int d = 0; d < D / 32; ++d) dk[d] = product(qs.across(half + 16 * p, d), db, dk[d]);
+      for (int d = 0; d < D / 32; ++d) dk[d] = product(qs.across(part + 16 * p, d), db, dk[d]);
     }
+  }
+
+  // A wave's sums to and from another's, through two buffers.
+  __device__ __forceinline__ void hand(float* a, float* b) const {
+    const int lane = int(threadIdx.x) % kWave;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        a[(d * 16 + i) * kWave + lane] = dk[d][i];
+        b[(d * 16 + i) * kWave + lane] = dv[d][i];
+      }
+  }
+  __device__ __forceinline__ void take(const float* a, const float* b) {
+    const int lane = int(threadIdx.x) % kWave;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        dk[d][i] += a[(d * 16 + i) * kWave + lane];
+        dv[d][i] += b[(d * 16 + i) * kWave + lane];
+      }
   }
 };
 
 // A block holds 64 keys; waves 0 and 1 take the even 32 rows of each tile with
 // keys 0 .. 31 and 32 .. 63, waves 2 and 3 the odd 32; their sums meet at the end.
 template <class T, int D>
-__global__ __launch_bounds__(kThreads, 1) void keys_kernel(AttendArgs a, int tiles) {
+__global__ __launch_bounds__(kThreads, 2) void keys_kernel(AttendArgs a, int tiles) {
   __shared__ __attribute__((aligned(16))) T q_even[kTile * D], o_even[kTile * D];
   __shared__ __attribute__((aligned(16))) T q_odd[kTile * D], o_odd[kTile * D];
+  __shared__ __attribute__((aligned(16))) T v_rest[KeySweep<T, D>::kHeld < D / 16 ? kKeysOfBlock * 64 : 8];
   __shared__ __attribute__((aligned(16))) Stats s_even, s_odd;
   const Work work = work_of(int(blockIdx.x), tiles, a.q_heads / a.group);
   if (work.tile >= tiles) return;
@@ -165,70 +199,69 @@ __global__ __launch_bounds__(kThreads, 1) void keys_kernel(AttendArgs a, int til
   const int first = tile.index * kKeysOfBlock;
   if (tile.index < 0 || first >= s.slot) return;
   const int lane = int(threadIdx.x) % kWave, wave = int(threadIdx.x) / kWave;
-  const int kv = work.kv, half = wave / 2 * 32, wave_key = first + wave % 2 * 32;
+  const int kv = work.kv, part = wave / 2 * 32, wave_row = wave % 2 * 32, wave_key = first + wave_row;
+  const float c = a.scale * kLog2e;
+  const Places<D> places;
+  const Rows<T, 64> rest = {v_rest, Places<64>()};
+  const int rows = first < s.keys ? s.queries * a.group : 0, ahead = s.keys - s.queries;
+  // The first row that sees a key.
+  auto seen_from = [&](int key) { return a.causal ? max(0, key - ahead) * a.group : 0; };
   const int j = wave_key + lane % 32;
   const bool on = j < s.keys;
-  const int64_t key = int64_t(s.k0) + (on ? j : 0);
+  const int from = on ? seen_from(j) : rows;
   KeySweep<T, D> w;
+  {
+    const int64_t key = int64_t(s.k0) + (on ? j : 0);
+    const T *k_row = head_row<T>(a.k, key, kv), *v_row = head_row<T>(a.v, key, kv);
+    const int h = lane / 32, row = wave_row + lane % 32;
 #pragma unroll
-  for (int i = 0; i < D / 16; ++i) {
-    w.k[i] = piece(head_row<T>(a.k, key, kv), 16 * i + 8 * (lane / 32), a.dim, on);
-    w.v[i] = piece(head_row<T>(a.v, key, kv), 16 * i + 8 * (lane / 32), a.dim, on);
+    for (int i = 0; i < D / 16; ++i) {
+      w.k[i] = piece(k_row, 16 * i + 8 * h, a.dim, on);
+      const auto v = piece(v_row, 16 * i + 8 * h, a.dim, on);
+      if (i < KeySweep<T, D>::kHeld)
+        w.v[i] = v;
+      else if (part == 0)
+        *reinterpret_cast<typename Frag<T>::type*>(
+            v_rest + row * 64 + ((2 * (i - KeySweep<T, D>::kHeld) + h) ^ turn_of<64>(row)) * 8) = v;
+    }
   }
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) w.dk[i] = w.dv[i] = Acc(0.f);
-  const float c = a.scale * kLog2e;
-  const int rows = first < s.keys ? s.queries * a.group : 0, ahead = s.keys - s.queries;
-  // The first row that sees a key: the block's first, the lane's, the wave's
-  // last and first.
-  auto seen_from = [&](int key) { return a.causal ? max(0, key - ahead) * a.group : 0; };
   const int begin = rows > 0 ? seen_from(first) / kTile * kTile : 0;
-  const int from = on ? seen_from(j) : rows;
   const int all = wave_key + 31 < s.keys ? seen_from(wave_key + 31) : rows;
   const int any = wave_key < s.keys ? seen_from(wave_key) : rows;
   const Fill<T, D, kTile, kThreads> fill(a.dim);
-  RowTile t = row_tile(a, begin);
+  // From the last rows, which see every key, to the first: blocks that run side
+  // by side read the same rows at the same time.
+  const int end = rows > 0 ? (rows - 1) / kTile * kTile : -1;
+  RowTile t = row_tile(a, max(end, 0));
   auto step = [&](int r0, const T* q_tile, const T* o_tile, const Stats& stats) {
-    if (r0 + half + 31 < any || r0 + half >= rows) return;
-    w.add(q_tile, o_tile, stats, half, from - r0, rows - 1 - r0,
-          r0 + half >= all && r0 + half + 31 < rows, c);
+    const int r = r0 + part;
+    if (r + 31 < any || r >= rows) return;
+    w.add(q_tile, o_tile, stats, rest, wave_row, part, from - r0, rows - 1 - r0,
+          r >= all && r + 31 < rows, c, places);
   };
-  if (begin < rows) fetch_rows<T, D>(a, s, kv, rows, t, fill, q_even, o_even, &s_even);
-  for (int r0 = begin; r0 < rows; r0 += 2 * kTile) {
+  if (end >= begin) fetch_rows<T, D>(a, s, kv, rows, t, fill, q_even, o_even, &s_even);
+  for (int r0 = end; r0 >= begin; r0 -= 2 * kTile) {
     __syncthreads();  // the tile is there, and nobody reads the other buffer any more
-    advance(a, t);
-    if (t.r0 < rows) fetch_rows<T, D>(a, s, kv, rows, t, fill, q_odd, o_odd, &s_odd);
+    retreat(a, t);
+    if (t.r0 >= begin) fetch_rows<T, D>(a, s, kv, rows, t, fill, q_odd, o_odd, &s_odd);
     step(r0, q_even, o_even, s_even);
-    if (r0 + kTile >= rows) break;
+    if (r0 - kTile < begin) break;
     __syncthreads();
-    advance(a, t);
-    if (t.r0 < rows) fetch_rows<T, D>(a, s, kv, rows, t, fill, q_even, o_even, &s_even);
-    step(r0 + kTile, q_odd, o_odd, s_odd);
+    retreat(a, t);
+    if (t.r0 >= begin) fetch_rows<T, D>(a, s, kv, rows, t, fill, q_even, o_even, &s_even);
+    step(r0 - kTile, q_odd, o_odd, s_odd);
   }
-  // Waves 2 and 3 hand over their sums, D / 32 tiles of 16 values a lane, in
-  // two turns through one buffer each.
-  static_assert(sizeof(q_even) >= size_t(D) / 32 * 16 * kWave * 2 * sizeof(T), "a wave's sums");
-  float* const hand = reinterpret_cast<float*>(wave % 2 ? o_even : q_even);
-  float* const hand2 = reinterpret_cast<float*>(wave % 2 ? o_odd : q_odd);
+  // Waves 2 and 3 hand their sums to waves 0 and 1.
+  static_assert(sizeof(q_even) == size_t(D) / 32 * 16 * kWave * sizeof(float), "a wave's sums");
+  float* const buf_k = reinterpret_cast<float*>(wave % 2 ? q_odd : q_even);
+  float* const buf_v = reinterpret_cast<float*>(wave % 2 ? o_odd : o_even);
   __syncthreads();
-  if (wave >= 2) {
-#pragma unroll
-    for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        hand[(d * 16 + i) * kWave + lane] = w.dk[d][i];
-        hand2[(d * 16 + i) * kWave + lane] = w.dv[d][i];
-      }
-  }
+  if (wave >= 2) w.hand(buf_k, buf_v);
   __syncthreads();
   if (wave >= 2 || j >= s.slot) return;
-#pragma unroll
-  for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      w.dk[d][i] += hand[(d * 16 + i) * kWave + lane];
-      w.dv[d][i] += hand2[(d * 16 + i) * kWave + lane];
-    }
+  w.take(buf_k, buf_v);
   store_column<T, D>(head_row<T>(a.d_k, int64_t(s.k0) + j, kv), w.dk, a.dim, a.scale);
   store_column<T, D>(head_row<T>(a.d_v, int64_t(s.k0) + j, kv), w.dv, a.dim, 1.f);
 }
@@ -257,8 +290,8 @@ struct RowSweep {
   float lse2, delta;
 
   __device__ __forceinline__ void add(const T* k_tile, const T* v_tile, int j0, int last,
-                                      bool whole, float c) {
-    const Rows<T, D> ks = {const_cast<T*>(k_tile)}, vs = {const_cast<T*>(v_tile)};
+                                      bool whole, float c, const Places<D>& places) {
+    const Rows<T, D> ks = {k_tile, places.fresh()}, vs = {v_tile, ks.places};
 #pragma unroll
     for (int t = 0; t < kTile / 32; ++t) {
       Acc x = Acc(0.f), y = Acc(delta);
@@ -321,16 +354,17 @@ __global__ __launch_bounds__(kThreads, 2) void queries_kernel(AttendArgs a, int 
   w.lse2 = on ? a.lse2[n] : INFINITY;
   w.delta = on ? a.delta[n] : 0.f;
   const float c = a.scale * kLog2e;
+  const Places<D> places;
   const Fill<T, D, kTile, kThreads> fill(a.dim);
   if (end > 0) fetch_keys<T, D>(a, s, kv, 0, fill, k_even, v_even);
   for (int j0 = 0; j0 < end; j0 += 2 * kTile) {
     __syncthreads();
     if (j0 + kTile < end) fetch_keys<T, D>(a, s, kv, j0 + kTile, fill, k_odd, v_odd);
-    if (j0 <= any) w.add(k_even, v_even, j0, last, j0 + kTile - 1 <= all, c);
+    if (j0 <= any) w.add(k_even, v_even, j0, last, j0 + kTile - 1 <= all, c, places);
     if (j0 + kTile >= end) break;
     __syncthreads();
     if (j0 + 2 * kTile < end) fetch_keys<T, D>(a, s, kv, j0 + 2 * kTile, fill, k_even, v_even);
-    if (j0 + kTile <= any) w.add(k_odd, v_odd, j0 + kTile, last, j0 + 2 * kTile - 1 <= all, c);
+    if (j0 + kTile <= any) w.add(k_odd, v_odd, j0 + kTile, last, j0 + 2 * kTile - 1 <= all, c, places);
   }
   if (on) store_column<T, D>(head_row<T>(a.d_q, s.q0 + me.query, me.head), w.dq, a.dim, a.scale);
 }
