@@ -45,6 +45,10 @@ struct AttendArgs {
   const int32_t *q_offsets, *k_offsets, *k_lengths;
   int32_t n_seqs, q_rows, k_rows, q_heads, group, dim, causal;
   uint32_t per_group;  // ceil(2^32 / group), in 32 bits: quotients of small numbers
+  // Rows of a tile lie within 2^31 bytes, and those that one thread brings are
+  // at equal distances (groups of 1, 2, 4, 8 or 16): addresses are a sum for
+  // the block and a distance for the lane.
+  int32_t near_k, near_q;
   float scale;
 };
 
@@ -53,6 +57,10 @@ __device__ __forceinline__ T* head_row(const HeadsView& x, int64_t row, int head
   return reinterpret_cast<T*>(x.data) + row * x.row + int64_t(head) * x.head;
 }
 
+// A value that all lanes of a wave share, held once for the wave.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int wave_id() { return uniform(int(threadIdx.x) / kWave); }
+
 // A sequence: where its queries and keys begin, and how many there are; slot
 // counts the key rows that it owns, keys those in use.
 struct Seq {
@@ -60,11 +68,11 @@ struct Seq {
 };
 __device__ __forceinline__ Seq sequence(const AttendArgs& a, int b) {
   Seq s;
-  s.q0 = offset_at(a.q_offsets, b, a.q_rows);
-  s.k0 = offset_at(a.k_offsets, b, a.k_rows);
-  s.queries = max(0, offset_at(a.q_offsets, b + 1, a.q_rows) - s.q0);
-  s.slot = max(0, offset_at(a.k_offsets, b + 1, a.k_rows) - s.k0);
-  s.keys = a.k_lengths ? min(s.slot, max(0, a.k_lengths[b])) : s.slot;
+  s.q0 = uniform(offset_at(a.q_offsets, b, a.q_rows));
+  s.k0 = uniform(offset_at(a.k_offsets, b, a.k_rows));
+  s.queries = max(0, uniform(offset_at(a.q_offsets, b + 1, a.q_rows)) - s.q0);
+  s.slot = max(0, uniform(offset_at(a.k_offsets, b + 1, a.k_rows)) - s.k0);
+  s.keys = a.k_lengths ? min(s.slot, max(0, uniform(a.k_lengths[b]))) : s.slot;
   return s;
 }
 
@@ -80,10 +88,10 @@ __device__ __forceinline__ Tile tile_of(const int32_t* offsets, int n_seqs, int 
   int lo = 0, hi = n_seqs;
   while (hi - lo > 1) {
     const int mid = (lo + hi) / 2;
-    if (offset_at(offsets, mid, rows) * group / tile + mid <= number) lo = mid;
+    if (uniform(offset_at(offsets, mid, rows)) * group / tile + mid <= number) lo = mid;
     else hi = mid;
   }
-  return {lo, number - (offset_at(offsets, lo, rows) * group / tile + lo)};
+  return {lo, number - (uniform(offset_at(offsets, lo, rows)) * group / tile + lo)};
 }
 
 inline int64_t tile_count(int64_t rows, int n_seqs, int tile) { return rows / tile + n_seqs; }
@@ -186,11 +194,10 @@ struct Rows {
 // A tile's 16 bytes per thread from memory to LDS without a register between:
 // a wave fills 1024 bytes in a row, so the permutation is in what a lane reads.
 // Nothing waits for it until the next barrier.
-template <class T>
-__device__ __forceinline__ void to_lds(const T* from, T* wave_at) {
+__device__ __forceinline__ void to_lds(const char* from, uint32_t lane_bytes, void* wave_at) {
   typedef __attribute__((address_space(1))) const void Global;
   typedef __attribute__((address_space(3))) void Lds;
-  __builtin_amdgcn_global_load_lds((Global*)from, (Lds*)wave_at, 16, 0, 0);
+  __builtin_amdgcn_global_load_lds((Global*)(from + lane_bytes), (Lds*)wave_at, 16, 0, 0);
 }
 
 // Threads of a block over a tile of kRows rows: round p of a thread brings one
@@ -201,17 +208,56 @@ struct Fill {
   int row, d;  // of this thread
 
   __device__ __forceinline__ Fill(int dim) {
-    row = int(threadIdx.x) / (D / 8);
-    const int c = int(threadIdx.x) % (D / 8) ^ turn_of<D>(row);
+    int t = int(threadIdx.x);
+    asm volatile("" : "+v"(t));  // formed where it is used, not held in registers
+    row = t / (D / 8);
+    const int c = t % (D / 8) ^ turn_of<D>(row);
     d = min(8 * c, dim - 8);  // behind the head's last element: what is there twice is not used
   }
-  __device__ __forceinline__ Fill fresh() const {  // as Places::fresh
-    Fill f = *this;
-    asm volatile("" : "+v"(f.row), "+v"(f.d));
-    return f;
+  // The lane's bytes from row 0 of the tile, rows of a head `row_stride` apart.
+  __device__ __forceinline__ uint32_t bytes(int64_t row_stride) const {
+    return uint32_t(row * row_stride + d) * 2;
   }
   __device__ __forceinline__ static T* at(T* tile, int p) {
-    return tile + (p * kThreads + int(threadIdx.x) / kWave * kWave) * 8;
+    return tile + (p * kThreads + wave_id() * kWave) * 8;
+  }
+};
+
+// Tiles of kRows keys and values of one sequence and key head.
+template <class T, int D, int kRows, int kThreads>
+struct KeyTiles {
+  typedef Fill<T, D, kRows, kThreads> F;
+  const char *k, *v;     // the sequence's first row
+  uint32_t k_lane, v_lane;
+  int64_t k_row, v_row;  // bytes
+  int keys, near;
+
+  __device__ __forceinline__ KeyTiles(const AttendArgs& a, const Seq& s, int kv)
+      : k(reinterpret_cast<const char*>(head_row<T>(a.k, s.k0, kv))),
+        v(reinterpret_cast<const char*>(head_row<T>(a.v, s.k0, kv))),
+        k_row(a.k.row * 2), v_row(a.v.row * 2), keys(s.keys), near(a.near_k) {
+    const F fill(a.dim);
+    k_lane = fill.bytes(a.k.row);
+    v_lane = fill.bytes(a.v.row);
+  }
+  // Rows j0 .. to LDS; those behind the last key repeat it, their probabilities
+  // are zero.
+  __device__ __forceinline__ void fetch(int j0, T* k_tile, T* v_tile, int dim) const {
+    if (near && j0 + kRows <= keys) {
+#pragma unroll
+      for (int p = 0; p < F::kRounds; ++p) {
+        to_lds(k + (j0 + p * F::kStep) * k_row, k_lane, F::at(k_tile, p));
+        to_lds(v + (j0 + p * F::kStep) * v_row, v_lane, F::at(v_tile, p));
+      }
+      return;
+    }
+    const F fill(dim);
+#pragma unroll
+    for (int p = 0; p < F::kRounds; ++p) {
+      const int row = min(j0 + fill.row + p * F::kStep, keys - 1);
+      to_lds(k + row * k_row + fill.d * 2, 0, F::at(k_tile, p));
+      to_lds(v + row * v_row + fill.d * 2, 0, F::at(v_tile, p));
+    }
   }
 };
 

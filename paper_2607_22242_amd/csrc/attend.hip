@@ -19,21 +19,6 @@ constexpr int kKeys = 64;          // of a tile
 // reference moves: the sums stay in 32 bits, and rescaling is rare.
 constexpr float kSlack = 8.f;
 
-// Keys and values of a tile to LDS; rows behind the last key repeat it, their
-// probabilities are zero.
-template <class T, int D>
-__device__ __forceinline__ void fetch(const AttendArgs& a, const Seq& s, int kv, int j0,
-                                      const Fill<T, D, kKeys, kThreads>& fill, T* k_tile,
-                                      T* v_tile) {
-  typedef Fill<T, D, kKeys, kThreads> F;
-#pragma unroll
-  for (int p = 0; p < F::kRounds; ++p) {
-    const int64_t row = int64_t(s.k0) + min(j0 + fill.row + p * F::kStep, s.keys - 1);
-    to_lds(head_row<T>(a.k, row, kv) + fill.d, F::at(k_tile, p));
-    to_lds(head_row<T>(a.v, row, kv) + fill.d, F::at(v_tile, p));
-  }
-}
-
 // A wave's 32 query rows (lane l has row l % 32) and what has been added up
 // over the keys so far.
 template <class T, int D>
@@ -107,7 +92,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendArgs a, int t
   const Seq s = sequence(a, tile.seq);
   const int first = tile.index * kRowsOfBlock, rows = s.queries * a.group;
   if (tile.index < 0 || first >= rows) return;
-  const int lane = int(threadIdx.x) % kWave, wave = int(threadIdx.x) / kWave;
+  const int lane = int(threadIdx.x) % kWave, wave = wave_id();
   const int kv = work.kv, r = first + 32 * wave + lane % 32;
   const bool on = r < rows;
   const QueryRow me = query_row(a, kv, on ? r : 0);
@@ -131,15 +116,15 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendArgs a, int t
   w.sum = 0.f;
   const float c = a.scale * kLog2e;
   const Places<D> places;
-  const Fill<T, D, kKeys, kThreads> fill(a.dim);
-  if (end > 0) fetch<T, D>(a, s, kv, 0, fill, k_even, v_even);
+  const KeyTiles<T, D, kKeys, kThreads> tiles_of(a, s, kv);
+  if (end > 0) tiles_of.fetch(0, k_even, v_even, a.dim);
   for (int j0 = 0; j0 < end; j0 += 2 * kKeys) {
     __syncthreads();  // the tile is there, and nobody reads the other buffer any more
-    if (j0 + kKeys < end) fetch<T, D>(a, s, kv, j0 + kKeys, fill, k_odd, v_odd);
+    if (j0 + kKeys < end) tiles_of.fetch(j0 + kKeys, k_odd, v_odd, a.dim);
     if (j0 <= any) w.add(k_even, v_even, j0, last, j0 + kKeys - 1 <= all, c, places);
     if (j0 + kKeys >= end) break;
     __syncthreads();
-    if (j0 + 2 * kKeys < end) fetch<T, D>(a, s, kv, j0 + 2 * kKeys, fill, k_even, v_even);
+    if (j0 + 2 * kKeys < end) tiles_of.fetch(j0 + 2 * kKeys, k_even, v_even, a.dim);
     if (j0 + kKeys <= any) w.add(k_odd, v_odd, j0 + kKeys, last, j0 + 2 * kKeys - 1 <= all, c, places);
   }
   const float sum = w.sum + __shfl_xor(w.sum, 32);
@@ -182,6 +167,11 @@ AttendArgs attend_args(const sched_attention_desc& d) {
   a.group = d.q_heads / d.kv_heads;
   a.per_group = uint32_t(((uint64_t(1) << 32) + a.group - 1) / a.group);
   a.dim = d.head_dim;
+  auto near = [](const sched_heads& h) {
+    return h.row_stride < (int64_t(1) << 24) && h.head_stride < (int64_t(1) << 24);
+  };
+  a.near_k = near(d.k) && near(d.v);
+  a.near_q = near(d.q) && 16 % a.group == 0;
   a.causal = d.causal;
   a.scale = d.scale;
   return a;

@@ -70,39 +70,66 @@ struct Stats {
   float lse2[kTile], delta[kTile];
 };
 
-// Q, dO and the rows' statistics to LDS; rows behind the last repeat it.
+// Tiles of query rows of one sequence and the heads of one key head: Q, dO and
+// the rows' statistics.
 template <class T, int D>
-__device__ __forceinline__ void fetch_rows(const AttendArgs& a, const Seq& s, int kv, int rows,
-                                           const RowTile& t,
-                                           const Fill<T, D, kTile, kThreads>& held, T* q_tile,
-                                           T* o_tile, Stats* stats) {
+struct RowTiles {
   typedef Fill<T, D, kTile, kThreads> F;
-  const F fill = held.fresh();
-  const int most = t.rest + rows - 1 - t.r0;
-  auto row_of = [&](int i) -> QueryRow {
-    const int x = min(t.rest + i, most), y = int(__umulhi(uint32_t(x), a.per_group));
-    const int q = a.per_group ? y : x;  // 0: groups of one
-    return {t.query + q, kv * a.group + x - q * a.group};
-  };
+  uint32_t q_lane, o_lane;
+
+  __device__ __forceinline__ RowTiles(const AttendArgs& a) {
+    const F fill(a.dim);
+    auto lane = [&](const HeadsView& x) {
+      return uint32_t(fill.row / a.group * x.row + fill.row % a.group * x.head + fill.d) * 2;
+    };
+    q_lane = lane(a.q);
+    o_lane = lane(a.d_out);
+  }
+  // Rows behind the last repeat it.
+  __device__ __forceinline__ void fetch(const AttendArgs& a, const Seq& s, int kv, int rows,
+                                        const RowTile& t, T* q_tile, T* o_tile,
+                                        Stats* stats) const {
+    const int most = t.rest + rows - 1 - t.r0;
+    auto row_of = [&](int i) -> QueryRow {
+      const int x = min(t.rest + i, most), y = int(__umulhi(uint32_t(x), a.per_group));
+      const int q = a.per_group ? y : x;  // 0: groups of one
+      return {t.query + q, kv * a.group + x - q * a.group};
+    };
+    if (a.near_q && t.r0 + kTile <= rows) {
+      const int64_t row = int64_t(s.q0) + t.query;
+      const int step = F::kStep / a.group;
 #pragma unroll
-  for (int p = 0; p < F::kRounds; ++p) {
-    const QueryRow r = row_of(fill.row + p * F::kStep);
-    to_lds(head_row<T>(a.q, int64_t(s.q0) + r.query, r.head) + fill.d, F::at(q_tile, p));
-    to_lds(head_row<T>(a.d_out, int64_t(s.q0) + r.query, r.head) + fill.d, F::at(o_tile, p));
+      for (int p = 0; p < F::kRounds; ++p) {
+        to_lds(reinterpret_cast<const char*>(head_row<T>(a.q, row + p * step, kv * a.group)), q_lane,
+               F::at(q_tile, p));
+        to_lds(reinterpret_cast<const char*>(head_row<T>(a.d_out, row + p * step, kv * a.group)),
+               o_lane, F::at(o_tile, p));
+      }
+    } else {
+      const F fill(a.dim);
+#pragma unroll
+      for (int p = 0; p < F::kRounds; ++p) {
+        const QueryRow r = row_of(fill.row + p * F::kStep);
+        const int64_t row = int64_t(s.q0) + r.query;
+        to_lds(reinterpret_cast<const char*>(head_row<T>(a.q, row, r.head) + fill.d), 0,
+               F::at(q_tile, p));
+        to_lds(reinterpret_cast<const char*>(head_row<T>(a.d_out, row, r.head) + fill.d), 0,
+               F::at(o_tile, p));
+      }
+    }
+    const int wave = wave_id();
+    if (wave < 2) {
+      int lane = int(threadIdx.x) % kWave;
+      asm volatile("" : "+v"(lane));
+      const QueryRow r = row_of(lane);
+      const int64_t n = int64_t(r.head) * a.q_rows + s.q0 + r.query;
+      typedef __attribute__((address_space(1))) const void Global;
+      typedef __attribute__((address_space(3))) void Lds;
+      __builtin_amdgcn_global_load_lds((Global*)((wave ? a.delta : a.lse2) + n),
+                                       (Lds*)(wave ? stats->delta : stats->lse2), 4, 0, 0);
+    }
   }
-  const int wave = int(threadIdx.x) / kWave;
-  constexpr int kParts = kTile / kWave;  // waves that bring one of the statistics
-  if (wave < 2 * kParts) {
-    const int part = wave % kParts * kWave;
-    const QueryRow r = row_of(part + int(threadIdx.x) % kWave);
-    const int64_t n = int64_t(r.head) * a.q_rows + s.q0 + r.query;
-    const bool second = wave >= kParts;
-    typedef __attribute__((address_space(1))) const void Global;
-    typedef __attribute__((address_space(3))) void Lds;
-    __builtin_amdgcn_global_load_lds((Global*)((second ? a.delta : a.lse2) + n),
-                                     (Lds*)((second ? stats->delta : stats->lse2) + part), 4, 0, 0);
-  }
-}
+};
 
 // 32 keys of a wave (lane l has key l % 32) against the rows it is given: the
 // lanes' columns are keys, their values run along the query rows.  The sums
@@ -198,7 +225,7 @@ __global__ __launch_bounds__(kThreads, 2) void keys_kernel(AttendArgs a, int til
   const Seq s = sequence(a, tile.seq);
   const int first = tile.index * kKeysOfBlock;
   if (tile.index < 0 || first >= s.slot) return;
-  const int lane = int(threadIdx.x) % kWave, wave = int(threadIdx.x) / kWave;
+  const int lane = int(threadIdx.x) % kWave, wave = wave_id();
   const int kv = work.kv, part = wave / 2 * 32, wave_row = wave % 2 * 32, wave_key = first + wave_row;
   const float c = a.scale * kLog2e;
   const Places<D> places;
@@ -230,7 +257,7 @@ __global__ __launch_bounds__(kThreads, 2) void keys_kernel(AttendArgs a, int til
   const int begin = rows > 0 ? seen_from(first) / kTile * kTile : 0;
   const int all = wave_key + 31 < s.keys ? seen_from(wave_key + 31) : rows;
   const int any = wave_key < s.keys ? seen_from(wave_key) : rows;
-  const Fill<T, D, kTile, kThreads> fill(a.dim);
+  const RowTiles<T, D> tiles_of(a);
   // From the last rows, which see every key, to the first: blocks that run side
   // by side read the same rows at the same time.
   const int end = rows > 0 ? (rows - 1) / kTile * kTile : -1;
@@ -241,16 +268,16 @@ __global__ __launch_bounds__(kThreads, 2) void keys_kernel(AttendArgs a, int til
     w.add(q_tile, o_tile, stats, rest, wave_row, part, from - r0, rows - 1 - r0,
           r >= all && r + 31 < rows, c, places);
   };
-  if (end >= begin) fetch_rows<T, D>(a, s, kv, rows, t, fill, q_even, o_even, &s_even);
+  if (end >= begin) tiles_of.fetch(a, s, kv, rows, t, q_even, o_even, &s_even);
   for (int r0 = end; r0 >= begin; r0 -= 2 * kTile) {
     __syncthreads();  // the tile is there, and nobody reads the other buffer any more
     retreat(a, t);
-    if (t.r0 >= begin) fetch_rows<T, D>(a, s, kv, rows, t, fill, q_odd, o_odd, &s_odd);
+    if (t.r0 >= begin) tiles_of.fetch(a, s, kv, rows, t, q_odd, o_odd, &s_odd);
     step(r0, q_even, o_even, s_even);
     if (r0 - kTile < begin) break;
     __syncthreads();
     retreat(a, t);
-    if (t.r0 >= begin) fetch_rows<T, D>(a, s, kv, rows, t, fill, q_even, o_even, &s_even);
+    if (t.r0 >= begin) tiles_of.fetch(a, s, kv, rows, t, q_even, o_even, &s_even);
     step(r0 - kTile, q_odd, o_odd, s_odd);
   }
   // Waves 2 and 3 hand their sums to waves 0 and 1.
@@ -267,19 +294,6 @@ __global__ __launch_bounds__(kThreads, 2) void keys_kernel(AttendArgs a, int til
 }
 
 // --- dQ -----------------------------------------------------------------------
-
-template <class T, int D>
-__device__ __forceinline__ void fetch_keys(const AttendArgs& a, const Seq& s, int kv, int j0,
-                                           const Fill<T, D, kTile, kThreads>& fill, T* k_tile,
-                                           T* v_tile) {
-  typedef Fill<T, D, kTile, kThreads> F;
-#pragma unroll
-  for (int p = 0; p < F::kRounds; ++p) {
-    const int64_t row = int64_t(s.k0) + min(j0 + fill.row + p * F::kStep, s.keys - 1);
-    to_lds(head_row<T>(a.k, row, kv) + fill.d, F::at(k_tile, p));
-    to_lds(head_row<T>(a.v, row, kv) + fill.d, F::at(v_tile, p));
-  }
-}
 
 // 32 query rows of a wave (lane l has row l % 32): the lanes' columns are query
 // rows, their values run along the keys.
@@ -328,7 +342,7 @@ __global__ __launch_bounds__(kThreads, 2) void queries_kernel(AttendArgs a, int 
   const Seq s = sequence(a, tile.seq);
   const int first = tile.index * kRowsOfBlock, rows = s.queries * a.group;
   if (tile.index < 0 || first >= rows) return;
-  const int lane = int(threadIdx.x) % kWave, wave = int(threadIdx.x) / kWave;
+  const int lane = int(threadIdx.x) % kWave, wave = wave_id();
   const int kv = work.kv, r = first + 32 * wave + lane % 32;
   const bool on = r < rows;
   const QueryRow me = query_row(a, kv, on ? r : 0);
@@ -355,15 +369,15 @@ __global__ __launch_bounds__(kThreads, 2) void queries_kernel(AttendArgs a, int 
   w.delta = on ? a.delta[n] : 0.f;
   const float c = a.scale * kLog2e;
   const Places<D> places;
-  const Fill<T, D, kTile, kThreads> fill(a.dim);
-  if (end > 0) fetch_keys<T, D>(a, s, kv, 0, fill, k_even, v_even);
+  const KeyTiles<T, D, kTile, kThreads> tiles_of(a, s, kv);
+  if (end > 0) tiles_of.fetch(0, k_even, v_even, a.dim);
   for (int j0 = 0; j0 < end; j0 += 2 * kTile) {
     __syncthreads();
-    if (j0 + kTile < end) fetch_keys<T, D>(a, s, kv, j0 + kTile, fill, k_odd, v_odd);
+    if (j0 + kTile < end) tiles_of.fetch(j0 + kTile, k_odd, v_odd, a.dim);
     if (j0 <= any) w.add(k_even, v_even, j0, last, j0 + kTile - 1 <= all, c, places);
     if (j0 + kTile >= end) break;
     __syncthreads();
-    if (j0 + 2 * kTile < end) fetch_keys<T, D>(a, s, kv, j0 + 2 * kTile, fill, k_even, v_even);
+    if (j0 + 2 * kTile < end) tiles_of.fetch(j0 + 2 * kTile, k_even, v_even, a.dim);
     if (j0 + kTile <= any) w.add(k_odd, v_odd, j0 + kTile, last, j0 + 2 * kTile - 1 <= all, c, places);
   }
   if (on) store_column<T, D>(head_row<T>(a.d_q, s.q0 + me.query, me.head), w.dq, a.dim, a.scale);
@@ -415,6 +429,8 @@ hipError_t launch_attention_grad(const sched_attention_desc& d, const sched_head
   a.d_k = view(d_k);
   a.d_v = view(d_v);
   a.lse2 = static_cast<float*>(ws);
+  a.near_q = a.near_q && d_out.row_stride < (int64_t(1) << 24) &&
+             d_out.head_stride < (int64_t(1) << 24);
   a.delta = a.lse2 + size_t(d.q_rows) * size_t(d.q_heads);
   const bool wide = d.head_dim > 64;
   if (d.dtype == SCHED_F16)
