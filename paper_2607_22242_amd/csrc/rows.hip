@@ -18,8 +18,6 @@
 namespace policy {
 namespace {
 
-constexpr int kRowThreads = 256;
-
 struct RowArgs {
   const void* logits;
   int64_t n, vocab, stride;
@@ -90,84 +88,79 @@ __device__ __forceinline__ void widen(float (&x)[N], typename Vec<T>::type v) {
   for (int i = 0; i < N; ++i) x[i] = float(v[i]);
 }
 
-// Statistics of a row, read once by a block.
-template <class T>
-__device__ __forceinline__ Soft row_soft(const T* row, int64_t vocab, float c, Soft* part) {
-  constexpr int N = Vec<T>::kN;
-  Soft a = {-INFINITY, 0.f};
-  const int64_t whole = vocab / N * N;
-  for (int64_t j = int64_t(threadIdx.x) * N; j < whole; j += kRowThreads * N) {
-    float x[N];
-    widen<T>(x, load16(row + j));
-    take(a, x, c);
-  }
-  if (whole + threadIdx.x < vocab) {
-    const float x[1] = {float(row[whole + threadIdx.x])};
-    take(a, x, c);
-  }
-  return block_join(a, c, part);
-}
+// How a row is taken.  Rows of up to 64 logits: a power of two of lanes each, a
+// logit a lane.  Rows whose 16-byte pieces fit the registers of a wave or of a
+// block (kVecs pieces a thread): read once, so that a loss with its gradient
+// costs one read and one write.  Longer ones: read twice by a block of 1024,
+// two of which fill a unit: no more rows are under way than the last cache
+// holds, and the second read comes from there.  131072 logits in bf16 (8,000
+// rows): 0.95 ms so, 1.15 with blocks of 512, 1.22 with 256.
+constexpr int kBlock = 256;  // of rows of lanes or waves
+constexpr int kLongThreads = 1024;
 
-// d_logits of a row: gain (e_t - 2^((x - f) c + u)).  Every element is read
-// and written by the same thread, so that the two may be one.
-template <class T>
-__device__ __forceinline__ void row_grad(const T* row, T* out, int64_t vocab, float c, float f,
-                                         float u, float gain, int64_t t) {
-  constexpr int N = Vec<T>::kN;
-  const int64_t whole = vocab / N * N;
-  for (int64_t j = int64_t(threadIdx.x) * N; j < whole; j += kRowThreads * N) {
-    float x[N];
-    widen<T>(x, load16(row + j));
-    typename Vec<T>::type v;
+// A row's logits in registers: pieces i * kThreads + t of thread t, and one of
+// the logits behind the last whole piece.
+template <class T, int kThreads, int kVecs>
+struct Held {
+  static constexpr int N = Vec<T>::kN;
+  typedef typename Vec<T>::type V;
+  V v[kVecs];
+  float tail;
+
+  __device__ __forceinline__ void load(const T* row, int vocab, int t) {
+    const int pieces = vocab / N;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float p = pow2(__builtin_fmaf(x[i] - f, c, u));
-      v[i] = T(gain * (j + i == t ? 1.f - p : -p));
+    for (int i = 0; i < kVecs; ++i) {
+      v[i] = V(T(-INFINITY));
+      if (i * kThreads + t < pieces) v[i] = load16(row + int64_t(i * kThreads + t) * N);
     }
-    store16(out + j, v);
+    tail = -INFINITY;
+    if (pieces * N + t < vocab) tail = float(row[pieces * N + t]);
   }
-  const int64_t j = whole + threadIdx.x;
-  if (j < vocab) {
-    const float p = pow2(__builtin_fmaf(float(row[j]) - f, c, u));
-    out[j] = T(gain * (j == t ? 1.f - p : -p));
+  __device__ __forceinline__ float most() const {
+    float m = tail;
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+      for (int e = 0; e < N; ++e) m = fmaxf(m, float(v[i][e]));
+    return m;
   }
-}
-
-template <class T>
-__device__ __forceinline__ void row_zero(T* out, int64_t vocab) {
-  constexpr int N = Vec<T>::kN;
-  const int64_t whole = vocab / N * N;
-  for (int64_t j = int64_t(threadIdx.x) * N; j < whole; j += kRowThreads * N)
-    store16(out + j, typename Vec<T>::type(T(0)));
-  if (whole + threadIdx.x < vocab) out[whole + threadIdx.x] = T(0);
-}
-
-template <class T>
-__global__ __launch_bounds__(kRowThreads) void logprobs_kernel(RowArgs a) {
-  __shared__ Soft part[kRowThreads / kWave];
-  const int64_t i = a.first + blockIdx.x;
-  const int64_t t = token_in(a.tokens, i, a.vocab);
-  if (t < 0) {
-    if (threadIdx.x == 0) a.logp[i] = 0.f;
-    return;
+  __device__ __forceinline__ float sum(float f, float c) const {
+    float s = pow2((tail - f) * c);
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+      for (int e = 0; e < N; ++e) s += pow2((float(v[i][e]) - f) * c);
+    return s;
   }
-  const T* row = static_cast<const T*>(a.logits) + i * a.stride;
-  const Soft r = row_soft(row, a.vocab, a.c, part);
-  if (threadIdx.x == 0) a.logp[i] = log_prob(float(row[t]), r, a.c);
-}
-
-template <class T>
-__global__ __launch_bounds__(kRowThreads) void logprobs_grad_kernel(RowArgs a) {
-  const int64_t i = a.first + blockIdx.x;
-  const int64_t t = token_in(a.tokens, i, a.vocab);
-  T* out = static_cast<T*>(a.d_logits) + i * a.d_stride;
-  const float l = a.logp_in[i];
-  if (t < 0 || l == -INFINITY) return row_zero(out, a.vocab);
-  const T* row = static_cast<const T*>(a.logits) + i * a.stride;
-  const float xt = float(row[t]);
-  __syncthreads();  // every thread has the token's logit before one writes there
-  row_grad(row, out, a.vocab, a.c, xt, l * kLog2e, a.d_logp[i] * a.inv_t, t);
-}
+  // gain (e_t - 2^((x - f) c + u)) to the row's place.
+  __device__ __forceinline__ void store(T* out, int vocab, int t, float f, float c, float u,
+                                        float gain, int token) const {
+    const int pieces = vocab / N;
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      const int at = (i * kThreads + t) * N;
+      if (i * kThreads + t >= pieces) continue;
+      V d;
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float p = pow2(__builtin_fmaf(float(v[i][e]) - f, c, u));
+        d[e] = T(gain * (at + e == token ? 1.f - p : -p));
+      }
+      store16(out + at, d);
+    }
+    const int at = pieces * N + t;
+    if (at < vocab) {
+      const float p = pow2(__builtin_fmaf(tail - f, c, u));
+      out[at] = T(gain * (at == token ? 1.f - p : -p));
+    }
+  }
+  __device__ __forceinline__ static void zero(T* out, int vocab, int t) {
+    const int pieces = vocab / N;
+    for (int i = t; i < pieces; i += kThreads) store16(out + int64_t(i) * N, V(T(0)));
+    if (pieces * N + t < vocab) out[pieces * N + t] = T(0);
+  }
+};
 
 // Loss of one token with log-probability l, and its derivative.
 struct TokenLoss {
@@ -186,27 +179,210 @@ __device__ __forceinline__ TokenLoss token_loss(const RowArgs& a, int64_t i, flo
   return {w * loss, w * slope * a.loss_scale};
 }
 
+// kPolicy: the policy loss with the gradient; else log-probabilities alone.
+
+// `lanes` (a power of two up to 64) of a wave take a row of at most as many
+// logits.
+template <class T, bool kPolicy>
+__global__ __launch_bounds__(kBlock) void lanes_kernel(RowArgs a, int lanes) {
+  const int64_t i = a.first + int64_t(blockIdx.x) * (kBlock / lanes) + int(threadIdx.x) / lanes;
+  if (i >= a.n) return;  // all of a row's lanes
+  const int t = int(threadIdx.x) % lanes, vocab = int(a.vocab);
+  const int token = int(token_in(a.tokens, i, a.vocab));
+  const float x = t < vocab && token >= 0 ? float(static_cast<const T*>(a.logits)[i * a.stride + t])
+                                          : -INFINITY;
+  float m = x;
+  for (int d = 1; d < lanes; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+  const float f = finite_max(m), e = pow2((x - f) * a.c);
+  float sum = e;
+  for (int d = 1; d < lanes; d <<= 1) sum += __shfl_xor(sum, d);
+  const float xt = __shfl(x, (int(threadIdx.x) % kWave) / lanes * lanes + max(token, 0));
+  const float l = token < 0 ? 0.f : log_prob(xt, {m, sum}, a.c);
+  if (t == 0) a.logp[i] = l;
+  if (!kPolicy) return;
+  TokenLoss k = {0.f, 0.f};
+  if (token >= 0) k = token_loss(a, i, l);
+  if (t == 0) a.losses[i] = k.loss;
+  if (t >= vocab) return;
+  float d = 0.f;
+  if (token >= 0 && l != -INFINITY) {
+    const float p = pow2(__builtin_fmaf(x - f, a.c, -log_2(sum)));
+    d = k.slope * a.inv_t * (t == token ? 1.f - p : -p);
+  }
+  static_cast<T*>(a.d_logits)[i * a.d_stride + t] = T(d);
+}
+
+// A wave (kThreads = 64, four rows a block) or a block takes a row that its
+// registers hold.
+template <class T, bool kPolicy, int kThreads, int kVecs>
+__global__ __launch_bounds__(kThreads < kBlock ? kBlock : kThreads) void held_kernel(RowArgs a) {
+  constexpr bool kWaves = kThreads == kWave;
+  __shared__ float part[2][kWaves ? 1 : kThreads / kWave];
+  const int64_t i = a.first + (kWaves ? int64_t(blockIdx.x) * (kBlock / kWave) + threadIdx.x / kWave
+                                      : int64_t(blockIdx.x));
+  if (i >= a.n) return;
+  const int t = int(threadIdx.x) % kThreads, vocab = int(a.vocab);
+  const int token = int(token_in(a.tokens, i, a.vocab));
+  typedef Held<T, kThreads, kVecs> Row;
+  T* const out = kPolicy ? static_cast<T*>(a.d_logits) + i * a.d_stride : nullptr;
+  if (token < 0) {
+    if (t == 0) {
+      a.logp[i] = 0.f;
+      if (kPolicy) a.losses[i] = 0.f;
+    }
+    if (kPolicy) Row::zero(out, vocab, t);
+    return;
+  }
+  const T* const row = static_cast<const T*>(a.logits) + i * a.stride;
+  const float xt = float(row[token]);
+  Row r;
+  r.load(row, vocab, t);
+  float m = wave_max(r.most());
+  if (!kWaves) {
+    if (t % kWave == 0) part[0][t / kWave] = m;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kThreads / kWave; ++w) m = fmaxf(m, part[0][w]);
+  }
+  const float f = finite_max(m);
+  float sum = wave_sum(r.sum(f, a.c));
+  if (!kWaves) {
+    if (t % kWave == 0) part[1][t / kWave] = sum;
+    __syncthreads();
+    sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kThreads / kWave; ++w) sum += part[1][w];
+  }
+  const float l = log_prob(xt, {m, sum}, a.c);
+  if (t == 0) a.logp[i] = l;
+  if (!kPolicy) return;
+  const TokenLoss k = token_loss(a, i, l);
+  if (t == 0) a.losses[i] = k.loss;
+  if (l == -INFINITY) return Row::zero(out, vocab, t);
+  r.store(out, vocab, t, f, a.c, -log_2(sum), k.slope * a.inv_t, token);
+}
+
+// Statistics of a long row, four pieces of a thread under way at once.
 template <class T>
-__global__ __launch_bounds__(kRowThreads) void policy_kernel(RowArgs a) {
-  __shared__ Soft part[kRowThreads / kWave];
+__device__ __forceinline__ Soft row_soft(const T* row, int64_t vocab, float c, Soft* part) {
+  constexpr int N = Vec<T>::kN;
+  Soft a = {-INFINITY, 0.f};
+  const int64_t whole = vocab / N * N, step = int64_t(kLongThreads) * N;
+  int64_t j = int64_t(threadIdx.x) * N;
+  for (; j + 3 * step < whole; j += 4 * step) {
+    typename Vec<T>::type v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = load16(row + j + k * step);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      float x[N];
+      widen<T>(x, v[k]);
+      take(a, x, c);
+    }
+  }
+  for (; j < whole; j += step) {
+    float x[N];
+    widen<T>(x, load16(row + j));
+    take(a, x, c);
+  }
+  if (whole + threadIdx.x < vocab) {
+    const float x[1] = {float(row[whole + threadIdx.x])};
+    take(a, x, c);
+  }
+  return block_join(a, c, part);
+}
+
+// d_logits of a row by kThreads threads: gain (e_t - 2^((x - f) c + u)).  Every
+// element is read and written by the same thread, so that the two may be one.
+template <class T, int kThreads>
+__device__ __forceinline__ void row_grad(const T* row, T* out, int64_t vocab, float c, float f,
+                                         float u, float gain, int64_t token) {
+  constexpr int N = Vec<T>::kN;
+  const int64_t whole = vocab / N * N;
+  for (int64_t j = int64_t(threadIdx.x) * N; j < whole; j += kThreads * N) {
+    float x[N];
+    widen<T>(x, load16(row + j));
+    typename Vec<T>::type v;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float p = pow2(__builtin_fmaf(x[i] - f, c, u));
+      v[i] = T(gain * (j + i == token ? 1.f - p : -p));
+    }
+    store16(out + j, v);
+  }
+  const int64_t j = whole + threadIdx.x;
+  if (j < vocab) {
+    const float p = pow2(__builtin_fmaf(float(row[j]) - f, c, u));
+    out[j] = T(gain * (j == token ? 1.f - p : -p));
+  }
+}
+
+template <class T, int kThreads>
+__device__ __forceinline__ void row_zero(T* out, int64_t vocab) {
+  constexpr int N = Vec<T>::kN;
+  const int64_t whole = vocab / N * N;
+  for (int64_t j = int64_t(threadIdx.x) * N; j < whole; j += kThreads * N)
+    store16(out + j, typename Vec<T>::type(T(0)));
+  if (whole + threadIdx.x < vocab) out[whole + threadIdx.x] = T(0);
+}
+
+template <class T, bool kPolicy>
+__global__ __launch_bounds__(kLongThreads) void long_kernel(RowArgs a) {
+  __shared__ Soft part[kLongThreads / kWave];
   const int64_t i = a.first + blockIdx.x;
-  const int64_t t = token_in(a.tokens, i, a.vocab);
-  T* out = static_cast<T*>(a.d_logits) + i * a.d_stride;
-  if (t < 0) {
-    if (threadIdx.x == 0) a.losses[i] = a.logp[i] = 0.f;
-    return row_zero(out, a.vocab);
+  const int64_t token = token_in(a.tokens, i, a.vocab);
+  T* const out = kPolicy ? static_cast<T*>(a.d_logits) + i * a.d_stride : nullptr;
+  if (token < 0) {
+    if (threadIdx.x == 0) {
+      a.logp[i] = 0.f;
+      if (kPolicy) a.losses[i] = 0.f;
+    }
+    if (kPolicy) row_zero<T, kLongThreads>(out, a.vocab);
+    return;
   }
   const T* row = static_cast<const T*>(a.logits) + i * a.stride;
-  const float xt = float(row[t]);
+  const float xt = float(row[token]);
   const Soft r = row_soft(row, a.vocab, a.c, part);
   const float l = log_prob(xt, r, a.c);
+  if (threadIdx.x == 0) a.logp[i] = l;
+  if (!kPolicy) return;
   const TokenLoss k = token_loss(a, i, l);
-  if (threadIdx.x == 0) {
-    a.losses[i] = k.loss;
-    a.logp[i] = l;
+  if (threadIdx.x == 0) a.losses[i] = k.loss;
+  if (l == -INFINITY) return row_zero<T, kLongThreads>(out, a.vocab);
+  row_grad<T, kLongThreads>(row, out, a.vocab, a.c, finite_max(r.m), -log_2(r.s),
+                            k.slope * a.inv_t, token);
+}
+
+// The gradient alone, of rows of more than 64 logits: 1024 threads a row from
+// 32,768 logits on (48 pairs, 50021 logits: 589 us, 626 with 256), else 256.
+template <class T, int kThreads>
+__global__ __launch_bounds__(kThreads) void grad_kernel(RowArgs a) {
+  const int64_t i = a.first + blockIdx.x;
+  const int64_t token = token_in(a.tokens, i, a.vocab);
+  T* out = static_cast<T*>(a.d_logits) + i * a.d_stride;
+  const float l = a.logp_in[i];
+  if (token < 0 || l == -INFINITY) return row_zero<T, kThreads>(out, a.vocab);
+  const T* row = static_cast<const T*>(a.logits) + i * a.stride;
+  const float xt = float(row[token]);
+  __syncthreads();  // every thread has the token's logit before one writes there
+  row_grad<T, kThreads>(row, out, a.vocab, a.c, xt, l * kLog2e, a.d_logp[i] * a.inv_t, token);
+}
+
+template <class T>
+__global__ __launch_bounds__(kBlock) void lanes_grad_kernel(RowArgs a, int lanes) {
+  const int64_t i = a.first + int64_t(blockIdx.x) * (kBlock / lanes) + int(threadIdx.x) / lanes;
+  const int t = int(threadIdx.x) % lanes;
+  if (i >= a.n || t >= int(a.vocab)) return;
+  const int token = int(token_in(a.tokens, i, a.vocab));
+  const float l = a.logp_in[i];
+  float d = 0.f;
+  if (token >= 0 && l != -INFINITY) {
+    const T* row = static_cast<const T*>(a.logits) + i * a.stride;
+    // The token's logit is read by all of the row's lanes before one writes.
+    const float p = pow2(__builtin_fmaf(float(row[t]) - float(row[token]), a.c, l * kLog2e));
+    d = a.d_logp[i] * a.inv_t * (t == token ? 1.f - p : -p);
   }
-  if (l == -INFINITY) return row_zero(out, a.vocab);
-  row_grad(row, out, a.vocab, a.c, finite_max(r.m), -log_2(r.s), k.slope * a.inv_t, t);
+  static_cast<T*>(a.d_logits)[i * a.d_stride + t] = T(d);
 }
 
 // loss[0] = scale * the sum of n values, added in a fixed order in 64 bits.
@@ -336,21 +512,61 @@ __global__ __launch_bounds__(1024) void pairs_total_kernel(const float* margins,
   if (threadIdx.x == 0) loss[0] = float(s * double(scale) / n);
 }
 
-template <template <class> class K>
-hipError_t by_type(int32_t dtype, RowArgs a, hipStream_t s) {
+// Launches over all rows, `per` of them a block.
+template <class K, class... A>
+hipError_t over_rows(K kernel, RowArgs a, int per, int threads, hipStream_t s, A... more) {
+  const int64_t blocks = (a.n + per - 1) / per;
   hipError_t e = hipSuccess;
-  for (a.first = 0; a.first < a.n && e == hipSuccess; a.first += kMostBlocks) {
-    const dim3 grid(unsigned(std::min(a.n - a.first, kMostBlocks))), block(kRowThreads);
-    if (dtype == SCHED_F32) hipLaunchKernelGGL(K<float>::fn, grid, block, 0, s, a);
-    else if (dtype == SCHED_F16) hipLaunchKernelGGL(K<f16>::fn, grid, block, 0, s, a);
-    else hipLaunchKernelGGL(K<bf16>::fn, grid, block, 0, s, a);
+  for (int64_t b = 0; b < blocks && e == hipSuccess; b += kMostBlocks) {
+    a.first = b * per;
+    hipLaunchKernelGGL(kernel, dim3(unsigned(std::min(blocks - b, kMostBlocks))), dim3(threads), 0,
+                       s, a, more...);
     e = hipGetLastError();
   }
   return e;
 }
-template <class T> struct LogprobsK { static constexpr auto fn = logprobs_kernel<T>; };
-template <class T> struct LogprobsGradK { static constexpr auto fn = logprobs_grad_kernel<T>; };
-template <class T> struct PolicyK { static constexpr auto fn = policy_kernel<T>; };
+
+int lanes_for(int64_t vocab) {
+  int l = 1;
+  while (l < vocab) l *= 2;
+  return l;
+}
+
+template <class T, bool kPolicy>
+hipError_t rows_of(const RowArgs& a, hipStream_t s) {
+  if (a.vocab <= kWave) {
+    const int lanes = lanes_for(a.vocab);
+    return over_rows(lanes_kernel<T, kPolicy>, a, kBlock / lanes, kBlock, s, lanes);
+  }
+  const int64_t pieces = a.vocab / Vec<T>::kN;
+  constexpr int kPer = kBlock / kWave;
+  if (pieces <= 64) return over_rows(held_kernel<T, kPolicy, 64, 1>, a, kPer, kBlock, s);
+  if (pieces <= 128) return over_rows(held_kernel<T, kPolicy, 64, 2>, a, kPer, kBlock, s);
+  if (pieces <= 256) return over_rows(held_kernel<T, kPolicy, 64, 4>, a, kPer, kBlock, s);
+  if (pieces <= 512) return over_rows(held_kernel<T, kPolicy, 64, 8>, a, kPer, kBlock, s);
+  if (pieces <= 1024) return over_rows(held_kernel<T, kPolicy, 256, 4>, a, 1, 256, s);
+  if (pieces <= 2048) return over_rows(held_kernel<T, kPolicy, 256, 8>, a, 1, 256, s);
+  if (pieces <= 4096) return over_rows(held_kernel<T, kPolicy, 256, 16>, a, 1, 256, s);
+  if (pieces <= 8192) return over_rows(held_kernel<T, kPolicy, 512, 16>, a, 1, 512, s);
+  return over_rows(long_kernel<T, kPolicy>, a, 1, kLongThreads, s);
+}
+
+template <class T>
+hipError_t grads_of(const RowArgs& a, hipStream_t s) {
+  if (a.vocab <= kWave) {
+    const int lanes = lanes_for(a.vocab);
+    return over_rows(lanes_grad_kernel<T>, a, kBlock / lanes, kBlock, s, lanes);
+  }
+  if (a.vocab < 32768) return over_rows(grad_kernel<T, 256>, a, 1, 256, s);
+  return over_rows(grad_kernel<T, 1024>, a, 1, 1024, s);
+}
+
+template <bool kPolicy>
+hipError_t rows_by_type(int32_t dtype, const RowArgs& a, hipStream_t s) {
+  return dtype == SCHED_F32   ? rows_of<float, kPolicy>(a, s)
+         : dtype == SCHED_F16 ? rows_of<f16, kPolicy>(a, s)
+                              : rows_of<bf16, kPolicy>(a, s);
+}
 
 Tokens tokens_of(const sched_tokens& t) { return {t.data, t.bits == 64}; }
 
@@ -372,7 +588,7 @@ hipError_t launch_logprobs(const sched_matrix& logits, const sched_tokens& token
                            float temperature, float* logp, hipStream_t s) {
   RowArgs a = row_args(logits, tokens, temperature);
   a.logp = logp;
-  return by_type<LogprobsK>(logits.dtype, a, s);
+  return rows_by_type<false>(logits.dtype, a, s);
 }
 
 hipError_t launch_logprobs_grad(const sched_matrix& logits, const sched_tokens& tokens,
@@ -383,7 +599,9 @@ hipError_t launch_logprobs_grad(const sched_matrix& logits, const sched_tokens& 
   a.d_logp = d_logp;
   a.d_logits = d_logits.data;
   a.d_stride = d_logits.stride;
-  return by_type<LogprobsGradK>(logits.dtype, a, s);
+  return logits.dtype == SCHED_F32   ? grads_of<float>(a, s)
+         : logits.dtype == SCHED_F16 ? grads_of<f16>(a, s)
+                                     : grads_of<bf16>(a, s);
 }
 
 hipError_t launch_policy(const sched_policy_desc& d, hipStream_t s) {
@@ -400,7 +618,7 @@ hipError_t launch_policy(const sched_policy_desc& d, hipStream_t s) {
   a.logp = d.logp;
   a.d_logits = d.d_logits.data;
   a.d_stride = d.d_logits.stride;
-  const hipError_t e = by_type<PolicyK>(d.logits.dtype, a, s);
+  const hipError_t e = rows_by_type<true>(d.logits.dtype, a, s);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(total_kernel, dim3(1), dim3(1024), 0, s, d.losses, d.logits.rows, 1.f, d.loss);
   return hipGetLastError();
