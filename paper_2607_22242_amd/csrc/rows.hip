@@ -117,6 +117,17 @@ struct Held {
     tail = -INFINITY;
     if (pieces * N + t < vocab) tail = float(row[pieces * N + t]);
   }
+  // Keeps the compiler from holding the logits in 32 bits too between two uses,
+  // which takes twice the registers.
+  __device__ __forceinline__ void fresh() {
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      typedef uint32_t Raw __attribute__((ext_vector_type(4)));
+      Raw x = __builtin_bit_cast(Raw, v[i]);
+      asm volatile("" : "+v"(x));
+      v[i] = __builtin_bit_cast(V, x);
+    }
+  }
   __device__ __forceinline__ float most() const {
     float m = tail;
 #pragma unroll
@@ -238,6 +249,7 @@ __global__ __launch_bounds__(kThreads < kBlock ? kBlock : kThreads) void held_ke
   Row r;
   r.load(row, vocab, t);
   float m = wave_max(r.most());
+  r.fresh();
   if (!kWaves) {
     if (t % kWave == 0) part[0][t / kWave] = m;
     __syncthreads();
@@ -246,6 +258,7 @@ __global__ __launch_bounds__(kThreads < kBlock ? kBlock : kThreads) void held_ke
   }
   const float f = finite_max(m);
   float sum = wave_sum(r.sum(f, a.c));
+  r.fresh();
   if (!kWaves) {
     if (t % kWave == 0) part[1][t / kWave] = sum;
     __syncthreads();
