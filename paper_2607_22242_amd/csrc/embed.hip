@@ -23,7 +23,8 @@ constexpr int kSmall = 8192;             // tokens that one block sorts in LDS
 constexpr int kSmallThreads = 1024;
 constexpr int kTile = 4096;              // tokens of a block otherwise
 constexpr int kTileThreads = 512;
-constexpr int kRowsPerBlock = 16;
+constexpr int kMostThreads = 512;       // of a block of a row's waves
+constexpr int kPer = 8;                 // rows of the table, or places, of a wave
 
 __device__ __forceinline__ uint64_t below(int lane) { return (1ull << lane) - 1; }
 
@@ -76,12 +77,15 @@ __device__ __forceinline__ void count_digits(const uint32_t (&key)[kRounds], con
 
 // Lanes of the wave with this lane's digit, of those taking part.
 __device__ __forceinline__ uint64_t peers_of(uint32_t digit, bool on, int bits) {
-  uint64_t peers = __ballot(on);
+  const uint64_t all = __ballot(on);
+  uint32_t lo = uint32_t(all), hi = uint32_t(all >> 32);
   for (int b = 0; b < bits; ++b) {
-    const uint64_t set = __ballot((digit >> b) & 1);
-    peers &= (digit >> b) & 1 ? set : ~set;
+    const int32_t own = int32_t(digit << (31 - b)) >> 31;  // the bit, in every place
+    const uint64_t set = __ballot(own);
+    lo &= ~(uint32_t(set) ^ uint32_t(own));
+    hi &= ~(uint32_t(set >> 32) ^ uint32_t(own));
   }
-  return peers;
+  return uint64_t(hi) << 32 | lo;
 }
 
 // Exclusive sum over 512 or 1024 threads' values.
@@ -261,28 +265,112 @@ struct SumArgs {
   void* table;
   int64_t table_stride;
   int lanes;                 // of a row's piece: a power of two up to 64
-  int64_t first;             // row of the table that the launch starts with
+  int across, width;         // waves of a block that share a row, and pieces of each
+  int64_t first;             // row of the table or place of the list that the launch starts with
 };
 
-// Sum of rows in the order of the list, by a wave: 64 / lanes entries at once,
-// 16-byte pieces; the groups' sums are added in one order at the end.
+// N values of a row from element j on, those that there are, in 16-byte pieces.
+template <class T, int N>
+__device__ __forceinline__ void read_piece(const T* row, int64_t j, int64_t dim, float (&x)[N]) {
+  constexpr int M = Vec<T>::kN;
+  if (j + N <= dim) {
+#pragma unroll
+    for (int k = 0; k < N; k += M) {
+      const typename Vec<T>::type v = load16(row + j + k);
+#pragma unroll
+      for (int e = 0; e < M; ++e) x[k + e] = float(v[e]);
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < N; ++k) x[k] = j + k < dim ? float(row[j + k]) : 0.f;
+  }
+}
+template <class T, int N>
+__device__ __forceinline__ void write_piece(T* row, int64_t j, int64_t dim, const float (&x)[N]) {
+  constexpr int M = Vec<T>::kN;
+  if (j + N <= dim) {
+#pragma unroll
+    for (int k = 0; k < N; k += M) {
+      typename Vec<T>::type v;
+#pragma unroll
+      for (int e = 0; e < M; ++e) v[e] = T(x[k + e]);
+      store16(row + j + k, v);
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if (j + k < dim) row[j + k] = T(x[k]);
+  }
+}
+
+// kRows entries of each group of lanes, i, i + groups, .., all under way at once.
+template <class T, int kRows>
+__device__ __forceinline__ void add_batch(const SumArgs& a, uint32_t mine, int i, int64_t j,
+                                          float (&acc)[Vec<T>::kN]) {
+  constexpr int N = Vec<T>::kN;
+  const T* rows = static_cast<const T*>(a.d_rows) + j;
+  uint32_t at[kRows];  // by all lanes, before their ways part
+#pragma unroll
+  for (int k = 0; k < kRows; ++k) at[k] = __shfl(mine, i + k * (kWave / a.lanes));
+  if (j + N <= a.dim) {
+    typename Vec<T>::type v[kRows];
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) v[k] = load16(rows + int64_t(at[k]) * a.row_stride);
+#pragma unroll
+    for (int k = 0; k < kRows; ++k)
+#pragma unroll
+      for (int q = 0; q < N; ++q) acc[q] += float(v[k][q]);
+  } else {
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) {
+      const T* row = rows + int64_t(at[k]) * a.row_stride;
+#pragma unroll
+      for (int q = 0; q < N; ++q)
+        if (j + q < a.dim) acc[q] += float(row[q]);
+    }
+  }
+}
+
+template <class T>
+__device__ __forceinline__ void add_last(const SumArgs& a, uint32_t mine, int i, int count,
+                                         int64_t j, float (&acc)[Vec<T>::kN]) {
+  const int64_t row = __shfl(mine, min(i, kWave - 1));
+  if (i >= count) return;
+  float x[Vec<T>::kN];
+  read_piece(static_cast<const T*>(a.d_rows) + row * a.row_stride, j, a.dim, x);
+#pragma unroll
+  for (int q = 0; q < Vec<T>::kN; ++q) acc[q] += x[q];
+}
+
+// Sum of rows in the order of the list, by a wave: 64 / lanes groups of lanes
+// take an entry each, in 16-byte pieces; the groups' sums are added in one order
+// at the end.
 template <class T>
 __device__ __forceinline__ void add_rows(const SumArgs& a, uint32_t b, uint32_t e, int64_t j,
                                          float (&acc)[Vec<T>::kN]) {
-  constexpr int N = Vec<T>::kN;
-  const int lane = int(threadIdx.x) % kWave, groups = kWave / a.lanes;
-  const T* rows = static_cast<const T*>(a.d_rows);
-  for (uint32_t i = b + uint32_t(lane / a.lanes); i < e; i += uint32_t(groups)) {
-    const T* row = rows + int64_t(a.at[i]) * a.row_stride + j;
-    if (j + N <= a.dim) {
-      const typename Vec<T>::type v = load16(row);
-#pragma unroll
-      for (int k = 0; k < N; ++k) acc[k] += float(v[k]);
-    } else {
-#pragma unroll
-      for (int k = 0; k < N; ++k)
-        if (j + k < a.dim) acc[k] += float(row[k]);
+  const int lane = int(threadIdx.x) % kWave, groups = kWave / a.lanes, group = lane / a.lanes;
+  for (uint32_t base = b; base < e; base += kWave) {
+    const int count = int(min(e - base, uint32_t(kWave)));
+    const uint32_t mine = lane < count ? a.at[base + lane] : 0;
+    int i = 0;
+    for (; i + 16 * groups <= count; i += 16 * groups) add_batch<T, 16>(a, mine, i + group, j, acc);
+    if (i + 8 * groups <= count) {
+      add_batch<T, 8>(a, mine, i + group, j, acc);
+      i += 8 * groups;
     }
+    if (i + 4 * groups <= count) {
+      add_batch<T, 4>(a, mine, i + group, j, acc);
+      i += 4 * groups;
+    }
+    if (i + 2 * groups <= count) {
+      add_batch<T, 2>(a, mine, i + group, j, acc);
+      i += 2 * groups;
+    }
+    if (i + groups <= count) {
+      add_batch<T, 1>(a, mine, i + group, j, acc);
+      i += groups;
+    }
+    if (i < count) add_last<T>(a, mine, i + group, count, j, acc);
   }
 }
 
@@ -293,70 +381,123 @@ __device__ __forceinline__ void join_groups(const SumArgs& a, float (&acc)[N]) {
     for (int k = 0; k < N; ++k) acc[k] += __shfl_xor(acc[k], d);
 }
 
+// The columns of a wave: `width` pieces of tile `tile`; lanes behind them (and
+// behind the row) get a column that is not there.
+template <class T>
+__device__ __forceinline__ int64_t column(const SumArgs& a, int64_t tile) {
+  const int lane = int(threadIdx.x) % kWave % a.lanes;
+  return lane < a.width ? (tile * a.width + lane) * Vec<T>::kN : a.dim;
+}
+
 // Chunks of the list that hold one token only (parts of long runs).
 template <class T>
-__global__ __launch_bounds__(kBlock) void chunk_kernel(SumArgs a) {
+__global__ __launch_bounds__(kMostThreads) void chunk_kernel(SumArgs a) {
   constexpr int N = Vec<T>::kN;
-  const uint32_t c = blockIdx.x * (kBlock / kWave) + threadIdx.x / kWave;
+  const int wave = int(threadIdx.x) / kWave, at_once = int(blockDim.x) / kWave / a.across;
+  const uint32_t c = blockIdx.x * uint32_t(at_once) + uint32_t(wave / a.across);
   if (c >= a.n / a.chunk) return;
   const uint32_t b = c * a.chunk, e = b + a.chunk, v = a.key[b];
   if (v != a.key[e - 1] || v >= uint32_t(a.vocab)) return;
-  const int lane = int(threadIdx.x) % kWave;
-  const int64_t j = (int64_t(blockIdx.y) * a.lanes + lane % a.lanes) * N;
+  const int64_t j = column<T>(a, int64_t(blockIdx.y) * a.across + wave % a.across);
   float acc[N] = {};
-  if (j < a.dim) add_rows<T>(a, b, e, j, acc);
+  add_rows<T>(a, b, e, j, acc);
   join_groups(a, acc);
-  if (lane < a.lanes)
-#pragma unroll
-    for (int k = 0; k < N; ++k)
-      if (j + k < a.dim) a.partial[int64_t(c) * a.dim + j + k] = acc[k];
+  if (int(threadIdx.x) % kWave < a.lanes) write_piece(a.partial + int64_t(c) * a.dim, j, a.dim, acc);
 }
 
-// First place of the sorted list whose token is at least v.
+// First place of the sorted list whose token is at least v, by a wave: 64 probes
+// at once.
 __device__ __forceinline__ uint32_t place_of(const uint32_t* key, uint32_t n, uint32_t v) {
-  uint32_t lo = 0, hi = n;
-  while (lo < hi) {
-    const uint32_t mid = lo + (hi - lo) / 2;
-    if (key[mid] < v) lo = mid + 1;
-    else hi = mid;
+  const uint32_t lane = threadIdx.x % kWave;
+  uint32_t lo = 0, hi = n;  // the place is in [lo, hi]
+  while (hi - lo > kWave) {
+    const uint32_t step = (hi - lo + kWave - 1) / kWave, at = lo + lane * step;
+    const uint32_t less = uint32_t(__popcll(__ballot(at < hi && key[at] < v)));
+    if (less == 0) return lo;
+    hi = min(hi, lo + less * step);
+    lo += (less - 1) * step + 1;
   }
-  return lo;
+  return lo + uint32_t(__popcll(__ballot(lo + lane < hi && key[lo + lane] < v)));
 }
 
-// Rows of the table, one wave each in turn: the entries before the first whole
-// chunk of the run, the chunks' sums, the entries behind the last.
+// Row v of the table from the run [s, e): the entries before the first whole
+// chunk, the chunks' sums, the entries behind the last.
 template <class T, class O, bool kAdd>
-__global__ __launch_bounds__(kBlock) void table_kernel(SumArgs a) {
-  constexpr int N = Vec<T>::kN;
-  constexpr int kPer = kRowsPerBlock / (kBlock / kWave);
-  const int lane = int(threadIdx.x) % kWave;
-  const int64_t v0 = a.first + int64_t(blockIdx.x) * kRowsPerBlock + int(threadIdx.x) / kWave * kPer;
-  const uint32_t mine = place_of(a.key, a.n, uint32_t(v0 + (lane < kPer ? lane : kPer)));
-  const int64_t j = (int64_t(blockIdx.y) * a.lanes + lane % a.lanes) * N;
-  const int group = lane / a.lanes, groups = kWave / a.lanes;
-  for (int r = 0; r < kPer && v0 + r < a.vocab; ++r) {
-    const uint32_t s = __shfl(mine, r), e = __shfl(mine, r + 1);
-    if (kAdd && s == e) continue;
-    float acc[N] = {};
-    const uint32_t c0 = (s + a.chunk - 1) / a.chunk, c1 = e / a.chunk;
-    if (j < a.dim) {
-      if (c1 > c0) {
-        add_rows<T>(a, s, c0 * a.chunk, j, acc);
-        for (uint32_t c = c0 + uint32_t(group); c < c1; c += uint32_t(groups))
+__device__ __forceinline__ void table_row(const SumArgs& a, int64_t v, uint32_t s, uint32_t e,
+                                          int64_t j) {
+  constexpr int N = Vec<T>::kN, kAhead = 8;
+  const int lane = int(threadIdx.x) % kWave, group = lane / a.lanes, groups = kWave / a.lanes;
+  O* to = static_cast<O*>(a.table) + v * a.table_stride;
+  float x[N] = {}, acc[N] = {};
+  if (kAdd) read_piece(to, j, a.dim, x);
+  const uint32_t c0 = (s + a.chunk - 1) / a.chunk, c1 = e / a.chunk;
+  if (c1 > c0) {
+    add_rows<T>(a, s, c0 * a.chunk, j, acc);
+    for (uint32_t c = c0 + uint32_t(group); c < c1; c += uint32_t(groups * kAhead)) {
+      float y[kAhead][N];
 #pragma unroll
-          for (int k = 0; k < N; ++k)
-            if (j + k < a.dim) acc[k] += a.partial[int64_t(c) * a.dim + j + k];
-        add_rows<T>(a, c1 * a.chunk, e, j, acc);
-      } else {
-        add_rows<T>(a, s, e, j, acc);
+      for (int i = 0; i < kAhead; ++i) {
+        const uint32_t part = min(c + uint32_t(i * groups), c1 - 1);
+        read_piece(a.partial + int64_t(part) * a.dim, j, a.dim, y[i]);
       }
-    }
-    join_groups(a, acc);
-    O* to = static_cast<O*>(a.table) + (v0 + r) * a.table_stride + j;
 #pragma unroll
-    for (int k = 0; k < N; ++k)
-      if (lane < a.lanes && j + k < a.dim)
-        to[k] = O((kAdd ? float(to[k]) : 0.f) + acc[k] * a.scale);
+      for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+        for (int k = 0; k < N; ++k) acc[k] += c + uint32_t(i * groups) < c1 ? y[i][k] : 0.f;
+    }
+    add_rows<T>(a, c1 * a.chunk, e, j, acc);
+  } else {
+    add_rows<T>(a, s, e, j, acc);
+  }
+  join_groups(a, acc);
+  if (lane < a.lanes) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) x[k] += acc[k] * a.scale;
+    write_piece(to, j, a.dim, x);
+  }
+}
+
+// Every row of the table, kPer in turn by each wave, zeros for those without a
+// run.
+template <class T, class O>
+__global__ __launch_bounds__(kMostThreads) void table_kernel(SumArgs a) {
+  const int lane = int(threadIdx.x) % kWave, wave = int(threadIdx.x) / kWave;
+  const int at_once = int(blockDim.x) / kWave / a.across;
+  const int64_t v0 = a.first + (int64_t(blockIdx.x) * at_once + wave / a.across) * kPer;
+  if (v0 >= a.vocab) return;
+  const int64_t j = column<T>(a, int64_t(blockIdx.y) * a.across + wave % a.across);
+  const uint32_t first = place_of(a.key, a.n, uint32_t(v0));
+  const uint32_t near = first + lane < a.n ? a.key[first + lane] : ~0u;
+  uint32_t s = first;
+  for (int r = 0; r < kPer && v0 + r < a.vocab; ++r) {
+    // The run's end is among the 64 entries at hand, or it is looked for.
+    const int passed = __popcll(__ballot(near <= uint32_t(v0 + r)));
+    const uint32_t e = passed < kWave ? first + uint32_t(passed)
+                                      : place_of(a.key, a.n, uint32_t(v0 + r + 1));
+    table_row<T, O, false>(a, v0 + r, s, e, j);
+    s = e;
+  }
+}
+
+// The rows that have a run, added to what is there: a wave takes the runs that
+// begin at kPer places of the list.
+template <class T, class O>
+__global__ __launch_bounds__(kMostThreads) void add_kernel(SumArgs a) {
+  const int lane = int(threadIdx.x) % kWave, wave = int(threadIdx.x) / kWave;
+  const int at_once = int(blockDim.x) / kWave / a.across;
+  const int64_t first = a.first + (int64_t(blockIdx.x) * at_once + wave / a.across) * kPer;
+  if (first >= a.n) return;
+  const int64_t j = column<T>(a, int64_t(blockIdx.y) * a.across + wave % a.across);
+  const uint32_t i = uint32_t(first) + uint32_t(lane);
+  const uint32_t near = i < a.n ? a.key[i] : ~0u;
+  const bool begins = lane < kPer && near < uint32_t(a.vocab) && (i == 0 || a.key[i - 1] != near);
+  for (uint64_t heads = __ballot(begins); heads; heads &= heads - 1) {
+    const int at = __ffsll((unsigned long long)heads) - 1;
+    const uint32_t v = uint32_t(__shfl(near, at));
+    const int passed = __popcll(__ballot(near <= v));
+    const uint32_t e = passed < kWave ? uint32_t(first) + uint32_t(passed)
+                                      : place_of(a.key, a.n, v + 1);
+    table_row<T, O, true>(a, v, uint32_t(first) + uint32_t(at), e, j);
   }
 }
 
@@ -367,7 +508,7 @@ int lanes_for(int64_t pieces, int most) {
 }
 
 uint32_t chunk_for(int64_t n) {
-  uint32_t c = 64;
+  uint32_t c = 32;
   while (n / c > 4096) c *= 2;
   return c;
 }
@@ -397,21 +538,29 @@ hipError_t sums_of(const SumArgs& in, bool accumulate, hipStream_t s) {
   SumArgs a = in;
   const int64_t pieces = (a.dim + Vec<T>::kN - 1) / Vec<T>::kN;
   a.lanes = lanes_for(pieces, kWave);
-  const unsigned tiles = unsigned((pieces + a.lanes - 1) / a.lanes);
+  // A row's waves stand in one block, up to 8 of them, and share its pieces
+  // evenly; blocks of short rows take several rows.
+  const int64_t waves = (pieces + kWave - 1) / kWave, parts = (waves + 7) / 8;
+  a.across = int((waves + parts - 1) / parts);
+  a.width = int((pieces + parts * a.across - 1) / (parts * a.across));
+  const int at_once = std::max(1, 4 / a.across);
+  const dim3 block(unsigned(kWave * a.across * at_once));
   if (const uint32_t chunks = a.n / a.chunk) {
-    hipLaunchKernelGGL(chunk_kernel<T>, dim3((chunks + 3) / 4, tiles), dim3(kBlock), 0, s, a);
+    const unsigned blocks = (chunks + unsigned(at_once) - 1) / unsigned(at_once);
+    hipLaunchKernelGGL(chunk_kernel<T>, dim3(blocks, unsigned(parts)), block, 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  const int64_t blocks = (a.vocab + kRowsPerBlock - 1) / kRowsPerBlock;
+  const int64_t per = at_once * kPer, all = accumulate ? int64_t(a.n) : a.vocab;
+  const int64_t blocks = (all + per - 1) / per;
   hipError_t e = hipSuccess;
   for (int64_t b = 0; b < blocks && e == hipSuccess; b += kMostBlocks) {
-    a.first = b * kRowsPerBlock;
-    const dim3 grid(unsigned(std::min(blocks - b, kMostBlocks)), tiles);
+    a.first = b * per;
+    const dim3 grid(unsigned(std::min(blocks - b, kMostBlocks)), unsigned(parts));
     if (accumulate)
-      hipLaunchKernelGGL((table_kernel<T, O, true>), grid, dim3(kBlock), 0, s, a);
+      hipLaunchKernelGGL((add_kernel<T, O>), grid, block, 0, s, a);
     else
-      hipLaunchKernelGGL((table_kernel<T, O, false>), grid, dim3(kBlock), 0, s, a);
+      hipLaunchKernelGGL((table_kernel<T, O>), grid, block, 0, s, a);
     e = hipGetLastError();
   }
   return e;

@@ -9,7 +9,7 @@ namespace policy {
 
 // Blocks of a launch at most (a grid has less than 2^32 threads a side); more
 // work is launched in parts.
-constexpr int64_t kMostBlocks = int64_t(1) << 22;
+constexpr int64_t kMostBlocks = (int64_t(1) << 22) - 1;
 
 // Bytes of the matrix' element, 0 for a type that is not taken.
 inline int element_bytes(int32_t dtype) {

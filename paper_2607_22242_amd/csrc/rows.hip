@@ -276,11 +276,11 @@ __global__ __launch_bounds__(kThreads < kBlock ? kBlock : kThreads) void held_ke
 }
 
 // Statistics of a long row, four pieces of a thread under way at once.
-template <class T>
+template <class T, int kThreads>
 __device__ __forceinline__ Soft row_soft(const T* row, int64_t vocab, float c, Soft* part) {
   constexpr int N = Vec<T>::kN;
   Soft a = {-INFINITY, 0.f};
-  const int64_t whole = vocab / N * N, step = int64_t(kLongThreads) * N;
+  const int64_t whole = vocab / N * N, step = int64_t(kThreads) * N;
   int64_t j = int64_t(threadIdx.x) * N;
   for (; j + 3 * step < whole; j += 4 * step) {
     typename Vec<T>::type v[4];
@@ -307,7 +307,8 @@ __device__ __forceinline__ Soft row_soft(const T* row, int64_t vocab, float c, S
 
 // d_logits of a row by kThreads threads: gain (e_t - 2^((x - f) c + u)).  Every
 // element is read and written by the same thread, so that the two may be one.
-template <class T, int kThreads>
+// kPast: past the caches, which then hold more rows that are still to be read.
+template <class T, int kThreads, bool kPast>
 __device__ __forceinline__ void row_grad(const T* row, T* out, int64_t vocab, float c, float f,
                                          float u, float gain, int64_t token) {
   constexpr int N = Vec<T>::kN;
@@ -321,7 +322,8 @@ __device__ __forceinline__ void row_grad(const T* row, T* out, int64_t vocab, fl
       const float p = pow2(__builtin_fmaf(x[i] - f, c, u));
       v[i] = T(gain * (j + i == token ? 1.f - p : -p));
     }
-    store16(out + j, v);
+    if (kPast) stream16(out + j, v);
+    else store16(out + j, v);
   }
   const int64_t j = whole + threadIdx.x;
   if (j < vocab) {
@@ -339,9 +341,9 @@ __device__ __forceinline__ void row_zero(T* out, int64_t vocab) {
   if (whole + threadIdx.x < vocab) out[whole + threadIdx.x] = T(0);
 }
 
-template <class T, bool kPolicy>
-__global__ __launch_bounds__(kLongThreads) void long_kernel(RowArgs a) {
-  __shared__ Soft part[kLongThreads / kWave];
+template <class T, bool kPolicy, int kThreads>
+__global__ __launch_bounds__(kThreads) void long_kernel(RowArgs a) {
+  __shared__ Soft part[kThreads / kWave];
   const int64_t i = a.first + blockIdx.x;
   const int64_t token = token_in(a.tokens, i, a.vocab);
   T* const out = kPolicy ? static_cast<T*>(a.d_logits) + i * a.d_stride : nullptr;
@@ -350,20 +352,20 @@ __global__ __launch_bounds__(kLongThreads) void long_kernel(RowArgs a) {
       a.logp[i] = 0.f;
       if (kPolicy) a.losses[i] = 0.f;
     }
-    if (kPolicy) row_zero<T, kLongThreads>(out, a.vocab);
+    if (kPolicy) row_zero<T, kThreads>(out, a.vocab);
     return;
   }
   const T* row = static_cast<const T*>(a.logits) + i * a.stride;
   const float xt = float(row[token]);
-  const Soft r = row_soft(row, a.vocab, a.c, part);
+  const Soft r = row_soft<T, kThreads>(row, a.vocab, a.c, part);
   const float l = log_prob(xt, r, a.c);
   if (threadIdx.x == 0) a.logp[i] = l;
   if (!kPolicy) return;
   const TokenLoss k = token_loss(a, i, l);
   if (threadIdx.x == 0) a.losses[i] = k.loss;
-  if (l == -INFINITY) return row_zero<T, kLongThreads>(out, a.vocab);
-  row_grad<T, kLongThreads>(row, out, a.vocab, a.c, finite_max(r.m), -log_2(r.s),
-                            k.slope * a.inv_t, token);
+  if (l == -INFINITY) return row_zero<T, kThreads>(out, a.vocab);
+  row_grad<T, kThreads, true>(row, out, a.vocab, a.c, finite_max(r.m), -log_2(r.s),
+                               k.slope * a.inv_t, token);
 }
 
 // The gradient alone, of rows of more than 64 logits: 1024 threads a row from
@@ -378,7 +380,7 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(RowArgs a) {
   const T* row = static_cast<const T*>(a.logits) + i * a.stride;
   const float xt = float(row[token]);
   __syncthreads();  // every thread has the token's logit before one writes there
-  row_grad<T, kThreads>(row, out, a.vocab, a.c, xt, l * kLog2e, a.d_logp[i] * a.inv_t, token);
+  row_grad<T, kThreads, false>(row, out, a.vocab, a.c, xt, l * kLog2e, a.d_logp[i] * a.inv_t, token);
 }
 
 template <class T>
@@ -561,7 +563,7 @@ hipError_t rows_of(const RowArgs& a, hipStream_t s) {
   if (pieces <= 2048) return over_rows(held_kernel<T, kPolicy, 256, 8>, a, 1, 256, s);
   if (pieces <= 4096) return over_rows(held_kernel<T, kPolicy, 256, 16>, a, 1, 256, s);
   if (pieces <= 8192) return over_rows(held_kernel<T, kPolicy, 512, 16>, a, 1, 512, s);
-  return over_rows(long_kernel<T, kPolicy>, a, 1, kLongThreads, s);
+  return over_rows(long_kernel<T, kPolicy, kLongThreads>, a, 1, kLongThreads, s);
 }
 
 template <class T>

@@ -32,6 +32,13 @@ __device__ __forceinline__ void store16(T* p, typename Vec<T>::type v) {
   __builtin_memcpy(p, &v, 16);
 }
 
+// The same past the caches, for what this launch does not read again.
+template <class T>
+__device__ __forceinline__ void stream16(T* p, typename Vec<T>::type v) {
+  typedef typename Vec<T>::type Loose __attribute__((aligned(sizeof(T))));
+  __builtin_nontemporal_store(v, reinterpret_cast<Loose*>(p));
+}
+
 // Powers and logarithms to the base 2 as the hardware has them (1 ulp).
 __device__ __forceinline__ float pow2(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log_2(float x) { return __builtin_amdgcn_logf(x); }
