@@ -169,7 +169,8 @@ typedef struct {
  * A row that sees no key gives zeros, lse = -inf and zero gradients.
  * head_dim: a multiple of 8 up to 128.  dtype: SCHED_F16 or SCHED_BF16; the
  * probabilities are rounded to it before they are multiplied with the values.
- * Tensors of less than 2^31 rows. */
+ * q_rows * q_heads / 32 + n_seqs * kv_heads and k_rows * kv_heads / 64 + n_seqs *
+ * kv_heads stay below 2^24 - 8, and a key head has up to 4096 query heads. */
 typedef struct {
     sched_heads q, k, v, out; /* out: q_rows x q_heads x head_dim */
     float *lse;               /* q_heads x q_rows, natural logarithm */

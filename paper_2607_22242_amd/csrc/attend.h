@@ -193,11 +193,19 @@ struct Rows {
 
 // A tile's 16 bytes per thread from memory to LDS without a register between:
 // a wave fills 1024 bytes in a row, so the permutation is in what a lane reads.
-// Nothing waits for it until the next barrier.
+// Nothing waits for it until the next tiles_barrier().
 __device__ __forceinline__ void to_lds(const char* from, uint32_t lane_bytes, void* wave_at) {
   typedef __attribute__((address_space(1))) const void Global;
   typedef __attribute__((address_space(3))) void Lds;
   __builtin_amdgcn_global_load_lds((Global*)(from + lane_bytes), (Lds*)wave_at, 16, 0, 0);
+}
+
+// A barrier behind which tiles that were on their way are there: each wave waits
+// for what it has brought itself (the compiler's barrier waits for LDS, and not
+// in every place for loads into it), and then for the others.
+__device__ __forceinline__ void tiles_barrier() {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
 }
 
 // Threads of a block over a tile of kRows rows: round p of a thread brings one

@@ -6,6 +6,8 @@
 // when the maximum moves.  4 D operations per pair of a query row and a key.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "attend.h"
 #include "policy_launch.h"
 
@@ -20,35 +22,45 @@ constexpr int kKeys = 64;          // of a tile
 constexpr float kSlack = 8.f;
 
 // A wave's 32 query rows (lane l has row l % 32) and what has been added up
-// over the keys so far.
-template <class T, int D>
+// over the keys so far, 32 kSubs of them at a time.
+template <class T, int D, int kSubs>
 struct Sweep {
   typename Frag<T>::type q[D / 16];
   Acc o[D / 32];
   float most, sum;  // reference of the powers; their sum over this lane's half of the keys
 
-  // Adds a tile of keys, of which the lane's row sees those up to `last`
-  // (`whole`: all rows of the wave see all).
-  __device__ __forceinline__ void add(const T* k_tile, const T* v_tile, int j0, int last,
-                                      bool whole, float c, const Places<D>& places) {
-    const Rows<T, D> ks = {k_tile, places.fresh()}, vs = {v_tile, ks.places};
-    Acc x[kKeys / 32];
+  __device__ __forceinline__ void start(const T* q_row, int dim, bool on) {
+    const int h = int(threadIdx.x) % kWave / 32;
 #pragma unroll
-    for (int t = 0; t < kKeys / 32; ++t) {
+    for (int k = 0; k < D / 16; ++k) q[k] = piece(q_row, 16 * k + 8 * h, dim, on);
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) o[d] = Acc(0.f);
+    most = -INFINITY;
+    sum = 0.f;
+  }
+
+  // Adds the keys of a tile from its row `row` on, the first of them key j0; the
+  // lane's row sees those up to `last` (`whole`: all rows of the wave see all).
+  __device__ __forceinline__ void add(const T* k_tile, const T* v_tile, int row, int j0,
+                                      int last, bool whole, float c, const Places<D>& places) {
+    const Rows<T, D> ks = {k_tile, places.fresh()}, vs = {v_tile, ks.places};
+    Acc x[kSubs];
+#pragma unroll
+    for (int t = 0; t < kSubs; ++t) {
       x[t] = Acc(0.f);
 #pragma unroll
-      for (int k = 0; k < D / 16; ++k) x[t] = product(ks.along(32 * t, k), q[k], x[t]);
+      for (int k = 0; k < D / 16; ++k) x[t] = product(ks.along(row + 32 * t, k), q[k], x[t]);
     }
     if (!whole) {
 #pragma unroll
-      for (int t = 0; t < kKeys / 32; ++t)
+      for (int t = 0; t < kSubs; ++t)
 #pragma unroll
         for (int i = 0; i < 16; ++i)
           if (j0 + 32 * t + c_row(i) > last) x[t][i] = -INFINITY;
     }
     float m = -INFINITY;
 #pragma unroll
-    for (int t = 0; t < kKeys / 32; ++t)
+    for (int t = 0; t < kSubs; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i) m = fmaxf(m, x[t][i]);
     m = fmaxf(m, __shfl_xor(m, 32));
@@ -62,20 +74,20 @@ struct Sweep {
     }
     const float fc = (most == -INFINITY ? 0.f : most) * c;
 #pragma unroll
-    for (int t = 0; t < kKeys / 32; ++t)
+    for (int t = 0; t < kSubs; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         x[t][i] = pow2(__builtin_fmaf(x[t][i], c, -fc));
         sum += x[t][i];
       }
 #pragma unroll
-    for (int t = 0; t < kKeys / 32; ++t)
+    for (int t = 0; t < kSubs; ++t)
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
         const auto b = narrow<T>(x[t], p);
 #pragma unroll
         for (int d = 0; d < D / 32; ++d)
-          o[d] = product(vs.across(32 * t + 16 * p, d), b, o[d]);
+          o[d] = product(vs.across(row + 32 * t + 16 * p, d), b, o[d]);
       }
   }
 };
@@ -106,26 +118,20 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendArgs a, int t
   const int all = !a.causal ? s.keys - 1 : min(s.keys - 1, wave_first / a.group + ahead);
   const int any = !a.causal ? s.keys - 1 : min(s.keys - 1, wave_last / a.group + ahead);
 
-  Sweep<T, D> w;
-  const T* q_row = head_row<T>(a.q, s.q0 + me.query, me.head);
-#pragma unroll
-  for (int k = 0; k < D / 16; ++k) w.q[k] = piece(q_row, 16 * k + 8 * (lane / 32), a.dim, on);
-#pragma unroll
-  for (int d = 0; d < D / 32; ++d) w.o[d] = Acc(0.f);
-  w.most = -INFINITY;
-  w.sum = 0.f;
+  Sweep<T, D, kKeys / 32> w;
+  w.start(head_row<T>(a.q, s.q0 + me.query, me.head), a.dim, on);
   const float c = a.scale * kLog2e;
   const Places<D> places;
   const KeyTiles<T, D, kKeys, kThreads> tiles_of(a, s, kv);
   if (end > 0) tiles_of.fetch(0, k_even, v_even, a.dim);
   for (int j0 = 0; j0 < end; j0 += 2 * kKeys) {
-    __syncthreads();  // the tile is there, and nobody reads the other buffer any more
+    tiles_barrier();  // the tile is there, and nobody reads the other buffer any more
     if (j0 + kKeys < end) tiles_of.fetch(j0 + kKeys, k_odd, v_odd, a.dim);
-    if (j0 <= any) w.add(k_even, v_even, j0, last, j0 + kKeys - 1 <= all, c, places);
+    if (j0 <= any) w.add(k_even, v_even, 0, j0, last, j0 + kKeys - 1 <= all, c, places);
     if (j0 + kKeys >= end) break;
-    __syncthreads();
+    tiles_barrier();
     if (j0 + 2 * kKeys < end) tiles_of.fetch(j0 + 2 * kKeys, k_even, v_even, a.dim);
-    if (j0 + kKeys <= any) w.add(k_odd, v_odd, j0 + kKeys, last, j0 + 2 * kKeys - 1 <= all, c, places);
+    if (j0 + kKeys <= any) w.add(k_odd, v_odd, 0, j0 + kKeys, last, j0 + 2 * kKeys - 1 <= all, c, places);
   }
   const float sum = w.sum + __shfl_xor(w.sum, 32);
   if (!on) return;
@@ -136,12 +142,150 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendArgs a, int t
         sum > 0.f ? (w.most * c + log_2(sum)) * kLn2 : -INFINITY;
 }
 
+// --- few query rows -----------------------------------------------------------
+//
+// Where the query rows alone would leave the card idle, a sequence's keys are
+// read by `splits` blocks, each for up to 32 rows (a single token's heads of one
+// key head), and two waves of a block take 32 of each tile's 64 keys.  Their
+// sums, in 32 bits and each with a reference of its own, are joined after them.
+// Bound by the keys' and values' bytes.
+
+struct Split {
+  float* sums;     // a part: D of a row's sums and, behind all of them,
+  float* weights;  // reference (to the base 2) and sum of powers
+  int parts;       // of a row: two per split
+};
+__device__ __forceinline__ int64_t part_of(const AttendArgs& a, const Split& p, int64_t row, int head,
+                                           int part) {
+  return (row * a.q_heads + head) * p.parts + part;
+}
+
 template <class T, int D>
-hipError_t attend(const AttendArgs& a, int kv_heads, hipStream_t s) {
-  const int64_t tiles = tile_count(int64_t(a.q_rows) * a.group, a.n_seqs, kRowsOfBlock);
-  hipLaunchKernelGGL((attend_kernel<T, D>), dim3(unsigned(work_blocks(tiles, kv_heads))),
-                     dim3(kThreads), 0, s, a, int(tiles));
-  return hipGetLastError();
+__global__ __launch_bounds__(kThreads, 2) void split_kernel(AttendArgs a, Split p, int tiles) {
+  __shared__ __attribute__((aligned(16))) T k_even[kKeys * D], v_even[kKeys * D];
+  __shared__ __attribute__((aligned(16))) T k_odd[kKeys * D], v_odd[kKeys * D];
+  const int kv = int(blockIdx.x) / tiles, split = int(blockIdx.y);
+  const Tile tile = tile_of(a.q_offsets, a.n_seqs, a.q_rows, a.group, 32, int(blockIdx.x) % tiles);
+  const Seq s = sequence(a, tile.seq);
+  const int first = tile.index * 32, rows = s.queries * a.group;
+  if (tile.index < 0 || first >= rows) return;
+  const int lane = int(threadIdx.x) % kWave, wave = wave_id();
+  const bool on = first + lane % 32 < rows;
+  const QueryRow me = query_row(a, kv, on ? first + lane % 32 : 0);
+  const int ahead = s.keys - s.queries;
+  const int last = !on || !a.causal ? s.keys - 1 : min(s.keys - 1, me.query + ahead);
+  const int last_row = min(first + 32, rows) - 1;
+  const int seen = a.causal ? min(s.keys, last_row / a.group + ahead + 1) : s.keys;
+  const int all = a.causal ? min(s.keys - 1, first / a.group + ahead) : s.keys - 1;
+  // This split's share of the keys that are seen, in whole tiles.
+  const int share = ((max(seen, 0) + kKeys - 1) / kKeys + p.parts / 2 - 1) / (p.parts / 2) * kKeys;
+  const int begin = min(split * share, max(seen, 0)), end = min(begin + share, seen);
+
+  Sweep<T, D, 1> w;
+  w.start(head_row<T>(a.q, s.q0 + me.query, me.head), a.dim, on);
+  const float c = a.scale * kLog2e;
+  const Places<D> places;
+  const KeyTiles<T, D, kKeys, kThreads> tiles_of(a, s, kv);
+  const int row = wave * 32;  // of the tile; waves 2 and 3 bring tiles only
+  auto step = [&](int j0, const T* k_tile, const T* v_tile) {
+    if (wave < 2 && j0 + row < end)
+      w.add(k_tile, v_tile, row, j0 + row, last, j0 + row + 31 <= min(all, end - 1), c, places);
+  };
+  if (begin < end) tiles_of.fetch(begin, k_even, v_even, a.dim);
+  for (int j0 = begin; j0 < end; j0 += 2 * kKeys) {
+    tiles_barrier();
+    if (j0 + kKeys < end) tiles_of.fetch(j0 + kKeys, k_odd, v_odd, a.dim);
+    step(j0, k_even, v_even);
+    if (j0 + kKeys >= end) break;
+    tiles_barrier();
+    if (j0 + 2 * kKeys < end) tiles_of.fetch(j0 + 2 * kKeys, k_even, v_even, a.dim);
+    step(j0 + kKeys, k_odd, v_odd);
+  }
+  if (wave >= 2 || !on) return;
+  const float sum = w.sum + __shfl_xor(w.sum, 32);
+  const int64_t part = part_of(a, p, s.q0 + me.query, me.head, 2 * split + wave);
+  store_column<float, D>(p.sums + part * D, w.o, D, 1.f);
+  if (lane < 32) {
+    p.weights[2 * part] = w.most * c;
+    p.weights[2 * part + 1] = sum;
+  }
+}
+
+// A wave joins a row's parts.
+template <class T, int D>
+__global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs a, Split p, int64_t first) {
+  const int64_t i = first + int64_t(blockIdx.x) * (kThreads / kWave) + int(threadIdx.x) / kWave;
+  if (i >= int64_t(a.q_rows) * a.q_heads) return;
+  const int lane = int(threadIdx.x) % kWave;
+  const float* const weights = p.weights + i * p.parts * 2;
+  float most = -INFINITY;
+  for (int k = lane; k < p.parts; k += kWave)
+    if (weights[2 * k + 1] > 0.f) most = fmaxf(most, weights[2 * k]);
+  most = wave_max(most);
+  float o[D / kWave] = {}, sum = 0.f;
+  for (int k0 = 0; k0 < p.parts; k0 += kWave) {
+    // A part's factor and sum, by the lane that has it.
+    float f = 0.f, s = 0.f;
+    if (k0 + lane < p.parts && weights[2 * (k0 + lane) + 1] > 0.f) {
+      f = pow2(weights[2 * (k0 + lane)] - most);
+      s = weights[2 * (k0 + lane) + 1] * f;
+    }
+    sum += wave_sum(s);
+    for (int k = k0; k < min(k0 + kWave, p.parts); ++k) {
+      const float g = __shfl(f, k - k0);
+      if (g == 0.f) continue;  // what such a part holds is not used
+#pragma unroll
+      for (int d = 0; d < D / kWave; ++d)
+        o[d] += g * p.sums[(i * p.parts + k) * D + d * kWave + lane];
+    }
+  }
+  const int64_t row = i / a.q_heads;
+  const int head = int(i % a.q_heads);
+  T* const out = head_row<T>(a.out, row, head);
+#pragma unroll
+  for (int d = 0; d < D / kWave; ++d)
+    if (d * kWave + lane < a.dim) out[d * kWave + lane] = T(sum > 0.f ? o[d] / sum : 0.f);
+  if (lane == 0)
+    a.lse[int64_t(head) * a.q_rows + row] = sum > 0.f ? (most + log_2(sum)) * kLn2 : -INFINITY;
+}
+
+// Blocks that a sequence's keys are shared by: 1 where the query rows fill the
+// card (two blocks of 128 rows a unit), else as many as give it 4096 blocks,
+// none of them with less than 256 keys of a sequence of the mean length.
+int splits_of(const sched_attention_desc& d) {
+  if (d.n_seqs == 0 || d.q_rows == 0) return 1;
+  const int64_t rows = d.q_rows * (d.q_heads / d.kv_heads);
+  if ((rows / kRowsOfBlock + d.n_seqs) * d.kv_heads >= 2 * 256 && rows / d.n_seqs > 32) return 1;
+  const int64_t blocks = tile_count(rows, d.n_seqs, 32) * d.kv_heads;
+  const int64_t want = (4096 + blocks - 1) / blocks, most = d.k_rows / d.n_seqs / 256;
+  return int(std::max<int64_t>(1, std::min<int64_t>({want, most, 256})));
+}
+
+size_t part_count(const sched_attention_desc& d, int splits) {
+  return size_t(d.q_rows) * size_t(d.q_heads) * size_t(2 * splits);
+}
+
+template <class T, int D>
+hipError_t attend(const AttendArgs& a, int kv_heads, int splits, void* ws, size_t parts,
+                  hipStream_t s) {
+  if (splits == 1) {
+    const int64_t tiles = tile_count(int64_t(a.q_rows) * a.group, a.n_seqs, kRowsOfBlock);
+    hipLaunchKernelGGL((attend_kernel<T, D>), dim3(unsigned(work_blocks(tiles, kv_heads))),
+                       dim3(kThreads), 0, s, a, int(tiles));
+    return hipGetLastError();
+  }
+  const Split p = {static_cast<float*>(ws), static_cast<float*>(ws) + parts * D, 2 * splits};
+  const int64_t tiles = tile_count(int64_t(a.q_rows) * a.group, a.n_seqs, 32);
+  hipLaunchKernelGGL((split_kernel<T, D>), dim3(unsigned(tiles * kv_heads), unsigned(splits)),
+                     dim3(kThreads), 0, s, a, p, int(tiles));
+  hipError_t e = hipGetLastError();
+  const int64_t blocks = (int64_t(a.q_rows) * a.q_heads + 3) / 4;
+  for (int64_t b = 0; b < blocks && e == hipSuccess; b += kMostBlocks) {
+    hipLaunchKernelGGL((join_kernel<T, D>), dim3(unsigned(std::min(blocks - b, kMostBlocks))),
+                       dim3(kThreads), 0, s, a, p, b * 4);
+    e = hipGetLastError();
+  }
+  return e;
 }
 
 HeadsView view(const sched_heads& h) {
@@ -177,15 +321,22 @@ AttendArgs attend_args(const sched_attention_desc& d) {
   return a;
 }
 
-size_t attention_bytes(const sched_attention_desc&) { return 0; }
+size_t attention_bytes(const sched_attention_desc& d) {
+  const int splits = splits_of(d);
+  return splits == 1 ? 0 : part_count(d, splits) * ((d.head_dim > 64 ? 128 : 64) + 2) * sizeof(float);
+}
 
-hipError_t launch_attention(const sched_attention_desc& d, void*, hipStream_t s) {
+hipError_t launch_attention(const sched_attention_desc& d, void* ws, hipStream_t s) {
   if (d.n_seqs == 0 || d.q_rows == 0) return hipSuccess;
   const AttendArgs a = attend_args(d);
+  const int splits = splits_of(d);
+  const size_t parts = part_count(d, splits);
   const bool wide = d.head_dim > 64;
   if (d.dtype == SCHED_F16)
-    return wide ? attend<f16, 128>(a, d.kv_heads, s) : attend<f16, 64>(a, d.kv_heads, s);
-  return wide ? attend<bf16, 128>(a, d.kv_heads, s) : attend<bf16, 64>(a, d.kv_heads, s);
+    return wide ? attend<f16, 128>(a, d.kv_heads, splits, ws, parts, s)
+                : attend<f16, 64>(a, d.kv_heads, splits, ws, parts, s);
+  return wide ? attend<bf16, 128>(a, d.kv_heads, splits, ws, parts, s)
+              : attend<bf16, 64>(a, d.kv_heads, splits, ws, parts, s);
 }
 
 }  // namespace policy

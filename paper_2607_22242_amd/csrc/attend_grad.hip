@@ -270,12 +270,12 @@ __global__ __launch_bounds__(kThreads, 2) void keys_kernel(AttendArgs a, int til
   };
   if (end >= begin) tiles_of.fetch(a, s, kv, rows, t, q_even, o_even, &s_even);
   for (int r0 = end; r0 >= begin; r0 -= 2 * kTile) {
-    __syncthreads();  // the tile is there, and nobody reads the other buffer any more
+    tiles_barrier();  // the tile is there, and nobody reads the other buffer any more
     retreat(a, t);
     if (t.r0 >= begin) tiles_of.fetch(a, s, kv, rows, t, q_odd, o_odd, &s_odd);
     step(r0, q_even, o_even, s_even);
     if (r0 - kTile < begin) break;
-    __syncthreads();
+    tiles_barrier();
     retreat(a, t);
     if (t.r0 >= begin) tiles_of.fetch(a, s, kv, rows, t, q_even, o_even, &s_even);
     step(r0 - kTile, q_odd, o_odd, s_odd);
@@ -284,9 +284,9 @@ __global__ __launch_bounds__(kThreads, 2) void keys_kernel(AttendArgs a, int til
   static_assert(sizeof(q_even) == size_t(D) / 32 * 16 * kWave * sizeof(float), "a wave's sums");
   float* const buf_k = reinterpret_cast<float*>(wave % 2 ? q_odd : q_even);
   float* const buf_v = reinterpret_cast<float*>(wave % 2 ? o_odd : o_even);
-  __syncthreads();
+  tiles_barrier();
   if (wave >= 2) w.hand(buf_k, buf_v);
-  __syncthreads();
+  tiles_barrier();
   if (wave >= 2 || j >= s.slot) return;
   w.take(buf_k, buf_v);
   store_column<T, D>(head_row<T>(a.d_k, int64_t(s.k0) + j, kv), w.dk, a.dim, a.scale);
@@ -372,11 +372,11 @@ __global__ __launch_bounds__(kThreads, 2) void queries_kernel(AttendArgs a, int 
   const KeyTiles<T, D, kTile, kThreads> tiles_of(a, s, kv);
   if (end > 0) tiles_of.fetch(0, k_even, v_even, a.dim);
   for (int j0 = 0; j0 < end; j0 += 2 * kTile) {
-    __syncthreads();
+    tiles_barrier();
     if (j0 + kTile < end) tiles_of.fetch(j0 + kTile, k_odd, v_odd, a.dim);
     if (j0 <= any) w.add(k_even, v_even, j0, last, j0 + kTile - 1 <= all, c, places);
     if (j0 + kTile >= end) break;
-    __syncthreads();
+    tiles_barrier();
     if (j0 + 2 * kTile < end) tiles_of.fetch(j0 + 2 * kTile, k_even, v_even, a.dim);
     if (j0 + kTile <= any) w.add(k_odd, v_odd, j0 + kTile, last, j0 + 2 * kTile - 1 <= all, c, places);
   }

@@ -21,7 +21,7 @@ constexpr int kDigit = 9;                // bits of a digit at most
 constexpr int kBins = 1 << kDigit;
 constexpr int kSmall = 8192;             // tokens that one block sorts in LDS
 constexpr int kSmallThreads = 1024;
-constexpr int kTile = 4096;              // tokens of a block otherwise
+constexpr int kTile = 2048;              // tokens of a block otherwise
 constexpr int kTileThreads = 512;
 constexpr int kMostThreads = 512;       // of a block of a row's waves
 constexpr int kPer = 8;                 // rows of the table, or places, of a wave
@@ -221,10 +221,16 @@ __global__ __launch_bounds__(kTileThreads) void sort_place_kernel(SortArgs a, in
   // same digit in earlier blocks.
   uint32_t total = 0, earlier = 0;
   if (int(threadIdx.x) < bins)
-    for (uint32_t b = 0; b < gridDim.x; ++b) {
-      const uint32_t c = a.hist[b * uint32_t(bins) + threadIdx.x];
-      total += c;
-      earlier += b < blockIdx.x ? c : 0;
+    for (uint32_t b = 0; b < gridDim.x; b += 16) {
+      uint32_t c[16];  // under way at once
+#pragma unroll
+      for (uint32_t k = 0; k < 16; ++k)
+        c[k] = a.hist[min(b + k, gridDim.x - 1) * uint32_t(bins) + threadIdx.x];
+#pragma unroll
+      for (uint32_t k = 0; k < 16; ++k) {
+        total += b + k < gridDim.x ? c[k] : 0;
+        earlier += b + k < blockIdx.x ? c[k] : 0;
+      }
     }
   uint32_t before = block_before<kTileThreads>(total, part) + earlier;
   if (int(threadIdx.x) < bins)
@@ -285,7 +291,7 @@ __device__ __forceinline__ void read_piece(const T* row, int64_t j, int64_t dim,
     for (int k = 0; k < N; ++k) x[k] = j + k < dim ? float(row[j + k]) : 0.f;
   }
 }
-template <class T, int N>
+template <class T, int N, bool kPast = false>
 __device__ __forceinline__ void write_piece(T* row, int64_t j, int64_t dim, const float (&x)[N]) {
   constexpr int M = Vec<T>::kN;
   if (j + N <= dim) {
@@ -294,7 +300,8 @@ __device__ __forceinline__ void write_piece(T* row, int64_t j, int64_t dim, cons
       typename Vec<T>::type v;
 #pragma unroll
       for (int e = 0; e < M; ++e) v[e] = T(x[k + e]);
-      store16(row + j + k, v);
+      if (kPast) stream16(row + j + k, v);
+      else store16(row + j + k, v);
     }
   } else {
 #pragma unroll
@@ -453,7 +460,7 @@ __device__ __forceinline__ void table_row(const SumArgs& a, int64_t v, uint32_t 
   if (lane < a.lanes) {
 #pragma unroll
     for (int k = 0; k < N; ++k) x[k] += acc[k] * a.scale;
-    write_piece(to, j, a.dim, x);
+    write_piece<O, N, !kAdd>(to, j, a.dim, x);
   }
 }
 
@@ -543,6 +550,7 @@ hipError_t sums_of(const SumArgs& in, bool accumulate, hipStream_t s) {
   const int64_t waves = (pieces + kWave - 1) / kWave, parts = (waves + 7) / 8;
   a.across = int((waves + parts - 1) / parts);
   a.width = int((pieces + parts * a.across - 1) / (parts * a.across));
+  if (a.width > 8) a.width = std::min((a.width + 7) / 8 * 8, kWave);  // whole lines
   const int at_once = std::max(1, 4 / a.across);
   const dim3 block(unsigned(kWave * a.across * at_once));
   if (const uint32_t chunks = a.n / a.chunk) {

@@ -13,6 +13,7 @@ namespace {
 constexpr int64_t kMostRows = (int64_t(1) << 31) - 1;
 constexpr int64_t kMostDim = int64_t(1) << 24;    // of an embedding
 constexpr int32_t kMostAnswers = 1 << 24;
+constexpr int64_t kMostTiles = (1 << 24) - 8;     // blocks of 256 threads in a grid
 
 int done(hipError_t e) { return e == hipSuccess ? SCHED_OK : SCHED_E_DEVICE; }
 
@@ -86,6 +87,9 @@ int check_attention_sizes(const sched_attention_desc& d) {
       d.q_rows < 0 || d.k_rows < 0 || d.k_rows > kMostRows - 256 || d.q_rows > kMostRows ||
       d.q_rows * (d.q_heads / d.kv_heads) > kMostRows - 256)
     return SCHED_E_SIZE;
+  const int64_t q_tiles = d.q_rows * (d.q_heads / d.kv_heads) / 32 + d.n_seqs;
+  const int64_t k_tiles = d.k_rows / 64 + d.n_seqs;
+  if (q_tiles * d.kv_heads >= kMostTiles || k_tiles * d.kv_heads >= kMostTiles) return SCHED_E_SIZE;
   return SCHED_OK;
 }
 
