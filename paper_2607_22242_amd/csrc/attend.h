@@ -85,13 +85,22 @@ struct Tile {
 };
 __device__ __forceinline__ Tile tile_of(const int32_t* offsets, int n_seqs, int rows, int group,
                                         int tile, int number) {
-  int lo = 0, hi = n_seqs;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) / 2;
-    if (uniform(offset_at(offsets, mid, rows)) * group / tile + mid <= number) lo = mid;
-    else hi = mid;
+  // The last sequence that begins at or before the number, 64 of them asked at once.
+  const int lane = int(threadIdx.x) % kWave;
+  int lo = 0, left = n_seqs, base = 0;  // of `left` sequences from lo on
+  for (;;) {
+    const int step = (left + kWave - 1) / kWave, at = lo + lane * step;
+    int begin = 0;
+    if (lane * step < left) begin = offset_at(offsets, at, rows) * group / tile + at;
+    const uint64_t before = __ballot(lane * step < left && begin <= number);
+    // The first one counts even where it begins behind the number.
+    const int last = before ? 63 - __builtin_clzll(before) : 0;
+    base = __shfl(begin, last);
+    lo = uniform(lo + last * step);
+    if (step == 1) break;
+    left = uniform(min(step, left - last * step));
   }
-  return {lo, number - (uniform(offset_at(offsets, lo, rows)) * group / tile + lo)};
+  return {lo, number - uniform(base)};
 }
 
 inline int64_t tile_count(int64_t rows, int n_seqs, int tile) { return rows / tile + n_seqs; }

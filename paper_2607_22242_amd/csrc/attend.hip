@@ -216,6 +216,7 @@ template <class T, int D>
 __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs a, Split p, int64_t first) {
   const int64_t i = first + int64_t(blockIdx.x) * (kThreads / kWave) + int(threadIdx.x) / kWave;
   if (i >= int64_t(a.q_rows) * a.q_heads) return;
+  constexpr int kAhead = 8;  // parts under way at once
   const int lane = int(threadIdx.x) % kWave;
   const float* const weights = p.weights + i * p.parts * 2;
   float most = -INFINITY;
@@ -231,12 +232,21 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs a, Split p, i
       s = weights[2 * (k0 + lane) + 1] * f;
     }
     sum += wave_sum(s);
-    for (int k = k0; k < min(k0 + kWave, p.parts); ++k) {
-      const float g = __shfl(f, k - k0);
-      if (g == 0.f) continue;  // what such a part holds is not used
+    for (int k = 0; k < min(kWave, p.parts - k0); k += kAhead) {
+      float g[kAhead], x[kAhead][D / kWave];
 #pragma unroll
-      for (int d = 0; d < D / kWave; ++d)
-        o[d] += g * p.sums[(i * p.parts + k) * D + d * kWave + lane];
+      for (int n = 0; n < kAhead; ++n) {
+        const int part = min(k0 + k + n, p.parts - 1);
+        g[n] = k0 + k + n < p.parts ? __shfl(f, k + n) : 0.f;
+#pragma unroll
+        for (int d = 0; d < D / kWave; ++d)
+          x[n][d] = p.sums[(i * p.parts + part) * D + d * kWave + lane];
+      }
+#pragma unroll
+      for (int n = 0; n < kAhead; ++n)
+#pragma unroll
+        for (int d = 0; d < D / kWave; ++d)  // what a part of no weight holds is not used
+          o[d] += g[n] == 0.f ? 0.f : g[n] * x[n][d];
     }
   }
   const int64_t row = i / a.q_heads;

@@ -8,8 +8,6 @@
 // one order and no atomics: 14 D operations per pair in place of 10 D.
 #include <hip/hip_runtime.h>
 
-#include <algorithm>
-
 #include "attend.h"
 #include "policy_launch.h"
 
@@ -23,28 +21,6 @@ constexpr int kThreads = 256;
 constexpr int kTile = 64;          // rows of a tile that is walked over
 constexpr int kKeysOfBlock = 64;   // keys that a block holds for dK and dV
 constexpr int kRowsOfBlock = 128;  // query rows that a block holds for dQ, 32 of each wave
-
-// lse2 and delta of every query row and head; 16 lanes a row.
-template <class T>
-__global__ __launch_bounds__(kThreads) void delta_kernel(AttendArgs a, int64_t first) {
-  const int64_t i = first + int64_t(blockIdx.x) * (kThreads / 16) + int(threadIdx.x) / 16;
-  if (i >= int64_t(a.q_rows) * a.q_heads) return;
-  const int64_t row = i / a.q_heads;
-  const int head = int(i % a.q_heads), d = int(threadIdx.x) % 16 * 8;
-  const auto x = piece(head_row<T>(a.out, row, head), d, a.dim, true);
-  const auto y = piece(head_row<T>(a.d_out, row, head), d, a.dim, true);
-  float sum = 0.f;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) sum += float(x[e]) * float(y[e]);
-#pragma unroll
-  for (int k = 8; k; k >>= 1) sum += __shfl_xor(sum, k);
-  if (threadIdx.x % 16 == 0) {
-    const int64_t n = int64_t(head) * a.q_rows + row;
-    const float lse = a.lse[n];
-    a.delta[n] = -sum;
-    a.lse2[n] = lse == -INFINITY ? INFINITY : lse * kLog2e;
-  }
-}
 
 // --- dK and dV ----------------------------------------------------------------
 
@@ -364,9 +340,23 @@ __global__ __launch_bounds__(kThreads, 2) void queries_kernel(AttendArgs a, int 
   }
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) w.dq[i] = Acc(0.f);
+  // The row's statistics, which the kernel of dK and dV reads too.
   const int64_t n = int64_t(me.head) * a.q_rows + s.q0 + me.query;
-  w.lse2 = on ? a.lse2[n] : INFINITY;
-  w.delta = on ? a.delta[n] : 0.f;
+  const T* const out_row = head_row<T>(a.out, s.q0 + me.query, me.head);
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) {
+    const auto x = piece(out_row, 16 * i + 8 * (lane / 32), a.dim, on);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum += float(x[e]) * float(w.o[i][e]);
+  }
+  w.delta = -(sum + __shfl_xor(sum, 32));
+  const float lse = on ? a.lse[n] : -INFINITY;
+  w.lse2 = lse == -INFINITY ? INFINITY : lse * kLog2e;  // powers of rows that see nothing are 0
+  if (on && lane < 32) {
+    a.lse2[n] = w.lse2;
+    a.delta[n] = w.delta;
+  }
   const float c = a.scale * kLog2e;
   const Places<D> places;
   const KeyTiles<T, D, kTile, kThreads> tiles_of(a, s, kv);
@@ -385,24 +375,17 @@ __global__ __launch_bounds__(kThreads, 2) void queries_kernel(AttendArgs a, int 
 
 template <class T, int D>
 hipError_t attend_grad(const AttendArgs& a, int kv_heads, hipStream_t s) {
-  const int64_t rows = int64_t(a.q_rows) * a.q_heads, blocks = (rows + 15) / 16;
   hipError_t e = hipSuccess;
-  for (int64_t b = 0; b < blocks && e == hipSuccess; b += kMostBlocks) {
-    hipLaunchKernelGGL(delta_kernel<T>, dim3(unsigned(std::min(blocks - b, kMostBlocks))),
-                       dim3(kThreads), 0, s, a, b * 16);
-    e = hipGetLastError();
-  }
-  if (e != hipSuccess) return e;
-  if (a.k_rows > 0) {
-    const int64_t tiles = tile_count(a.k_rows, a.n_seqs, kKeysOfBlock);
-    hipLaunchKernelGGL((keys_kernel<T, D>), dim3(unsigned(work_blocks(tiles, kv_heads))),
+  if (a.q_rows > 0) {  // first: it leaves the rows' statistics
+    const int64_t tiles = tile_count(int64_t(a.q_rows) * a.group, a.n_seqs, kRowsOfBlock);
+    hipLaunchKernelGGL((queries_kernel<T, D>), dim3(unsigned(work_blocks(tiles, kv_heads))),
                        dim3(kThreads), 0, s, a, int(tiles));
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (a.q_rows > 0) {
-    const int64_t tiles = tile_count(int64_t(a.q_rows) * a.group, a.n_seqs, kRowsOfBlock);
-    hipLaunchKernelGGL((queries_kernel<T, D>), dim3(unsigned(work_blocks(tiles, kv_heads))),
+  if (a.k_rows > 0) {
+    const int64_t tiles = tile_count(a.k_rows, a.n_seqs, kKeysOfBlock);
+    hipLaunchKernelGGL((keys_kernel<T, D>), dim3(unsigned(work_blocks(tiles, kv_heads))),
                        dim3(kThreads), 0, s, a, int(tiles));
     e = hipGetLastError();
   }
