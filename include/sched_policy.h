@@ -22,12 +22,12 @@
  * Types: 32-bit, 16-bit and bfloat16 floating point (SCHED_F32, SCHED_F16,
  * SCHED_BF16).  Sums, softmax statistics and losses are held in 32 bits or
  * more; results are rounded once to their type.  Probabilities below 2^-126
- * count as zero.  Tokens are 32- or 64-bit
- * integers; one outside [0, vocab) (-1, say) is padding: it carries no loss,
- * looks up zeros and takes no part in a gradient.  Offsets are 32-bit
- * integers on the device, ascending, and tensors have less than 2^31 rows; sequence i of n holds the rows
- * offsets[i] .. offsets[i+1] - 1 of its packed tensor, perhaps none, and the n
- * sequences cover it.  Offsets that leave the tensor are cut to it.
+ * count as zero.  Tokens are 32- or 64-bit integers; one outside [0, vocab) (-1,
+ * say) is padding: it carries no loss, looks up zeros and takes no part in a
+ * gradient.  Tensors have less than 2^31 rows.  Offsets are 32-bit integers on
+ * the device, ascending; sequence i of n holds the rows offsets[i] ..
+ * offsets[i+1] - 1 of its packed tensor, perhaps none, and the n sequences cover
+ * it.  Offsets that leave the tensor are cut to it.
  */
 #ifndef SCHED_POLICY_H
 #define SCHED_POLICY_H

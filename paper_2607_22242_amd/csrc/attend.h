@@ -41,7 +41,8 @@ struct HeadsView {
 struct AttendArgs {
   HeadsView q, k, v, out, d_out, d_q, d_k, d_v;
   float* lse;
-  float *lse2, *delta;  // q_heads x q_rows each: lse log2(e) (+inf in place of -inf), -rowsum(dO o O)
+  // q_heads x q_rows each: lse log2(e) (+inf in place of -inf), -rowsum(dO o O).
+  float *lse2, *delta;
   const int32_t *q_offsets, *k_offsets, *k_lengths;
   int32_t n_seqs, q_rows, k_rows, q_heads, group, dim, causal;
   uint32_t per_group;  // ceil(2^32 / group), in 32 bits: quotients of small numbers

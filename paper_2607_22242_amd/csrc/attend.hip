@@ -131,7 +131,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendArgs a, int t
     if (j0 + kKeys >= end) break;
     tiles_barrier();
     if (j0 + 2 * kKeys < end) tiles_of.fetch(j0 + 2 * kKeys, k_even, v_even, a.dim);
-    if (j0 + kKeys <= any) w.add(k_odd, v_odd, 0, j0 + kKeys, last, j0 + 2 * kKeys - 1 <= all, c, places);
+    if (j0 + kKeys <= any)
+      w.add(k_odd, v_odd, 0, j0 + kKeys, last, j0 + 2 * kKeys - 1 <= all, c, places);
   }
   const float sum = w.sum + __shfl_xor(w.sum, 32);
   if (!on) return;
@@ -155,8 +156,8 @@ struct Split {
   float* weights;  // reference (to the base 2) and sum of powers
   int parts;       // of a row: two per split
 };
-__device__ __forceinline__ int64_t part_of(const AttendArgs& a, const Split& p, int64_t row, int head,
-                                           int part) {
+__device__ __forceinline__ int64_t part_of(const AttendArgs& a, const Split& p, int64_t row,
+                                           int head, int part) {
   return (row * a.q_heads + head) * p.parts + part;
 }
 
@@ -333,7 +334,8 @@ AttendArgs attend_args(const sched_attention_desc& d) {
 
 size_t attention_bytes(const sched_attention_desc& d) {
   const int splits = splits_of(d);
-  return splits == 1 ? 0 : part_count(d, splits) * ((d.head_dim > 64 ? 128 : 64) + 2) * sizeof(float);
+  const size_t each = size_t(d.head_dim > 64 ? 128 : 64) + 2;
+  return splits == 1 ? 0 : part_count(d, splits) * each * sizeof(float);
 }
 
 hipError_t launch_attention(const sched_attention_desc& d, void* ws, hipStream_t s) {

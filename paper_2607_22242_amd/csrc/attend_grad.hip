@@ -76,10 +76,10 @@ struct RowTiles {
       const int step = F::kStep / a.group;
 #pragma unroll
       for (int p = 0; p < F::kRounds; ++p) {
-        to_lds(reinterpret_cast<const char*>(head_row<T>(a.q, row + p * step, kv * a.group)), q_lane,
-               F::at(q_tile, p));
-        to_lds(reinterpret_cast<const char*>(head_row<T>(a.d_out, row + p * step, kv * a.group)),
-               o_lane, F::at(o_tile, p));
+        const T* q = head_row<T>(a.q, row + p * step, kv * a.group);
+        const T* o = head_row<T>(a.d_out, row + p * step, kv * a.group);
+        to_lds(reinterpret_cast<const char*>(q), q_lane, F::at(q_tile, p));
+        to_lds(reinterpret_cast<const char*>(o), o_lane, F::at(o_tile, p));
       }
     } else {
       const F fill(a.dim);
@@ -193,7 +193,8 @@ template <class T, int D>
 __global__ __launch_bounds__(kThreads, 2) void keys_kernel(AttendArgs a, int tiles) {
   __shared__ __attribute__((aligned(16))) T q_even[kTile * D], o_even[kTile * D];
   __shared__ __attribute__((aligned(16))) T q_odd[kTile * D], o_odd[kTile * D];
-  __shared__ __attribute__((aligned(16))) T v_rest[KeySweep<T, D>::kHeld < D / 16 ? kKeysOfBlock * 64 : 8];
+  constexpr int kRest = KeySweep<T, D>::kHeld < D / 16 ? kKeysOfBlock * 64 : 8;
+  __shared__ __attribute__((aligned(16))) T v_rest[kRest];
   __shared__ __attribute__((aligned(16))) Stats s_even, s_odd;
   const Work work = work_of(int(blockIdx.x), tiles, a.q_heads / a.group);
   if (work.tile >= tiles) return;
@@ -202,7 +203,8 @@ __global__ __launch_bounds__(kThreads, 2) void keys_kernel(AttendArgs a, int til
   const int first = tile.index * kKeysOfBlock;
   if (tile.index < 0 || first >= s.slot) return;
   const int lane = int(threadIdx.x) % kWave, wave = wave_id();
-  const int kv = work.kv, part = wave / 2 * 32, wave_row = wave % 2 * 32, wave_key = first + wave_row;
+  const int kv = work.kv, part = wave / 2 * 32, wave_row = wave % 2 * 32;
+  const int wave_key = first + wave_row;
   const float c = a.scale * kLog2e;
   const Places<D> places;
   const Rows<T, 64> rest = {v_rest, Places<64>()};
@@ -368,7 +370,8 @@ __global__ __launch_bounds__(kThreads, 2) void queries_kernel(AttendArgs a, int 
     if (j0 + kTile >= end) break;
     tiles_barrier();
     if (j0 + 2 * kTile < end) tiles_of.fetch(j0 + 2 * kTile, k_even, v_even, a.dim);
-    if (j0 + kTile <= any) w.add(k_odd, v_odd, j0 + kTile, last, j0 + 2 * kTile - 1 <= all, c, places);
+    if (j0 + kTile <= any)
+      w.add(k_odd, v_odd, j0 + kTile, last, j0 + 2 * kTile - 1 <= all, c, places);
   }
   if (on) store_column<T, D>(head_row<T>(a.d_q, s.q0 + me.query, me.head), w.dq, a.dim, a.scale);
 }

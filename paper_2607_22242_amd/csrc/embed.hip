@@ -64,8 +64,9 @@ __global__ __launch_bounds__(kBlock) void embed_kernel(const T* table, int64_t v
 // (waves x kBins in LDS) ends as each wave's running count per digit; place()
 // is called for every key with its number among the block's keys of its digit.
 template <int kRounds, int kThreads>
-__device__ __forceinline__ void count_digits(const uint32_t (&key)[kRounds], const bool (&on)[kRounds],
-                                             int shift, int bins, uint32_t* counts) {
+__device__ __forceinline__ void count_digits(const uint32_t (&key)[kRounds],
+                                             const bool (&on)[kRounds], int shift, int bins,
+                                             uint32_t* counts) {
   for (int i = int(threadIdx.x); i < bins * (kThreads / kWave); i += kThreads) counts[i] = 0;
   __syncthreads();
   uint32_t* mine = counts + int(threadIdx.x) / kWave * bins;
@@ -409,7 +410,8 @@ __global__ __launch_bounds__(kMostThreads) void chunk_kernel(SumArgs a) {
   float acc[N] = {};
   add_rows<T>(a, b, e, j, acc);
   join_groups(a, acc);
-  if (int(threadIdx.x) % kWave < a.lanes) write_piece(a.partial + int64_t(c) * a.dim, j, a.dim, acc);
+  if (int(threadIdx.x) % kWave < a.lanes)
+    write_piece(a.partial + int64_t(c) * a.dim, j, a.dim, acc);
 }
 
 // First place of the sorted list whose token is at least v, by a wave: 64 probes

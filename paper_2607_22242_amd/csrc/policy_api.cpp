@@ -174,7 +174,8 @@ int sched_group_advantages(const int64_t* makespan_us, const int64_t* limit_us,
   if (n_answers < 0 || n_answers >= kMostAnswers || n_groups < 0 || (n_answers > 0 && n_groups < 1))
     return SCHED_E_SIZE;
   if (mean != 0 && mean != 1) return SCHED_E_VALUE;
-  if (n_answers > 0 && (!makespan_us || !limit_us || !group_offsets || !offsets)) return SCHED_E_NULL;
+  if (n_answers > 0 && (!makespan_us || !limit_us || !group_offsets || !offsets))
+    return SCHED_E_NULL;
   if (tokens->n > 0 && (!advantages || !weights)) return SCHED_E_NULL;
   if (int e = check_workspace(d_workspace, ws_bytes, size_t(n_answers) * 4)) return e;
   return done(launch_advantages(makespan_us, limit_us, group_offsets, n_groups, offsets, n_answers,

@@ -380,7 +380,8 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(RowArgs a) {
   const T* row = static_cast<const T*>(a.logits) + i * a.stride;
   const float xt = float(row[token]);
   __syncthreads();  // every thread has the token's logit before one writes there
-  row_grad<T, kThreads, false>(row, out, a.vocab, a.c, xt, l * kLog2e, a.d_logp[i] * a.inv_t, token);
+  row_grad<T, kThreads, false>(row, out, a.vocab, a.c, xt, l * kLog2e, a.d_logp[i] * a.inv_t,
+                               token);
 }
 
 template <class T>

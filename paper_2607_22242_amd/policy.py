@@ -68,21 +68,23 @@ _ARGS = {
     "sched_attention_grad": [_P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P],
 }
 
-_lib = None
-_types = None
+_F32 = _F16 = _BF16 = _INT32 = _INT64 = None  # torch's types, once it is loaded
+_torch = _types = None
+_call = {}  # the library's functions
 
 
 def _load():
-    global _lib, _types
-    if _lib is None:
-        import torch
-        L = _b.lib()
-        for name, args in _ARGS.items():
-            fn = getattr(L, name)
-            fn.restype, fn.argtypes = ctypes.c_int, args
-        _types = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
-        _lib = L
-    return _lib
+    global _torch, _types, _F32, _F16, _BF16, _INT32, _INT64
+    import torch
+    L = _b.lib()
+    for name, args in _ARGS.items():
+        fn = getattr(L, name)
+        fn.restype, fn.argtypes = ctypes.c_int, args
+        _call[name] = fn
+    _F32, _F16, _BF16 = torch.float32, torch.float16, torch.bfloat16
+    _INT32, _INT64 = torch.int32, torch.int64
+    _types = {_F32: 0, _F16: 1, _BF16: 2}
+    _torch = torch
 
 
 def _refuse(code: int, where: str):
@@ -90,33 +92,36 @@ def _refuse(code: int, where: str):
 
 
 class _Call:
-    """The tensors of one call: their GPU, its stream, and what they are."""
+    """The tensors of one call: their GPU, its stream, and what they are.  A
+    call of some microseconds is mostly what happens here, so it asks each
+    tensor for as little as it needs."""
+
+    __slots__ = ("where", "device", "index", "stream", "ptr", "other")
 
     def __init__(self, where: str, first, stream):
-        import torch
-        self.torch, self.where = torch, where
-        if not isinstance(first, torch.Tensor) or not first.is_cuda:
+        if _torch is None:
+            _load()
+        self.where = where
+        index = first.get_device() if isinstance(first, _torch.Tensor) else -1
+        if index < 0 or not first.is_cuda:
             _refuse(-3, where + ": tensors are on a GPU")
-        self.device = first.device
-        current = torch.cuda.current_stream(self.device)
-        self.stream = current if stream is None else stream
-        self.ptr = self.stream.cuda_stream
-        # Tensors made here belong to the current stream, inputs to any.
-        self.other = stream is not None and stream != current
-        self.lib = _load()
+        self.index, self.device, self.stream = index, first.device, stream
+        current = _torch._C._cuda_getCurrentRawStream(index)
+        self.ptr = current if stream is None else stream.cuda_stream
+        # Tensors made here belong to the call's stream, inputs to any.
+        self.other = self.ptr != current
 
     def use(self, t):
-        if t.device != self.device:
+        if t.get_device() != self.index:
             _refuse(-3, self.where + ": tensors are on one GPU")
         if self.other:
             t.record_stream(self.stream)
-        return t
 
     def new(self, shape, dtype):
         if not self.other:
-            return self.torch.empty(shape, dtype=dtype, device=self.device)
-        with self.torch.cuda.stream(self.stream):
-            return self.torch.empty(shape, dtype=dtype, device=self.device)
+            return _torch.empty(shape, dtype=dtype, device=self.device)
+        with _torch.cuda.stream(self.stream):
+            return _torch.empty(shape, dtype=dtype, device=self.device)
 
     def matrix(self, t) -> sched_matrix:
         self.use(t)
@@ -129,14 +134,15 @@ class _Call:
         stride, step = t.stride()
         if step != 1 and cols > 1:
             _refuse(-3, self.where + ": the elements of a row are next to each other")
-        return sched_matrix(t.data_ptr(), kind, rows, cols, stride if rows > 1 else max(stride, cols))
+        stride = stride if rows > 1 else max(stride, cols)
+        return sched_matrix(t.data_ptr(), kind, rows, cols, stride)
 
     def tokens(self, t) -> sched_tokens:
         self.use(t)
-        torch = self.torch
-        if t.dtype not in (torch.int64, torch.int32) or not t.is_contiguous():
+        bits = 64 if t.dtype == _INT64 else 32 if t.dtype == _INT32 else 0
+        if not bits or not t.is_contiguous():
             _refuse(-3, self.where + ": tokens are contiguous int32 or int64")
-        return sched_tokens(t.data_ptr(), 8 * t.element_size(), t.numel())
+        return sched_tokens(t.data_ptr(), bits, t.numel())
 
     def vector(self, t, dtype, n: Optional[int] = None) -> int:
         self.use(t)
@@ -149,8 +155,8 @@ class _Call:
     def floats(self, t, n: int):
         """A 32-bit result of n values: new, or the tensor that is given."""
         if t is None:
-            t = self.new((n,), self.torch.float32)
-        self.vector(t, self.torch.float32, n)
+            return self.new((n,), _F32)
+        self.vector(t, _F32, n)
         return t
 
     def workspace(self, given, nbytes: int):
@@ -160,19 +166,28 @@ class _Call:
             return given, given.data_ptr(), given.numel() * given.element_size()
         if nbytes == 0:
             return None, None, 0
-        ws = self.new((nbytes + 256,), self.torch.uint8)
-        at = (ws.data_ptr() + 255) // 256 * 256
+        ws = self.new((nbytes,), _torch.uint8)
+        at = ws.data_ptr()
+        if at % 256:  # not from torch's own allocator
+            ws = self.new((nbytes + 256,), _torch.uint8)
+            at = (ws.data_ptr() + 255) // 256 * 256
         return ws, at, nbytes
 
     def done(self, name: str, *args):
-        fn = getattr(self.lib, name)
-        if self.torch.cuda.current_device() == self.device.index:
-            rc = fn(*args, self.ptr)
+        if _torch._C._cuda_getDevice() == self.index:
+            rc = _call[name](*args, self.ptr)
         else:
-            with self.torch.cuda.device(self.device):
-                rc = fn(*args, self.ptr)
+            with _torch.cuda.device(self.index):
+                rc = _call[name](*args, self.ptr)
         if rc:
             _refuse(rc, self.where)
+
+    def bytes(self, name: str, *args) -> int:
+        need = ctypes.c_size_t()
+        rc = _call[name](*args, ctypes.byref(need))
+        if rc:
+            _refuse(rc, self.where)
+        return need.value
 
 
 def sched_embed(table, tokens, scale: float = 1.0, out=None, stream=None):
@@ -203,11 +218,8 @@ def sched_embed_grad(d_rows, tokens, vocab: int, scale: float = 1.0, out=None,
     o = c.matrix(out)
     if o.rows != vocab:
         _refuse(-2, c.where + ": out has a row per token of the vocabulary")
-    need = ctypes.c_size_t()
-    rc = c.lib.sched_embed_grad_workspace_bytes(t.n, m.cols, ctypes.byref(need))
-    if rc:
-        _refuse(rc, c.where)
-    ws, at, nbytes = c.workspace(workspace, need.value)
+    need = c.bytes("sched_embed_grad_workspace_bytes", t.n, m.cols)
+    ws, at, nbytes = c.workspace(workspace, need)
     c.done("sched_embed_grad", ctypes.byref(m), ctypes.byref(t), scale, int(accumulate),
            ctypes.byref(o), at, nbytes)
     return out
@@ -230,9 +242,9 @@ def sched_token_logprobs_grad(logits, tokens, logp, d_logp, temperature: float =
     m, t = c.matrix(logits), c.tokens(tokens)
     if d_logits is None:
         d_logits = c.new((m.rows, m.cols), logits.dtype)
-    d, f32 = c.matrix(d_logits), c.torch.float32
+    d = c.matrix(d_logits)
     c.done("sched_token_logprobs_grad", ctypes.byref(m), ctypes.byref(t), temperature,
-           c.vector(logp, f32, t.n), c.vector(d_logp, f32, t.n), ctypes.byref(d))
+           c.vector(logp, _F32, t.n), c.vector(d_logp, _F32, t.n), ctypes.byref(d))
     return d_logits
 
 
@@ -246,15 +258,15 @@ def sched_group_advantages(makespans, limits, group_offsets, offsets, tokens, me
     makespans count up to limits[g]; answer a holds the tokens
     offsets[a]..offsets[a+1].  mean: "tokens" or "sequences"."""
     c = _Call("sched_group_advantages", makespans, stream)
-    torch, t = c.torch, c.tokens(tokens)
+    t = c.tokens(tokens)
     if mean not in _MEANS:
         _refuse(-3, c.where + ": mean is 'tokens' or 'sequences'")
     n, g = makespans.numel(), limits.numel()
     advantages, weights = c.floats(advantages, t.n), c.floats(weights, t.n)
     ws, at, nbytes = c.workspace(workspace, 4 * n)
-    c.done("sched_group_advantages", c.vector(makespans, torch.int64, n),
-           c.vector(limits, torch.int64, g), c.vector(group_offsets, torch.int32, g + 1), g,
-           c.vector(offsets, torch.int32, n + 1), n, ctypes.byref(t), _MEANS[mean],
+    c.done("sched_group_advantages", c.vector(makespans, _INT64, n),
+           c.vector(limits, _INT64, g), c.vector(group_offsets, _INT32, g + 1), g,
+           c.vector(offsets, _INT32, n + 1), n, ctypes.byref(t), _MEANS[mean],
            advantages.data_ptr(), weights.data_ptr(), at, nbytes)
     return advantages, weights
 
@@ -266,7 +278,7 @@ def sched_policy_loss(logits, tokens, old_logp, ref_logp, advantages, weights,
     """(loss, losses, logp, d_logits) of the clipped policy loss; ref_logp may
     be None where kl_weight is 0, d_logits the logits themselves."""
     c = _Call("sched_policy_loss", logits, stream)
-    m, t, f32 = c.matrix(logits), c.tokens(tokens), c.torch.float32
+    m, t, f32 = c.matrix(logits), c.tokens(tokens), _F32
     if d_logits is None:
         d_logits = c.new((m.rows, m.cols), logits.dtype)
     loss, losses, logp = c.floats(loss, 1), c.floats(losses, t.n), c.floats(logp, t.n)
@@ -286,15 +298,14 @@ def sched_preference_loss(logp, ref_logp, tokens, offsets, beta: float = 0.1,
     """(loss, margins, d_logp) over pairs: sequence 2p of offsets is the better
     mapping's, 2p + 1 the worse one's."""
     c = _Call("sched_preference_loss", logp, stream)
-    t, torch = c.tokens(tokens), c.torch
+    t = c.tokens(tokens)
     pairs, odd = divmod(offsets.numel() - 1, 2)
     if odd:
         _refuse(-2, c.where + ": two sequences per pair")
     loss, margins, d_logp = c.floats(loss, 1), c.floats(margins, pairs), c.floats(d_logp, t.n)
-    c.done("sched_preference_loss", c.vector(logp, torch.float32, t.n),
-           c.vector(ref_logp, torch.float32, t.n), ctypes.byref(t),
-           c.vector(offsets, torch.int32), pairs, beta, smoothing, loss_scale, loss.data_ptr(),
-           margins.data_ptr(), d_logp.data_ptr())
+    c.done("sched_preference_loss", c.vector(logp, _F32, t.n), c.vector(ref_logp, _F32, t.n),
+           ctypes.byref(t), c.vector(offsets, _INT32), pairs, beta, smoothing, loss_scale,
+           loss.data_ptr(), margins.data_ptr(), d_logp.data_ptr())
     return loss, margins, d_logp
 
 
@@ -311,7 +322,6 @@ def _heads(c: _Call, t, dtype, heads: int, dim: int) -> sched_heads:
 
 
 def _attention_desc(c, q, k, v, out, lse, q_offsets, k_offsets, k_lengths, causal, scale):
-    i32 = c.torch.int32
     if q.dim() != 3 or k.dim() != 3 or k.shape[0] != v.shape[0]:
         _refuse(-2, c.where + ": q, k and v are rows x heads x dim")
     rows, heads, dim = q.shape
@@ -319,21 +329,14 @@ def _attention_desc(c, q, k, v, out, lse, q_offsets, k_offsets, k_lengths, causa
     d = sched_attention_desc(
         _heads(c, q, q.dtype, heads, dim), _heads(c, k, q.dtype, k.shape[1], dim),
         _heads(c, v, q.dtype, k.shape[1], dim), _heads(c, out, q.dtype, heads, dim),
-        c.vector(lse, c.torch.float32, heads * rows), _types.get(q.dtype, -1), dim, heads,
-        k.shape[1], rows, k.shape[0], c.vector(q_offsets, i32), c.vector(k_offsets, i32, n + 1),
-        None if k_lengths is None else c.vector(k_lengths, i32, n), n, int(causal),
+        c.vector(lse, _F32, heads * rows), _types.get(q.dtype, -1), dim, heads,
+        k.shape[1], rows, k.shape[0], c.vector(q_offsets, _INT32),
+        c.vector(k_offsets, _INT32, n + 1),
+        None if k_lengths is None else c.vector(k_lengths, _INT32, n), n, int(causal),
         1.0 / math.sqrt(max(dim, 1)) if scale is None else scale)
     if out.shape[0] != rows:
         _refuse(-2, c.where + ": out has a row per query")
     return d
-
-
-def _bytes(c, name, d) -> int:
-    need = ctypes.c_size_t()
-    rc = getattr(c.lib, name)(ctypes.byref(d), ctypes.byref(need))
-    if rc:
-        _refuse(rc, c.where)
-    return need.value
 
 
 def sched_attention(q, k, v, q_offsets, k_offsets, k_lengths=None, causal: bool = True,
@@ -346,9 +349,10 @@ def sched_attention(q, k, v, q_offsets, k_offsets, k_lengths=None, causal: bool 
     if out is None:
         out = c.new(tuple(q.shape), q.dtype)
     if lse is None:
-        lse = c.new((q.shape[1], q.shape[0]) if q.dim() == 3 else (0,), c.torch.float32)
+        lse = c.new((q.shape[1], q.shape[0]) if q.dim() == 3 else (0,), _F32)
     d = _attention_desc(c, q, k, v, out, lse, q_offsets, k_offsets, k_lengths, causal, scale)
-    ws, at, nbytes = c.workspace(workspace, _bytes(c, "sched_attention_workspace_bytes", d))
+    need = c.bytes("sched_attention_workspace_bytes", ctypes.byref(d))
+    ws, at, nbytes = c.workspace(workspace, need)
     c.done("sched_attention", ctypes.byref(d), at, nbytes)
     return out, lse
 
@@ -369,7 +373,8 @@ def sched_attention_grad(q, k, v, out, lse, d_out, q_offsets, k_offsets, k_lengt
         _refuse(-2, c.where + ": d_out has a row per query")
     do = _heads(c, d_out, q.dtype, q.shape[1], q.shape[2])
     g = [_heads(c, t, q.dtype, like.shape[1], q.shape[2]) for t, like in zip(grads, (q, k, v))]
-    ws, at, nbytes = c.workspace(workspace, _bytes(c, "sched_attention_grad_workspace_bytes", d))
+    need = c.bytes("sched_attention_grad_workspace_bytes", ctypes.byref(d))
+    ws, at, nbytes = c.workspace(workspace, need)
     c.done("sched_attention_grad", ctypes.byref(d), ctypes.byref(do), ctypes.byref(g[0]),
            ctypes.byref(g[1]), ctypes.byref(g[2]), at, nbytes)
     return tuple(grads)

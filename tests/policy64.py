@@ -169,11 +169,12 @@ class Attention:
                 out = P @ V
                 # A score's error: D + 8 roundings of terms of its products, and
                 # those of the exponent and the sum.
-                ds = F * ((dim + 16) * (Q.abs() @ K.abs().T * scale) + 4 * s.nan_to_num(0, 0, 0).abs()
-                          + n / 16 + 64)
+                size = s.nan_to_num(0, 0, 0).abs()
+                ds = F * ((dim + 16) * (Q.abs() @ K.abs().T * scale) + 4 * size + n / 16 + 64)
                 ds = 2 * ds.amax(1, keepdim=True)
                 self.out[rq, h], self.lse[h, rq] = out, lse[:, 0]
-                self.out_b[rq, h] = (u + ds) * (P @ V.abs()) + u * out.abs() + tiny * (1 + n * V.abs().amax())
+                self.out_b[rq, h] = (u + ds) * (P @ V.abs()) + u * out.abs()
+                self.out_b[rq, h] += tiny * (1 + n * V.abs().amax())
                 self.lse_b[h, rq] = ds[:, 0] + 4 * F * lse[:, 0].nan_to_num(0, 0, 0).abs()
                 if d_out is None:
                     continue
