@@ -50,6 +50,7 @@ struct AttendArgs {
   // at equal distances (groups of 1, 2, 4, 8 or 16): addresses are a sum for
   // the block and a distance for the lane.
   int32_t near_k, near_q;
+  int32_t ranked;  // tiles go by their work (ranked_tile)
   float scale;
 };
 
@@ -67,14 +68,18 @@ __device__ __forceinline__ int wave_id() { return uniform(int(threadIdx.x) / kWa
 struct Seq {
   int q0, k0, queries, keys, slot;
 };
-__device__ __forceinline__ Seq sequence(const AttendArgs& a, int b) {
+__device__ __forceinline__ Seq lane_sequence(const AttendArgs& a, int b) {
   Seq s;
-  s.q0 = uniform(offset_at(a.q_offsets, b, a.q_rows));
-  s.k0 = uniform(offset_at(a.k_offsets, b, a.k_rows));
-  s.queries = max(0, uniform(offset_at(a.q_offsets, b + 1, a.q_rows)) - s.q0);
-  s.slot = max(0, uniform(offset_at(a.k_offsets, b + 1, a.k_rows)) - s.k0);
-  s.keys = a.k_lengths ? min(s.slot, max(0, uniform(a.k_lengths[b]))) : s.slot;
+  s.q0 = offset_at(a.q_offsets, b, a.q_rows);
+  s.k0 = offset_at(a.k_offsets, b, a.k_rows);
+  s.queries = max(0, offset_at(a.q_offsets, b + 1, a.q_rows) - s.q0);
+  s.slot = max(0, offset_at(a.k_offsets, b + 1, a.k_rows) - s.k0);
+  s.keys = a.k_lengths ? min(s.slot, max(0, a.k_lengths[b])) : s.slot;
   return s;
+}
+__device__ __forceinline__ Seq sequence(const AttendArgs& a, int b) {
+  const Seq s = lane_sequence(a, b);
+  return {uniform(s.q0), uniform(s.k0), uniform(s.queries), uniform(s.keys), uniform(s.slot)};
 }
 
 // Tiles of `tile` rows without a list of them: sequence b begins at tile
@@ -104,6 +109,50 @@ __device__ __forceinline__ Tile tile_of(const int32_t* offsets, int n_seqs, int 
   return {lo, number - uniform(base)};
 }
 
+// Tiles of up to 64 sequences from the one with most work to the one with least,
+// so that no long one begins when the others end.  Along a causal sequence the
+// work falls by one level a tile from the tile that sees (or, of keys, is seen
+// by) most; otherwise all tiles of a sequence have the same.  Returns the tile
+// of a rank, counted within its sequence from the one with most work; index -1
+// behind the last.  Every lane brings a sequence: its tiles and its top level.
+__device__ __forceinline__ int wave_total(int x) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
+  return uniform(x);
+}
+__device__ __forceinline__ Tile ranked_tile(int tiles, int top, bool falls, int rank) {
+  // Tiles of this lane's sequence at a level or above.
+  auto above = [&](int level) {
+    return top < level ? 0 : falls ? min(tiles, top - level + 1) : tiles;
+  };
+  int hi = tiles > 0 ? top : -(1 << 30);
+  int lo = tiles > 0 ? (falls ? top - tiles + 1 : top) : 1 << 30;
+#pragma unroll
+  for (int d = 32; d; d >>= 1) {
+    hi = max(hi, __shfl_xor(hi, d));
+    lo = min(lo, __shfl_xor(lo, d));
+  }
+  lo = uniform(lo);
+  hi = uniform(hi);
+  if (lo > hi || wave_total(above(lo)) <= rank) return {0, -1};
+  while (lo < hi) {  // the highest level with more than `rank` tiles at it or above
+    const int mid = lo + (hi - lo + 1) / 2;
+    if (wave_total(above(mid)) > rank) lo = mid;
+    else hi = mid - 1;
+  }
+  const int here = above(lo) - above(lo + 1), behind = rank - wave_total(above(lo + 1));
+  int before = here;  // of this level in earlier sequences, with this one
+#pragma unroll
+  for (int d = 1; d < kWave; d <<= 1) {
+    const int up = __shfl_up(before, d);
+    if (int(threadIdx.x) % kWave >= d) before += up;
+  }
+  before -= here;
+  const int seq = __ffsll((unsigned long long)__ballot(here > 0 && behind < before + here)) - 1;
+  const int index = falls ? top - lo : behind - before;
+  return {seq, uniform(__shfl(index, seq))};
+}
+
 inline int64_t tile_count(int64_t rows, int n_seqs, int tile) { return rows / tile + n_seqs; }
 
 // Query rows of a block: the heads that share a key head are rows of their own,
@@ -111,6 +160,33 @@ inline int64_t tile_count(int64_t rows, int n_seqs, int tile) { return rows / ti
 struct QueryRow {
   int query, head;
 };
+// The tile of query rows of a rank, from most keys to least where the call ranks
+// its tiles, else from the packed tensor's end (of one sequence the same).
+__device__ __forceinline__ Tile query_tile(const AttendArgs& a, int tile, int rank, int count) {
+  if (!a.ranked)
+    return tile_of(a.q_offsets, a.n_seqs, a.q_rows, a.group, tile, count - 1 - rank);
+  const int b = int(threadIdx.x) % kWave;
+  int tiles = 0, top = 0;
+  if (b < a.n_seqs) {
+    const Seq s = lane_sequence(a, b);
+    tiles = (s.queries * a.group + tile - 1) / tile;
+    top = int(min(int64_t(s.keys) * a.group / tile, int64_t(1) << 29));
+  }
+  const Tile t = ranked_tile(tiles, top, a.causal, rank);
+  return {t.seq, t.index < 0 ? -1 : a.causal ? __shfl(tiles, t.seq) - 1 - t.index : t.index};
+}
+// The same of keys, from most query rows to least.
+__device__ __forceinline__ Tile key_tile(const AttendArgs& a, int tile, int rank) {
+  if (!a.ranked) return tile_of(a.k_offsets, a.n_seqs, a.k_rows, 1, tile, rank);
+  const int b = int(threadIdx.x) % kWave;
+  int tiles = 0, top = 0;
+  if (b < a.n_seqs) {
+    const Seq s = lane_sequence(a, b);
+    tiles = (s.slot + tile - 1) / tile;
+    top = a.causal ? s.keys / tile : s.queries;
+  }
+  return ranked_tile(tiles, top, a.causal, rank);
+}
 __device__ __forceinline__ QueryRow query_row(const AttendArgs& a, int kv_head, int r) {
   return {r / a.group, kv_head * a.group + r % a.group};
 }

@@ -98,9 +98,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendArgs a, int t
   __shared__ __attribute__((aligned(16))) T k_odd[kKeys * D], v_odd[kKeys * D];
   const Work work = work_of(int(blockIdx.x), tiles, a.q_heads / a.group);
   if (work.tile >= tiles) return;
-  // The last tiles of a sequence see the most keys: they go first.
-  const Tile tile = tile_of(a.q_offsets, a.n_seqs, a.q_rows, a.group, kRowsOfBlock,
-                            tiles - 1 - work.tile);
+  const Tile tile = query_tile(a, kRowsOfBlock, work.tile, tiles);
   const Seq s = sequence(a, tile.seq);
   const int first = tile.index * kRowsOfBlock, rows = s.queries * a.group;
   if (tile.index < 0 || first >= rows) return;
@@ -260,13 +258,15 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs a, Split p, i
     a.lse[int64_t(head) * a.q_rows + row] = sum > 0.f ? (most + log_2(sum)) * kLn2 : -INFINITY;
 }
 
-// Blocks that a sequence's keys are shared by: 1 where the query rows fill the
-// card (two blocks of 128 rows a unit), else as many as give it 4096 blocks,
-// none of them with less than 256 keys of a sequence of the mean length.
+// Blocks that a sequence's keys are shared by: 1 where there are 64 blocks of
+// query rows (64 of them, 1,000 keys: 33 us so, 36 shared; 40 of them, 16,384
+// keys: 320 us so, 153 shared) unless sequences have a wave's rows at most; else
+// as many as give the card 4096 blocks, none of them with less than 256 keys of
+// a sequence of the mean length.
 int splits_of(const sched_attention_desc& d) {
   if (d.n_seqs == 0 || d.q_rows == 0) return 1;
   const int64_t rows = d.q_rows * (d.q_heads / d.kv_heads);
-  if ((rows / kRowsOfBlock + d.n_seqs) * d.kv_heads >= 2 * 256 && rows / d.n_seqs > 32) return 1;
+  if (rows / d.n_seqs > 32 && (rows / kRowsOfBlock + d.n_seqs) * d.kv_heads >= 64) return 1;
   const int64_t blocks = tile_count(rows, d.n_seqs, 32) * d.kv_heads;
   const int64_t want = (4096 + blocks - 1) / blocks, most = d.k_rows / d.n_seqs / 256;
   return int(std::max<int64_t>(1, std::min<int64_t>({want, most, 256})));
@@ -327,6 +327,9 @@ AttendArgs attend_args(const sched_attention_desc& d) {
   };
   a.near_k = near(d.k) && near(d.v);
   a.near_q = near(d.q) && 16 % a.group == 0;
+  // Several long sequences (8 of 1,500 rows, 16 heads: backward 412 -> 326 us,
+  // forward 108 -> 100; 40 of 400: forward 61 -> 70, so short ones do not).
+  a.ranked = d.n_seqs > 1 && d.n_seqs <= kWave && d.q_rows / d.n_seqs >= 1024;
   a.causal = d.causal;
   a.scale = d.scale;
   return a;

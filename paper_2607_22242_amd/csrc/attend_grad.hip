@@ -198,7 +198,7 @@ __global__ __launch_bounds__(kThreads, 2) void keys_kernel(AttendArgs a, int til
   __shared__ __attribute__((aligned(16))) Stats s_even, s_odd;
   const Work work = work_of(int(blockIdx.x), tiles, a.q_heads / a.group);
   if (work.tile >= tiles) return;
-  const Tile tile = tile_of(a.k_offsets, a.n_seqs, a.k_rows, 1, kKeysOfBlock, work.tile);
+  const Tile tile = key_tile(a, kKeysOfBlock, work.tile);
   const Seq s = sequence(a, tile.seq);
   const int first = tile.index * kKeysOfBlock;
   if (tile.index < 0 || first >= s.slot) return;
@@ -339,9 +339,7 @@ __global__ __launch_bounds__(kThreads, 2) void queries_kernel(AttendArgs a, int 
   __shared__ __attribute__((aligned(16))) T k_odd[kTile * D], v_odd[kTile * D];
   const Work work = work_of(int(blockIdx.x), tiles, a.q_heads / a.group);
   if (work.tile >= tiles) return;
-  // The last tiles of a sequence see the most keys: they go first.
-  const Tile tile = tile_of(a.q_offsets, a.n_seqs, a.q_rows, a.group, kRowsOfBlock,
-                            tiles - 1 - work.tile);
+  const Tile tile = query_tile(a, kRowsOfBlock, work.tile, tiles);
   const Seq s = sequence(a, tile.seq);
   const int first = tile.index * kRowsOfBlock, rows = s.queries * a.group;
   if (tile.index < 0 || first >= rows) return;

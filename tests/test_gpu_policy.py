@@ -361,6 +361,16 @@ def test_attention(dtype, layout):
     check_attention(q, k, v, do, qo, ko, causal)
 
 
+@pytest.mark.parametrize("q_len,k_len,heads,kv,causal", [
+    ([2700, 1, 900, 0, 1600], None, 4, 2, True), ([2300, 700, 1, 1340], None, 3, 1, False),
+    ([1513, 1260], [65, 900], 4, 4, True), ([1400, 1257, 900], [0, 1000, 31], 2, 1, False),
+    ([1024] * 3, None, 2, 2, True), ([20] * 40 + [9000] * 5, [40] * 40 + [80] * 5, 1, 1, True)])
+def test_attention_of_ranked_tiles(q_len, k_len, heads, kv, causal):
+    """Several sequences of some length: tiles go by their work, each once."""
+    q, k, v, do, qo, ko = attention_case(torch.bfloat16, q_len, k_len, heads, kv, 64, sum(q_len))
+    check_attention(q, k, v, do, qo, ko, causal)
+
+
 @pytest.mark.parametrize("dtype", HALVES)
 def test_attention_of_large_scores(dtype):
     """Scores of hundreds: one key takes all, others' powers vanish."""
