@@ -24,7 +24,6 @@ constexpr int kSmallThreads = 1024;
 constexpr int kTile = 2048;              // tokens of a block otherwise
 constexpr int kTileThreads = 512;
 constexpr int kMostThreads = 512;       // of a block of a row's waves
-constexpr int kPer = 8;                 // rows of the table, or places, of a wave
 
 __device__ __forceinline__ uint64_t below(int lane) { return (1ull << lane) - 1; }
 
@@ -273,6 +272,7 @@ struct SumArgs {
   int64_t table_stride;
   int lanes;                 // of a row's piece: a power of two up to 64
   int across, width;         // waves of a block that share a row, and pieces of each
+  int per;                   // rows of the table, or places of the list, of a wave
   int64_t first;             // row of the table or place of the list that the launch starts with
 };
 
@@ -361,11 +361,7 @@ __device__ __forceinline__ void add_rows(const SumArgs& a, uint32_t b, uint32_t 
     const int count = int(min(e - base, uint32_t(kWave)));
     const uint32_t mine = lane < count ? a.at[base + lane] : 0;
     int i = 0;
-    for (; i + 16 * groups <= count; i += 16 * groups) add_batch<T, 16>(a, mine, i + group, j, acc);
-    if (i + 8 * groups <= count) {
-      add_batch<T, 8>(a, mine, i + group, j, acc);
-      i += 8 * groups;
-    }
+    for (; i + 8 * groups <= count; i += 8 * groups) add_batch<T, 8>(a, mine, i + group, j, acc);
     if (i + 4 * groups <= count) {
       add_batch<T, 4>(a, mine, i + group, j, acc);
       i += 4 * groups;
@@ -466,19 +462,19 @@ __device__ __forceinline__ void table_row(const SumArgs& a, int64_t v, uint32_t 
   }
 }
 
-// Every row of the table, kPer in turn by each wave, zeros for those without a
+// Every row of the table, a few in turn by each wave, zeros for those without a
 // run.
 template <class T, class O>
 __global__ __launch_bounds__(kMostThreads) void table_kernel(SumArgs a) {
   const int lane = int(threadIdx.x) % kWave, wave = int(threadIdx.x) / kWave;
   const int at_once = int(blockDim.x) / kWave / a.across;
-  const int64_t v0 = a.first + (int64_t(blockIdx.x) * at_once + wave / a.across) * kPer;
+  const int64_t v0 = a.first + (int64_t(blockIdx.x) * at_once + wave / a.across) * a.per;
   if (v0 >= a.vocab) return;
   const int64_t j = column<T>(a, int64_t(blockIdx.y) * a.across + wave % a.across);
   const uint32_t first = place_of(a.key, a.n, uint32_t(v0));
   const uint32_t near = first + lane < a.n ? a.key[first + lane] : ~0u;
   uint32_t s = first;
-  for (int r = 0; r < kPer && v0 + r < a.vocab; ++r) {
+  for (int r = 0; r < a.per && v0 + r < a.vocab; ++r) {
     // The run's end is among the 64 entries at hand, or it is looked for.
     const int passed = __popcll(__ballot(near <= uint32_t(v0 + r)));
     const uint32_t e = passed < kWave ? first + uint32_t(passed)
@@ -489,17 +485,17 @@ __global__ __launch_bounds__(kMostThreads) void table_kernel(SumArgs a) {
 }
 
 // The rows that have a run, added to what is there: a wave takes the runs that
-// begin at kPer places of the list.
+// begin at a few places of the list.
 template <class T, class O>
 __global__ __launch_bounds__(kMostThreads) void add_kernel(SumArgs a) {
   const int lane = int(threadIdx.x) % kWave, wave = int(threadIdx.x) / kWave;
   const int at_once = int(blockDim.x) / kWave / a.across;
-  const int64_t first = a.first + (int64_t(blockIdx.x) * at_once + wave / a.across) * kPer;
+  const int64_t first = a.first + (int64_t(blockIdx.x) * at_once + wave / a.across) * a.per;
   if (first >= a.n) return;
   const int64_t j = column<T>(a, int64_t(blockIdx.y) * a.across + wave % a.across);
   const uint32_t i = uint32_t(first) + uint32_t(lane);
   const uint32_t near = i < a.n ? a.key[i] : ~0u;
-  const bool begins = lane < kPer && near < uint32_t(a.vocab) && (i == 0 || a.key[i - 1] != near);
+  const bool begins = lane < a.per && near < uint32_t(a.vocab) && (i == 0 || a.key[i - 1] != near);
   for (uint64_t heads = __ballot(begins); heads; heads &= heads - 1) {
     const int at = __ffsll((unsigned long long)heads) - 1;
     const uint32_t v = uint32_t(__shfl(near, at));
@@ -561,7 +557,14 @@ hipError_t sums_of(const SumArgs& in, bool accumulate, hipStream_t s) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  const int64_t per = at_once * kPer, all = accumulate ? int64_t(a.n) : a.vocab;
+  const int64_t all = accumulate ? int64_t(a.n) : a.vocab;
+  // Few rows a wave where there are few, many (one search in the list for all)
+  // where there are more than fill the card: 131072 x 4096, 65,536 tokens, 4, 8
+  // and 16 rows a wave 526, 490 and 467 us; 200 x 1024, 60,000 tokens, 115, 147
+  // and 183.
+  a.per = 1;
+  while (a.per < 16 && all * waves / (a.per * 2) >= 16384) a.per *= 2;
+  const int64_t per = int64_t(at_once) * a.per;
   const int64_t blocks = (all + per - 1) / per;
   hipError_t e = hipSuccess;
   for (int64_t b = 0; b < blocks && e == hipSuccess; b += kMostBlocks) {
