@@ -24,10 +24,10 @@
  * more; results are rounded once to their type.  Probabilities below 2^-126
  * count as zero.  Tokens are 32- or 64-bit integers; one outside [0, vocab) (-1,
  * say) is padding: it carries no loss, looks up zeros and takes no part in a
- * gradient.  Tensors have less than 2^31 rows.  Offsets are 32-bit integers on
- * the device, ascending; sequence i of n holds the rows offsets[i] ..
- * offsets[i+1] - 1 of its packed tensor, perhaps none, and the n sequences cover
- * it.  Offsets that leave the tensor are cut to it.
+ * gradient.  Tensors have up to 2^31 - 1024 rows and columns.  Offsets are
+ * 32-bit integers on the device, ascending; sequence i of n holds the rows
+ * offsets[i] .. offsets[i+1] - 1 of its packed tensor, perhaps none, and the n
+ * sequences cover it.  Offsets that leave the tensor are cut to it.
  */
 #ifndef SCHED_POLICY_H
 #define SCHED_POLICY_H
@@ -89,8 +89,8 @@ int sched_token_logprobs(const sched_matrix *logits, const sched_tokens *tokens,
                          float temperature, float *logp, void *hip_stream);
 
 /* Its gradient: d_logits[i][j] = d_logp[i] * ((j == tokens[i]) - q[j]) /
- * temperature with q the row's probabilities, taken from logp (of the call
- * above); zeros for padding and for tokens with logp = -inf.  d_logits: of
+ * temperature with q the row's probabilities (logp is the result of the call
+ * above, from which they are taken where it is no less than -32); zeros for padding and for tokens with logp = -inf.  d_logits: of
  * logits' type and size; it may be logits itself. */
 int sched_token_logprobs_grad(const sched_matrix *logits, const sched_tokens *tokens,
                               float temperature, const float *logp, const float *d_logp,
@@ -106,7 +106,7 @@ int sched_token_logprobs_grad(const sched_matrix *logits, const sched_tokens *to
  * weight is 1 / (tokens that are no padding) with mean = 0, and with mean = 1
  * 1 / (answers with such tokens * such tokens of its answer); 0 for padding.
  * advantages and weights: 32-bit values, tokens->n each.  tokens counts as
- * padding what is negative.  Fewer than 2^24 answers.  Workspace: 4 bytes per
+ * padding what is negative.  Up to 65,536 answers.  Workspace: 4 bytes per
  * answer. */
 int sched_group_advantages(const int64_t *makespan_us, const int64_t *limit_us,
                            const int32_t *group_offsets, int32_t n_groups,
@@ -166,7 +166,9 @@ typedef struct {
  * Query head h reads key head h / (q_heads / kv_heads).  With causal = 1 the
  * last query row sees every key and each one before it one less (query i of
  * n_q sees the keys j <= i + n_k - n_q).  scale is applied to the products.
- * A row that sees no key gives zeros, lse = -inf and zero gradients.
+ * A row that sees no key gives zeros, lse = -inf and zero gradients.  Key rows
+ * behind a length may hold anything; those of a sequence that causal = 1 alone
+ * hides from a row have weight zero there and have to be finite.
  * head_dim: a multiple of 8 up to 128.  dtype: SCHED_F16 or SCHED_BF16; the
  * probabilities are rounded to it before they are multiplied with the values.
  * q_rows * q_heads / 32 + n_seqs * kv_heads and k_rows * kv_heads / 64 + n_seqs *

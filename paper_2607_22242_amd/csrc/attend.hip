@@ -135,10 +135,10 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendArgs a, int t
   const float sum = w.sum + __shfl_xor(w.sum, 32);
   if (!on) return;
   store_column<T, D>(head_row<T>(a.out, s.q0 + me.query, me.head), w.o, a.dim,
-                     sum > 0.f ? 1.f / sum : 0.f);
+                     sum == 0.f ? 0.f : 1.f / sum);  // a sum of NaN stays one
   if (lane < 32)
     a.lse[int64_t(me.head) * a.q_rows + s.q0 + me.query] =
-        sum > 0.f ? (w.most * c + log_2(sum)) * kLn2 : -INFINITY;
+        sum == 0.f ? -INFINITY : (w.most * c + log_2(sum)) * kLn2;
 }
 
 // --- few query rows -----------------------------------------------------------
@@ -220,13 +220,13 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs a, Split p, i
   const float* const weights = p.weights + i * p.parts * 2;
   float most = -INFINITY;
   for (int k = lane; k < p.parts; k += kWave)
-    if (weights[2 * k + 1] > 0.f) most = fmaxf(most, weights[2 * k]);
+    if (weights[2 * k + 1] != 0.f) most = fmaxf(most, weights[2 * k]);
   most = wave_max(most);
   float o[D / kWave] = {}, sum = 0.f;
   for (int k0 = 0; k0 < p.parts; k0 += kWave) {
     // A part's factor and sum, by the lane that has it.
     float f = 0.f, s = 0.f;
-    if (k0 + lane < p.parts && weights[2 * (k0 + lane) + 1] > 0.f) {
+    if (k0 + lane < p.parts && weights[2 * (k0 + lane) + 1] != 0.f) {
       f = pow2(weights[2 * (k0 + lane)] - most);
       s = weights[2 * (k0 + lane) + 1] * f;
     }
@@ -253,9 +253,9 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs a, Split p, i
   T* const out = head_row<T>(a.out, row, head);
 #pragma unroll
   for (int d = 0; d < D / kWave; ++d)
-    if (d * kWave + lane < a.dim) out[d * kWave + lane] = T(sum > 0.f ? o[d] / sum : 0.f);
+    if (d * kWave + lane < a.dim) out[d * kWave + lane] = T(sum == 0.f ? 0.f : o[d] / sum);
   if (lane == 0)
-    a.lse[int64_t(head) * a.q_rows + row] = sum > 0.f ? (most + log_2(sum)) * kLn2 : -INFINITY;
+    a.lse[int64_t(head) * a.q_rows + row] = sum == 0.f ? -INFINITY : (most + log_2(sum)) * kLn2;
 }
 
 // Blocks that a sequence's keys are shared by: 1 where there are 64 blocks of

@@ -10,9 +10,10 @@ using namespace policy;
 
 namespace {
 
-constexpr int64_t kMostRows = (int64_t(1) << 31) - 1;
+constexpr int64_t kMostRows = (int64_t(1) << 31) - 1024;  // strides over rows stay in 32 bits
 constexpr int64_t kMostDim = int64_t(1) << 24;    // of an embedding
-constexpr int32_t kMostAnswers = 1 << 24;
+constexpr int32_t kMostPairs = 1 << 23;
+constexpr int32_t kMostAnswers = 1 << 16;         // every one's wave adds up all counts
 constexpr int64_t kMostTiles = (1 << 24) - 8;     // blocks of 256 threads in a grid
 
 int done(hipError_t e) { return e == hipSuccess ? SCHED_OK : SCHED_E_DEVICE; }
@@ -84,8 +85,8 @@ int check_attention_sizes(const sched_attention_desc& d) {
   if (d.head_dim < 8 || d.head_dim > 128 || d.head_dim % 8 || d.kv_heads < 1 ||
       d.kv_heads > 65535 || d.q_heads < 1 || d.q_heads % d.kv_heads ||
       d.q_heads / d.kv_heads > 4096 || d.n_seqs < 0 ||
-      d.q_rows < 0 || d.k_rows < 0 || d.k_rows > kMostRows - 256 || d.q_rows > kMostRows ||
-      d.q_rows * (d.q_heads / d.kv_heads) > kMostRows - 256)
+      d.q_rows < 0 || d.k_rows < 0 || d.k_rows > kMostRows || d.q_rows > kMostRows ||
+      d.q_rows * (d.q_heads / d.kv_heads) > kMostRows)
     return SCHED_E_SIZE;
   const int64_t q_tiles = d.q_rows * (d.q_heads / d.kv_heads) / 32 + d.n_seqs;
   const int64_t k_tiles = d.k_rows / 64 + d.n_seqs;
@@ -171,7 +172,7 @@ int sched_group_advantages(const int64_t* makespan_us, const int64_t* limit_us,
                            void* hip_stream) {
   if (!tokens) return SCHED_E_NULL;
   if (int e = check_tokens(*tokens)) return e;
-  if (n_answers < 0 || n_answers >= kMostAnswers || n_groups < 0 || (n_answers > 0 && n_groups < 1))
+  if (n_answers < 0 || n_answers > kMostAnswers || n_groups < 0 || (n_answers > 0 && n_groups < 1))
     return SCHED_E_SIZE;
   if (mean != 0 && mean != 1) return SCHED_E_VALUE;
   if (n_answers > 0 && (!makespan_us || !limit_us || !group_offsets || !offsets))
@@ -204,7 +205,7 @@ int sched_preference_loss(const float* logp, const float* ref_logp, const sched_
                           void* hip_stream) {
   if (!tokens) return SCHED_E_NULL;
   if (int e = check_tokens(*tokens)) return e;
-  if (n_pairs < 1 || 2 * int64_t(n_pairs) >= kMostAnswers) return SCHED_E_SIZE;
+  if (n_pairs < 1 || n_pairs >= kMostPairs) return SCHED_E_SIZE;
   if (!offsets || !loss || !margins || (tokens->n > 0 && (!logp || !ref_logp || !d_logp)))
     return SCHED_E_NULL;
   if (!std::isfinite(beta) || !std::isfinite(loss_scale) || !(smoothing >= 0) || !(smoothing <= 1))

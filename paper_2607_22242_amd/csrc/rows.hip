@@ -77,9 +77,10 @@ __device__ __forceinline__ Soft block_join(Soft a, float c, Soft* part) {
   return a;
 }
 
-// Log-probability of a token with logit x in a row with these statistics.
-__device__ __forceinline__ float log_prob(float x, Soft r, float c) {
-  return r.s == 0.f ? -INFINITY : ((x - finite_max(r.m)) * c - log_2(r.s)) * kLn2;
+// Log-probability of a token with logit x in a row with these statistics (not in
+// base 2: the type's lowest logit, a mask, would leave the range).
+__device__ __forceinline__ float log_prob(const RowArgs& a, float x, Soft r) {
+  return r.s == 0.f ? -INFINITY : (x - finite_max(r.m)) * a.inv_t - log_2(r.s) * kLn2;
 }
 
 template <class T, int N>
@@ -183,9 +184,10 @@ __device__ __forceinline__ TokenLoss token_loss(const RowArgs& a, int64_t i, flo
   const float free = -adv * r, held = -adv * fminf(fmaxf(r, a.lo), a.hi);
   float loss = fmaxf(free, held), slope = free >= held ? free : 0.f;
   if (a.kl != 0.f) {
-    const float e = a.ref_logp[i] - l, k = pow2(e * kLog2e);
-    loss += a.kl * (k - e - 1.f);
-    slope += a.kl * (1.f - k);
+    // exp(e) - 1 as such: e is mostly small, and the term is of its square.
+    const float e = a.ref_logp[i] - l, k = expm1f(e);
+    loss += a.kl * (k == INFINITY ? k : k - e);
+    slope -= a.kl * k;
   }
   return {w * loss, w * slope * a.loss_scale};
 }
@@ -193,22 +195,29 @@ __device__ __forceinline__ TokenLoss token_loss(const RowArgs& a, int64_t i, flo
 // kPolicy: the policy loss with the gradient; else log-probabilities alone.
 
 // `lanes` (a power of two up to 64) of a wave take a row of at most as many
-// logits.
+// logits, lane t of them logit t.
+template <class T>
+__device__ __forceinline__ Soft lanes_soft(const RowArgs& a, int64_t i, int t, bool on, int lanes,
+                                           float& x) {
+  x = on && t < int(a.vocab) ? float(static_cast<const T*>(a.logits)[i * a.stride + t]) : -INFINITY;
+  Soft r = {x, 0.f};
+  for (int d = 1; d < lanes; d <<= 1) r.m = fmaxf(r.m, __shfl_xor(r.m, d));
+  r.s = pow2((x - finite_max(r.m)) * a.c);
+  for (int d = 1; d < lanes; d <<= 1) r.s += __shfl_xor(r.s, d);
+  return r;
+}
+
 template <class T, bool kPolicy>
 __global__ __launch_bounds__(kBlock) void lanes_kernel(RowArgs a, int lanes) {
   const int64_t i = a.first + int64_t(blockIdx.x) * (kBlock / lanes) + int(threadIdx.x) / lanes;
   if (i >= a.n) return;  // all of a row's lanes
   const int t = int(threadIdx.x) % lanes, vocab = int(a.vocab);
   const int token = int(token_in(a.tokens, i, a.vocab));
-  const float x = t < vocab && token >= 0 ? float(static_cast<const T*>(a.logits)[i * a.stride + t])
-                                          : -INFINITY;
-  float m = x;
-  for (int d = 1; d < lanes; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
-  const float f = finite_max(m), e = pow2((x - f) * a.c);
-  float sum = e;
-  for (int d = 1; d < lanes; d <<= 1) sum += __shfl_xor(sum, d);
+  float x;
+  const Soft r = lanes_soft<T>(a, i, t, token >= 0, lanes, x);
+  const float f = finite_max(r.m);
   const float xt = __shfl(x, (int(threadIdx.x) % kWave) / lanes * lanes + max(token, 0));
-  const float l = token < 0 ? 0.f : log_prob(xt, {m, sum}, a.c);
+  const float l = token < 0 ? 0.f : log_prob(a, xt, r);
   if (t == 0) a.logp[i] = l;
   if (!kPolicy) return;
   TokenLoss k = {0.f, 0.f};
@@ -217,7 +226,7 @@ __global__ __launch_bounds__(kBlock) void lanes_kernel(RowArgs a, int lanes) {
   if (t >= vocab) return;
   float d = 0.f;
   if (token >= 0 && l != -INFINITY) {
-    const float p = pow2(__builtin_fmaf(x - f, a.c, -log_2(sum)));
+    const float p = pow2(__builtin_fmaf(x - f, a.c, -log_2(r.s)));
     d = k.slope * a.inv_t * (t == token ? 1.f - p : -p);
   }
   static_cast<T*>(a.d_logits)[i * a.d_stride + t] = T(d);
@@ -266,7 +275,7 @@ __global__ __launch_bounds__(kThreads < kBlock ? kBlock : kThreads) void held_ke
 #pragma unroll
     for (int w = 0; w < kThreads / kWave; ++w) sum += part[1][w];
   }
-  const float l = log_prob(xt, {m, sum}, a.c);
+  const float l = log_prob(a, xt, {m, sum});
   if (t == 0) a.logp[i] = l;
   if (!kPolicy) return;
   const TokenLoss k = token_loss(a, i, l);
@@ -358,7 +367,7 @@ __global__ __launch_bounds__(kThreads) void long_kernel(RowArgs a) {
   const T* row = static_cast<const T*>(a.logits) + i * a.stride;
   const float xt = float(row[token]);
   const Soft r = row_soft<T, kThreads>(row, a.vocab, a.c, part);
-  const float l = log_prob(xt, r, a.c);
+  const float l = log_prob(a, xt, r);
   if (threadIdx.x == 0) a.logp[i] = l;
   if (!kPolicy) return;
   const TokenLoss k = token_loss(a, i, l);
@@ -370,6 +379,10 @@ __global__ __launch_bounds__(kThreads) void long_kernel(RowArgs a) {
 
 // The gradient alone, of rows of more than 64 logits: 1024 threads a row from
 // 32,768 logits on (48 pairs, 50021 logits: 589 us, 626 with 256), else 256.
+// Powers count from the token's logit and its log-probability l, two numbers of
+// the size of l: where that is large (a token that was all but ruled out) their
+// roundings would show, and the row's statistics are taken again.
+constexpr float kFar = -32.f;
 template <class T, int kThreads>
 __global__ __launch_bounds__(kThreads) void grad_kernel(RowArgs a) {
   const int64_t i = a.first + blockIdx.x;
@@ -378,37 +391,55 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(RowArgs a) {
   const float l = a.logp_in[i];
   if (token < 0 || l == -INFINITY) return row_zero<T, kThreads>(out, a.vocab);
   const T* row = static_cast<const T*>(a.logits) + i * a.stride;
-  const float xt = float(row[token]);
+  float f = float(row[token]), u = l * kLog2e;
+  if (l < kFar) {
+    __shared__ Soft part[kThreads / kWave];
+    const Soft r = row_soft<T, kThreads>(row, a.vocab, a.c, part);
+    f = finite_max(r.m);
+    u = -log_2(r.s);
+  }
   __syncthreads();  // every thread has the token's logit before one writes there
-  row_grad<T, kThreads, false>(row, out, a.vocab, a.c, xt, l * kLog2e, a.d_logp[i] * a.inv_t,
-                               token);
+  row_grad<T, kThreads, false>(row, out, a.vocab, a.c, f, u, a.d_logp[i] * a.inv_t, token);
 }
 
 template <class T>
 __global__ __launch_bounds__(kBlock) void lanes_grad_kernel(RowArgs a, int lanes) {
   const int64_t i = a.first + int64_t(blockIdx.x) * (kBlock / lanes) + int(threadIdx.x) / lanes;
   const int t = int(threadIdx.x) % lanes;
-  if (i >= a.n || t >= int(a.vocab)) return;
+  if (i >= a.n) return;  // all of a row's lanes
   const int token = int(token_in(a.tokens, i, a.vocab));
-  const float l = a.logp_in[i];
+  float x;
+  const Soft r = lanes_soft<T>(a, i, t, token >= 0, lanes, x);
+  if (t >= int(a.vocab)) return;
   float d = 0.f;
-  if (token >= 0 && l != -INFINITY) {
-    const T* row = static_cast<const T*>(a.logits) + i * a.stride;
-    // The token's logit is read by all of the row's lanes before one writes.
-    const float p = pow2(__builtin_fmaf(float(row[t]) - float(row[token]), a.c, l * kLog2e));
+  if (token >= 0 && a.logp_in[i] != -INFINITY) {
+    const float p = pow2(__builtin_fmaf(x - finite_max(r.m), a.c, -log_2(r.s)));
     d = a.d_logp[i] * a.inv_t * (t == token ? 1.f - p : -p);
   }
   static_cast<T*>(a.d_logits)[i * a.d_stride + t] = T(d);
 }
 
-// loss[0] = scale * the sum of n values, added in a fixed order in 64 bits.
+// loss[0] = the sum of n values, added in a fixed order in 64 bits, eight pieces
+// of a thread under way at once.
 __global__ __launch_bounds__(1024) void total_kernel(const float* __restrict__ x, int64_t n,
-                                                     float scale, float* loss) {
+                                                     float* loss) {
+  constexpr int kAhead = 8;
   __shared__ double part[16];
+  const int64_t whole = n / 4 * 4;
   double s = 0;
-  for (int64_t i = threadIdx.x; i < n; i += 1024) s += double(x[i]);
+  for (int64_t i = int64_t(threadIdx.x) * 4; i < whole; i += 4096 * kAhead) {
+    Vec<float>::type v[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      v[k] = i + k * 4096 < whole ? load16(x + i + k * 4096) : Vec<float>::type(0.f);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s += double(v[k][e]);
+  }
+  if (whole + threadIdx.x < n) s += double(x[whole + threadIdx.x]);
   s = block_sum(s, part);
-  if (threadIdx.x == 0) loss[0] = float(s * scale);
+  if (threadIdx.x == 0) loss[0] = float(s);
 }
 
 // Tokens that are no padding, per answer; a wave each.
@@ -636,7 +667,7 @@ hipError_t launch_policy(const sched_policy_desc& d, hipStream_t s) {
   a.d_stride = d.d_logits.stride;
   const hipError_t e = rows_by_type<true>(d.logits.dtype, a, s);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(total_kernel, dim3(1), dim3(1024), 0, s, d.losses, d.logits.rows, 1.f, d.loss);
+  hipLaunchKernelGGL(total_kernel, dim3(1), dim3(1024), 0, s, d.losses, d.logits.rows, d.loss);
   return hipGetLastError();
 }
 

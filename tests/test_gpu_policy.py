@@ -212,6 +212,33 @@ def test_masked_logits(dtype, vocab):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab", [3, 64, 300, 5003, 66003])
+def test_tokens_that_are_all_but_ruled_out(dtype, vocab):
+    """Log-probabilities of -50 down to the type's lowest value stay finite, and
+    the other logits' gradients keep their digits."""
+    g = gen(vocab + 1)
+    x, _ = draw_rows(g, 5, vocab, dtype)
+    t = torch.randint(0, vocab, (5,), generator=g)
+    for i, low in enumerate((-50.0, -300.0, -1e4, -6e4, torch.finfo(dtype).min)):
+        x[i, t[i]] = low
+    d_logp = randn(g, 5)
+    logp, p, on = R.logprobs(x, t, 2.0)
+    got = S.sched_token_logprobs(x.cuda(), t.cuda(), temperature=2.0)
+    rest = x.clone()
+    rest[torch.arange(5), t] = 0  # the row's span is that of its other logits
+    err = R.logits_error(rest, 2.0)
+    R.close(got, logp, err + 4 * R.F * logp.abs(), "logp")
+    grad = S.sched_token_logprobs_grad(x.cuda(), t.cuda(), got, d_logp.cuda(), temperature=2.0)
+    want, bound = R.d_logits(rest, t, p, on, logp, d_logp, 2.0)
+    R.close(grad, want, bound, "d_logits")
+    one = torch.ones(5).cuda()
+    loss = S.sched_policy_loss(x.cuda(), t.cuda(), got, None, one, one, temperature=2.0)
+    assert torch.equal(loss[2], got)
+    want, bound = R.d_logits(rest, t, p, on, logp, -torch.ones(5), 2.0)
+    R.close(loss[3], want, bound, "policy's d_logits")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("n,vocab", ROWS)
 @pytest.mark.parametrize("kl", [0.0, 0.05])
 def test_policy_loss(dtype, n, vocab, kl):
@@ -392,6 +419,17 @@ def test_attention_over_a_cache(dtype, lengths, slot, heads, kv, dim):
     out, lse = check_attention(q, k, v, None, qo, ko, True, k_len=lengths, grads=False)
     flat, lse2 = check_attention(q, k, v, None, qo, ko, False, k_len=lengths, grads=False)
     assert torch.equal(out, flat) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("queries,keys", [(3, 40), (200, 200), (1, 5000), (70, 3000)])
+def test_attention_of_a_query_that_is_no_number(queries, keys):
+    """NaN in a query is seen in its row's results and in no other row's."""
+    q, k, v, do, qo, ko = attention_case(torch.bfloat16, [queries] * 2, [keys] * 2, 4, 2, 64, 5)
+    q = q.cuda().clone()
+    q[queries, 1, 3] = math.nan
+    out, lse = S.sched_attention(q, k.cuda(), v.cuda(), i32(qo), i32(ko))
+    assert bool(out[queries, 1].isnan().all()) and math.isnan(float(lse[1, queries]))
+    assert int(out.isnan().sum()) == out.shape[2] and int(lse.isnan().sum()) == 1
 
 
 def test_attention_gradient_over_slots():

@@ -137,6 +137,16 @@ def test_losses(lib):
     assert advantages(size=11) == advantages(ws=0) == WORKSPACE
 
 
+def test_most_answers_and_rows(lib):
+    def advantages(n, ws):
+        return lib.sched_group_advantages(FAKE, FAKE, FAKE, 1, FAKE, n, R(tokens()), 0, FAKE, FAKE,
+                                          ws, 0, 0)
+    assert advantages((1 << 16) + 1, FAKE) == SIZE and advantages(1 << 16, FAKE) == WORKSPACE
+    rows = (1 << 31) - 1023
+    assert lib.sched_embed_grad_workspace_bytes(rows, 8, R(ctypes.c_size_t())) == SIZE
+    assert lib.sched_embed_grad_workspace_bytes(rows - 1, 8, R(ctypes.c_size_t())) == 0
+
+
 def test_attention(lib):
     def desc(**kw):
         h = P.sched_heads(FAKE, 256, 64)
