@@ -153,6 +153,7 @@ __global__ __launch_bounds__(kSmallThreads) void sort_small_kernel(SortArgs a) {
     volatile uint32_t* mine = counts + wave * bins;
 #pragma unroll
     for (int r = 0; r < kRounds; ++r) {
+      if (uint32_t(r * kWave) >= span) continue;  // of all waves
       const uint32_t digit = (key[r] >> shift) & uint32_t(bins - 1);
       const uint64_t peers = peers_of(digit, on[r], a.bits);
       uint32_t base = 0;

@@ -23,7 +23,7 @@ struct RowArgs {
   int64_t n, vocab, stride;
   int64_t first;   // row that the launch starts with
   Tokens tokens;
-  float c, inv_t;  // log2(e) / T, 1 / T
+  float t, c, inv_t;  // T, log2(e) / T, 1 / T
   // log-probabilities
   float* logp;
   // gradient
@@ -77,10 +77,12 @@ __device__ __forceinline__ Soft block_join(Soft a, float c, Soft* part) {
   return a;
 }
 
-// Log-probability of a token with logit x in a row with these statistics (not in
-// base 2: the type's lowest logit, a mask, would leave the range).
+// Log-probability of a token with logit x in a row with these statistics.  Not in
+// base 2, where the type's lowest logit, a mask, would leave the range; and by
+// T itself: a rounded factor shifts all of a loss's terms the same way, which
+// shows in their sum.
 __device__ __forceinline__ float log_prob(const RowArgs& a, float x, Soft r) {
-  return r.s == 0.f ? -INFINITY : (x - finite_max(r.m)) * a.inv_t - log_2(r.s) * kLn2;
+  return r.s == 0.f ? -INFINITY : (x - finite_max(r.m)) / a.t - log_2(r.s) * kLn2;
 }
 
 template <class T, int N>
@@ -624,6 +626,7 @@ RowArgs row_args(const sched_matrix& logits, const sched_tokens& tokens, float t
   a.vocab = logits.cols;
   a.stride = logits.stride;
   a.tokens = tokens_of(tokens);
+  a.t = temperature;
   a.c = float(1.4426950408889634 / double(temperature));
   a.inv_t = float(1.0 / double(temperature));
   return a;
