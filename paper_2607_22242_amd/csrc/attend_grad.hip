@@ -8,6 +8,8 @@
 // one order and no atomics: 14 D operations per pair in place of 10 D.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "attend.h"
 #include "policy_launch.h"
 
@@ -187,10 +189,21 @@ struct KeySweep {
   }
 };
 
+// Where few keys would leave the card idle, a block's rows are shared by `parts`
+// blocks, whose sums, in 32 bits, are added after them in one order.
+struct KeyParts {
+  float *dk, *dv;  // parts x kv_heads x k_rows x D
+  int parts;
+};
+template <int D>
+__device__ __forceinline__ int64_t key_part(const AttendArgs& a, int part, int kv, int64_t row) {
+  return ((int64_t(part) * (a.q_heads / a.group) + kv) * a.k_rows + row) * D;
+}
+
 // A block holds 64 keys; waves 0 and 1 take the even 32 rows of each tile with
 // keys 0 .. 31 and 32 .. 63, waves 2 and 3 the odd 32; their sums meet at the end.
 template <class T, int D>
-__global__ __launch_bounds__(kThreads, 2) void keys_kernel(AttendArgs a, int tiles) {
+__global__ __launch_bounds__(kThreads, 2) void keys_kernel(AttendArgs a, KeyParts p, int tiles) {
   __shared__ __attribute__((aligned(16))) T q_even[kTile * D], o_even[kTile * D];
   __shared__ __attribute__((aligned(16))) T q_odd[kTile * D], o_odd[kTile * D];
   constexpr int kRest = KeySweep<T, D>::kHeld < D / 16 ? kKeysOfBlock * 64 : 8;
@@ -232,13 +245,18 @@ __global__ __launch_bounds__(kThreads, 2) void keys_kernel(AttendArgs a, int til
   }
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) w.dk[i] = w.dv[i] = Acc(0.f);
-  const int begin = rows > 0 ? seen_from(first) / kTile * kTile : 0;
+  int begin = rows > 0 ? seen_from(first) / kTile * kTile : 0;
   const int all = wave_key + 31 < s.keys ? seen_from(wave_key + 31) : rows;
   const int any = wave_key < s.keys ? seen_from(wave_key) : rows;
   const RowTiles<T, D> tiles_of(a);
   // From the last rows, which see every key, to the first: blocks that run side
   // by side read the same rows at the same time.
-  const int end = rows > 0 ? (rows - 1) / kTile * kTile : -1;
+  int end = rows > 0 ? (rows - 1) / kTile * kTile : -1;
+  if (p.parts > 1) {  // this block's share of the row tiles
+    const int share = (max(end - begin + kTile, 0) / kTile + p.parts - 1) / p.parts;
+    end -= int(blockIdx.y) * share * kTile;
+    begin = max(begin, end - (share - 1) * kTile);
+  }
   RowTile t = row_tile(a, max(end, 0));
   auto step = [&](int r0, const T* q_tile, const T* o_tile, const Stats& stats) {
     const int r = r0 + part;
@@ -267,8 +285,63 @@ __global__ __launch_bounds__(kThreads, 2) void keys_kernel(AttendArgs a, int til
   tiles_barrier();
   if (wave >= 2 || j >= s.slot) return;
   w.take(buf_k, buf_v);
+  if (p.parts > 1) {
+    const int64_t at = key_part<D>(a, int(blockIdx.y), kv, int64_t(s.k0) + j);
+    store_column<float, D>(p.dk + at, w.dk, D, a.scale);
+    store_column<float, D>(p.dv + at, w.dv, D, 1.f);
+    return;
+  }
   store_column<T, D>(head_row<T>(a.d_k, int64_t(s.k0) + j, kv), w.dk, a.dim, a.scale);
   store_column<T, D>(head_row<T>(a.d_v, int64_t(s.k0) + j, kv), w.dv, a.dim, 1.f);
+}
+
+template <class T, int D>
+__global__ __launch_bounds__(kThreads) void add_parts_kernel(AttendArgs a, KeyParts p, int tiles) {
+  typedef float Four __attribute__((ext_vector_type(4)));
+  typedef T four __attribute__((ext_vector_type(4)));
+  const Work work = work_of(int(blockIdx.x), tiles, a.q_heads / a.group);
+  if (work.tile >= tiles) return;
+  const Tile tile = key_tile(a, kKeysOfBlock, work.tile);
+  const Seq s = sequence(a, tile.seq);
+  const int first = tile.index * kKeysOfBlock;
+  if (tile.index < 0 || first >= s.slot) return;
+  const int d = int(threadIdx.x) % (D / 4) * 4;
+  for (int j = first + int(threadIdx.x) / (D / 4); j < min(first + kKeysOfBlock, s.slot);
+       j += kThreads / (D / 4)) {
+    const int64_t row = int64_t(s.k0) + j;
+    Four x = Four(0.f), y = Four(0.f);
+    for (int i = 0; i < p.parts; ++i) {
+      const int64_t at = key_part<D>(a, i, work.kv, row) + d;
+      x += *reinterpret_cast<const Four*>(p.dk + at);
+      y += *reinterpret_cast<const Four*>(p.dv + at);
+    }
+    if (d >= a.dim) continue;
+    four u, v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      u[e] = T(x[e]);
+      v[e] = T(y[e]);
+    }
+    *reinterpret_cast<four*>(head_row<T>(a.d_k, row, work.kv) + d) = u;
+    *reinterpret_cast<four*>(head_row<T>(a.d_v, row, work.kv) + d) = v;
+  }
+}
+
+// As many parts as fill the 512 places that the card has for the kernel's blocks,
+// none with less than 8 tiles of a mean sequence's rows.
+int key_parts_of(const sched_attention_desc& d) {
+  if (d.n_seqs == 0 || d.k_rows == 0) return 1;
+  const int64_t blocks = tile_count(d.k_rows, d.n_seqs, kKeysOfBlock) * d.kv_heads;
+  const int64_t rows = d.q_rows * (d.q_heads / d.kv_heads) / d.n_seqs;
+  return int(std::max<int64_t>(1, std::min(512 / blocks, rows / (8 * kTile))));
+}
+size_t stats_bytes(const sched_attention_desc& d) {
+  return (size_t(d.q_rows) * size_t(d.q_heads) * 8 + 255) & ~size_t(255);
+}
+size_t key_part_count(const sched_attention_desc& d) {  // values of dK, or of dV
+  const int parts = key_parts_of(d);
+  if (parts == 1) return 0;
+  return size_t(parts) * size_t(d.k_rows) * size_t(d.kv_heads) * (d.head_dim > 64 ? 128 : 64);
 }
 
 // --- dQ -----------------------------------------------------------------------
@@ -402,7 +475,7 @@ __global__ __launch_bounds__(kThreads, 2) void queries_kernel(AttendArgs a, int 
 }
 
 template <class T, int D>
-hipError_t attend_grad(const AttendArgs& a, int kv_heads, hipStream_t s) {
+hipError_t attend_grad(const AttendArgs& a, const KeyParts& p, int kv_heads, hipStream_t s) {
   hipError_t e = hipSuccess;
   if (a.q_rows > 0) {  // first: it leaves the rows' statistics
     const int64_t tiles = tile_count(int64_t(a.q_rows) * a.group, a.n_seqs, kRowsOfBlock);
@@ -413,9 +486,14 @@ hipError_t attend_grad(const AttendArgs& a, int kv_heads, hipStream_t s) {
   }
   if (a.k_rows > 0) {
     const int64_t tiles = tile_count(a.k_rows, a.n_seqs, kKeysOfBlock);
-    hipLaunchKernelGGL((keys_kernel<T, D>), dim3(unsigned(work_blocks(tiles, kv_heads))),
-                       dim3(kThreads), 0, s, a, int(tiles));
+    const dim3 grid(unsigned(work_blocks(tiles, kv_heads)), unsigned(p.parts));
+    hipLaunchKernelGGL((keys_kernel<T, D>), grid, dim3(kThreads), 0, s, a, p, int(tiles));
     e = hipGetLastError();
+    if (p.parts > 1 && e == hipSuccess) {
+      hipLaunchKernelGGL((add_parts_kernel<T, D>), dim3(grid.x), dim3(kThreads), 0, s, a, p,
+                         int(tiles));
+      e = hipGetLastError();
+    }
   }
   return e;
 }
@@ -427,7 +505,7 @@ HeadsView view(const sched_heads& h) {
 }  // namespace
 
 size_t attention_grad_bytes(const sched_attention_desc& d) {
-  return size_t(d.q_rows) * size_t(d.q_heads) * 8;
+  return stats_bytes(d) + 2 * key_part_count(d) * sizeof(float);
 }
 
 hipError_t launch_attention_grad(const sched_attention_desc& d, const sched_heads& d_out,
@@ -444,9 +522,13 @@ hipError_t launch_attention_grad(const sched_attention_desc& d, const sched_head
              d_out.head_stride < (int64_t(1) << 24);
   a.delta = a.lse2 + size_t(d.q_rows) * size_t(d.q_heads);
   const bool wide = d.head_dim > 64;
+  float* const parts = reinterpret_cast<float*>(static_cast<char*>(ws) + stats_bytes(d));
+  const KeyParts p = {parts, parts + key_part_count(d), key_parts_of(d)};
   if (d.dtype == SCHED_F16)
-    return wide ? attend_grad<f16, 128>(a, d.kv_heads, s) : attend_grad<f16, 64>(a, d.kv_heads, s);
-  return wide ? attend_grad<bf16, 128>(a, d.kv_heads, s) : attend_grad<bf16, 64>(a, d.kv_heads, s);
+    return wide ? attend_grad<f16, 128>(a, p, d.kv_heads, s)
+                : attend_grad<f16, 64>(a, p, d.kv_heads, s);
+  return wide ? attend_grad<bf16, 128>(a, p, d.kv_heads, s)
+              : attend_grad<bf16, 64>(a, p, d.kv_heads, s);
 }
 
 }  // namespace policy

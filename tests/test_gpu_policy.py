@@ -421,6 +421,15 @@ def test_attention_over_a_cache(dtype, lengths, slot, heads, kv, dim):
     assert torch.equal(out, flat) and torch.equal(lse, lse2)
 
 
+@pytest.mark.parametrize("q_len,k_len,heads,kv,dim,causal", [
+    ([1100], [1100], 2, 1, 64, True), ([700, 0, 900], [700, 50, 400], 6, 2, 128, True),
+    ([600], [65], 5, 1, 72, False), ([1030, 990], [3, 1200], 4, 2, 40, True)])
+def test_attention_gradient_of_few_keys_and_many_rows(q_len, k_len, heads, kv, dim, causal):
+    """The rows of a block of keys are shared by several blocks."""
+    q, k, v, do, qo, ko = attention_case(torch.bfloat16, q_len, k_len, heads, kv, dim, 6)
+    check_attention(q, k, v, do, qo, ko, causal)
+
+
 @pytest.mark.parametrize("queries,keys", [(3, 40), (200, 200), (1, 5000), (70, 3000)])
 def test_attention_of_a_query_that_is_no_number(queries, keys):
     """NaN in a query is seen in its row's results and in no other row's."""
