@@ -138,7 +138,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendArgs a, int t
                      sum == 0.f ? 0.f : 1.f / sum);  // a sum of NaN stays one
   if (lane < 32)
     a.lse[int64_t(me.head) * a.q_rows + s.q0 + me.query] =
-        sum == 0.f ? -INFINITY : (w.most * c + log_2(sum)) * kLn2;
+        sum == 0.f ? -INFINITY : __builtin_fmaf(w.most * c, kLn2, ln(sum));
 }
 
 // --- few query rows -----------------------------------------------------------
@@ -255,7 +255,8 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs a, Split p, i
   for (int d = 0; d < D / kWave; ++d)
     if (d * kWave + lane < a.dim) out[d * kWave + lane] = T(sum == 0.f ? 0.f : o[d] / sum);
   if (lane == 0)
-    a.lse[int64_t(head) * a.q_rows + row] = sum == 0.f ? -INFINITY : (most + log_2(sum)) * kLn2;
+    a.lse[int64_t(head) * a.q_rows + row] =
+        sum == 0.f ? -INFINITY : __builtin_fmaf(most, kLn2, ln(sum));
 }
 
 // Blocks that a sequence's keys are shared by: 1 where there are 64 blocks of

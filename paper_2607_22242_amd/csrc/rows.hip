@@ -82,7 +82,7 @@ __device__ __forceinline__ Soft block_join(Soft a, float c, Soft* part) {
 // T itself: a rounded factor shifts all of a loss's terms the same way, which
 // shows in their sum.
 __device__ __forceinline__ float log_prob(const RowArgs& a, float x, Soft r) {
-  return r.s == 0.f ? -INFINITY : (x - finite_max(r.m)) / a.t - log_2(r.s) * kLn2;
+  return r.s == 0.f ? -INFINITY : (x - finite_max(r.m)) / a.t - ln(r.s);
 }
 
 template <class T, int N>
