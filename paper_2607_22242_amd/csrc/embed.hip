@@ -23,6 +23,11 @@ constexpr int kSmall = 8192;             // tokens that one block sorts in LDS
 constexpr int kSmallThreads = 1024;
 constexpr int kTile = 2048;              // tokens of a block otherwise
 constexpr int kTileThreads = 512;
+// Tiles from whose number on their counts are scanned first; below, every block
+// adds up the others' by itself, a launch less but as the square of the tiles
+// (131,072 tokens, 64 of them: 54 us both ways; 2^20: 140 us so, 188 without;
+// 2^22: 337 and 1,148).
+constexpr uint32_t kScanned = 128;
 constexpr int kMostThreads = 512;       // of a block of a row's waves
 
 __device__ __forceinline__ uint64_t below(int lane) { return (1ull << lane) - 1; }
@@ -110,7 +115,8 @@ struct SortArgs {
   uint32_t n, vocab;
   int bits, passes;  // of a digit, and digits
   uint32_t *key[2], *at[2];
-  uint32_t* hist;    // blocks x bins
+  uint32_t* hist;    // blocks x bins, and a row of sums
+  int scanned;       // the counts have become those of earlier blocks
 };
 
 __device__ __forceinline__ uint32_t key_of(const SortArgs& a, uint32_t i) {
@@ -201,6 +207,25 @@ __global__ __launch_bounds__(kTileThreads) void sort_count_kernel(SortArgs a, in
     a.hist[blockIdx.x * uint32_t(bins) + i] = counts[i];
 }
 
+// A block per digit: every tile's count becomes the sum of the tiles before it,
+// and the last row the sum of all.
+__global__ __launch_bounds__(kTileThreads) void sort_scan_kernel(SortArgs a, uint32_t tiles) {
+  __shared__ uint32_t part[kTileThreads / kWave], carry;
+  const uint32_t bins = 1u << a.bits;
+  if (threadIdx.x == 0) carry = 0;
+  for (uint32_t t0 = 0; t0 < tiles; t0 += kTileThreads) {
+    const uint32_t t = t0 + threadIdx.x;
+    const uint32_t x = t < tiles ? a.hist[t * bins + blockIdx.x] : 0;
+    __syncthreads();  // the carry is there, and `part` has been read
+    const uint32_t before = carry + block_before<kTileThreads>(x, part);
+    if (t < tiles) a.hist[t * bins + blockIdx.x] = before;
+    __syncthreads();
+    if (threadIdx.x == kTileThreads - 1) carry = before + x;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) a.hist[tiles * bins + blockIdx.x] = carry;
+}
+
 __global__ __launch_bounds__(kTileThreads) void sort_place_kernel(SortArgs a, int p) {
   constexpr int kRounds = kTile / kTileThreads, kWaves = kTileThreads / kWave;
   static_assert(kBins <= kTileThreads, "a thread per digit");
@@ -221,7 +246,10 @@ __global__ __launch_bounds__(kTileThreads) void sort_place_kernel(SortArgs a, in
   // This block's first place of each digit: keys of lower digits, and of the
   // same digit in earlier blocks.
   uint32_t total = 0, earlier = 0;
-  if (int(threadIdx.x) < bins)
+  if (int(threadIdx.x) < bins && a.scanned) {
+    total = a.hist[gridDim.x * uint32_t(bins) + threadIdx.x];
+    earlier = a.hist[blockIdx.x * uint32_t(bins) + threadIdx.x];
+  } else if (int(threadIdx.x) < bins) {
     for (uint32_t b = 0; b < gridDim.x; b += 16) {
       uint32_t c[16];  // under way at once
 #pragma unroll
@@ -233,6 +261,7 @@ __global__ __launch_bounds__(kTileThreads) void sort_place_kernel(SortArgs a, in
         earlier += b + k < blockIdx.x ? c[k] : 0;
       }
     }
+  }
   uint32_t before = block_before<kTileThreads>(total, part) + earlier;
   if (int(threadIdx.x) < bins)
     for (int w = 0; w < kWaves; ++w) {
@@ -597,7 +626,7 @@ hipError_t launch_embed(const sched_matrix& table, const sched_tokens& tokens, f
 
 size_t embed_grad_bytes(int64_t n, int64_t dim) {
   const size_t lists = n <= kSmall ? 2 : 4;
-  return lists * up(size_t(n) * 4) + (n <= kSmall ? 0 : up(size_t(tiles_for(n)) * kBins * 4)) +
+  return lists * up(size_t(n) * 4) + (n <= kSmall ? 0 : up(size_t(tiles_for(n) + 1) * kBins * 4)) +
          up(size_t(n / chunk_for(n)) * size_t(dim) * 4);
 }
 
@@ -626,11 +655,18 @@ hipError_t launch_embed_grad(const sched_matrix& d_rows, const sched_tokens& tok
     a.key[1] = reinterpret_cast<uint32_t*>(take(size_t(a.n) * 4));
     a.at[1] = reinterpret_cast<uint32_t*>(take(size_t(a.n) * 4));
     const uint32_t tiles = tiles_for(a.n);
-    a.hist = reinterpret_cast<uint32_t*>(take(size_t(tiles) * kBins * 4));
+    a.hist = reinterpret_cast<uint32_t*>(take(size_t(tiles + 1) * kBins * 4));
+    // With few tiles every block adds up the counts of the others by itself.
+    a.scanned = tiles > kScanned;
     for (int p = 0; p < a.passes && e == hipSuccess; ++p) {
       hipLaunchKernelGGL(sort_count_kernel, dim3(tiles), dim3(kTileThreads), 0, s, a, p);
       e = hipGetLastError();
       if (e != hipSuccess) break;
+      if (a.scanned) {
+        hipLaunchKernelGGL(sort_scan_kernel, dim3(1u << a.bits), dim3(kTileThreads), 0, s, a, tiles);
+        e = hipGetLastError();
+        if (e != hipSuccess) break;
+      }
       hipLaunchKernelGGL(sort_place_kernel, dim3(tiles), dim3(kTileThreads), 0, s, a, p);
       e = hipGetLastError();
     }

@@ -100,6 +100,17 @@ def test_embed_grad_of_long_lists(n, vocab):
     check_embed_grad(d_rows, tokens, vocab, 1.0)
 
 
+@pytest.mark.parametrize("n,vocab", [(262_144, 900), (300_001, 70_000), (1_100_000, 3)])
+def test_embed_grad_of_very_long_lists(n, vocab):
+    """Rows of small whole numbers, whose sums are exact in 32 bits."""
+    g = gen(n)
+    t = torch.randint(-1, vocab, (n,), generator=g)
+    d = torch.randint(-2, 3, (n, 4), generator=g).float()
+    got = S.sched_embed_grad(d.cuda(), t.cuda(), vocab)
+    want = torch.zeros((vocab + 1, 4), dtype=torch.float64).index_add_(0, t + 1, d.double())[1:]
+    assert torch.equal(got.cpu().double(), want)
+
+
 def test_embed_grad_against_differences():
     g = gen(5)
     table, tokens = randn(g, 11, 24), draw_tokens(g, 60, 11)
