@@ -408,8 +408,19 @@ struct RowSweep {
   }
 };
 
+// Where few query rows would leave the card idle, the keys of a block's rows are
+// shared by `parts` blocks in the same way.
+struct RowParts {
+  float* dq;  // parts x q_rows x q_heads x D
+  int parts;
+};
+template <int D>
+__device__ __forceinline__ int64_t row_part(const AttendArgs& a, int part, int64_t row, int head) {
+  return ((int64_t(part) * a.q_rows + row) * a.q_heads + head) * D;
+}
+
 template <class T, int D>
-__global__ __launch_bounds__(kThreads, 2) void queries_kernel(AttendArgs a, int tiles) {
+__global__ __launch_bounds__(kThreads, 2) void queries_kernel(AttendArgs a, RowParts p, int tiles) {
   __shared__ __attribute__((aligned(16))) T k_even[kTile * D], v_even[kTile * D];
   __shared__ __attribute__((aligned(16))) T k_odd[kTile * D], v_odd[kTile * D];
   const Work work = work_of(int(blockIdx.x), tiles, a.q_heads / a.group);
@@ -425,7 +436,12 @@ __global__ __launch_bounds__(kThreads, 2) void queries_kernel(AttendArgs a, int 
   const int ahead = s.keys - s.queries;
   const int last = !on || !a.causal ? s.keys - 1 : min(s.keys - 1, me.query + ahead);
   const int last_row = min(first + kRowsOfBlock, rows) - 1;
-  const int end = a.causal ? min(s.keys, last_row / a.group + ahead + 1) : s.keys;
+  int begin = 0, end = a.causal ? min(s.keys, last_row / a.group + ahead + 1) : s.keys;
+  if (p.parts > 1) {  // this block's share of the tiles
+    const int share = ((max(end, 0) + kTile - 1) / kTile + p.parts - 1) / p.parts * kTile;
+    begin = min(int(blockIdx.y) * share, max(end, 0));
+    end = min(begin + share, end);
+  }
   const int wave_first = min(first + 32 * wave, rows - 1);
   const int wave_last = min(wave_first + 31, rows - 1);
   const int all = !a.causal ? s.keys - 1 : min(s.keys - 1, wave_first / a.group + ahead);
@@ -456,8 +472,8 @@ __global__ __launch_bounds__(kThreads, 2) void queries_kernel(AttendArgs a, int 
   const float c = a.scale * kLog2e;
   const Places<D> places;
   const KeyTiles<T, D, kTile, kThreads> tiles_of(a, s, kv);
-  if (end > 0) tiles_of.fetch(0, k_even, v_even, a.dim);
-  for (int j0 = 0; j0 < end; j0 += 2 * kTile) {
+  if (begin < end) tiles_of.fetch(begin, k_even, v_even, a.dim);
+  for (int j0 = begin; j0 < end; j0 += 2 * kTile) {
     tiles_barrier();
     if (j0 + kTile < end) tiles_of.fetch(j0 + kTile, k_odd, v_odd, a.dim);
     if (any < kTile && j0 <= any) w.exact_delta(k_even, v_even, last, c, places);
@@ -469,21 +485,74 @@ __global__ __launch_bounds__(kThreads, 2) void queries_kernel(AttendArgs a, int 
       w.add(k_odd, v_odd, j0 + kTile, last, j0 + 2 * kTile - 1 <= all, c, places);
   }
   if (!on) return;
-  store_column<T, D>(head_row<T>(a.d_q, s.q0 + me.query, me.head), w.dq, a.dim, a.scale);
-  if (lane < 32) {
+  if (p.parts > 1)
+    store_column<float, D>(p.dq + row_part<D>(a, int(blockIdx.y), s.q0 + me.query, me.head), w.dq, D,
+                           a.scale);
+  else
+    store_column<T, D>(head_row<T>(a.d_q, s.q0 + me.query, me.head), w.dq, a.dim, a.scale);
+  if (lane < 32 && blockIdx.y == 0) {  // the part that has the first tile
     a.lse2[n] = w.lse2;
     a.delta[n] = w.delta;
   }
 }
 
 template <class T, int D>
-hipError_t attend_grad(const AttendArgs& a, const KeyParts& p, int kv_heads, hipStream_t s) {
+__global__ __launch_bounds__(kThreads) void add_row_parts_kernel(AttendArgs a, RowParts p,
+                                                                 int tiles) {
+  typedef float Four __attribute__((ext_vector_type(4)));
+  typedef T four __attribute__((ext_vector_type(4)));
+  const Work work = work_of(int(blockIdx.x), tiles, a.q_heads / a.group);
+  if (work.tile >= tiles) return;
+  const Tile tile = query_tile(a, kRowsOfBlock, work.tile, tiles);
+  const Seq s = sequence(a, tile.seq);
+  const int first = tile.index * kRowsOfBlock, rows = s.queries * a.group;
+  if (tile.index < 0 || first >= rows) return;
+  const int d = int(threadIdx.x) % (D / 4) * 4;
+  if (d >= a.dim) return;
+  for (int r = first + int(threadIdx.x) / (D / 4); r < min(first + kRowsOfBlock, rows);
+       r += kThreads / (D / 4)) {
+    const QueryRow me = query_row(a, work.kv, r);
+    const int64_t row = int64_t(s.q0) + me.query;
+    Four x = Four(0.f);
+    for (int i = 0; i < p.parts; ++i)
+      x += *reinterpret_cast<const Four*>(p.dq + row_part<D>(a, i, row, me.head) + d);
+    four u;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) u[e] = T(x[e]);
+    *reinterpret_cast<four*>(head_row<T>(a.d_q, row, me.head) + d) = u;
+  }
+}
+
+// As above, none with less than 12 tiles of a mean sequence's keys.  The whole
+// pass over 8,192 tokens of one head: 184 us so, 344 in one part; 4,000 tokens, 8
+// heads of 2 key heads: 246 and 274; with parts of 8 tiles 1,100 tokens, 2 heads of
+// one, would lose 44 to 46.
+int row_parts_of(const sched_attention_desc& d) {
+  if (d.n_seqs == 0 || d.q_rows == 0) return 1;
+  const int64_t blocks =
+      tile_count(d.q_rows * (d.q_heads / d.kv_heads), d.n_seqs, kRowsOfBlock) * d.kv_heads;
+  return int(std::max<int64_t>(1, std::min(512 / blocks, d.k_rows / d.n_seqs / (12 * kTile))));
+}
+size_t row_part_count(const sched_attention_desc& d) {
+  const int parts = row_parts_of(d);
+  if (parts == 1) return 0;
+  return size_t(parts) * size_t(d.q_rows) * size_t(d.q_heads) * (d.head_dim > 64 ? 128 : 64);
+}
+
+template <class T, int D>
+hipError_t attend_grad(const AttendArgs& a, const KeyParts& p, const RowParts& r, int kv_heads,
+                       hipStream_t s) {
   hipError_t e = hipSuccess;
   if (a.q_rows > 0) {  // first: it leaves the rows' statistics
     const int64_t tiles = tile_count(int64_t(a.q_rows) * a.group, a.n_seqs, kRowsOfBlock);
-    hipLaunchKernelGGL((queries_kernel<T, D>), dim3(unsigned(work_blocks(tiles, kv_heads))),
-                       dim3(kThreads), 0, s, a, int(tiles));
+    const dim3 grid(unsigned(work_blocks(tiles, kv_heads)), unsigned(r.parts));
+    hipLaunchKernelGGL((queries_kernel<T, D>), grid, dim3(kThreads), 0, s, a, r, int(tiles));
     e = hipGetLastError();
+    if (r.parts > 1 && e == hipSuccess) {
+      hipLaunchKernelGGL((add_row_parts_kernel<T, D>), dim3(grid.x), dim3(kThreads), 0, s, a, r,
+                         int(tiles));
+      e = hipGetLastError();
+    }
     if (e != hipSuccess) return e;
   }
   if (a.k_rows > 0) {
@@ -507,7 +576,8 @@ HeadsView view(const sched_heads& h) {
 }  // namespace
 
 size_t attention_grad_bytes(const sched_attention_desc& d) {
-  return stats_bytes(d) + 2 * key_part_count(d) * sizeof(float);
+  // The parts of dQ have been added when those of dK and dV are written.
+  return stats_bytes(d) + std::max(row_part_count(d), 2 * key_part_count(d)) * sizeof(float);
 }
 
 hipError_t launch_attention_grad(const sched_attention_desc& d, const sched_heads& d_out,
@@ -526,11 +596,12 @@ hipError_t launch_attention_grad(const sched_attention_desc& d, const sched_head
   const bool wide = d.head_dim > 64;
   float* const parts = reinterpret_cast<float*>(static_cast<char*>(ws) + stats_bytes(d));
   const KeyParts p = {parts, parts + key_part_count(d), key_parts_of(d)};
+  const RowParts r = {parts, row_parts_of(d)};
   if (d.dtype == SCHED_F16)
-    return wide ? attend_grad<f16, 128>(a, p, d.kv_heads, s)
-                : attend_grad<f16, 64>(a, p, d.kv_heads, s);
-  return wide ? attend_grad<bf16, 128>(a, p, d.kv_heads, s)
-              : attend_grad<bf16, 64>(a, p, d.kv_heads, s);
+    return wide ? attend_grad<f16, 128>(a, p, r, d.kv_heads, s)
+                : attend_grad<f16, 64>(a, p, r, d.kv_heads, s);
+  return wide ? attend_grad<bf16, 128>(a, p, r, d.kv_heads, s)
+              : attend_grad<bf16, 64>(a, p, r, d.kv_heads, s);
 }
 
 }  // namespace policy

@@ -441,6 +441,15 @@ def test_attention_gradient_of_few_keys_and_many_rows(q_len, k_len, heads, kv, d
     check_attention(q, k, v, do, qo, ko, causal)
 
 
+@pytest.mark.parametrize("q_len,k_len,heads,kv,dim,causal", [
+    ([300], [1700], 2, 1, 128, True), ([70, 0, 200], [3100, 50, 1900], 6, 2, 64, True),
+    ([65], [1600], 5, 1, 72, False), ([900, 50], [700, 2400], 4, 2, 40, True)])
+def test_attention_gradient_of_few_rows_and_many_keys(q_len, k_len, heads, kv, dim, causal):
+    """The keys of a block of query rows are shared by several blocks."""
+    q, k, v, do, qo, ko = attention_case(torch.float16, q_len, k_len, heads, kv, dim, 7)
+    check_attention(q, k, v, do, qo, ko, causal)
+
+
 @pytest.mark.parametrize("queries,keys", [(3, 40), (200, 200), (1, 5000), (70, 3000)])
 def test_attention_of_a_query_that_is_no_number(queries, keys):
     """NaN in a query is seen in its row's results and in no other row's."""
