@@ -89,8 +89,8 @@ int sched_token_logprobs(const sched_matrix *logits, const sched_tokens *tokens,
                          float temperature, float *logp, void *hip_stream);
 
 /* Its gradient: d_logits[i][j] = d_logp[i] * ((j == tokens[i]) - q[j]) /
- * temperature with q the row's probabilities (logp is the result of the call
- * above, from which they are taken where it is no less than -32); zeros for padding and for tokens with logp = -inf.  d_logits: of
+ * temperature with q the row's probabilities (logp, the result of the call
+ * above, is what they may be taken from); zeros for padding and for tokens with logp = -inf.  d_logits: of
  * logits' type and size; it may be logits itself. */
 int sched_token_logprobs_grad(const sched_matrix *logits, const sched_tokens *tokens,
                               float temperature, const float *logp, const float *d_logp,
@@ -191,7 +191,8 @@ int sched_attention(const sched_attention_desc *desc, void *d_workspace, size_t 
 
 /* The backward pass: d_q, d_k and d_v from d_out and the forward pass's out
  * and lse (read here); the probabilities are computed again.  Key rows of a
- * slot beyond its length get zeros. */
+ * slot beyond its length get zeros.  With few rows or keys their sums too are
+ * joined through the workspace. */
 int sched_attention_grad_workspace_bytes(const sched_attention_desc *desc, size_t *out);
 int sched_attention_grad(const sched_attention_desc *desc, const sched_heads *d_out,
                          const sched_heads *d_q, const sched_heads *d_k, const sched_heads *d_v,
