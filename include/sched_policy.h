@@ -90,8 +90,8 @@ int sched_token_logprobs(const sched_matrix *logits, const sched_tokens *tokens,
 
 /* Its gradient: d_logits[i][j] = d_logp[i] * ((j == tokens[i]) - q[j]) /
  * temperature with q the row's probabilities (logp, the result of the call
- * above, is what they may be taken from); zeros for padding and for tokens with logp = -inf.  d_logits: of
- * logits' type and size; it may be logits itself. */
+ * above, is what they may be taken from); zeros for padding and for tokens with
+ * logp = -inf.  d_logits: of logits' type and size; it may be logits itself. */
 int sched_token_logprobs_grad(const sched_matrix *logits, const sched_tokens *tokens,
                               float temperature, const float *logp, const float *d_logp,
                               const sched_matrix *d_logits, void *hip_stream);
