@@ -183,8 +183,11 @@ struct TokenLoss {
 __device__ __forceinline__ TokenLoss token_loss(const RowArgs& a, int64_t i, float l) {
   const float w = a.weights[i], adv = a.advantages[i];
   const float r = pow2((l - a.old_logp[i]) * kLog2e);
-  const float free = -adv * r, held = -adv * fminf(fmaxf(r, a.lo), a.hi);
-  float loss = fmaxf(free, held), slope = free >= held ? free : 0.f;
+  // By comparisons that keep what is no number, where fmin and fmax drop it.  A
+  // ratio beyond 32 bits times an advantage of 0 is 0.
+  const float free = adv == 0.f && r == INFINITY ? 0.f : -adv * r;
+  const float held = -adv * (r < a.lo ? a.lo : r > a.hi ? a.hi : r);
+  float loss = held > free ? held : free, slope = held > free ? 0.f : free;
   if (a.kl != 0.f) {
     // exp(e) - 1 as such: e is mostly small, and the term is of its square.
     const float e = a.ref_logp[i] - l, k = expm1f(e);

@@ -635,3 +635,45 @@ def test_offsets_that_leave_the_tensor_are_cut():
     assert torch.equal(got, want)
     got, _ = S.sched_attention(q, q, q, i32([0, 40]), i32([0, 40]), k_lengths=i32([90]), causal=False)
     assert torch.equal(got, want)
+
+
+# --- what is no number, and what is too large ---------------------------------
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab", [3, 64, 300, 5003, 32003, 66003])
+@pytest.mark.parametrize("kl", [0.0, 0.1])
+def test_policy_loss_of_what_is_no_number(dtype, vocab, kl):
+    """NaN in a logit, an old log-probability, an advantage or a weight is seen
+    in its token's loss and gradient and in the total, and in no other token's."""
+    g = gen(vocab + 2)
+    x, t = draw_rows(g, 8, vocab, dtype)  # row 1 is padding
+    old = S.sched_token_logprobs(x.cuda(), t.cuda()).cpu() - 0.1
+    adv, w = randn(g, 8), torch.rand(8, generator=g) + 0.5
+
+    def run(x, old, adv, w):
+        ref = (old.nan_to_num(0) + 0.2).cuda()
+        return S.sched_policy_loss(x.cuda(), t.cuda(), old.cuda(), ref, adv.cuda(), w.cuda(), kl_weight=kl)
+
+    want = run(x, old, adv, w)
+    x, old, adv, w = x.clone(), old.clone(), adv.clone(), w.clone()
+    x[1], old[1], adv[1], w[1] = math.nan, math.nan, math.nan, math.nan
+    x[2, vocab - 1], old[3], adv[4], w[5] = math.nan, math.nan, math.nan, math.nan
+    loss, losses, logp, d = run(x, old, adv, w)
+    odd, rest = [2, 3, 4, 5], [0, 1, 6, 7]
+    assert bool(losses[odd].isnan().all()) and bool(loss.isnan().all()) and bool(d[odd].isnan().all())
+    assert logp.isnan().tolist() == [False, False, True] + [False] * 5
+    assert torch.equal(losses[rest], want[1][rest]) and torch.equal(d[rest], want[3][rest])
+    assert float(losses[1]) == 0 and not d[1].any()
+
+
+@pytest.mark.parametrize("vocab", [3, 300, 66003])
+def test_policy_loss_of_a_ratio_beyond_32_bits(vocab):
+    """An old log-probability far below the new one: an advantage of 0 has loss
+    and gradient 0, one above 0 is clipped."""
+    g = gen(vocab + 3)
+    x, t = randn(g, 4, vocab).cuda(), torch.randint(0, vocab, (4,), generator=g).cuda()
+    old, w = torch.full((4,), -400.0).cuda(), torch.ones(4).cuda()
+    adv = torch.tensor([0.0, 2.0, 0.0, 0.5]).cuda()
+    _, losses, _, d = S.sched_policy_loss(x, t, old, None, adv, w, clip_high=0.25)
+    assert losses.tolist() == [0.0, -2.5, 0.0, -0.625] and not d.any()
