@@ -558,7 +558,8 @@ __global__ __launch_bounds__(1024) void pairs_total_kernel(const float* margins,
   double s = 0;
   for (int i = int(threadIdx.x); i < n; i += 1024) {
     const double m = margins[i], soft = log1p(exp(-fabs(m)));
-    s += soft + (1 - eps) * fmax(-m, 0.0) + eps * fmax(m, 0.0);
+    // A side of no weight adds nothing, be its margin infinite.
+    s += soft + (eps < 1 ? (1 - eps) * fmax(-m, 0.0) : 0.0) + (eps > 0 ? eps * fmax(m, 0.0) : 0.0);
   }
   s = block_sum(s, part);
   if (threadIdx.x == 0) loss[0] = float(s * double(scale) / n);

@@ -677,3 +677,31 @@ def test_policy_loss_of_a_ratio_beyond_32_bits(vocab):
     adv = torch.tensor([0.0, 2.0, 0.0, 0.5]).cuda()
     _, losses, _, d = S.sched_policy_loss(x, t, old, None, adv, w, clip_high=0.25)
     assert losses.tolist() == [0.0, -2.5, 0.0, -0.625] and not d.any()
+
+
+@pytest.mark.parametrize("eps", [0.0, 0.25, 1.0])
+def test_preference_loss_of_infinite_margins(eps):
+    """A disallowed token (log-probability -inf) on the worse side costs nothing
+    without smoothing, one on the better side everything; the gradient is finite."""
+    inf, ln2 = math.inf, math.log(2.0)
+    tokens = torch.zeros(8, dtype=torch.int64).cuda()
+    logp, ref = torch.full((8,), -1.0), torch.full((8,), -1.0).cuda()
+
+    def run(at):
+        x = logp.clone()
+        x[at] = -inf
+        return S.sched_preference_loss(x.cuda(), ref, tokens, i32([0, 2, 4, 6, 8]), beta=0.5, smoothing=eps)
+
+    # Two pairs; the other pair's margin is 0: log 2.
+    for at, margin, weight in ((2, inf, eps), (1, -inf, 1 - eps)):
+        loss, margins, d = run(at)
+        assert margins.tolist() == [margin, 0.0]
+        want = ln2 / 2 if weight == 0 else inf
+        assert float(loss) == inf if want == inf else abs(float(loss) - want) < 4 * R.F
+        slope = 0.5 / 2 * (eps if margin > 0 else eps - 1)
+        R.close(d[:4], torch.tensor([slope, slope, -slope, -slope]).double(), 4 * R.F * abs(slope))
+        other = 0.5 / 2 * (eps - 0.5)
+        R.close(d[4:], torch.tensor([other, other, -other, -other]).double(), 4 * R.F * abs(other))
+    loss, margins, d = run([1, 2])  # both sides: no number
+    assert bool(loss.isnan().all()) and bool(margins[0].isnan()) and bool(d[:4].isnan().all())
+    assert not d[4:].isnan().any()
