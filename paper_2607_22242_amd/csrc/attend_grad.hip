@@ -285,6 +285,10 @@ __global__ __launch_bounds__(kThreads, 2) void keys_kernel(AttendArgs a, KeyPart
   tiles_barrier();
   if (wave >= 2 || j >= s.slot) return;
   w.take(buf_k, buf_v);
+  if (!on) {  // also where a row that was NaN has met the tile's zeros
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) w.dk[i] = w.dv[i] = Acc(0.f);
+  }
   if (p.parts > 1) {
     const int64_t at = key_part<D>(a, int(blockIdx.y), kv, int64_t(s.k0) + j);
     store_column<float, D>(p.dk + at, w.dk, D, a.scale);
@@ -485,6 +489,10 @@ __global__ __launch_bounds__(kThreads, 2) void queries_kernel(AttendArgs a, RowP
       w.add(k_odd, v_odd, j0 + kTile, last, j0 + 2 * kTile - 1 <= all, c, places);
   }
   if (!on) return;
+  if (last < 0) {  // a row that sees nothing, whatever it holds
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) w.dq[i] = Acc(0.f);
+  }
   if (p.parts > 1)
     store_column<float, D>(p.dq + row_part<D>(a, int(blockIdx.y), s.q0 + me.query, me.head), w.dq, D,
                            a.scale);

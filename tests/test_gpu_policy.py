@@ -705,3 +705,52 @@ def test_preference_loss_of_infinite_margins(eps):
     loss, margins, d = run([1, 2])  # both sides: no number
     assert bool(loss.isnan().all()) and bool(margins[0].isnan()) and bool(d[:4].isnan().all())
     assert not d[4:].isnan().any()
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("queries,lengths,slot,heads,kv,dim", [
+    (40, [5, 0, 64, 33], 70, 4, 2, 64), (9, [20], 40, 2, 2, 128), (600, [130, 17], 200, 4, 1, 128),
+    (30, [1900, 2000], 2100, 2, 1, 64)])
+def test_attention_gradient_behind_lengths_of_rows_that_are_no_number(dtype, queries, lengths, slot,
+                                                                      heads, kv, dim):
+    """NaN in a query, and in the gradient of another's result, leaves the key
+    rows behind a length at zero, and the other sequences' as they were."""
+    b = len(lengths)
+    q, k, v, do, qo, ko = attention_case(dtype, [queries] * b, [slot] * b, heads, kv, dim, slot + dim)
+    for causal in (True, False):
+        def run(q, do):
+            kw = dict(k_lengths=i32(lengths), causal=causal)
+            a = (q.cuda(), k.cuda(), v.cuda())
+            out, lse = S.sched_attention(*a, i32(qo), i32(ko), **kw)
+            return S.sched_attention_grad(*a, out, lse, do.cuda(), i32(qo), i32(ko), **kw)
+
+        want = run(q, do)
+        x, y = q.clone(), do.clone()
+        x[queries - 1, 0, 1], y[queries // 2, heads - 1, 2] = math.nan, math.nan
+        dq, dk, dv = run(x, y)
+        assert bool(dq[queries - 1, 0].isnan().all())
+        for i, n in enumerate(lengths):
+            behind = slice(i * slot + n, (i + 1) * slot)
+            assert not dk[behind].any() and not dv[behind].any()
+            if i:
+                own, rows = slice(i * slot, (i + 1) * slot), slice(i * queries, (i + 1) * queries)
+                assert torch.equal(dk[own], want[1][own]) and torch.equal(dv[own], want[2][own])
+                assert torch.equal(dq[rows], want[0][rows])
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("queries,keys", [(40, 10), (129, 65), (900, 800)])
+def test_attention_gradient_of_rows_that_see_nothing(dtype, queries, keys):
+    """Rows before the first that sees a key: NaN in their query and in the
+    gradient of their result stay out of their gradient."""
+    q, k, v, do, qo, ko = attention_case(dtype, [queries], [keys], 2, 1, 64, 3)
+    blind = queries - keys
+    q[:blind], do[:blind] = math.nan, math.nan
+    a = (q.cuda(), k.cuda(), v.cuda())
+    out, lse = S.sched_attention(*a, i32(qo), i32(ko))
+    dq = S.sched_attention_grad(*a, out, lse, do.cuda(), i32(qo), i32(ko))[0]
+    assert not out[:blind].any() and bool((lse[:, :blind] == -math.inf).all())
+    assert not dq[:blind].any()
+    want = R.Attention(q[blind:], k, v, [0, keys], [0, keys], None, True, 64 ** -0.5, do[blind:])
+    R.close(out[blind:], want.out, want.out_b, "out")
+    R.close(dq[blind:], want.dq, want.dq_b, "dq")
