@@ -84,7 +84,7 @@ int sched_embed_grad(const sched_matrix *d_rows, const sched_tokens *tokens, flo
  * z = row i of logits / temperature (n 32-bit values; 0 for padding, whose rows
  * are not read).  A logit of -inf is a mode or token that is not allowed and
  * has log-probability -inf, as has every token of a row of nothing else.
- * temperature > 0. */
+ * temperature > 0, and log2(e) / temperature is finite in 32 bits. */
 int sched_token_logprobs(const sched_matrix *logits, const sched_tokens *tokens,
                          float temperature, float *logp, void *hip_stream);
 

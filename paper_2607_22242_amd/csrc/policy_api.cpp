@@ -52,7 +52,9 @@ int check_logits(const sched_matrix& logits, const sched_tokens& tokens, float t
   if (int e = check_matrix(logits, false)) return e;
   if (int e = check_tokens(tokens)) return e;
   if (logits.rows != tokens.n || logits.cols < 1) return SCHED_E_SIZE;
-  if (!positive(temperature) || !std::isfinite(1.f / temperature)) return SCHED_E_VALUE;
+  // The factor of the powers, log2(e) / temperature, is the largest that is used.
+  if (!positive(temperature) || !std::isfinite(float(1.4426950408889634 / double(temperature))))
+    return SCHED_E_VALUE;
   return SCHED_OK;
 }
 

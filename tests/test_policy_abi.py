@@ -194,3 +194,14 @@ def test_binding_refuses_tensors_of_the_host():
         with pytest.raises(S.SchedError) as e:
             call()
         assert e.value.name == "SCHED_E_VALUE"
+
+
+def test_temperatures_whose_factors_leave_32_bits(lib):
+    """log2(e) / temperature is what the rows are multiplied with: refused where
+    it is infinite, though 1 / temperature is not."""
+    for t in (3.5e-39, 4.0e-39, 2.94e-39):
+        assert 1.0 / t < 3.4028e38 < math.log2(math.e) / t
+        assert lib.sched_token_logprobs(R(matrix()), R(tokens()), t, FAKE, 0) == VALUE
+        desc = P.sched_policy_desc(matrix(), tokens(), FAKE, FAKE, FAKE, FAKE, 0.2, 0.2, 0.0, t, 1.0, FAKE,
+                                   FAKE, FAKE, matrix(data=FAKE * 2))
+        assert lib.sched_policy_loss(R(desc), 0) == VALUE
