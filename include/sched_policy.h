@@ -170,7 +170,8 @@ typedef struct {
  * behind a length may hold anything; those of a sequence that causal = 1 alone
  * hides from a row have weight zero there and have to be finite.
  * head_dim: a multiple of 8 up to 128.  dtype: SCHED_F16 or SCHED_BF16; the
- * probabilities are rounded to it before they are multiplied with the values.
+ * probabilities are rounded to it before they are multiplied with the values
+ * (SCHED_F16: small ones in steps of 2^-31 of the row's largest).
  * q_rows * q_heads / 32 + n_seqs * kv_heads and k_rows * kv_heads / 64 + n_seqs *
  * kv_heads stay below 2^24 - 8, and a key head has up to 4096 query heads. */
 typedef struct {

@@ -14,6 +14,8 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "sched_policy.h"
 #include "tensors.h"
 
@@ -32,6 +34,16 @@ __device__ __forceinline__ Acc product(Frag<bf16>::type a, Frag<bf16>::type b, A
 __device__ __forceinline__ Acc product(Frag<f16>::type a, Frag<f16>::type b, Acc c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
+
+// Probabilities are rounded to the operands' 16 bits for their product: in 32 bits
+// it would run at a sixteenth of the rate.  f16 is normal from 2^-14 to 2^16 only,
+// with steps of 2^-24 below: there the forward pass' powers, 2^8 at most, are
+// multiplied with 2^kLift; what is lost of 65,536 keys then stays below 2^-16 of
+// the largest value.
+template <class T>
+constexpr bool kShort = std::is_same<T, f16>::value;
+template <class T>
+constexpr float kLift = kShort<T> ? 7.f : 0.f;
 
 struct HeadsView {
   char* data;

@@ -29,6 +29,11 @@ struct Sweep {
   Acc o[D / 32];
   float most, sum;  // reference of the powers; their sum over this lane's half of the keys
 
+  // What is taken from the scores, to the base 2.
+  __device__ __forceinline__ float reference(float c) const {
+    return (most == -INFINITY ? 0.f : most) * c - kLift<T>;
+  }
+
   __device__ __forceinline__ void start(const T* q_row, int dim, bool on) {
     const int h = int(threadIdx.x) % kWave / 32;
 #pragma unroll
@@ -72,7 +77,7 @@ struct Sweep {
 #pragma unroll
       for (int d = 0; d < D / 32; ++d) o[d] *= keep;
     }
-    const float fc = (most == -INFINITY ? 0.f : most) * c;
+    const float fc = reference(c);
 #pragma unroll
     for (int t = 0; t < kSubs; ++t)
 #pragma unroll
@@ -138,7 +143,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendArgs a, int t
                      sum == 0.f ? 0.f : 1.f / sum);  // a sum of NaN stays one
   if (lane < 32)
     a.lse[int64_t(me.head) * a.q_rows + s.q0 + me.query] =
-        sum == 0.f ? -INFINITY : __builtin_fmaf(w.most * c, kLn2, ln(sum));
+        sum == 0.f ? -INFINITY : __builtin_fmaf(w.reference(c), kLn2, ln(sum));
 }
 
 // --- few query rows -----------------------------------------------------------
@@ -205,7 +210,7 @@ __global__ __launch_bounds__(kThreads, 2) void split_kernel(AttendArgs a, Split 
   const int64_t part = part_of(a, p, s.q0 + me.query, me.head, 2 * split + wave);
   store_column<float, D>(p.sums + part * D, w.o, D, 1.f);
   if (lane < 32) {
-    p.weights[2 * part] = w.most * c;
+    p.weights[2 * part] = w.reference(c);
     p.weights[2 * part + 1] = sum;
   }
 }

@@ -754,3 +754,28 @@ def test_attention_gradient_of_rows_that_see_nothing(dtype, queries, keys):
     want = R.Attention(q[blind:], k, v, [0, keys], [0, keys], None, True, 64 ** -0.5, do[blind:])
     R.close(out[blind:], want.out, want.out_b, "out")
     R.close(dq[blind:], want.dq, want.dq_b, "dq")
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("queries,keys", [(1, 65), (1, 700), (1, 3001), (200, 700)])
+@pytest.mark.parametrize("gap", [14.0, 18.0, 20.0])
+@pytest.mark.parametrize("first", [True, False])
+def test_attention_beside_a_key_that_takes_all(dtype, queries, keys, gap, first):
+    """One key of value 0 has all but exp(-gap) of a key's weight: the results
+    are the other keys', whose probabilities are as small as 2^-28."""
+    g = gen(keys)
+    q = torch.zeros((queries, 1, 64), dtype=dtype)
+    k, v = torch.zeros((keys, 1, 64), dtype=dtype), (torch.rand((keys, 1, 64), generator=g) * 60).to(dtype)
+    at = 0 if first else keys - 1
+    q[:, 0, 0], k[at, 0, 0], v[at] = 1, gap, 0  # the scores are gap and zeros
+    out, lse = S.sched_attention(q.cuda(), k.cuda(), v.cuda(), i32([0, queries]), i32([0, keys]),
+                                 causal=False, scale=1.0)
+    rest = math.exp(-gap)
+    want = (v.double().sum(0) * rest / (1 + (keys - 1) * rest)).expand(queries, 1, 64)
+    u = R.U[dtype]
+    # Of f16 a power has steps of 2^-31 of the largest; its score is rounded at 2^-24 of 20 and
+    # of the sums' terms.
+    short = keys * 2.0 ** -32 * 60 + 2.0 ** -25 if dtype == torch.float16 else 0.0
+    R.close(out, want, (2 * u + R.F * (4 * gap + keys / 16 + 64)) * want + short)
+    full = math.log(math.exp(gap) + keys - 1)
+    R.close(lse, torch.full((1, queries), full).double(), R.F * (8 * full + keys / 16 + 64))
