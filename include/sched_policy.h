@@ -191,9 +191,11 @@ int sched_attention(const sched_attention_desc *desc, void *d_workspace, size_t 
                     void *hip_stream);
 
 /* The backward pass: d_q, d_k and d_v from d_out and the forward pass's out
- * and lse (read here); the probabilities are computed again.  Key rows of a
- * slot beyond its length get zeros.  With few rows or keys their sums too are
- * joined through the workspace. */
+ * and lse (read here); the probabilities are computed again.  They and the
+ * products' gradients are rounded to dtype before they are multiplied (SCHED_F16:
+ * held times powers of two that follow from their size).  Key rows of a slot
+ * beyond its length get zeros.  With few rows or keys their sums too are joined
+ * through the workspace. */
 int sched_attention_grad_workspace_bytes(const sched_attention_desc *desc, size_t *out);
 int sched_attention_grad(const sched_attention_desc *desc, const sched_heads *d_out,
                          const sched_heads *d_q, const sched_heads *d_k, const sched_heads *d_v,

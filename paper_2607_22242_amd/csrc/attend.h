@@ -35,15 +35,20 @@ __device__ __forceinline__ Acc product(Frag<f16>::type a, Frag<f16>::type b, Acc
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
 
-// Probabilities are rounded to the operands' 16 bits for their product: in 32 bits
-// it would run at a sixteenth of the rate.  f16 is normal from 2^-14 to 2^16 only,
-// with steps of 2^-24 below: there the forward pass' powers, 2^8 at most, are
-// multiplied with 2^kLift; what is lost of 65,536 keys then stays below 2^-16 of
-// the largest value.
+// Probabilities and dS are rounded to the operands' 16 bits for their products:
+// in 32 bits those would run at a sixteenth of the rate.  The error of a result
+// against 64 bits is 1.4 times that of one rounding of it (f16 and bf16, 2,048 and
+// 4,096 tokens).  f16 is normal from 2^-14 to 2^16 only, with steps of 2^-24 below:
+// there both are multiplied with powers of two, which results are divided by.
+// kLift: of the forward pass' powers, 2^8 at most: what is lost of 65,536 keys
+// stays below 2^-16 of the largest value.  kLiftGrad: of the backward pass'
+// probabilities, 1 at most.  dS takes the factor that its values ask for (fit).
 template <class T>
 constexpr bool kShort = std::is_same<T, f16>::value;
 template <class T>
 constexpr float kLift = kShort<T> ? 7.f : 0.f;
+template <class T>
+constexpr float kLiftGrad = kShort<T> ? 14.f : 0.f;
 
 struct HeadsView {
   char* data;
@@ -373,6 +378,36 @@ __device__ __forceinline__ typename Frag<T>::type narrow(const Acc& x, int s) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] = T(x[8 * s + e]);
   return v;
+}
+
+// Values of f16 of one row or key (a lane's and those of the lane 32 on) that pass
+// 2^15 go down to 2^10, and all that come after them with them: fit() returns the
+// power of two that they were divided by.  What is infinite is left out.  The first
+// values come with 2^kLargest, so that every sum meets its own size: steps are
+// 2^-34 of the largest value that it has had.
+constexpr int kLargest = 60;
+__device__ __forceinline__ bool passes(const Acc& x) {
+  float m = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) m = fmaxf(m, fabsf(x[i]));
+  return m > 32768.f;
+}
+__device__ __forceinline__ int fit(Acc& x) {
+  float m = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) m = fmaxf(m, fabsf(x[i]) < INFINITY ? fabsf(x[i]) : 0.f);
+  m = fmaxf(m, __shfl_xor(m, 32));
+  const int e = m > 32768.f ? __builtin_amdgcn_frexp_expf(m) - 11 : 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) x[i] = __builtin_ldexpf(x[i], -e);
+  return e;
+}
+template <int N>
+__device__ __forceinline__ void shift(Acc (&x)[N], int e) {
+#pragma unroll
+  for (int d = 0; d < N; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[d][i] = __builtin_ldexpf(x[d][i], e);
 }
 
 // Row of C that element i of lane l holds.

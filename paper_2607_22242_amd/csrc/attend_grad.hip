@@ -119,6 +119,7 @@ struct KeySweep {
   static constexpr int kHeld = D == 128 ? D / 32 : D / 16;  // pieces of the values in registers
   typename Frag<T>::type k[D / 16], v[kHeld];
   Acc dk[D / 32], dv[D / 32];
+  int up;  // f16: dS is held 2^up times
 
   // Rows part .. part + 31 of a tile; the lane's key is seen by the tile's rows
   // from `from` to `upto` (`whole`: all of the wave's are by all).
@@ -154,7 +155,13 @@ struct KeySweep {
       for (int e = 0; e < 4; ++e) {
         x[i + e] = pow2(__builtin_fmaf(x[i + e], c, -l[e]));
         y[i + e] *= x[i + e];
+        if (kShort<T>) y[i + e] = __builtin_ldexpf(y[i + e], up);
       }
+    }
+    if (kShort<T> && __any(passes(y))) {
+      const int e = fit(y);
+      up -= e;
+      shift(dk, -e);
     }
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
@@ -245,6 +252,7 @@ __global__ __launch_bounds__(kThreads, 2) void keys_kernel(AttendArgs a, KeyPart
   }
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) w.dk[i] = w.dv[i] = Acc(0.f);
+  w.up = kLargest;
   int begin = rows > 0 ? seen_from(first) / kTile * kTile : 0;
   const int all = wave_key + 31 < s.keys ? seen_from(wave_key + 31) : rows;
   const int any = wave_key < s.keys ? seen_from(wave_key) : rows;
@@ -281,6 +289,10 @@ __global__ __launch_bounds__(kThreads, 2) void keys_kernel(AttendArgs a, KeyPart
   float* const buf_k = reinterpret_cast<float*>(wave % 2 ? q_odd : q_even);
   float* const buf_v = reinterpret_cast<float*>(wave % 2 ? o_odd : o_even);
   tiles_barrier();
+  if (kShort<T>) {
+    shift(w.dk, -w.up - int(kLiftGrad<T>));
+    shift(w.dv, -int(kLiftGrad<T>));
+  }
   if (wave >= 2) w.hand(buf_k, buf_v);
   tiles_barrier();
   if (wave >= 2 || j >= s.slot) return;
@@ -359,6 +371,7 @@ struct RowSweep {
   typename Frag<T>::type q[D / 16], o[D / 16];
   Acc dq[D / 32];
   float lse2, delta;
+  int up;  // f16: the powers, and dS, are held 2^up times, which lse2 has in it
 
   __device__ __forceinline__ void add(const T* k_tile, const T* v_tile, int j0, int last,
                                       bool whole, float c, const Places<D>& places) {
@@ -377,6 +390,12 @@ struct RowSweep {
       }
 #pragma unroll
       for (int i = 0; i < 16; ++i) y[i] *= pow2(__builtin_fmaf(x[i], c, -lse2));
+      if (kShort<T> && __any(passes(y))) {
+        const int e = fit(y);
+        up -= e;
+        lse2 += float(e);
+        shift(dq, -e);
+      }
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
         const auto b = narrow<T>(y, p);
@@ -408,7 +427,7 @@ struct RowSweep {
         sum += pow2(__builtin_fmaf(s, c, -lse2)) * y[i];
       }
     }
-    delta = -(sum + __shfl_xor(sum, 32));
+    delta = -__builtin_ldexpf(sum + __shfl_xor(sum, 32), -up);
   }
 };
 
@@ -473,6 +492,10 @@ __global__ __launch_bounds__(kThreads, 2) void queries_kernel(AttendArgs a, RowP
   w.delta = -(sum + __shfl_xor(sum, 32));
   const float lse = on ? a.lse[n] : -INFINITY;
   w.lse2 = lse == -INFINITY ? INFINITY : lse * kLog2e;  // powers of rows that see nothing are 0
+  const bool first_part = lane < 32 && on && blockIdx.y == 0;  // the part of the first tile
+  if (first_part) a.lse2[n] = w.lse2 - kLiftGrad<T>;
+  w.up = kShort<T> ? kLargest : 0;
+  w.lse2 -= float(w.up);
   const float c = a.scale * kLog2e;
   const Places<D> places;
   const KeyTiles<T, D, kTile, kThreads> tiles_of(a, s, kv);
@@ -489,6 +512,7 @@ __global__ __launch_bounds__(kThreads, 2) void queries_kernel(AttendArgs a, RowP
       w.add(k_odd, v_odd, j0 + kTile, last, j0 + 2 * kTile - 1 <= all, c, places);
   }
   if (!on) return;
+  if (kShort<T>) shift(w.dq, -w.up);
   if (last < 0) {  // a row that sees nothing, whatever it holds
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) w.dq[i] = Acc(0.f);
@@ -498,10 +522,7 @@ __global__ __launch_bounds__(kThreads, 2) void queries_kernel(AttendArgs a, RowP
                            a.scale);
   else
     store_column<T, D>(head_row<T>(a.d_q, s.q0 + me.query, me.head), w.dq, a.dim, a.scale);
-  if (lane < 32 && blockIdx.y == 0) {  // the part that has the first tile
-    a.lse2[n] = w.lse2;
-    a.delta[n] = w.delta;
-  }
+  if (first_part) a.delta[n] = w.delta;
 }
 
 template <class T, int D>

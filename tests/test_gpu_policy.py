@@ -779,3 +779,63 @@ def test_attention_beside_a_key_that_takes_all(dtype, queries, keys, gap, first)
     R.close(out, want, (2 * u + R.F * (4 * gap + keys / 16 + 64)) * want + short)
     full = math.log(math.exp(gap) + keys - 1)
     R.close(lse, torch.full((1, queries), full).double(), R.F * (8 * full + keys / 16 + 64))
+
+
+def check_gradient_norms(q, k, v, do, grads, scale):
+    """Every row of dQ and every key of dK and dV of one causal sequence by the
+    norm of its error: what the result's own rounding gives, twice the roundings
+    of dS, of the probabilities and of the result in delta (each at most u of
+    its term, independent), and 32-bit steps of the products."""
+    dtype, (rows, heads, dim) = q.dtype, q.shape
+    u, group = R.U[dtype], heads // k.shape[1]
+    grads = [t.cpu().double() for t in grads]
+    assert all(bool(torch.isfinite(t).all()) for t in grads)
+    q, k, v, do = [t.double() for t in (q, k, v, do)]
+    seen = torch.ones((rows, rows), dtype=torch.bool).tril()
+    dk, dv = torch.zeros_like(k), torch.zeros_like(v)
+    dk_b, dv_b = torch.zeros(k.shape[:2]).double(), torch.zeros(k.shape[:2]).double()
+
+    def check(name, got, want, most):
+        one = (want.to(dtype).double() - want).norm(dim=-1)
+        off = (got - want).norm(dim=-1)
+        assert bool((off <= one + most).all()), (name, float((off / (one + most)).max()))
+
+    for h in range(heads):
+        Q, K, V, dO = q[:, h], k[:, h // group], v[:, h // group], do[:, h]
+        P = torch.softmax((Q @ K.T * scale).masked_fill(~seen, -math.inf), 1)
+        out = P @ V
+        dS = P * (dO @ V.T - (dO * out).sum(1, keepdim=True))
+        step = 2.0 ** -17 * P * (dO.abs() @ V.abs().T)
+        noise = (2 * u * (dO * out).norm(dim=1, keepdim=True)) * P  # of delta
+        size = ((2 * u * dS) ** 2 + step ** 2) * scale ** 2
+        kn, qn = K.norm(dim=1) ** 2, Q.norm(dim=1) ** 2
+        check("dq", grads[0][:, h], dS @ K * scale,
+              torch.sqrt(size @ kn) + (noise @ K).norm(dim=1) * scale)
+        dk[:, h // group] += dS.T @ Q * scale
+        dv[:, h // group] += P.T @ dO
+        dk_b[:, h // group] += (size + (noise * scale) ** 2).T @ qn
+        dv_b[:, h // group] += ((2 * u + 2.0 ** -17) * P).square().T @ dO.norm(dim=1) ** 2
+    check("dk", grads[1], dk, torch.sqrt(dk_b))
+    check("dv", grads[2], dv, torch.sqrt(dv_b))
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("rows,heads,kv,dim", [(2048, 2, 1, 64), (1500, 2, 2, 128), (100, 6, 2, 40)])
+@pytest.mark.parametrize("size", [1.0, 1e-3, 1e-4, 1e-5, "falls", "rises", "large"])
+def test_attention_gradient_of_every_size(dtype, rows, heads, kv, dim, size):
+    """Gradients of the result from 1e-5 on, of one size or from row to row, as
+    training has them, and such that dS passes the largest f16 value."""
+    q, k, v, do, qo, ko = attention_case(dtype, [rows], None, heads, kv, dim, rows)
+    if size == "large":
+        q, k, v, do = q * 0.05, k * 0.05, v * 4, (do * 8e3).to(dtype)
+    elif isinstance(size, float):
+        do = (do.float() * size).to(dtype)
+    else:
+        fall = 10.0 ** (-4 * torch.arange(rows) / rows)
+        do = (do.float() * (fall if size == "falls" else fall.flip(0))[:, None, None]).to(dtype)
+    a = (q.cuda(), k.cuda(), v.cuda())
+    out, lse = S.sched_attention(*a, i32(qo), i32(ko))
+    grads = S.sched_attention_grad(*a, out, lse, do.cuda(), i32(qo), i32(ko))
+    check_gradient_norms(q, k, v, do, grads, dim ** -0.5)
+    again = S.sched_attention_grad(*a, out, lse, do.cuda(), i32(qo), i32(ko))
+    assert all(torch.equal(x, y) for x, y in zip(grads, again))
