@@ -42,8 +42,23 @@ struct Soft {
   float m, s;
 };
 
+// What a row's gradient takes its probabilities from, p_j = k 2^((x_j - f) c + u):
+// its statistics (f the maximum, k one over the sum: the large ones then have
+// small exponents, which are rounded least), or a token's logit and
+// log-probability.  d_j = gain (e_t - p_j).
+struct Grad {
+  float f, u, gain, gain_k;
+  __device__ __forceinline__ float at(float x, float c, bool token) const {
+    return __builtin_fmaf(-gain_k, pow2(__builtin_fmaf(x - f, c, u)), token ? gain : 0.f);
+  }
+};
+
 // 0 in place of a maximum of -inf: powers of -inf then are zeros.
 __device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.f : m; }
+
+__device__ __forceinline__ Grad grad_of(Soft a, float gain) {
+  return {finite_max(a.m), 0.f, gain, gain / a.s};
+}
 
 __device__ __forceinline__ Soft join(Soft a, Soft b, float c) {
   const float m = fmaxf(a.m, b.m), f = finite_max(m);
@@ -147,9 +162,9 @@ struct Held {
       for (int e = 0; e < N; ++e) s += pow2((float(v[i][e]) - f) * c);
     return s;
   }
-  // gain (e_t - 2^((x - f) c + u)) to the row's place.
-  __device__ __forceinline__ void store(T* out, int vocab, int t, float f, float c, float u,
-                                        float gain, int token) const {
+  // The gradient to the row's place.
+  __device__ __forceinline__ void store(T* out, int vocab, int t, float c, const Grad& g,
+                                        int token) const {
     const int pieces = vocab / N;
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
@@ -157,17 +172,11 @@ struct Held {
       if (i * kThreads + t >= pieces) continue;
       V d;
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
-        const float p = pow2(__builtin_fmaf(float(v[i][e]) - f, c, u));
-        d[e] = T(gain * (at + e == token ? 1.f - p : -p));
-      }
+      for (int e = 0; e < N; ++e) d[e] = T(g.at(float(v[i][e]), c, at + e == token));
       store16(out + at, d);
     }
     const int at = pieces * N + t;
-    if (at < vocab) {
-      const float p = pow2(__builtin_fmaf(tail - f, c, u));
-      out[at] = T(gain * (at == token ? 1.f - p : -p));
-    }
+    if (at < vocab) out[at] = T(g.at(tail, c, at == token));
   }
   __device__ __forceinline__ static void zero(T* out, int vocab, int t) {
     const int pieces = vocab / N;
@@ -197,7 +206,9 @@ __device__ __forceinline__ TokenLoss token_loss(const RowArgs& a, int64_t i, flo
   return {w * loss, w * slope * a.loss_scale};
 }
 
-// kPolicy: the policy loss with the gradient; else log-probabilities alone.
+// What a row is taken for: its token's log-probability, the policy loss with the
+// gradient, or the gradient of log-probabilities that are known.
+enum For { kLogp, kPolicy, kGrad };
 
 // `lanes` (a power of two up to 64) of a wave take a row of at most as many
 // logits, lane t of them logit t.
@@ -212,7 +223,7 @@ __device__ __forceinline__ Soft lanes_soft(const RowArgs& a, int64_t i, int t, b
   return r;
 }
 
-template <class T, bool kPolicy>
+template <class T, For kFor>
 __global__ __launch_bounds__(kBlock) void lanes_kernel(RowArgs a, int lanes) {
   const int64_t i = a.first + int64_t(blockIdx.x) * (kBlock / lanes) + int(threadIdx.x) / lanes;
   if (i >= a.n) return;  // all of a row's lanes
@@ -220,26 +231,22 @@ __global__ __launch_bounds__(kBlock) void lanes_kernel(RowArgs a, int lanes) {
   const int token = int(token_in(a.tokens, i, a.vocab));
   float x;
   const Soft r = lanes_soft<T>(a, i, t, token >= 0, lanes, x);
-  const float f = finite_max(r.m);
   const float xt = __shfl(x, (int(threadIdx.x) % kWave) / lanes * lanes + max(token, 0));
   const float l = token < 0 ? 0.f : log_prob(a, xt, r);
   if (t == 0) a.logp[i] = l;
-  if (!kPolicy) return;
+  if (kFor == kLogp) return;
   TokenLoss k = {0.f, 0.f};
   if (token >= 0) k = token_loss(a, i, l);
   if (t == 0) a.losses[i] = k.loss;
   if (t >= vocab) return;
   float d = 0.f;
-  if (token >= 0 && l != -INFINITY) {
-    const float p = pow2(__builtin_fmaf(x - f, a.c, -log_2(r.s)));
-    d = k.slope * a.inv_t * (t == token ? 1.f - p : -p);
-  }
+  if (token >= 0 && l != -INFINITY) d = grad_of(r, k.slope * a.inv_t).at(x, a.c, t == token);
   static_cast<T*>(a.d_logits)[i * a.d_stride + t] = T(d);
 }
 
 // A wave (kThreads = 64, four rows a block) or a block takes a row that its
 // registers hold.
-template <class T, bool kPolicy, int kThreads, int kVecs>
+template <class T, For kFor, int kThreads, int kVecs>
 __global__ __launch_bounds__(kThreads < kBlock ? kBlock : kThreads) void held_kernel(RowArgs a) {
   constexpr bool kWaves = kThreads == kWave;
   __shared__ float part[2][kWaves ? 1 : kThreads / kWave];
@@ -249,13 +256,14 @@ __global__ __launch_bounds__(kThreads < kBlock ? kBlock : kThreads) void held_ke
   const int t = int(threadIdx.x) % kThreads, vocab = int(a.vocab);
   const int token = int(token_in(a.tokens, i, a.vocab));
   typedef Held<T, kThreads, kVecs> Row;
-  T* const out = kPolicy ? static_cast<T*>(a.d_logits) + i * a.d_stride : nullptr;
+  T* const out = kFor != kLogp ? static_cast<T*>(a.d_logits) + i * a.d_stride : nullptr;
+  if (kFor == kGrad && (token < 0 || a.logp_in[i] == -INFINITY)) return Row::zero(out, vocab, t);
   if (token < 0) {
     if (t == 0) {
       a.logp[i] = 0.f;
-      if (kPolicy) a.losses[i] = 0.f;
+      if (kFor == kPolicy) a.losses[i] = 0.f;
     }
-    if (kPolicy) Row::zero(out, vocab, t);
+    if (kFor == kPolicy) Row::zero(out, vocab, t);
     return;
   }
   const T* const row = static_cast<const T*>(a.logits) + i * a.stride;
@@ -280,13 +288,15 @@ __global__ __launch_bounds__(kThreads < kBlock ? kBlock : kThreads) void held_ke
 #pragma unroll
     for (int w = 0; w < kThreads / kWave; ++w) sum += part[1][w];
   }
+  if (kFor == kGrad)
+    return r.store(out, vocab, t, a.c, grad_of({m, sum}, a.d_logp[i] * a.inv_t), token);
   const float l = log_prob(a, xt, {m, sum});
   if (t == 0) a.logp[i] = l;
-  if (!kPolicy) return;
+  if (kFor == kLogp) return;
   const TokenLoss k = token_loss(a, i, l);
   if (t == 0) a.losses[i] = k.loss;
   if (l == -INFINITY) return Row::zero(out, vocab, t);
-  r.store(out, vocab, t, f, a.c, -log_2(sum), k.slope * a.inv_t, token);
+  r.store(out, vocab, t, a.c, grad_of({m, sum}, k.slope * a.inv_t), token);
 }
 
 // Statistics of a long row, four pieces of a thread under way at once.
@@ -319,12 +329,12 @@ __device__ __forceinline__ Soft row_soft(const T* row, int64_t vocab, float c, S
   return block_join(a, c, part);
 }
 
-// d_logits of a row by kThreads threads: gain (e_t - 2^((x - f) c + u)).  Every
-// element is read and written by the same thread, so that the two may be one.
+// d_logits of a row by kThreads threads.  Every element is read and written by the
+// same thread, so that the two may be one.
 // kPast: past the caches, which then hold more rows that are still to be read.
 template <class T, int kThreads, bool kPast>
-__device__ __forceinline__ void row_grad(const T* row, T* out, int64_t vocab, float c, float f,
-                                         float u, float gain, int64_t token) {
+__device__ __forceinline__ void row_grad(const T* row, T* out, int64_t vocab, float c,
+                                         const Grad& g, int64_t token) {
   constexpr int N = Vec<T>::kN;
   const int64_t whole = vocab / N * N;
   for (int64_t j = int64_t(threadIdx.x) * N; j < whole; j += kThreads * N) {
@@ -332,18 +342,12 @@ __device__ __forceinline__ void row_grad(const T* row, T* out, int64_t vocab, fl
     widen<T>(x, load16(row + j));
     typename Vec<T>::type v;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float p = pow2(__builtin_fmaf(x[i] - f, c, u));
-      v[i] = T(gain * (j + i == token ? 1.f - p : -p));
-    }
+    for (int i = 0; i < N; ++i) v[i] = T(g.at(x[i], c, j + i == token));
     if (kPast) stream16(out + j, v);
     else store16(out + j, v);
   }
   const int64_t j = whole + threadIdx.x;
-  if (j < vocab) {
-    const float p = pow2(__builtin_fmaf(float(row[j]) - f, c, u));
-    out[j] = T(gain * (j == token ? 1.f - p : -p));
-  }
+  if (j < vocab) out[j] = T(g.at(float(row[j]), c, j == token));
 }
 
 template <class T, int kThreads>
@@ -355,18 +359,18 @@ __device__ __forceinline__ void row_zero(T* out, int64_t vocab) {
   if (whole + threadIdx.x < vocab) out[whole + threadIdx.x] = T(0);
 }
 
-template <class T, bool kPolicy, int kThreads>
+template <class T, For kFor, int kThreads>
 __global__ __launch_bounds__(kThreads) void long_kernel(RowArgs a) {
   __shared__ Soft part[kThreads / kWave];
   const int64_t i = a.first + blockIdx.x;
   const int64_t token = token_in(a.tokens, i, a.vocab);
-  T* const out = kPolicy ? static_cast<T*>(a.d_logits) + i * a.d_stride : nullptr;
+  T* const out = kFor == kPolicy ? static_cast<T*>(a.d_logits) + i * a.d_stride : nullptr;
   if (token < 0) {
     if (threadIdx.x == 0) {
       a.logp[i] = 0.f;
-      if (kPolicy) a.losses[i] = 0.f;
+      if (kFor == kPolicy) a.losses[i] = 0.f;
     }
-    if (kPolicy) row_zero<T, kThreads>(out, a.vocab);
+    if (kFor == kPolicy) row_zero<T, kThreads>(out, a.vocab);
     return;
   }
   const T* row = static_cast<const T*>(a.logits) + i * a.stride;
@@ -374,20 +378,24 @@ __global__ __launch_bounds__(kThreads) void long_kernel(RowArgs a) {
   const Soft r = row_soft<T, kThreads>(row, a.vocab, a.c, part);
   const float l = log_prob(a, xt, r);
   if (threadIdx.x == 0) a.logp[i] = l;
-  if (!kPolicy) return;
+  if (kFor == kLogp) return;
   const TokenLoss k = token_loss(a, i, l);
   if (threadIdx.x == 0) a.losses[i] = k.loss;
   if (l == -INFINITY) return row_zero<T, kThreads>(out, a.vocab);
-  row_grad<T, kThreads, true>(row, out, a.vocab, a.c, finite_max(r.m), -log_2(r.s),
-                               k.slope * a.inv_t, token);
+  row_grad<T, kThreads, true>(row, out, a.vocab, a.c, grad_of(r, k.slope * a.inv_t), token);
 }
 
 // The gradient alone, of rows of more than 64 logits: 1024 threads a row from
 // 32,768 logits on (48 pairs, 50021 logits: 589 us, 626 with 256), else 256.
 // Powers count from the token's logit and its log-probability l, two numbers of
-// the size of l: where that is large (a token that was all but ruled out) their
-// roundings would show, and the row's statistics are taken again.
-constexpr float kFar = -32.f;
+// the size of l: where their roundings, some 3e-8 |l| of every probability, would
+// show beside those of the result, the row's statistics are taken again.  That is
+// from -32 on in 16 bits (a token that was all but ruled out).  In 32 bits rows
+// that registers hold go by their statistics at all times (held_kernel; 8,000 rows
+// of 32003 logits 375 us, 426 here), longer ones, which are read twice for them
+// (3,000 rows of 131072: 835 us, 589 in one pass), from -4 on.
+template <class T>
+constexpr float kFar = sizeof(T) == 4 ? -4.f : -32.f;
 template <class T, int kThreads>
 __global__ __launch_bounds__(kThreads) void grad_kernel(RowArgs a) {
   const int64_t i = a.first + blockIdx.x;
@@ -396,15 +404,15 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(RowArgs a) {
   const float l = a.logp_in[i];
   if (token < 0 || l == -INFINITY) return row_zero<T, kThreads>(out, a.vocab);
   const T* row = static_cast<const T*>(a.logits) + i * a.stride;
-  float f = float(row[token]), u = l * kLog2e;
-  if (l < kFar) {
+  const float gain = a.d_logp[i] * a.inv_t;
+  Grad g = {float(row[token]), l * kLog2e, gain, gain};
+  if (l < kFar<T>) {
     __shared__ Soft part[kThreads / kWave];
     const Soft r = row_soft<T, kThreads>(row, a.vocab, a.c, part);
-    f = finite_max(r.m);
-    u = -log_2(r.s);
+    g = grad_of(r, gain);
   }
   __syncthreads();  // every thread has the token's logit before one writes there
-  row_grad<T, kThreads, false>(row, out, a.vocab, a.c, f, u, a.d_logp[i] * a.inv_t, token);
+  row_grad<T, kThreads, false>(row, out, a.vocab, a.c, g, token);
 }
 
 template <class T>
@@ -417,10 +425,8 @@ __global__ __launch_bounds__(kBlock) void lanes_grad_kernel(RowArgs a, int lanes
   const Soft r = lanes_soft<T>(a, i, t, token >= 0, lanes, x);
   if (t >= int(a.vocab)) return;
   float d = 0.f;
-  if (token >= 0 && a.logp_in[i] != -INFINITY) {
-    const float p = pow2(__builtin_fmaf(x - finite_max(r.m), a.c, -log_2(r.s)));
-    d = a.d_logp[i] * a.inv_t * (t == token ? 1.f - p : -p);
-  }
+  if (token >= 0 && a.logp_in[i] != -INFINITY)
+    d = grad_of(r, a.d_logp[i] * a.inv_t).at(x, a.c, t == token);
   static_cast<T*>(a.d_logits)[i * a.d_stride + t] = T(d);
 }
 
@@ -585,23 +591,31 @@ int lanes_for(int64_t vocab) {
   return l;
 }
 
-template <class T, bool kPolicy>
+// Rows of more than 64 logits that registers hold.
+template <class T>
+constexpr int64_t kMostHeld = 8192 * Vec<T>::kN + Vec<T>::kN - 1;
+template <class T, For kFor>
+hipError_t held_rows(const RowArgs& a, hipStream_t s) {
+  const int64_t pieces = a.vocab / Vec<T>::kN;
+  constexpr int kPer = kBlock / kWave;
+  if (pieces <= 64) return over_rows(held_kernel<T, kFor, 64, 1>, a, kPer, kBlock, s);
+  if (pieces <= 128) return over_rows(held_kernel<T, kFor, 64, 2>, a, kPer, kBlock, s);
+  if (pieces <= 256) return over_rows(held_kernel<T, kFor, 64, 4>, a, kPer, kBlock, s);
+  if (pieces <= 512) return over_rows(held_kernel<T, kFor, 64, 8>, a, kPer, kBlock, s);
+  if (pieces <= 1024) return over_rows(held_kernel<T, kFor, 256, 4>, a, 1, 256, s);
+  if (pieces <= 2048) return over_rows(held_kernel<T, kFor, 256, 8>, a, 1, 256, s);
+  if (pieces <= 4096) return over_rows(held_kernel<T, kFor, 256, 16>, a, 1, 256, s);
+  return over_rows(held_kernel<T, kFor, 512, 16>, a, 1, 512, s);
+}
+
+template <class T, For kFor>
 hipError_t rows_of(const RowArgs& a, hipStream_t s) {
   if (a.vocab <= kWave) {
     const int lanes = lanes_for(a.vocab);
-    return over_rows(lanes_kernel<T, kPolicy>, a, kBlock / lanes, kBlock, s, lanes);
+    return over_rows(lanes_kernel<T, kFor>, a, kBlock / lanes, kBlock, s, lanes);
   }
-  const int64_t pieces = a.vocab / Vec<T>::kN;
-  constexpr int kPer = kBlock / kWave;
-  if (pieces <= 64) return over_rows(held_kernel<T, kPolicy, 64, 1>, a, kPer, kBlock, s);
-  if (pieces <= 128) return over_rows(held_kernel<T, kPolicy, 64, 2>, a, kPer, kBlock, s);
-  if (pieces <= 256) return over_rows(held_kernel<T, kPolicy, 64, 4>, a, kPer, kBlock, s);
-  if (pieces <= 512) return over_rows(held_kernel<T, kPolicy, 64, 8>, a, kPer, kBlock, s);
-  if (pieces <= 1024) return over_rows(held_kernel<T, kPolicy, 256, 4>, a, 1, 256, s);
-  if (pieces <= 2048) return over_rows(held_kernel<T, kPolicy, 256, 8>, a, 1, 256, s);
-  if (pieces <= 4096) return over_rows(held_kernel<T, kPolicy, 256, 16>, a, 1, 256, s);
-  if (pieces <= 8192) return over_rows(held_kernel<T, kPolicy, 512, 16>, a, 1, 512, s);
-  return over_rows(long_kernel<T, kPolicy, kLongThreads>, a, 1, kLongThreads, s);
+  if (a.vocab <= kMostHeld<T>) return held_rows<T, kFor>(a, s);
+  return over_rows(long_kernel<T, kFor, kLongThreads>, a, 1, kLongThreads, s);
 }
 
 template <class T>
@@ -610,15 +624,19 @@ hipError_t grads_of(const RowArgs& a, hipStream_t s) {
     const int lanes = lanes_for(a.vocab);
     return over_rows(lanes_grad_kernel<T>, a, kBlock / lanes, kBlock, s, lanes);
   }
-  if (a.vocab < 32768) return over_rows(grad_kernel<T, 256>, a, 1, 256, s);
+  if constexpr (sizeof(T) == 4) {
+    if (a.vocab <= kMostHeld<T>) return held_rows<T, kGrad>(a, s);
+  } else if (a.vocab < 32768) {
+    return over_rows(grad_kernel<T, 256>, a, 1, 256, s);
+  }
   return over_rows(grad_kernel<T, 1024>, a, 1, 1024, s);
 }
 
-template <bool kPolicy>
+template <For kFor>
 hipError_t rows_by_type(int32_t dtype, const RowArgs& a, hipStream_t s) {
-  return dtype == SCHED_F32   ? rows_of<float, kPolicy>(a, s)
-         : dtype == SCHED_F16 ? rows_of<f16, kPolicy>(a, s)
-                              : rows_of<bf16, kPolicy>(a, s);
+  return dtype == SCHED_F32   ? rows_of<float, kFor>(a, s)
+         : dtype == SCHED_F16 ? rows_of<f16, kFor>(a, s)
+                              : rows_of<bf16, kFor>(a, s);
 }
 
 Tokens tokens_of(const sched_tokens& t) { return {t.data, t.bits == 64}; }
@@ -642,7 +660,7 @@ hipError_t launch_logprobs(const sched_matrix& logits, const sched_tokens& token
                            float temperature, float* logp, hipStream_t s) {
   RowArgs a = row_args(logits, tokens, temperature);
   a.logp = logp;
-  return rows_by_type<false>(logits.dtype, a, s);
+  return rows_by_type<kLogp>(logits.dtype, a, s);
 }
 
 hipError_t launch_logprobs_grad(const sched_matrix& logits, const sched_tokens& tokens,
@@ -672,7 +690,7 @@ hipError_t launch_policy(const sched_policy_desc& d, hipStream_t s) {
   a.logp = d.logp;
   a.d_logits = d.d_logits.data;
   a.d_stride = d.d_logits.stride;
-  const hipError_t e = rows_by_type<true>(d.logits.dtype, a, s);
+  const hipError_t e = rows_by_type<kPolicy>(d.logits.dtype, a, s);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(total_kernel, dim3(1), dim3(1024), 0, s, d.losses, d.logits.rows, d.loss);
   return hipGetLastError();

@@ -839,3 +839,23 @@ def test_attention_gradient_of_every_size(dtype, rows, heads, kv, dim, size):
     check_gradient_norms(q, k, v, do, grads, dim ** -0.5)
     again = S.sched_attention_grad(*a, out, lse, do.cuda(), i32(qo), i32(ko))
     assert all(torch.equal(x, y) for x, y in zip(grads, again))
+
+
+@pytest.mark.parametrize("vocab", [65, 500, 5003, 40009])
+@pytest.mark.parametrize("level", [0.0, -4.0, -10.0, -16.0, -25.0])
+def test_logprobs_gradient_in_32_bits_by_its_norm(vocab, level):
+    """Tokens from ordinary to unlikely: the norm of a row's error is that of some
+    roundings.  All probabilities share those of the sum (two, in units of 2^-24),
+    of one over it, of the factor before it and of their product (one and a half);
+    each has its own of the exponent (of 4 where most of the norm is: two), the
+    power and the result (one and a half), whose norm is at most 0.6 of that."""
+    g = gen(vocab)
+    x, t = randn(g, 24, vocab) * 2, torch.randint(0, vocab, (24,), generator=g)
+    x[torch.arange(24), t] += level
+    d_logp = randn(g, 24)
+    logp = S.sched_token_logprobs(x.cuda(), t.cuda())
+    grad = S.sched_token_logprobs_grad(x.cuda(), t.cuda(), logp, d_logp.cuda()).cpu().double()
+    want = -torch.softmax(x.double(), 1) * d_logp[:, None].double()
+    off = grad - want
+    off[torch.arange(24), t] = want[torch.arange(24), t] = 0  # the other logits
+    assert float((off.norm(dim=1) / want.norm(dim=1)).max()) < 6 * R.F
