@@ -859,3 +859,113 @@ def test_logprobs_gradient_in_32_bits_by_its_norm(vocab, level):
     off = grad - want
     off[torch.arange(24), t] = want[torch.arange(24), t] = 0  # the other logits
     assert float((off.norm(dim=1) / want.norm(dim=1)).max()) < 6 * R.F
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab", [3, 64, 65, 257, 700, 2053, 4099, 8200, 16003, 32003, 40009, 66003,
+                                   131072])
+@pytest.mark.parametrize("kl", [0.0, 0.05])
+def test_policy_gradient_of_every_layout(dtype, vocab, kl):
+    """The logits' gradient alone, within what its own slope and probabilities
+    may be off by: slopes are far from 0, and most elements far above the bound."""
+    g = gen(vocab + 11)
+    n, scale, temperature = 6, 2.5, 1.3
+    x, t = draw_rows(g, n, vocab, dtype, 2.0)
+    logp, p, on = R.logprobs(x, t, temperature)
+    old, ref = (logp - 0.06).float(), (logp + randn(g, n) * 0.3).float()
+    adv = torch.tensor([1.0, 1.0, -0.7, 0.6, -1.2, 0.9])
+    w = torch.rand(n, generator=g) + 0.5
+    args = (t.cuda(), old.cuda(), ref.cuda() if kl else None, adv.cuda(), w.cuda())
+    grad = S.sched_policy_loss(x.cuda(), *args, kl_weight=kl, temperature=temperature,
+                               loss_scale=scale)[3]
+    _, slope = R.policy(logp, on, old, ref, adv, w, 0.2, 0.2, kl)
+    assert bool((slope[on].abs() > 0.2).all())
+    err = R.logits_error(x, temperature) + 4 * R.F * logp.abs() + 2 * R.F * (old.abs() + ref.abs())
+    slope_off = (4 * (err + 8 * R.F) * w * (adv.abs() * 2 + kl * 4)).double()
+    want, bound = R.d_logits(x, t, p, on, logp, slope * scale, temperature)
+    hot = torch.zeros_like(p)
+    hot[torch.arange(n), torch.where(on, t, 0)] = 1
+    bound = bound + (scale * slope_off / temperature)[:, None] * (hot - p).abs()
+    R.close(grad, want, bound, "d_logits")
+    assert float((want.abs() > 2 * bound)[on].double().mean()) > 0.7
+
+
+@pytest.mark.parametrize("mean", ["tokens", "sequences"])
+@pytest.mark.parametrize("groups,samples", [(1, 3), (6, 5), (13, 23)])
+def test_policy_loss_of_whole_groups(mean, groups, samples):
+    """Advantages of a group add up to zero, so the loss is a small difference of
+    its terms.  With ratios of 1 it is the sum of -weight * advantage: off by the
+    roundings of the two and of their product."""
+    g = gen(groups)
+    n, vocab = groups * samples, 5
+    lengths = [int(x) for x in torch.randint(50, 60, (n,), generator=g)]
+    off, at = offsets(lengths), [i * samples for i in range(groups + 1)]
+    x, t = randn(g, off[-1], vocab), torch.randint(0, vocab, (off[-1],), generator=g)
+    m = torch.randint(400_000, 2_000_000, (n,), generator=g)
+    limits = torch.full((groups,), 2_500_000)
+    adv, w = S.sched_group_advantages(m.cuda(), limits.cuda(), i32(at), i32(off), t.cuda(), mean=mean)
+    old = S.sched_token_logprobs(x.cuda(), t.cuda())
+    loss, losses, _, _ = S.sched_policy_loss(x.cuda(), t.cuda(), old, None, adv, w)
+    a, weight = R.advantages(m, limits, at, off, t, mean)
+    R.close(losses, -a * weight, 3 * R.F * (a * weight).abs())
+    total = (a * weight).sum()
+    R.close(loss, -total.view(1), 3 * R.F * float((a * weight).abs().sum()) + R.F * total.abs())
+
+
+def far(shape, row, head, at, base, values):
+    """A view of `base` with these strides, from element `at` on, that holds values."""
+    t = torch.as_strided(base, shape, (row, head, 1), at)
+    return t.copy_(values) if values is not None else t
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("heads_first", [True, False])
+@pytest.mark.parametrize("queries,keys", [(130, 130), (1, 130), (70, 200), (1, 600)])
+def test_attention_with_rows_or_heads_far_apart(dtype, heads_first, queries, keys):
+    """Strides of 2^24 elements and more, tensors of more than 2^32 bytes."""
+    heads, kv, dim, step = 4, 2, 64, (1 << 24) + 8
+    q, k, v, do, qo, ko = attention_case(dtype, [queries], [keys], heads, kv, dim, 9)
+    a = [x.cuda() for x in (q, k, v)]
+    kw = (i32(qo), i32(ko))
+    out, lse = S.sched_attention(*a, *kw)
+    want = S.sched_attention_grad(*a, out, lse, do.cuda(), *kw)
+    rows = max(queries, keys)
+    base = torch.empty((heads if heads_first else rows) * step, dtype=dtype, device="cuda")
+    row, head = (256 * dim, step) if heads_first else (step, 16 * dim)
+    at = [i * 4 * 16 * dim for i in range(8)]  # of rows of 16 heads, or of their first heads
+
+    def put(i, shape, values):
+        return far(shape, row, head, at[i] if not heads_first else at[i] // 2, base, values)
+
+    y = [put(i, x.shape, x) for i, x in enumerate(a)]
+    d = put(3, do.shape, do.cuda())
+    o = put(4, out.shape, None)
+    got, lse2 = S.sched_attention(*y, *kw, out=o)
+    assert got is o and torch.equal(o, out) and torch.equal(lse, lse2)
+    grads = [put(5 + i, x.shape, None) for i, x in enumerate(a)]
+    S.sched_attention_grad(*y, o, lse2, d, *kw, d_q=grads[0], d_k=grads[1], d_v=grads[2])
+    for x, z in zip(grads, want):
+        assert torch.equal(x, z)
+    for x, z in zip(y, a):  # nothing else was written
+        assert torch.equal(x, z)
+
+
+@pytest.mark.parametrize("q_len,k_len,heads,kv,dim,causal", [
+    ([2000, 1900], None, 2, 1, 64, True), ([2500, 30, 2100], [1700, 900, 2600], 2, 1, 40, False),
+    ([1500, 1400], [3300, 800], 3, 1, 128, True)])
+def test_attention_gradient_of_ranked_tiles_in_parts(q_len, k_len, heads, kv, dim, causal):
+    """Tiles go by their work, and rows and keys are shared by several blocks too."""
+    q, k, v, do, qo, ko = attention_case(torch.bfloat16, q_len, k_len, heads, kv, dim, 17)
+    check_attention(q, k, v, do, qo, ko, causal)
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("queries,lengths,slot,heads,kv,dim", [
+    ([7, 1, 3], [3000, 1, 40], 3100, 5, 1, 64), ([16, 16], [16, 2500], 2600, 10, 2, 128),
+    ([40, 0, 33], [900, 10, 33], 1000, 40, 8, 128)])
+def test_attention_of_several_tokens_over_a_cache(dtype, queries, lengths, slot, heads, kv, dim):
+    """New tokens behind those of a filled cache, five heads a key head."""
+    q, k, v, _, qo, ko = attention_case(dtype, queries, [slot] * len(lengths), heads, kv, dim, slot)
+    for i, n in enumerate(lengths):
+        k[i * slot + n:(i + 1) * slot], v[i * slot + n:(i + 1) * slot] = math.nan, math.inf
+    check_attention(q, k, v, None, qo, ko, True, k_len=lengths, grads=False)
