@@ -5,7 +5,9 @@ Argument marshalling only.  Tensors are torch tensors on one GPU; results are
 new tensors unless they are given, and the calls enqueue their work on `stream`
 (default: the current stream of the tensors' GPU) and return.  A tensor that
 belongs to another stream is marked as used on this one; ordering the streams
-is the caller's.
+is the caller's.  The calls take no part in automatic differentiation: results
+of tensors that require a gradient do not, and each operator's gradient is a
+call of its own (workloads/agent.py joins them to torch's).
 """
 from __future__ import annotations
 

@@ -66,3 +66,19 @@ def test_training_lowers_the_makespans(loss):
     optimum = flow.optimum()
     assert best >= optimum
     assert means[-1] - optimum < 0.6 * (means[0] - optimum)
+
+
+def test_a_second_derivative_is_refused():
+    """The operators' gradients are no functions of their own to differentiate:
+    torch says so in place of taking them as constants."""
+    table = torch.randn(9, 16, device="cuda", requires_grad=True)
+    tokens = torch.tensor([1, 4, 4], device="cuda")
+    rows = A.Embed.apply(table, tokens, 2.0)
+    d, = torch.autograd.grad(rows.square().sum(), table, create_graph=True)
+    with pytest.raises(RuntimeError, match="differentiat"):
+        d.square().sum().backward()
+    x = torch.randn(5, 4, 16, device="cuda").bfloat16().requires_grad_()
+    out = A.Attend.apply(x, 2, torch.tensor([0, 5], dtype=torch.int32, device="cuda"))
+    d, = torch.autograd.grad(out.float().square().sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError, match="differentiat"):
+        d.float().square().sum().backward()

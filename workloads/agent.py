@@ -26,6 +26,7 @@ import argparse
 import math
 
 import torch
+from torch.autograd.function import once_differentiable
 
 import paper_2607_22242_amd as S
 from workloads import synth
@@ -53,6 +54,7 @@ class Embed(torch.autograd.Function):
         return S.sched_embed(table, tokens, scale=scale)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, d_rows):
         tokens, = ctx.saved_tensors
         return S.sched_embed_grad(d_rows.contiguous(), tokens, ctx.vocab, scale=ctx.scale), None, None
@@ -71,6 +73,7 @@ class Attend(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, d_out):
         x, out, lse, offsets = ctx.saved_tensors
         h, kv = ctx.heads, (x.shape[1] - ctx.heads) // 2
