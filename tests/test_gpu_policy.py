@@ -969,3 +969,22 @@ def test_attention_of_several_tokens_over_a_cache(dtype, queries, lengths, slot,
     for i, n in enumerate(lengths):
         k[i * slot + n:(i + 1) * slot], v[i * slot + n:(i + 1) * slot] = math.nan, math.inf
     check_attention(q, k, v, None, qo, ko, True, k_len=lengths, grads=False)
+
+
+def test_embedding_gradient_of_rows_in_several_dimensions():
+    """Rows of a batch that lie at one distance are taken as they are; others, and
+    those of another number of tokens, are refused by the library's error."""
+    g = gen(31)
+    d, t = randn(g, 6, 5, 16).cuda(), torch.randint(0, 9, (6, 5), generator=g).cuda()
+    want = S.sched_embed_grad(d.view(30, 16), t.view(30), 9)
+    assert torch.equal(S.sched_embed_grad(d, t, 9), want)
+    wide = torch.zeros((6, 5, 40), device="cuda")
+    wide[..., 7:23] = d
+    assert torch.equal(S.sched_embed_grad(wide[..., 7:23], t, 9), want)
+    refused("SCHED_E_VALUE", S.sched_embed_grad, d.transpose(0, 1), t, 9)
+    refused("SCHED_E_SIZE", S.sched_embed_grad, d[:4], t, 9)
+    refused("SCHED_E_SIZE", S.sched_embed_grad, d[0, 0], t, 9)
+    one = S.sched_embed_grad(d[0, 0], t[0, :1], 9)
+    assert torch.equal(one, S.sched_embed_grad(d[0, :1], t[0, :1], 9))
+    none = S.sched_embed_grad(d[:0], t[:0], 9)
+    assert none.shape == (9, 16) and not none.any()
