@@ -71,10 +71,11 @@ int sched_embed(const sched_matrix *table, const sched_tokens *tokens, float sca
                 const sched_matrix *out, void *hip_stream);
 
 /* Its gradient: d_table[v] = scale * the sum of d_rows[i] over the i with
- * tokens[i] = v, in the order of i, zeros for tokens that do not occur; with
- * accumulate = 1 the sum is added to d_table.  d_table: vocab x dim, of
- * d_rows' type or SCHED_F32.  The tokens are sorted in the workspace, and each
- * row is summed over its run.  dim <= 2^24. */
+ * tokens[i] = v, zeros for tokens that do not occur; with accumulate = 1 the sum
+ * is added to d_table.  d_table: vocab x dim, of d_rows' type or SCHED_F32.  The
+ * tokens are sorted in the workspace, and each row is summed over its run, in 32
+ * bits and in one order, which is not that of i: it follows from n, dim and where
+ * the run lies in the sorted list.  dim <= 2^24. */
 int sched_embed_grad_workspace_bytes(int64_t n, int64_t dim, size_t *out);
 int sched_embed_grad(const sched_matrix *d_rows, const sched_tokens *tokens, float scale,
                      int32_t accumulate, const sched_matrix *d_table, void *d_workspace,
@@ -121,8 +122,11 @@ int sched_group_advantages(const int64_t *makespan_us, const int64_t *limit_us,
  *   losses[i] = weights[i] * (max(-A r, -A min(max(r, 1 - clip_low), 1 + clip_high))
  *                             + kl_weight * (exp(e) - e - 1))
  *
- * loss[0] is their sum, logp[i] = l, and d_logits the gradient of loss[0]
- * times loss_scale.  Where both terms of the max are equal the first one's
+ * loss[0] is their sum (a group's advantages add up to zero, so it is mostly a
+ * small difference of its terms: it is good to some 2^-24 of the sum of their
+ * magnitudes, as its 32-bit inputs are, and where that is 1,000 times the loss to
+ * 6e-5 of itself; the gradient has no such sum), logp[i] = l, and d_logits the
+ * gradient of loss[0] times loss_scale.  Where both terms of the max are equal the first one's
  * gradient counts.  ref_logp may be null if kl_weight is 0.  Padding and tokens
  * with logp = -inf have zero gradient; padding has losses and logp 0. */
 typedef struct {

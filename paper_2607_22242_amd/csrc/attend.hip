@@ -334,7 +334,9 @@ AttendArgs attend_args(const sched_attention_desc& d) {
   a.near_k = near(d.k) && near(d.v);
   a.near_q = near(d.q) && 16 % a.group == 0;
   // Several long sequences (8 of 1,500 rows, 16 heads: backward 412 -> 326 us,
-  // forward 108 -> 100; 40 of 400: forward 61 -> 70, so short ones do not).
+  // forward 108 -> 100; 40 of 400: forward 61 -> 70, so short ones do not), as many
+  // as a wave has lanes: more fill the card in any order (64 of 300 to 2,500 rows, 8
+  // heads of 2: forward and backward 466 and 1,500 us, 65 of them 428 and 1,485).
   a.ranked = d.n_seqs > 1 && d.n_seqs <= kWave && d.q_rows / d.n_seqs >= 1024;
   a.causal = d.causal;
   a.scale = d.scale;

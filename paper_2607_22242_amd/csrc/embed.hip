@@ -3,9 +3,9 @@
 // Lookup: out[i] = scale * table[t_i], a copy of rows.  Gradient: row v of the
 // table gets scale * the sum of d_rows[i] over the i with t_i = v.  The pairs
 // (t_i, i) are sorted by token, stable, so that every row's sum runs over one
-// run of the list in the order of i: no atomics on values, one order.  A run
-// may hold one token or all of them; whole chunks of a run are summed first by
-// waves of their own and the row adds their sums.
+// run of the list: no atomics on values, one order, dealt to the groups of lanes
+// of a wave.  A run may hold one token or all of them; whole chunks of a run are
+// summed first by waves of their own and the row adds their sums.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -380,7 +380,7 @@ __device__ __forceinline__ void add_last(const SumArgs& a, uint32_t mine, int i,
   for (int q = 0; q < Vec<T>::kN; ++q) acc[q] += x[q];
 }
 
-// Sum of rows in the order of the list, by a wave: 64 / lanes groups of lanes
+// Sum of rows by a wave: 64 / lanes groups of lanes
 // take an entry each, in 16-byte pieces; the groups' sums are added in one order
 // at the end.
 template <class T>
