@@ -122,13 +122,16 @@ int sched_group_advantages(const int64_t *makespan_us, const int64_t *limit_us,
  *   losses[i] = weights[i] * (max(-A r, -A min(max(r, 1 - clip_low), 1 + clip_high))
  *                             + kl_weight * (exp(e) - e - 1))
  *
- * loss[0] is their sum (a group's advantages add up to zero, so it is mostly a
- * small difference of its terms: it is good to some 2^-24 of the sum of their
- * magnitudes, as its 32-bit inputs are, and where that is 1,000 times the loss to
- * 6e-5 of itself; the gradient has no such sum), logp[i] = l, and d_logits the
- * gradient of loss[0] times loss_scale.  Where both terms of the max are equal the first one's
+ * loss[0] is their sum, logp[i] = l, and d_logits the gradient of loss[0]
+ * times loss_scale.  Where both terms of the max are equal the first one's
  * gradient counts.  ref_logp may be null if kl_weight is 0.  Padding and tokens
- * with logp = -inf have zero gradient; padding has losses and logp 0. */
+ * with logp = -inf have zero gradient; padding has losses and logp 0.  What is
+ * no number shows in its token's loss and gradient and in loss[0].
+ *
+ * A group's advantages add up to zero, so loss[0] is mostly a small difference
+ * of its terms: like its 32-bit inputs it is good to some 2^-24 of the sum of
+ * their magnitudes, which, where that is 1,000 times the loss, is 6e-5 of the
+ * loss itself.  The gradient has no such sum. */
 typedef struct {
     sched_matrix logits;
     sched_tokens tokens;

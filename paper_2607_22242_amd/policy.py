@@ -215,7 +215,7 @@ def sched_embed_grad(d_rows, tokens, vocab: int, scale: float = 1.0, out=None,
             d_rows = d_rows.view(tokens.numel(), d_rows.shape[-1])
         except RuntimeError:
             _refuse(-3 if d_rows.shape[:-1].numel() == tokens.numel() else -2,
-                    c.where + ": d_rows is a matrix, or its rows follow one another at one distance")
+                    c.where + ": d_rows is a matrix, or its rows lie at one distance")
     m, t = c.matrix(d_rows), c.tokens(tokens)
     if out is None:
         if accumulate:
