@@ -208,6 +208,98 @@ int sched_attention_grad(const sched_attention_desc *desc, const sched_heads *d_
                          const sched_heads *d_q, const sched_heads *d_k, const sched_heads *d_v,
                          void *d_workspace, size_t ws_bytes, void *hip_stream);
 
+/* Norms of the heads of queries and keys and their rotation by position, in one
+ * pass.  With x a head of row i, p = positions[i] and w the heads' weights:
+ *
+ *   n = x * w / sqrt(mean over the head of x^2 + eps)     (norm = 0: n = x)
+ *   y[a] = n[a] cos(p f[j]) - n[b] sin(p f[j])
+ *   y[b] = n[a] sin(p f[j]) + n[b] cos(p f[j])            j < turned / 2
+ *
+ * over the pairs a = j, b = j + turned / 2 (interleaved = 0) or a = 2 j, b = 2 j
+ * + 1 (interleaved = 1) of the head's first `turned` elements; the others stay n.
+ * Angles are formed in 64 bits and reduced before they are rounded: positions up
+ * to 2^31 in magnitude turn as well as small ones.  Row i of k goes to row
+ * places[i] of k_out, and of v, as it is, to that of v_out: rows of a cache; a
+ * place outside [0, out_rows) writes none, and no two rows have one place.
+ * Without places (data null) row i goes to row i.  v.data may be null: no
+ * values.  q_out may be q itself, and without places k_out k itself; outputs
+ * overlap no input otherwise.  head_dim: a multiple of 8 up to 256.  turned:
+ * even, up to head_dim (0: norms alone).  Weights are 32-bit (null: ones; with
+ * norm = 0 they have to be).  eps >= 0. */
+typedef struct {
+    sched_heads q, k, v;             /* rows x q_heads (kv_heads) x head_dim */
+    sched_heads q_out, k_out, v_out; /* q_out has `rows` rows, the others out_rows */
+    int32_t dtype, head_dim, q_heads, kv_heads;
+    int64_t rows, out_rows;          /* without places both are the same */
+    sched_tokens positions, places;  /* one per row */
+    const float *q_weight, *k_weight, *frequencies; /* head_dim, head_dim, turned / 2 */
+    int32_t turned, interleaved, norm;
+    float eps;
+} sched_norm_rotate_desc;
+int sched_norm_rotate(const sched_norm_rotate_desc *desc, void *hip_stream);
+
+/* Its gradient: d_q and d_k from d_q_out and d_k_out (row i's at row places[i];
+ * a place outside has none: zeros), and of the weights, summed over all rows and
+ * heads (32-bit; null: not formed).  Reads q, k and the rest of desc but v and
+ * the outputs.  d_q may be d_q_out or q itself, and d_k k itself or, without
+ * places, d_k_out. */
+int sched_norm_rotate_grad_workspace_bytes(const sched_norm_rotate_desc *desc, size_t *out);
+int sched_norm_rotate_grad(const sched_norm_rotate_desc *desc, const sched_heads *d_q_out,
+                           const sched_heads *d_k_out, const sched_heads *d_q,
+                           const sched_heads *d_k, float *d_q_weight, float *d_k_weight,
+                           void *d_workspace, size_t ws_bytes, void *hip_stream);
+
+/* Beam search: the `width` best continuations of each group's beams.  Beam i of
+ * group g is row g * beams + i of logits; its candidates are the tokens t with
+ * the score
+ *
+ *   scores[row] + z[t] - log sum_j exp z[j],   z = the row's logits / temperature,
+ *
+ * formed in 64 bits from sums in 32, in the order of their scores; of equal ones
+ * the lower beam, then the lower token comes first.  A logit of -inf is no
+ * candidate; neither is anything of a row with NaN or +inf in it, or of a beam
+ * whose score is not finite (-inf: a beam that is not there).  A beam whose last
+ * token is end_token is finished (last.data null or end_token -1: none is): its
+ * one candidate is end_token, with the score that it has.
+ *
+ * With stay = 0 the results of a group are its `width` best candidates from the
+ * best on.  With stay = 1 (width = beams) they are the same, laid out so that
+ * few states move: a beam's best continuation keeps the beam's slot, the others,
+ * best first, take the slots that are left, from the lowest.  A result has its
+ * new score, its parent's row and its token; where there are fewer candidates
+ * than `width` the others' scores are -inf and parents and tokens -1.
+ * beams and width: 1 to 128.  logits: up to 2^22 columns.  temperature as above. */
+typedef struct {
+    sched_matrix logits;
+    const float *scores; /* one per row */
+    sched_tokens last;   /* one per row */
+    int64_t end_token;
+    int32_t n_groups, beams, width, stay;
+    float temperature;
+    float *new_scores;   /* n_groups * width, as are the next two */
+    int32_t *parents;
+    void *tokens;
+    int32_t token_bits;  /* 32 or 64 */
+} sched_beam_desc;
+int sched_beam_workspace_bytes(const sched_beam_desc *desc, size_t *out);
+int sched_beam_select(const sched_beam_desc *desc, void *d_workspace, size_t ws_bytes,
+                      void *hip_stream);
+
+/* The beams' states follow their parents, in place: slot s gets what the first
+ * lengths[p] rows (null: all) of slot p = parents[s] held before the call; its
+ * other rows stay.  A parent outside the slot's group of `beams` slots (-1, say)
+ * leaves the slot as it is, as does the slot itself.  States: `outer` tensors
+ * (layers, keys and values) of `slots` slots of `rows` rows of row_bytes bytes,
+ * strides in bytes, none of them overlapping.  Lengths are those before the
+ * call, one per slot.  beams: 1 to 128; slots is a multiple of it. */
+typedef struct {
+    void *data;
+    int64_t outer, slots, rows, row_bytes;
+    int64_t outer_stride, slot_stride, row_stride;
+} sched_states;
+int sched_beam_reorder(const sched_states *states, const int32_t *parents, const int32_t *lengths,
+                       int32_t beams, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -17,6 +17,7 @@ from .binding import (  # noqa: F401
     sched_pruned_workspace_bytes, pruned_workspace, sched_strerror, sched_valu_probe,
     sched_wave_or_probe, sched_workspace_bytes, workspace)
 from .policy import (  # noqa: F401
-    POLICY_EXPORTED, sched_attention, sched_attention_grad, sched_embed, sched_embed_grad,
-    sched_group_advantages, sched_policy_loss, sched_preference_loss, sched_token_logprobs,
+    POLICY_EXPORTED, sched_attention, sched_attention_grad, sched_beam_reorder, sched_beam_select,
+    sched_embed, sched_embed_grad, sched_group_advantages, sched_norm_rotate,
+    sched_norm_rotate_grad, sched_policy_loss, sched_preference_loss, sched_token_logprobs,
     sched_token_logprobs_grad)

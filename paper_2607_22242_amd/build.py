@@ -17,7 +17,8 @@ INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 UNITS = [("inst.hip", [f"-DINST_N={n}"]) for n in range(40, 0, -1)] + [
     ("api.cpp", []), ("monitor.cpp", []), ("dispatch.hip", []), ("probe.hip", []),
     ("scratch.hip", []), ("closed.hip", []), ("attend_grad.hip", []), ("attend.hip", []),
-    ("rows.hip", []), ("embed.hip", []), ("policy_api.cpp", [])]
+    ("rows.hip", []), ("embed.hip", []), ("rotate.hip", []), ("beam.hip", []),
+    ("policy_api.cpp", [])]
 ARCH = "gfx950"
 
 

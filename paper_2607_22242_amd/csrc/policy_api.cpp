@@ -2,6 +2,7 @@
 // then the launches.  Nothing here allocates or waits.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "policy_launch.h"
@@ -14,6 +15,9 @@ constexpr int64_t kMostRows = (int64_t(1) << 31) - 1024;  // strides over rows s
 constexpr int64_t kMostDim = int64_t(1) << 24;    // of an embedding
 constexpr int32_t kMostPairs = 1 << 23;
 constexpr int32_t kMostAnswers = 1 << 16;         // every one's wave adds up all counts
+constexpr int32_t kMostHeads = 1 << 16;
+constexpr int32_t kMostBeams = 128;
+constexpr int64_t kMostChoices = int64_t(1) << 22;  // logits that a beam chooses among
 constexpr int64_t kMostTiles = (1 << 24) - 8;     // blocks of 256 threads in a grid
 
 int done(hipError_t e) { return e == hipSuccess ? SCHED_OK : SCHED_E_DEVICE; }
@@ -47,15 +51,19 @@ int check_workspace(const void* ws, size_t have, size_t need) {
 
 bool positive(float x) { return std::isfinite(x) && x > 0; }
 
+// The factor of the powers, log2(e) / temperature, is the largest that is used.
+int check_temperature(float temperature) {
+  if (!positive(temperature) || !std::isfinite(float(1.4426950408889634 / double(temperature))))
+    return SCHED_E_VALUE;
+  return SCHED_OK;
+}
+
 // A matrix of logits with a token per row and factors that can be used.
 int check_logits(const sched_matrix& logits, const sched_tokens& tokens, float temperature) {
   if (int e = check_matrix(logits, false)) return e;
   if (int e = check_tokens(tokens)) return e;
   if (logits.rows != tokens.n || logits.cols < 1) return SCHED_E_SIZE;
-  // The factor of the powers, log2(e) / temperature, is the largest that is used.
-  if (!positive(temperature) || !std::isfinite(float(1.4426950408889634 / double(temperature))))
-    return SCHED_E_VALUE;
-  return SCHED_OK;
+  return check_temperature(temperature);
 }
 
 int check_d_logits(const sched_matrix& logits, const sched_matrix& d) {
@@ -105,6 +113,51 @@ int check_attention(const sched_attention_desc& d) {
   if (int e = check_heads(d.out, d.q_rows, d.q_heads, d.head_dim, true)) return e;
   if (d.n_seqs > 0 && (!d.q_offsets || !d.k_offsets)) return SCHED_E_NULL;
   if (d.q_rows > 0 && !d.lse) return SCHED_E_NULL;
+  return SCHED_OK;
+}
+
+// Where tensors are the same memory they have to be the same rows and heads.
+bool in_step(const sched_heads& a, const sched_heads& b) {
+  return a.data != b.data || (a.row_stride == b.row_stride && a.head_stride == b.head_stride);
+}
+
+// Heads of 32-bit values are read in two such pieces: their alignment is the same.
+int check_rotate_sizes(const sched_norm_rotate_desc& d) {
+  if (element_bytes(d.dtype) == 0 || d.norm < 0 || d.norm > 1) return SCHED_E_VALUE;
+  if (d.head_dim < 8 || d.head_dim > 256 || d.head_dim % 8 || d.q_heads < 1 || d.kv_heads < 1 ||
+      d.q_heads > kMostHeads || d.kv_heads > kMostHeads || d.rows < 0 || d.rows > kMostRows)
+    return SCHED_E_SIZE;
+  return SCHED_OK;
+}
+int check_rotate(const sched_norm_rotate_desc& d) {
+  if (int e = check_rotate_sizes(d)) return e;
+  if (d.turned < 0 || d.turned > d.head_dim || d.turned % 2 || d.out_rows < 0 ||
+      d.out_rows > kMostRows)
+    return SCHED_E_SIZE;
+  if (d.interleaved < 0 || d.interleaved > 1 || !std::isfinite(d.eps) || d.eps < 0 ||
+      (!d.norm && (d.q_weight || d.k_weight)))
+    return SCHED_E_VALUE;
+  if (int e = check_tokens(d.positions)) return e;
+  if (d.positions.n != d.rows) return SCHED_E_SIZE;
+  if (d.places.data) {
+    if (int e = check_tokens(d.places)) return e;
+    if (d.places.n != d.rows) return SCHED_E_SIZE;
+  } else if (d.out_rows != d.rows) {
+    return SCHED_E_SIZE;
+  }
+  if (d.turned > 0 && !d.frequencies) return SCHED_E_NULL;
+  if (int e = check_heads(d.q, d.rows, d.q_heads, d.head_dim, false)) return e;
+  return check_heads(d.k, d.rows, d.kv_heads, d.head_dim, false);
+}
+
+int check_beam(const sched_beam_desc& d) {
+  if (d.n_groups < 0 || d.n_groups > kMostBlocks || d.beams < 1 || d.beams > kMostBeams ||
+      d.width < 1 || d.width > kMostBeams || d.logits.cols < 1 || d.logits.cols > kMostChoices)
+    return SCHED_E_SIZE;
+  if (int e = check_matrix(d.logits, false)) return e;
+  if (d.logits.rows != int64_t(d.n_groups) * d.beams) return SCHED_E_SIZE;
+  if (d.stay < 0 || d.stay > 1) return SCHED_E_VALUE;
+  if (d.stay && d.width != d.beams) return SCHED_E_SIZE;
   return SCHED_OK;
 }
 
@@ -250,6 +303,104 @@ int sched_attention_grad(const sched_attention_desc* d, const sched_heads* d_out
   if (int e = check_workspace(d_workspace, ws_bytes, attention_grad_bytes(*d))) return e;
   return done(launch_attention_grad(*d, *d_out, *d_q, *d_k, *d_v, d_workspace,
                                     stream_of(hip_stream)));
+}
+
+int sched_norm_rotate(const sched_norm_rotate_desc* d, void* hip_stream) {
+  if (!d) return SCHED_E_NULL;
+  if (int e = check_rotate(*d)) return e;
+  const int32_t dim = d->head_dim, heads = d->kv_heads;
+  const bool placed = d->places.data != nullptr, values = d->v.data != nullptr;
+  if (int e = check_heads(d->q_out, d->rows, d->q_heads, dim, true)) return e;
+  if (int e = check_heads(d->k_out, d->out_rows, heads, dim, true)) return e;
+  if (values) {
+    if (int e = check_heads(d->v, d->rows, heads, dim, false)) return e;
+    if (int e = check_heads(d->v_out, d->out_rows, heads, dim, true)) return e;
+  }
+  // In place is the same rows and heads; a row that goes to another's place is not.
+  if (!in_step(d->q, d->q_out) || !in_step(d->k, d->k_out) || (values && !in_step(d->v, d->v_out)))
+    return SCHED_E_VALUE;
+  if (placed && d->rows > 0 &&
+      (d->k.data == d->k_out.data || (values && d->v.data == d->v_out.data)))
+    return SCHED_E_VALUE;
+  return done(launch_norm_rotate(*d, stream_of(hip_stream)));
+}
+
+int sched_norm_rotate_grad_workspace_bytes(const sched_norm_rotate_desc* d, size_t* out) {
+  if (!d || !out) return SCHED_E_NULL;
+  if (int e = check_rotate_sizes(*d)) return e;
+  *out = norm_rotate_grad_bytes(*d);
+  return SCHED_OK;
+}
+
+int sched_norm_rotate_grad(const sched_norm_rotate_desc* d, const sched_heads* d_q_out,
+                           const sched_heads* d_k_out, const sched_heads* d_q,
+                           const sched_heads* d_k, float* d_q_weight, float* d_k_weight,
+                           void* d_workspace, size_t ws_bytes, void* hip_stream) {
+  if (!d || !d_q_out || !d_k_out || !d_q || !d_k) return SCHED_E_NULL;
+  if (int e = check_rotate(*d)) return e;
+  const int32_t dim = d->head_dim;
+  if (int e = check_heads(*d_q_out, d->rows, d->q_heads, dim, false)) return e;
+  if (int e = check_heads(*d_k_out, d->out_rows, d->kv_heads, dim, false)) return e;
+  if (int e = check_heads(*d_q, d->rows, d->q_heads, dim, true)) return e;
+  if (int e = check_heads(*d_k, d->rows, d->kv_heads, dim, true)) return e;
+  if (!d->norm && (d_q_weight || d_k_weight)) return SCHED_E_VALUE;
+  if (!in_step(*d_q, d->q) || !in_step(*d_q, *d_q_out) || !in_step(*d_k, d->k) ||
+      !in_step(*d_k, *d_k_out) ||
+      (d->places.data && d->rows > 0 && d_k->data == d_k_out->data))
+    return SCHED_E_VALUE;
+  if (d_q_weight || d_k_weight)
+    if (int e = check_workspace(d_workspace, ws_bytes, norm_rotate_grad_bytes(*d))) return e;
+  return done(launch_norm_rotate_grad(*d, *d_q_out, *d_k_out, *d_q, *d_k, d_q_weight, d_k_weight,
+                                      d_workspace, stream_of(hip_stream)));
+}
+
+int sched_beam_workspace_bytes(const sched_beam_desc* d, size_t* out) {
+  if (!d || !out) return SCHED_E_NULL;
+  if (int e = check_beam(*d)) return e;
+  *out = beam_bytes(*d);
+  return SCHED_OK;
+}
+
+int sched_beam_select(const sched_beam_desc* d, void* d_workspace, size_t ws_bytes,
+                      void* hip_stream) {
+  if (!d) return SCHED_E_NULL;
+  if (int e = check_beam(*d)) return e;
+  if (d->last.data) {
+    if (int e = check_tokens(d->last)) return e;
+    if (d->last.n != d->logits.rows) return SCHED_E_SIZE;
+  }
+  const sched_tokens tokens = {d->tokens, d->token_bits, int64_t(d->n_groups) * d->width};
+  if (int e = check_tokens(tokens)) return e;
+  if (d->end_token < -1 || (d->token_bits == 32 && d->end_token > INT32_MAX)) return SCHED_E_VALUE;
+  if (int e = check_temperature(d->temperature)) return e;
+  if (d->n_groups > 0 && (!d->scores || !d->new_scores || !d->parents)) return SCHED_E_NULL;
+  if (int e = check_workspace(d_workspace, ws_bytes, beam_bytes(*d))) return e;
+  return done(launch_beam_select(*d, d_workspace, stream_of(hip_stream)));
+}
+
+int sched_beam_reorder(const sched_states* x, const int32_t* parents, const int32_t* lengths,
+                       int32_t beams, void* hip_stream) {
+  if (!x) return SCHED_E_NULL;
+  if (beams < 1 || beams > kMostBeams || x->outer < 0 || x->slots < 0 || x->rows < 0 ||
+      x->row_bytes < 0 || x->slots > kMostRows || x->slots % beams || x->rows > kMostRows ||
+      x->row_bytes > kMostRows || x->outer > kMostRows)
+    return SCHED_E_SIZE;
+  if (x->outer == 0 || x->slots == 0 || x->rows == 0 || x->row_bytes == 0) return SCHED_OK;
+  if (!x->data || !parents) return SCHED_E_NULL;
+  // Rows, slots and tensors one behind the other, in this order or with the
+  // slots outermost: none may overlap.
+  if (x->row_stride < 0 || x->slot_stride < 0 || x->outer_stride < 0) return SCHED_E_VALUE;
+  struct Axis {
+    int64_t n, stride;
+  } axes[3] = {{x->rows, x->row_stride}, {x->slots, x->slot_stride}, {x->outer, x->outer_stride}};
+  std::sort(axes, axes + 3, [](const Axis& a, const Axis& b) { return a.stride < b.stride; });
+  int64_t extent = x->row_bytes;
+  for (const Axis& axis : axes) {
+    if (axis.n == 1) continue;
+    if (axis.stride < extent || axis.stride > (int64_t(1) << 62) / axis.n) return SCHED_E_VALUE;
+    extent = axis.stride * (axis.n - 1) + extent;
+  }
+  return done(launch_beam_reorder(*x, parents, lengths, beams, stream_of(hip_stream)));
 }
 
 }  // extern "C"

@@ -41,5 +41,15 @@ size_t attention_grad_bytes(const sched_attention_desc& d);
 hipError_t launch_attention_grad(const sched_attention_desc& d, const sched_heads& d_out,
                                  const sched_heads& d_q, const sched_heads& d_k,
                                  const sched_heads& d_v, void* ws, hipStream_t s);
+hipError_t launch_norm_rotate(const sched_norm_rotate_desc& d, hipStream_t s);
+size_t norm_rotate_grad_bytes(const sched_norm_rotate_desc& d);
+hipError_t launch_norm_rotate_grad(const sched_norm_rotate_desc& d, const sched_heads& d_q_out,
+                                   const sched_heads& d_k_out, const sched_heads& d_q,
+                                   const sched_heads& d_k, float* d_q_weight, float* d_k_weight,
+                                   void* ws, hipStream_t s);
+size_t beam_bytes(const sched_beam_desc& d);
+hipError_t launch_beam_select(const sched_beam_desc& d, void* ws, hipStream_t s);
+hipError_t launch_beam_reorder(const sched_states& x, const int32_t* parents,
+                               const int32_t* lengths, int32_t beams, hipStream_t s);
 
 }  // namespace policy

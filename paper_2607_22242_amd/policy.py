@@ -22,7 +22,10 @@ POLICY_EXPORTED = ["sched_embed", "sched_embed_grad_workspace_bytes", "sched_emb
                    "sched_token_logprobs", "sched_token_logprobs_grad", "sched_group_advantages",
                    "sched_policy_loss", "sched_preference_loss",
                    "sched_attention_workspace_bytes", "sched_attention",
-                   "sched_attention_grad_workspace_bytes", "sched_attention_grad"]
+                   "sched_attention_grad_workspace_bytes", "sched_attention_grad",
+                   "sched_norm_rotate", "sched_norm_rotate_grad_workspace_bytes",
+                   "sched_norm_rotate_grad", "sched_beam_workspace_bytes", "sched_beam_select",
+                   "sched_beam_reorder"]
 
 _P, _I32, _I64, _F = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
 
@@ -54,6 +57,29 @@ class sched_attention_desc(ctypes.Structure):
                 ("scale", _F)]
 
 
+class sched_norm_rotate_desc(ctypes.Structure):
+    _fields_ = [("q", sched_heads), ("k", sched_heads), ("v", sched_heads),
+                ("q_out", sched_heads), ("k_out", sched_heads), ("v_out", sched_heads),
+                ("dtype", _I32), ("head_dim", _I32), ("q_heads", _I32), ("kv_heads", _I32),
+                ("rows", _I64), ("out_rows", _I64), ("positions", sched_tokens),
+                ("places", sched_tokens), ("q_weight", _P), ("k_weight", _P),
+                ("frequencies", _P), ("turned", _I32), ("interleaved", _I32), ("norm", _I32),
+                ("eps", _F)]
+
+
+class sched_beam_desc(ctypes.Structure):
+    _fields_ = [("logits", sched_matrix), ("scores", _P), ("last", sched_tokens),
+                ("end_token", _I64), ("n_groups", _I32), ("beams", _I32), ("width", _I32),
+                ("stay", _I32), ("temperature", _F), ("new_scores", _P), ("parents", _P),
+                ("tokens", _P), ("token_bits", _I32)]
+
+
+class sched_states(ctypes.Structure):
+    _fields_ = [("data", _P), ("outer", _I64), ("slots", _I64), ("rows", _I64),
+                ("row_bytes", _I64), ("outer_stride", _I64), ("slot_stride", _I64),
+                ("row_stride", _I64)]
+
+
 _ARGS = {
     "sched_embed": [_P, _P, _F, _P, _P],
     "sched_embed_grad_workspace_bytes": [_I64, _I64, _P],
@@ -68,6 +94,12 @@ _ARGS = {
     "sched_attention": [_P, _P, ctypes.c_size_t, _P],
     "sched_attention_grad_workspace_bytes": [_P, _P],
     "sched_attention_grad": [_P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P],
+    "sched_norm_rotate": [_P, _P],
+    "sched_norm_rotate_grad_workspace_bytes": [_P, _P],
+    "sched_norm_rotate_grad": [_P, _P, _P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P],
+    "sched_beam_workspace_bytes": [_P, _P],
+    "sched_beam_select": [_P, _P, ctypes.c_size_t, _P],
+    "sched_beam_reorder": [_P, _P, _P, _I32, _P],
 }
 
 _F32 = _F16 = _BF16 = _INT32 = _INT64 = None  # torch's types, once it is loaded
@@ -384,3 +416,142 @@ def sched_attention_grad(q, k, v, out, lse, d_out, q_offsets, k_offsets, k_lengt
     c.done("sched_attention_grad", ctypes.byref(d), ctypes.byref(do), ctypes.byref(g[0]),
            ctypes.byref(g[1]), ctypes.byref(g[2]), at, nbytes)
     return tuple(grads)
+
+
+def _rotate_desc(c, q, k, positions, frequencies, q_weight, k_weight, places, out_rows, norm, eps,
+                 interleaved):
+    if q.dim() != 3 or k.dim() != 3 or k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2]:
+        _refuse(-2, c.where + ": q and k are rows x heads x dim")
+    rows, heads, dim = q.shape
+    turned = 2 * frequencies.numel() if frequencies is not None else 0
+    d = sched_norm_rotate_desc()
+    d.q, d.k = _heads(c, q, q.dtype, heads, dim), _heads(c, k, q.dtype, k.shape[1], dim)
+    d.dtype, d.head_dim, d.q_heads, d.kv_heads = _types.get(q.dtype, -1), dim, heads, k.shape[1]
+    d.rows, d.out_rows = rows, rows if places is None else out_rows
+    d.positions = c.tokens(positions)
+    if places is not None:
+        d.places = c.tokens(places)
+        if rows == 0:  # an empty tensor has no address
+            d.places = sched_tokens(256, d.places.bits, d.places.n)
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None:
+            setattr(d, name, c.vector(w, _F32, dim))
+    d.frequencies = c.vector(frequencies, _F32) if turned else None
+    d.turned, d.interleaved, d.norm, d.eps = turned, int(interleaved), int(norm), eps
+    return d
+
+
+def sched_norm_rotate(q, k, positions, frequencies, q_weight=None, k_weight=None, v=None,
+                      places=None, norm: bool = True, eps: float = 1e-6, interleaved: bool = False,
+                      q_out=None, k_out=None, v_out=None, stream=None) -> Tuple:
+    """(q_out, k_out), and v_out where v is given: heads normed, weighted and
+    turned by their rows' positions (int32 or int64) times `frequencies`
+    (float32, one per pair; None: not turned).  With `places` row i of k and v
+    goes to that row of k_out and v_out (caches, which are given)."""
+    c = _Call("sched_norm_rotate", q, stream)
+    if places is not None and (k_out is None or (v is not None and v_out is None)):
+        _refuse(-1, c.where + ": places are rows of a given k_out and v_out")
+    if q_out is None:
+        q_out = c.new(tuple(q.shape), q.dtype)
+    if k_out is None:
+        k_out = c.new(tuple(k.shape), q.dtype)
+    d = _rotate_desc(c, q, k, positions, frequencies, q_weight, k_weight, places, k_out.shape[0], norm,
+                     eps, interleaved)
+    kv, dim = d.kv_heads, d.head_dim
+    d.q_out, d.k_out = _heads(c, q_out, q.dtype, d.q_heads, dim), _heads(c, k_out, q.dtype, kv, dim)
+    if q_out.shape[0] != d.rows or k_out.shape[0] != d.out_rows:
+        _refuse(-2, c.where + ": outputs have a row per input row")
+    if v is not None:
+        if v_out is None:
+            v_out = c.new(tuple(v.shape), q.dtype)
+        d.v, d.v_out = _heads(c, v, q.dtype, kv, dim), _heads(c, v_out, q.dtype, kv, dim)
+        if v.shape[0] != d.rows or v_out.shape[0] != d.out_rows:
+            _refuse(-2, c.where + ": v has k's rows")
+    c.done("sched_norm_rotate", ctypes.byref(d))
+    return (q_out, k_out) if v is None else (q_out, k_out, v_out)
+
+
+def sched_norm_rotate_grad(q, k, d_q_out, d_k_out, positions, frequencies, q_weight=None,
+                           k_weight=None, places=None, norm: bool = True, eps: float = 1e-6,
+                           interleaved: bool = False, d_q=None, d_k=None, d_q_weight=None,
+                           d_k_weight=None, workspace=None, stream=None) -> Tuple:
+    """(d_q, d_k, d_q_weight, d_k_weight) from sched_norm_rotate's inputs and
+    the gradients of its results; of a weight that is not given None."""
+    c = _Call("sched_norm_rotate_grad", q, stream)
+    d = _rotate_desc(c, q, k, positions, frequencies, q_weight, k_weight, places, d_k_out.shape[0],
+                     norm, eps, interleaved)
+    dim = d.head_dim
+    if d_q is None:
+        d_q = c.new(tuple(q.shape), q.dtype)
+    if d_k is None:
+        d_k = c.new(tuple(k.shape), q.dtype)
+    if d_q_weight is None and q_weight is not None:
+        d_q_weight = c.new((dim,), _F32)
+    if d_k_weight is None and k_weight is not None:
+        d_k_weight = c.new((dim,), _F32)
+    if d_q_out.shape[0] != d.rows or d_k_out.shape[0] != d.out_rows or d_q.shape[0] != d.rows or \
+            d_k.shape[0] != d.rows:
+        _refuse(-2, c.where + ": a gradient has its tensor's rows")
+    h = [_heads(c, t, q.dtype, n, dim) for t, n in ((d_q_out, d.q_heads), (d_k_out, d.kv_heads),
+                                                   (d_q, d.q_heads), (d_k, d.kv_heads))]
+    w = [None if t is None else c.vector(t, _F32, dim) for t in (d_q_weight, d_k_weight)]
+    need = c.bytes("sched_norm_rotate_grad_workspace_bytes", ctypes.byref(d))
+    ws, at, nbytes = c.workspace(workspace, need if any(w) else 0)
+    c.done("sched_norm_rotate_grad", ctypes.byref(d), *map(ctypes.byref, h), *w, at, nbytes)
+    return d_q, d_k, d_q_weight, d_k_weight
+
+
+def sched_beam_select(logits, scores, beams: int, width: Optional[int] = None, last=None,
+                      end_token: int = -1, temperature: float = 1.0, stay: bool = False,
+                      new_scores=None, parents=None, tokens=None, workspace=None,
+                      stream=None) -> Tuple:
+    """(new_scores, parents, tokens) of the `width` (default: beams) best
+    continuations of each group of `beams` rows: float32, int32 row of the
+    parent, and int64 (or as `tokens` is).  `last` has the beams' last tokens; a
+    beam that ends in end_token is finished.  stay: a beam's best continuation
+    keeps its slot; otherwise results are ordered by score."""
+    c = _Call("sched_beam_select", logits, stream)
+    m = c.matrix(logits)
+    width = beams if width is None else width
+    if beams < 1 or width < 1 or m.rows % beams:
+        _refuse(-2, c.where + ": a row per beam")
+    groups = m.rows // beams
+    n = groups * width
+    if new_scores is None:
+        new_scores = c.new((n,), _F32)
+    if parents is None:
+        parents = c.new((n,), _INT32)
+    if tokens is None:
+        tokens = c.new((n,), _INT64)
+    t = c.tokens(tokens)
+    if t.n != n:
+        _refuse(-2, f"{c.where}: {n} tokens, not {t.n}")
+    d = sched_beam_desc(m, c.vector(scores, _F32, m.rows),
+                        sched_tokens(None, 64, 0) if last is None else c.tokens(last), end_token,
+                        groups, beams, width, int(stay), temperature, c.vector(new_scores, _F32, n),
+                        c.vector(parents, _INT32, n), t.data, t.bits)
+    need = c.bytes("sched_beam_workspace_bytes", ctypes.byref(d))
+    ws, at, nbytes = c.workspace(workspace, need)
+    c.done("sched_beam_select", ctypes.byref(d), at, nbytes)
+    return new_scores, parents, tokens
+
+
+def sched_beam_reorder(states, parents, beams: int, lengths=None, stream=None):
+    """Slot s of states (outer x slots x rows x ..., a row's elements next to
+    each other) gets the first lengths[p] rows (None: all) of slot p =
+    parents[s] of its group of `beams`, in place; returns states."""
+    c = _Call("sched_beam_reorder", states, stream)
+    c.use(states)
+    if states.dim() < 3:
+        _refuse(-2, c.where + ": states are outer x slots x rows x ...")
+    size, row = states.element_size(), 1
+    for n, step in zip(reversed(states.shape[3:]), reversed(states.stride()[3:])):
+        if n != 1 and step != row:
+            _refuse(-3, c.where + ": the elements of a row are next to each other")
+        row *= n
+    outer, slots, rows = states.shape[:3]
+    a, b, e = (x * size for x in states.stride()[:3])
+    d = sched_states(states.data_ptr(), outer, slots, rows, row * size, a, b, e)
+    c.done("sched_beam_reorder", ctypes.byref(d), c.vector(parents, _INT32, slots),
+           None if lengths is None else c.vector(lengths, _INT32, slots), beams)
+    return states

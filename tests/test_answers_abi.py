@@ -1,0 +1,168 @@
+"""The C ABI of the operators that serve many answers to one prompt, on the
+host: what is refused before any device work."""
+import ctypes
+import math
+
+import pytest
+
+import paper_2607_22242_amd as S
+from paper_2607_22242_amd import binding as B
+from paper_2607_22242_amd import policy as P
+
+NULL, SIZE, VALUE, WORKSPACE = -1, -2, -3, -8
+FAKE = 1 << 20  # never dereferenced: every call here is refused first
+R = ctypes.byref
+
+
+@pytest.fixture(scope="module")
+def lib():
+    L = B.lib()
+    for name, args in P._ARGS.items():
+        fn = getattr(L, name)
+        fn.restype, fn.argtypes = ctypes.c_int, args
+    return L
+
+
+def heads(data=FAKE, row=128, head=32):
+    return P.sched_heads(data, row, head)
+
+
+def tokens(n=6, bits=64, data=FAKE):
+    return P.sched_tokens(data, bits, n)
+
+
+def rotate(**kw):
+    a = dict(q=heads(), k=heads(FAKE * 2), v=heads(FAKE * 3), q_out=heads(FAKE * 4), k_out=heads(FAKE * 5),
+             v_out=heads(FAKE * 6), dtype=2, head_dim=32, q_heads=4, kv_heads=2, rows=6, out_rows=6,
+             positions=tokens(), places=tokens(0, data=0), q_weight=FAKE, k_weight=FAKE, frequencies=FAKE,
+             turned=32, interleaved=0, norm=1, eps=1e-6)
+    a.update(kw)
+    return P.sched_norm_rotate_desc(*a.values())
+
+
+BAD_ROTATE = [
+    (SIZE, dict(head_dim=0)), (SIZE, dict(head_dim=264)), (SIZE, dict(head_dim=20)), (SIZE, dict(q_heads=0)),
+    (SIZE, dict(kv_heads=0)), (SIZE, dict(q_heads=(1 << 16) + 1)), (SIZE, dict(rows=-1)), (SIZE, dict(rows=1 << 31)),
+    (SIZE, dict(rows=7)), (SIZE, dict(out_rows=7)), (SIZE, dict(out_rows=-1)), (SIZE, dict(turned=34)),
+    (SIZE, dict(turned=31)), (SIZE, dict(turned=-2)), (SIZE, dict(positions=tokens(5))),
+    (SIZE, dict(places=tokens(5))), (VALUE, dict(dtype=3)), (VALUE, dict(norm=2)), (VALUE, dict(norm=-1)),
+    (VALUE, dict(interleaved=2)), (VALUE, dict(eps=-1e-6)), (VALUE, dict(eps=math.nan)), (VALUE, dict(eps=math.inf)),
+    (VALUE, dict(norm=0)),                      # weights of no norm
+    (VALUE, dict(positions=tokens(bits=16))), (VALUE, dict(places=tokens(bits=8))),
+    (VALUE, dict(q=heads(FAKE + 8))), (VALUE, dict(k=heads(FAKE, 132))), (VALUE, dict(q=heads(FAKE, -128))),
+    (NULL, dict(q=heads(0))), (NULL, dict(k=heads(0))), (NULL, dict(frequencies=0)),
+    (NULL, dict(positions=tokens(data=0)))]
+
+
+def test_norm_rotate(lib):
+    rc = lambda **kw: lib.sched_norm_rotate(R(rotate(**kw)), 0)  # noqa: E731
+    assert lib.sched_norm_rotate(None, 0) == NULL
+    for code, bad in BAD_ROTATE:
+        assert rc(**bad) == code, bad
+    for name in ("q_out", "k_out", "v_out"):
+        assert rc(**{name: heads(0)}) == NULL
+        assert rc(**{name: heads(FAKE * 4, 128, 24)}) == VALUE, name    # heads that overlap
+        assert rc(**{name: heads(FAKE * 4, 24, 32)}) == VALUE, name
+    assert rc(v=heads(FAKE + 2)) == VALUE
+    # In place is the same rows and heads, and has no places.
+    assert rc(q_out=heads(FAKE, 256)) == VALUE
+    assert rc(k_out=heads(FAKE * 2, 64)) == VALUE
+    assert rc(k_out=heads(FAKE * 2), places=tokens(), out_rows=9) == VALUE
+    assert rc(v_out=heads(FAKE * 3), places=tokens(), out_rows=9) == VALUE
+    # Nothing to do is no error, and starts nothing.
+    assert rc(rows=0, out_rows=0, positions=tokens(0, data=0), q=heads(0), k=heads(0), v=heads(0),
+              q_out=heads(0), k_out=heads(0)) == 0
+
+
+def test_norm_rotate_grad(lib):
+    need = ctypes.c_size_t()
+    assert lib.sched_norm_rotate_grad_workspace_bytes(R(rotate()), None) == NULL
+    assert lib.sched_norm_rotate_grad_workspace_bytes(R(rotate(head_dim=12)), R(need)) == SIZE
+    assert lib.sched_norm_rotate_grad_workspace_bytes(R(rotate()), R(need)) == 0
+    assert need.value >= 2 * 32 * 4
+
+    def rc(d_q_out=None, d_k_out=None, d_q=None, d_k=None, w=FAKE, ws=FAKE, size=need.value, **kw):
+        given = [d_q_out or heads(FAKE * 7), d_k_out or heads(FAKE * 8), d_q or heads(FAKE * 9),
+                 d_k or heads(FAKE * 10)]
+        return lib.sched_norm_rotate_grad(R(rotate(**kw)), *map(R, given), w, w, ws, size, 0)
+    for code, bad in BAD_ROTATE:
+        assert rc(**bad) == code, bad
+    for name in ("d_q_out", "d_k_out", "d_q", "d_k"):
+        assert rc(**{name: heads(0)}) == NULL
+        assert rc(**{name: heads(FAKE + 4)}) == VALUE
+    assert rc(d_q=heads(FAKE, 256)) == VALUE            # q's memory, other rows
+    assert rc(d_q=heads(FAKE * 7, 256)) == VALUE
+    assert rc(d_k=heads(FAKE * 8, 64, 32)) == VALUE
+    assert rc(d_k=heads(FAKE * 8), places=tokens(), out_rows=9) == VALUE
+    assert rc(ws=0) == rc(ws=FAKE + 8) == rc(size=need.value - 1) == WORKSPACE
+    assert rc(norm=0, q_weight=0, k_weight=0) == VALUE  # a weight's gradient without weights
+    assert lib.sched_norm_rotate_grad(R(rotate()), None, R(heads()), R(heads()), R(heads()), 0, 0, 0, 0, 0) == NULL
+
+
+def matrix(rows=12, cols=50, dtype=0, data=FAKE, stride=None):
+    return P.sched_matrix(data, dtype, rows, cols, cols if stride is None else stride)
+
+
+def beam(**kw):
+    a = dict(logits=matrix(), scores=FAKE, last=tokens(12), end_token=3, n_groups=3, beams=4, width=4, stay=1,
+             temperature=1.0, new_scores=FAKE, parents=FAKE, tokens=FAKE, token_bits=64)
+    a.update(kw)
+    return P.sched_beam_desc(*a.values())
+
+
+def test_beam_select(lib):
+    rc = lambda **kw: lib.sched_beam_select(R(beam(**kw)), FAKE, 1 << 30, 0)  # noqa: E731
+    assert lib.sched_beam_select(None, FAKE, 0, 0) == NULL
+    for bad in (dict(beams=0), dict(beams=129, n_groups=0, logits=matrix(0)), dict(width=0), dict(width=129, stay=0),
+                dict(n_groups=-1), dict(n_groups=2), dict(logits=matrix(13)), dict(logits=matrix(12, 0)),
+                dict(logits=matrix(12, (1 << 22) + 1)), dict(last=tokens(11)), dict(width=5),
+                dict(n_groups=1 << 22, beams=1, logits=matrix(1 << 22), width=1, last=tokens(1 << 22))):
+        assert rc(**bad) == SIZE, bad
+    for bad in (dict(stay=2), dict(temperature=0.0), dict(temperature=math.nan), dict(temperature=3e-39),
+                dict(token_bits=16), dict(end_token=-2), dict(end_token=1 << 31, token_bits=32),
+                dict(last=tokens(12, 8)), dict(logits=matrix(dtype=5)), dict(logits=matrix(data=FAKE + 2)),
+                dict(tokens=FAKE + 4)):
+        assert rc(**bad) == VALUE, bad
+    for bad in (dict(logits=matrix(data=0)), dict(scores=0), dict(new_scores=0), dict(parents=0), dict(tokens=0)):
+        assert rc(**bad) == NULL, bad
+    need = ctypes.c_size_t()
+    assert lib.sched_beam_workspace_bytes(None, R(need)) == NULL
+    assert lib.sched_beam_workspace_bytes(R(beam(beams=3)), R(need)) == SIZE
+    long = dict(logits=matrix(12, 40000))
+    assert lib.sched_beam_workspace_bytes(R(beam(**long)), R(need)) == 0 and need.value > 0
+    for ws, size in ((0, need.value), (FAKE + 128, need.value), (FAKE, need.value - 1)):
+        assert lib.sched_beam_select(R(beam(**long)), ws, size, 0) == WORKSPACE
+    assert rc(n_groups=0, logits=matrix(0, data=0), last=tokens(0, data=0), scores=0, new_scores=0, parents=0,
+              tokens=0) == 0
+
+
+def states(**kw):
+    a = dict(data=FAKE, outer=2, slots=8, rows=5, row_bytes=64, outer_stride=8 * 320, slot_stride=320, row_stride=64)
+    a.update(kw)
+    return P.sched_states(*a.values())
+
+
+def test_beam_reorder(lib):
+    rc = lambda beams=4, parents=FAKE, **kw: lib.sched_beam_reorder(R(states(**kw)), parents, 0, beams, 0)  # noqa: E731
+    assert lib.sched_beam_reorder(None, FAKE, 0, 4, 0) == NULL
+    assert rc(data=0) == rc(parents=0) == NULL
+    for bad in (dict(beams=0), dict(beams=129), dict(beams=3), dict(outer=-1), dict(slots=-4), dict(rows=-1),
+                dict(row_bytes=-1), dict(rows=1 << 31), dict(slots=1 << 31), dict(row_bytes=1 << 31)):
+        assert rc(**bad) == SIZE, bad
+    for bad in (dict(row_stride=63), dict(slot_stride=319), dict(outer_stride=2559), dict(row_stride=-64),
+                dict(slot_stride=0), dict(outer_stride=0), dict(outer_stride=1 << 62)):
+        assert rc(**bad) == VALUE, bad
+    for none in (dict(outer=0), dict(slots=0), dict(rows=0), dict(row_bytes=0)):
+        assert rc(parents=0, data=0, **none) == 0, none
+    assert rc(beams=1) == 0  # a beam alone has no other to follow
+
+
+def test_binding_refuses_tensors_of_the_host():
+    torch = pytest.importorskip("torch")
+    x, t = torch.zeros(4, 2, 16), torch.zeros(4, dtype=torch.int64)
+    for call in (lambda: S.sched_norm_rotate(x, x, t, None), lambda: S.sched_beam_select(x[0], x[0, 0], 2),
+                 lambda: S.sched_norm_rotate_grad(x, x, x, x, t, None),
+                 lambda: S.sched_beam_reorder(x, t.int(), 2)):
+        with pytest.raises(S.SchedError) as e:
+            call()
+        assert e.value.name == "SCHED_E_VALUE"
