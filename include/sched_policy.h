@@ -208,6 +208,36 @@ int sched_attention_grad(const sched_attention_desc *desc, const sched_heads *d_
                          const sched_heads *d_q, const sched_heads *d_k, const sched_heads *d_v,
                          void *d_workspace, size_t ws_bytes, void *hip_stream);
 
+/* Attention of groups of sequences that share a prefix.  Sequence b of group g
+ * (sequences group_offsets[g] .. group_offsets[g+1] - 1; the groups cover them)
+ * sees the first prefix_lengths[g] rows (null: all) of prefix_offsets[g] ..
+ * prefix_offsets[g+1] - 1 of the prefix' keys and values, all of them from every
+ * query row, and after them its own as in sched_attention: `own` describes the
+ * sequences, and own.causal = 1 hides own keys behind a query's place only.
+ * prefix_k and prefix_v: prefix_rows x own.kv_heads x head_dim of own's type.  A
+ * prefix key is read, and its gradient summed, once for all rows of its group.
+ * Limits are those of sched_attention, for groups and prefix rows as for
+ * sequences and key rows.  Rows outside the groups are neither read nor written. */
+typedef struct {
+    sched_attention_desc own;
+    sched_heads prefix_k, prefix_v;
+    int64_t prefix_rows;
+    const int32_t *prefix_offsets, *prefix_lengths, *group_offsets;
+    int32_t n_groups;
+} sched_shared_desc;
+int sched_shared_attention_workspace_bytes(const sched_shared_desc *desc, size_t *out);
+int sched_shared_attention(const sched_shared_desc *desc, void *d_workspace, size_t ws_bytes,
+                           void *hip_stream);
+
+/* Its backward pass, from d_out and the forward pass's out and lse (read here).
+ * Key rows of a slot beyond its length, and prefix rows beyond theirs, get zeros. */
+typedef struct {
+    sched_heads d_out, d_q, d_k, d_v, d_prefix_k, d_prefix_v;
+} sched_shared_grads;
+int sched_shared_attention_grad_workspace_bytes(const sched_shared_desc *desc, size_t *out);
+int sched_shared_attention_grad(const sched_shared_desc *desc, const sched_shared_grads *grads,
+                                void *d_workspace, size_t ws_bytes, void *hip_stream);
+
 /* Norms of the heads of queries and keys and their rotation by position, in one
  * pass.  With x a head of row i, p = positions[i] and w the heads' weights:
  *

@@ -19,5 +19,5 @@ from .binding import (  # noqa: F401
 from .policy import (  # noqa: F401
     POLICY_EXPORTED, sched_attention, sched_attention_grad, sched_beam_reorder, sched_beam_select,
     sched_embed, sched_embed_grad, sched_group_advantages, sched_norm_rotate,
-    sched_norm_rotate_grad, sched_policy_loss, sched_preference_loss, sched_token_logprobs,
-    sched_token_logprobs_grad)
+    sched_norm_rotate_grad, sched_policy_loss, sched_preference_loss, sched_shared_attention,
+    sched_shared_attention_grad, sched_token_logprobs, sched_token_logprobs_grad)

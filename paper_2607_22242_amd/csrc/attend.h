@@ -107,15 +107,15 @@ __device__ __forceinline__ Seq sequence(const AttendArgs& a, int b) {
 struct Tile {
   int seq, index;
 };
-__device__ __forceinline__ Tile tile_of(const int32_t* offsets, int n_seqs, int rows, int group,
-                                        int tile, int number) {
+template <class Begin>
+__device__ __forceinline__ Tile tile_of(Begin begin_of, int n_seqs, int number) {
   // The last sequence that begins at or before the number, 64 of them asked at once.
   const int lane = int(threadIdx.x) % kWave;
   int lo = 0, left = n_seqs, base = 0;  // of `left` sequences from lo on
   for (;;) {
     const int step = (left + kWave - 1) / kWave, at = lo + lane * step;
     int begin = 0;
-    if (lane * step < left) begin = offset_at(offsets, at, rows) * group / tile + at;
+    if (lane * step < left) begin = begin_of(at);
     const uint64_t before = __ballot(lane * step < left && begin <= number);
     // The first one counts even where it begins behind the number.
     const int last = before ? 63 - __builtin_clzll(before) : 0;
@@ -125,6 +125,11 @@ __device__ __forceinline__ Tile tile_of(const int32_t* offsets, int n_seqs, int 
     left = uniform(min(step, left - last * step));
   }
   return {lo, number - uniform(base)};
+}
+__device__ __forceinline__ Tile tile_of(const int32_t* offsets, int n_seqs, int rows, int group,
+                                        int tile, int number) {
+  return tile_of([&](int at) { return offset_at(offsets, at, rows) * group / tile + at; }, n_seqs,
+                 number);
 }
 
 // Tiles of up to 64 sequences from the one with most work to the one with least,
@@ -345,12 +350,15 @@ struct KeyTiles {
   int keys, near;
 
   __device__ __forceinline__ KeyTiles(const AttendArgs& a, const Seq& s, int kv)
-      : k(reinterpret_cast<const char*>(head_row<T>(a.k, s.k0, kv))),
-        v(reinterpret_cast<const char*>(head_row<T>(a.v, s.k0, kv))),
-        k_row(a.k.row * 2), v_row(a.v.row * 2), keys(s.keys), near(a.near_k) {
-    const F fill(a.dim);
-    k_lane = fill.bytes(a.k.row);
-    v_lane = fill.bytes(a.v.row);
+      : KeyTiles(a.k, a.v, s.k0, s.keys, a.near_k, a.dim, kv) {}
+  __device__ __forceinline__ KeyTiles(const HeadsView& ks, const HeadsView& vs, int k0, int n_keys,
+                                      int is_near, int dim, int kv)
+      : k(reinterpret_cast<const char*>(head_row<T>(ks, k0, kv))),
+        v(reinterpret_cast<const char*>(head_row<T>(vs, k0, kv))),
+        k_row(ks.row * 2), v_row(vs.row * 2), keys(n_keys), near(is_near) {
+    const F fill(dim);
+    k_lane = fill.bytes(ks.row);
+    v_lane = fill.bytes(vs.row);
   }
   // Rows j0 .. to LDS; those behind the last key repeat it, their probabilities
   // are zero.

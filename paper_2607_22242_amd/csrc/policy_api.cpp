@@ -116,6 +116,30 @@ int check_attention(const sched_attention_desc& d) {
   return SCHED_OK;
 }
 
+int check_shared_sizes(const sched_shared_desc& x) {
+  const sched_attention_desc& d = x.own;
+  if (int e = check_attention_sizes(d)) return e;
+  if (x.n_groups < 0 || x.prefix_rows < 0 || x.prefix_rows > kMostRows) return SCHED_E_SIZE;
+  // Blocks of both kinds are in one grid.
+  const int64_t rows = d.q_rows * (d.q_heads / d.kv_heads);
+  const int64_t q_tiles = rows / 32 * 2 + int64_t(d.n_seqs) + x.n_groups;
+  const int64_t k_tiles = (d.k_rows + x.prefix_rows) / 64 + int64_t(d.n_seqs) + x.n_groups + 16;
+  if (q_tiles * d.kv_heads >= kMostTiles || k_tiles * d.kv_heads >= kMostTiles) return SCHED_E_SIZE;
+  return SCHED_OK;
+}
+int check_shared(const sched_shared_desc& x) {
+  if (int e = check_shared_sizes(x)) return e;
+  if (int e = check_attention(x.own)) return e;
+  const sched_attention_desc& d = x.own;
+  if (int e = check_heads(x.prefix_k, x.prefix_rows, d.kv_heads, d.head_dim, false)) return e;
+  if (int e = check_heads(x.prefix_v, x.prefix_rows, d.kv_heads, d.head_dim, false)) return e;
+  // Offsets are read for empty tensors too.
+  if (x.n_groups > 0 &&
+      (!x.prefix_offsets || !x.group_offsets || !d.q_offsets || !d.k_offsets))
+    return SCHED_E_NULL;
+  return SCHED_OK;
+}
+
 // Where tensors are the same memory they have to be the same rows and heads.
 bool in_step(const sched_heads& a, const sched_heads& b) {
   return a.data != b.data || (a.row_stride == b.row_stride && a.head_stride == b.head_stride);
@@ -303,6 +327,43 @@ int sched_attention_grad(const sched_attention_desc* d, const sched_heads* d_out
   if (int e = check_workspace(d_workspace, ws_bytes, attention_grad_bytes(*d))) return e;
   return done(launch_attention_grad(*d, *d_out, *d_q, *d_k, *d_v, d_workspace,
                                     stream_of(hip_stream)));
+}
+
+int sched_shared_attention_workspace_bytes(const sched_shared_desc* d, size_t* out) {
+  if (!d || !out) return SCHED_E_NULL;
+  if (int e = check_shared_sizes(*d)) return e;
+  *out = shared_bytes(*d);
+  return SCHED_OK;
+}
+
+int sched_shared_attention(const sched_shared_desc* d, void* d_workspace, size_t ws_bytes,
+                           void* hip_stream) {
+  if (!d) return SCHED_E_NULL;
+  if (int e = check_shared(*d)) return e;
+  if (int e = check_workspace(d_workspace, ws_bytes, shared_bytes(*d))) return e;
+  return done(launch_shared(*d, d_workspace, stream_of(hip_stream)));
+}
+
+int sched_shared_attention_grad_workspace_bytes(const sched_shared_desc* d, size_t* out) {
+  if (!d || !out) return SCHED_E_NULL;
+  if (int e = check_shared_sizes(*d)) return e;
+  *out = shared_grad_bytes(*d);
+  return SCHED_OK;
+}
+
+int sched_shared_attention_grad(const sched_shared_desc* x, const sched_shared_grads* g,
+                                void* d_workspace, size_t ws_bytes, void* hip_stream) {
+  if (!x || !g) return SCHED_E_NULL;
+  if (int e = check_shared(*x)) return e;
+  const sched_attention_desc& d = x->own;
+  if (int e = check_heads(g->d_out, d.q_rows, d.q_heads, d.head_dim, false)) return e;
+  if (int e = check_heads(g->d_q, d.q_rows, d.q_heads, d.head_dim, true)) return e;
+  if (int e = check_heads(g->d_k, d.k_rows, d.kv_heads, d.head_dim, true)) return e;
+  if (int e = check_heads(g->d_v, d.k_rows, d.kv_heads, d.head_dim, true)) return e;
+  if (int e = check_heads(g->d_prefix_k, x->prefix_rows, d.kv_heads, d.head_dim, true)) return e;
+  if (int e = check_heads(g->d_prefix_v, x->prefix_rows, d.kv_heads, d.head_dim, true)) return e;
+  if (int e = check_workspace(d_workspace, ws_bytes, shared_grad_bytes(*x))) return e;
+  return done(launch_shared_grad(*x, *g, d_workspace, stream_of(hip_stream)));
 }
 
 int sched_norm_rotate(const sched_norm_rotate_desc* d, void* hip_stream) {

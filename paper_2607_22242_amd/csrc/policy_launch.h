@@ -41,6 +41,11 @@ size_t attention_grad_bytes(const sched_attention_desc& d);
 hipError_t launch_attention_grad(const sched_attention_desc& d, const sched_heads& d_out,
                                  const sched_heads& d_q, const sched_heads& d_k,
                                  const sched_heads& d_v, void* ws, hipStream_t s);
+size_t shared_bytes(const sched_shared_desc& d);
+hipError_t launch_shared(const sched_shared_desc& d, void* ws, hipStream_t s);
+size_t shared_grad_bytes(const sched_shared_desc& d);
+hipError_t launch_shared_grad(const sched_shared_desc& d, const sched_shared_grads& g, void* ws,
+                              hipStream_t s);
 hipError_t launch_norm_rotate(const sched_norm_rotate_desc& d, hipStream_t s);
 size_t norm_rotate_grad_bytes(const sched_norm_rotate_desc& d);
 hipError_t launch_norm_rotate_grad(const sched_norm_rotate_desc& d, const sched_heads& d_q_out,

@@ -1,0 +1,409 @@
+// shared_grad.hip -- the backward pass of attention over shared prefixes, which
+// computes the probabilities again from the products and lse.
+//
+// With P = exp(scale Q K^T - lse) and delta = rowsum(dO o O):
+// dV = P^T dO, dP = dO V^T, dS = P o (dP - delta), dQ = scale dS K,
+// dK = scale dS^T Q, over both kinds of keys; a prefix key's sums run over all
+// rows of its group.  One kernel holds query rows and walks over the keys (dQ),
+// one holds keys, of either kind, and walks over the rows (dK, dV): no atomics,
+// every sum has one order.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "attend_shared.h"
+#include "attend_grad_sweep.h"
+#include "policy_launch.h"
+
+namespace policy {
+namespace {
+
+// --- dQ -------------------------------------------------------------------------
+
+template <class T, int D>
+__global__ __launch_bounds__(kThreads, 2) void shared_queries_kernel(SharedArgs s, RowParts p,
+                                                                     int tiles) {
+  __shared__ __attribute__((aligned(16))) T k_even[kTile * D], v_even[kTile * D];
+  __shared__ __attribute__((aligned(16))) T k_odd[kTile * D], v_odd[kTile * D];
+  const AttendArgs& a = s.a;
+  const Work work = work_of(int(blockIdx.x), tiles, a.q_heads / a.group);
+  if (work.tile >= tiles) return;
+  const int lane = int(threadIdx.x) % kWave, part = int(blockIdx.y);
+  const RowsOf<kRowsOfBlock> r(s, work.kv, tiles - 1 - work.tile, 32 * wave_id() + lane % 32);
+  if (!r.there) return;
+  const Seen seen(r.mine);
+  // This block's share of the prefix; the last one has the own keys too.
+  const int share = ((r.g.keys + kTile - 1) / kTile + p.parts - 1) / p.parts * kTile;
+  const int begin = min(part * share, r.g.keys), end = min(begin + share, r.g.keys);
+  const bool with_own = part == p.parts - 1;
+
+  RowSweep<T, D> w;
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) {
+    const int d = 16 * i + 8 * (lane / 32);
+    w.q[i] = piece(head_row<T>(a.q, r.query, r.me.head), d, a.dim, r.on);
+    w.o[i] = piece(head_row<T>(a.d_out, r.query, r.me.head), d, a.dim, r.on);
+  }
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) w.dq[i] = Acc(0.f);
+  // The row's statistics, which the kernel of dK and dV reads too.
+  const int64_t n = int64_t(r.me.head) * a.q_rows + r.query;
+  const T* const out_row = head_row<T>(a.out, r.query, r.me.head);
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) {
+    const auto x = piece(out_row, 16 * i + 8 * (lane / 32), a.dim, r.on);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum += float(x[e]) * float(w.o[i][e]);
+  }
+  w.delta = -(sum + __shfl_xor(sum, 32));
+  const float lse = r.on ? a.lse[n] : -INFINITY;
+  w.lse2 = lse == -INFINITY ? INFINITY : lse * kLog2e;  // powers of rows that see nothing are 0
+  if (lane < 32 && r.on && part == 0) {
+    a.lse2[n] = w.lse2 - kLiftGrad<T>;
+    a.delta[n] = w.delta;
+  }
+  w.up = kShort<T> ? kLargest : 0;
+  w.lse2 -= float(w.up);
+  const float c = a.scale * kLog2e;
+  const Places<D> places;
+  Walk<T, D> walk(s, r.g, work.kv, begin, begin < end ? end : 0, r.first_seq,
+                  with_own ? r.last_seq : r.first_seq - 1, r.last_key);
+  auto add = [&](const Step& t, const T* k_tile, const T* v_tile) {
+    if (seen.any(t)) w.add(k_tile, v_tile, t.key0, seen.keys(t), seen.all(t), c, places);
+  };
+  Step even = walk.next(k_even, v_even), odd;
+  while (even.there) {
+    tiles_barrier();
+    odd = walk.next(k_odd, v_odd);
+    add(even, k_even, v_even);
+    if (!odd.there) break;
+    tiles_barrier();
+    even = walk.next(k_even, v_even);
+    add(odd, k_odd, v_odd);
+  }
+  if (!r.on) return;
+  if (kShort<T>) shift(w.dq, -w.up);
+  if (r.g.keys == 0 && r.mine.hi < r.mine.lo) {  // a row that sees nothing, whatever it holds
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) w.dq[i] = Acc(0.f);
+  }
+  if (p.parts > 1)
+    store_column<float, D>(p.dq + row_part<D>(a, part, r.query, r.me.head), w.dq, D, a.scale);
+  else
+    store_column<T, D>(head_row<T>(a.d_q, r.query, r.me.head), w.dq, a.dim, a.scale);
+}
+
+// Adds the parts of the groups' rows: four elements of a head a thread.
+template <class T, int D>
+__global__ __launch_bounds__(kThreads) void add_shared_rows_kernel(SharedArgs s, RowParts p,
+                                                                   int64_t first) {
+  typedef float Four __attribute__((ext_vector_type(4)));
+  typedef T four __attribute__((ext_vector_type(4)));
+  const AttendArgs& a = s.a;
+  const int64_t i = (first + int64_t(blockIdx.x)) * kThreads + int(threadIdx.x);
+  const int d = int(i % (D / 4)) * 4, head = int(i / (D / 4) % a.q_heads);
+  const int64_t row = i / (D / 4) / a.q_heads;
+  if (d >= a.dim || row < first_query(s, 0) || row >= first_query(s, s.n_groups)) return;
+  Four x = Four(0.f);
+  for (int n = 0; n < p.parts; ++n)
+    x += *reinterpret_cast<const Four*>(p.dq + row_part<D>(a, n, row, head) + d);
+  four u;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) u[e] = T(x[e]);
+  *reinterpret_cast<four*>(head_row<T>(a.d_q, row, head) + d) = u;
+}
+
+// --- dK and dV --------------------------------------------------------------------
+
+// Where prefix keys are few a block's rows are shared by `parts` blocks.
+struct PrefixParts {
+  float *dk, *dv;  // parts x kv_heads x prefix rows x D
+  int parts;
+};
+template <int D>
+__device__ __forceinline__ int64_t prefix_part(const SharedArgs& s, int part, int kv, int64_t row) {
+  return ((int64_t(part) * (s.a.q_heads / s.a.group) + kv) * s.p_rows + row) * D;
+}
+
+// A block holds 64 keys; waves 0 and 1 take the even 32 rows of each tile with
+// keys 0 .. 31 and 32 .. 63, waves 2 and 3 the odd 32; their sums meet at the end.
+// The first p_blocks blocks hold prefix keys; the others hold own keys, of one
+// sequence or several.
+template <class T, int D>
+__global__ __launch_bounds__(kThreads, 2) void shared_keys_kernel(SharedArgs s, PrefixParts p,
+                                                                  int p_tiles, int p_blocks,
+                                                                  int tiles) {
+  __shared__ __attribute__((aligned(16))) T q_even[kTile * D], o_even[kTile * D];
+  __shared__ __attribute__((aligned(16))) T q_odd[kTile * D], o_odd[kTile * D];
+  constexpr int kRest = KeySweep<T, D>::kHeld < D / 16 ? kKeysOfBlock * 64 : 8;
+  __shared__ __attribute__((aligned(16))) T v_rest[kRest];
+  __shared__ __attribute__((aligned(16))) Stats s_even, s_odd;
+  const AttendArgs& a = s.a;
+  const int kv_heads = a.q_heads / a.group;
+  const bool prefix = int(blockIdx.x) < p_blocks * p.parts;
+  const int part_of_rows = prefix ? int(blockIdx.x) / p_blocks : 0;
+  const Work work = prefix ? work_of(int(blockIdx.x) % p_blocks, p_tiles, kv_heads)
+                           : work_of(int(blockIdx.x) - p_blocks * p.parts, tiles, kv_heads);
+  if (work.tile >= (prefix ? p_tiles : tiles)) return;
+  const int lane = int(threadIdx.x) % kWave, wave = wave_id();
+  const int kv = work.kv, part = wave / 2 * 32, wave_row = wave % 2 * 32;
+  const HeadsView &ks = prefix ? s.p_k : a.k, &vs = prefix ? s.p_v : a.v;
+
+  // The lane's key (a row of its tensor), the rows that see it, from .. upto of
+  // the block's `rows` rows, which begin at query q0; block_from: none of the
+  // block's keys is seen by a row before it.
+  int key, q0, rows, from, upto, block_from;
+  bool held, on;  // is the row this block's; is it a key in use
+  if (prefix) {
+    const Tile tile = tile_of(s.p_offsets, s.n_groups, s.p_rows, 1, kKeysOfBlock, work.tile);
+    const Group g = group_at(s, tile.seq);
+    const int first = tile.index * kKeysOfBlock, j = first + wave_row + lane % 32;
+    if (tile.index < 0 || first >= g.slot) return;
+    key = g.p0 + j;
+    held = j < g.slot;
+    on = j < g.keys;
+    q0 = g.q0;
+    rows = first < g.keys ? g.queries * a.group : 0;
+    from = block_from = 0;
+    upto = rows - 1;
+  } else {
+    const int first_seq = uniform(first_sequence(s, 0));
+    const int seqs = uniform(first_sequence(s, s.n_groups)) - first_seq;
+    if (seqs <= 0) return;
+    const int behind = uniform(offset_at(a.k_offsets, first_seq + seqs, a.k_rows));
+    const int first =
+        uniform(offset_at(a.k_offsets, first_seq, a.k_rows)) + work.tile * kKeysOfBlock;
+    if (first >= behind) return;
+    const int last = min(first + kKeysOfBlock, behind) - 1;
+    key = first + wave_row + lane % 32;
+    held = key <= last;
+    const int mine = lane_sequence_of(a.k_offsets, a.k_rows, first_seq, seqs, first, last, min(key, last));
+    const Seq q = lane_sequence(a, mine);
+    const Seq head = sequence(a, uniform(lane_sequence_of(a.k_offsets, a.k_rows, first_seq, seqs, first,
+                                                          first, first)));
+    const Seq tail = sequence(a, uniform(lane_sequence_of(a.k_offsets, a.k_rows, first_seq, seqs, last,
+                                                          last, last)));
+    q0 = head.q0;
+    rows = max(0, tail.q0 + tail.queries - q0) * a.group;
+    // The first query that sees key j of a sequence; those behind it if none does.
+    auto seen_from = [&](const Seq& x, int j) {
+      return x.q0 - q0 + (a.causal ? min(max(0, j - (x.keys - x.queries)), x.queries) : 0);
+    };
+    on = held && key - q.k0 < q.keys;
+    from = on ? seen_from(q, key - q.k0) * a.group : rows;
+    upto = on ? (q.q0 - q0 + q.queries) * a.group - 1 : -1;
+    block_from = seen_from(head, first - head.k0) * a.group;
+  }
+  const float c = a.scale * kLog2e;
+  const Places<D> places;
+  const Rows<T, 64> rest = {v_rest, Places<64>()};
+  KeySweep<T, D> w;
+  {
+    const int64_t row = on ? key : 0;
+    const T *k_row = head_row<T>(ks, row, kv), *v_row = head_row<T>(vs, row, kv);
+    const int h = lane / 32, at = wave_row + lane % 32;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+      w.k[i] = piece(k_row, 16 * i + 8 * h, a.dim, on);
+      const auto v = piece(v_row, 16 * i + 8 * h, a.dim, on);
+      if (i < KeySweep<T, D>::kHeld)
+        w.v[i] = v;
+      else if (part == 0)
+        *reinterpret_cast<typename Frag<T>::type*>(
+            v_rest + at * 64 + ((2 * (i - KeySweep<T, D>::kHeld) + h) ^ turn_of<64>(at)) * 8) = v;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) w.dk[i] = w.dv[i] = Acc(0.f);
+  w.up = kLargest;
+  // Rows that all, or any, of the wave's keys are seen by; keys that are not in use
+  // are masked.
+  const int all_from = wave_most(on ? from : rows), all_upto = wave_least(on ? upto : -1);
+  const int any_from = wave_least(on ? from : rows), any_upto = wave_most(on ? upto : -1);
+  const RowTiles<T, D> tiles_of(a);
+  const Seq base = {q0, 0, 0, 0, 0};
+  // From the last rows to the first: blocks that run side by side read the same
+  // rows at the same time.
+  int begin = block_from / kTile * kTile;
+  int end = block_from < rows ? (rows - 1) / kTile * kTile : -1;
+  if (prefix && p.parts > 1) {  // this block's share of the row tiles
+    const int share = (max(end - begin + kTile, 0) / kTile + p.parts - 1) / p.parts;
+    end -= part_of_rows * share * kTile;
+    begin = max(begin, end - (share - 1) * kTile);
+  }
+  RowTile t = row_tile(a, max(end, 0));
+  auto step = [&](int r0, const T* q_tile, const T* o_tile, const Stats& stats) {
+    const int r = r0 + part;
+    if (r + 31 < any_from || r > any_upto) return;
+    w.add(q_tile, o_tile, stats, rest, wave_row, part, (on ? from : rows) - r0, (on ? upto : -1) - r0,
+          r >= all_from && r + 31 <= all_upto, c, places);
+  };
+  if (end >= begin) tiles_of.fetch(a, base, kv, rows, t, q_even, o_even, &s_even);
+  for (int r0 = end; r0 >= begin; r0 -= 2 * kTile) {
+    tiles_barrier();  // the tile is there, and nobody reads the other buffer any more
+    retreat(a, t);
+    if (t.r0 >= begin) tiles_of.fetch(a, base, kv, rows, t, q_odd, o_odd, &s_odd);
+    step(r0, q_even, o_even, s_even);
+    if (r0 - kTile < begin) break;
+    tiles_barrier();
+    retreat(a, t);
+    if (t.r0 >= begin) tiles_of.fetch(a, base, kv, rows, t, q_even, o_even, &s_even);
+    step(r0 - kTile, q_odd, o_odd, s_odd);
+  }
+  // Waves 2 and 3 hand their sums to waves 0 and 1.
+  static_assert(sizeof(q_even) == size_t(D) / 32 * 16 * kWave * sizeof(float), "a wave's sums");
+  float* const buf_k = reinterpret_cast<float*>(wave % 2 ? q_odd : q_even);
+  float* const buf_v = reinterpret_cast<float*>(wave % 2 ? o_odd : o_even);
+  tiles_barrier();
+  if (kShort<T>) {
+    shift(w.dk, -w.up - int(kLiftGrad<T>));
+    shift(w.dv, -int(kLiftGrad<T>));
+  }
+  if (wave >= 2) w.hand(buf_k, buf_v);
+  tiles_barrier();
+  if (wave >= 2 || !held) return;
+  w.take(buf_k, buf_v);
+  if (!on) {  // also where a row that was NaN has met the tile's zeros
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) w.dk[i] = w.dv[i] = Acc(0.f);
+  }
+  if (prefix && p.parts > 1) {
+    const int64_t at = prefix_part<D>(s, part_of_rows, kv, key);
+    store_column<float, D>(p.dk + at, w.dk, D, a.scale);
+    store_column<float, D>(p.dv + at, w.dv, D, 1.f);
+    return;
+  }
+  store_column<T, D>(head_row<T>(prefix ? s.d_p_k : a.d_k, key, kv), w.dk, a.dim, a.scale);
+  store_column<T, D>(head_row<T>(prefix ? s.d_p_v : a.d_v, key, kv), w.dv, a.dim, 1.f);
+}
+
+// Adds the parts of the prefixes' rows: four elements of a head a thread.
+template <class T, int D>
+__global__ __launch_bounds__(kThreads) void add_prefix_kernel(SharedArgs s, PrefixParts p,
+                                                              int64_t first) {
+  typedef float Four __attribute__((ext_vector_type(4)));
+  typedef T four __attribute__((ext_vector_type(4)));
+  const int64_t i = (first + int64_t(blockIdx.x)) * kThreads + int(threadIdx.x);
+  const int d = int(i % (D / 4)) * 4;
+  const int64_t row = i / (D / 4) % s.p_rows;
+  const int kv = int(i / (D / 4) / s.p_rows);
+  if (kv >= s.a.q_heads / s.a.group || d >= s.a.dim || row < offset_at(s.p_offsets, 0, s.p_rows) ||
+      row >= offset_at(s.p_offsets, s.n_groups, s.p_rows))
+    return;
+  Four x = Four(0.f), y = Four(0.f);
+  for (int n = 0; n < p.parts; ++n) {
+    const int64_t at = prefix_part<D>(s, n, kv, row) + d;
+    x += *reinterpret_cast<const Four*>(p.dk + at);
+    y += *reinterpret_cast<const Four*>(p.dv + at);
+  }
+  four u, v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    u[e] = T(x[e]);
+    v[e] = T(y[e]);
+  }
+  *reinterpret_cast<four*>(head_row<T>(s.d_p_k, row, kv) + d) = u;
+  *reinterpret_cast<four*>(head_row<T>(s.d_p_v, row, kv) + d) = v;
+}
+
+// --- launches -----------------------------------------------------------------------
+
+struct Plan {
+  int row_parts, prefix_parts;
+  size_t stats, row_values, prefix_values;  // bytes; values of dQ, and of dK or dV
+};
+
+Plan plan_of(const sched_shared_desc& x) {
+  const sched_attention_desc& d = x.own;
+  Plan p = {1, 1, 0, 0, 0};
+  if (x.n_groups == 0) return p;
+  const size_t width = d.head_dim > 64 ? 128 : 64;
+  const int64_t rows = d.q_rows * (d.q_heads / d.kv_heads);
+  p.stats = (size_t(d.q_rows) * size_t(d.q_heads) * 8 + 255) & ~size_t(255);
+  // As many parts as fill the 512 places that the card has for a kernel's blocks,
+  // none with less than 12 tiles of keys or 8 of rows of a mean group.
+  if (rows > 0) {
+    const int64_t blocks = tile_count(rows, x.n_groups, kRowsOfBlock) * d.kv_heads;
+    p.row_parts = int(std::max<int64_t>(
+        1, std::min(512 / blocks, x.prefix_rows / x.n_groups / (12 * kTile))));
+    if (p.row_parts > 1)
+      p.row_values = size_t(p.row_parts) * size_t(d.q_rows) * size_t(d.q_heads) * width;
+  }
+  if (x.prefix_rows > 0) {
+    const int64_t blocks = tile_count(x.prefix_rows, x.n_groups, kKeysOfBlock) * d.kv_heads;
+    p.prefix_parts =
+        int(std::max<int64_t>(1, std::min(512 / blocks, rows / x.n_groups / (8 * kTile))));
+    if (p.prefix_parts > 1)
+      p.prefix_values = size_t(p.prefix_parts) * size_t(x.prefix_rows) * size_t(d.kv_heads) * width;
+  }
+  return p;
+}
+
+template <class T, int D>
+hipError_t shared_grad(const SharedArgs& s, const Plan& n, float* parts, hipStream_t stream) {
+  const int kv_heads = s.a.q_heads / s.a.group;
+  hipError_t e = hipSuccess;
+  if (s.a.q_rows > 0 && s.a.n_seqs > 0) {  // first: it leaves the rows' statistics
+    const RowParts r = {parts, n.row_parts};
+    const int64_t tiles = tile_count(int64_t(s.a.q_rows) * s.a.group, s.n_groups, kRowsOfBlock);
+    const dim3 grid(unsigned(work_blocks(tiles, kv_heads)), unsigned(r.parts));
+    hipLaunchKernelGGL((shared_queries_kernel<T, D>), grid, dim3(kThreads), 0, stream, s, r,
+                       int(tiles));
+    e = hipGetLastError();
+    const int64_t adds = (int64_t(s.a.q_rows) * s.a.q_heads * (D / 4) + kThreads - 1) / kThreads;
+    for (int64_t b = 0; r.parts > 1 && b < adds && e == hipSuccess; b += kMostBlocks) {
+      hipLaunchKernelGGL((add_shared_rows_kernel<T, D>), dim3(unsigned(std::min(adds - b, kMostBlocks))),
+                         dim3(kThreads), 0, stream, s, r, b);
+      e = hipGetLastError();
+    }
+    if (e != hipSuccess) return e;
+  }
+  const PrefixParts p = {parts, parts + n.prefix_values, n.prefix_parts};
+  const int64_t p_tiles = s.p_rows > 0 ? tile_count(s.p_rows, s.n_groups, kKeysOfBlock) : 0;
+  const int64_t o_tiles = s.a.n_seqs > 0 ? (int64_t(s.a.k_rows) + kKeysOfBlock - 1) / kKeysOfBlock : 0;
+  const int64_t p_blocks = work_blocks(p_tiles, kv_heads), o_blocks = work_blocks(o_tiles, kv_heads);
+  if (p_blocks + o_blocks == 0) return hipSuccess;
+  hipLaunchKernelGGL((shared_keys_kernel<T, D>), dim3(unsigned(p_blocks * p.parts + o_blocks)),
+                     dim3(kThreads), 0, stream, s, p, int(p_tiles), int(p_blocks), int(o_tiles));
+  e = hipGetLastError();
+  const int64_t adds = (int64_t(s.p_rows) * kv_heads * (D / 4) + kThreads - 1) / kThreads;
+  for (int64_t b = 0; p.parts > 1 && b < adds && e == hipSuccess; b += kMostBlocks) {
+    hipLaunchKernelGGL((add_prefix_kernel<T, D>), dim3(unsigned(std::min(adds - b, kMostBlocks))),
+                       dim3(kThreads), 0, stream, s, p, b);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+}  // namespace
+
+size_t shared_grad_bytes(const sched_shared_desc& x) {
+  const Plan p = plan_of(x);
+  // The parts of dQ have been added when those of dK and dV are written.
+  return p.stats + std::max(p.row_values, 2 * p.prefix_values) * sizeof(float);
+}
+
+hipError_t launch_shared_grad(const sched_shared_desc& x, const sched_shared_grads& g, void* ws,
+                              hipStream_t stream) {
+  if (x.n_groups == 0) return hipSuccess;
+  const Plan p = plan_of(x);
+  SharedArgs s = shared_args(x);
+  s.a.d_out = heads_view(g.d_out);
+  s.a.d_q = heads_view(g.d_q);
+  s.a.d_k = heads_view(g.d_k);
+  s.a.d_v = heads_view(g.d_v);
+  s.d_p_k = heads_view(g.d_prefix_k);
+  s.d_p_v = heads_view(g.d_prefix_v);
+  s.a.lse2 = static_cast<float*>(ws);
+  s.a.delta = s.a.lse2 + size_t(x.own.q_rows) * size_t(x.own.q_heads);
+  s.a.near_q = s.a.near_q && g.d_out.row_stride < (int64_t(1) << 24) &&
+               g.d_out.head_stride < (int64_t(1) << 24);
+  float* const parts = reinterpret_cast<float*>(static_cast<char*>(ws) + p.stats);
+  const bool wide = x.own.head_dim > 64;
+  if (x.own.dtype == SCHED_F16)
+    return wide ? shared_grad<f16, 128>(s, p, parts, stream) : shared_grad<f16, 64>(s, p, parts, stream);
+  return wide ? shared_grad<bf16, 128>(s, p, parts, stream) : shared_grad<bf16, 64>(s, p, parts, stream);
+}
+
+}  // namespace policy

@@ -23,6 +23,8 @@ POLICY_EXPORTED = ["sched_embed", "sched_embed_grad_workspace_bytes", "sched_emb
                    "sched_policy_loss", "sched_preference_loss",
                    "sched_attention_workspace_bytes", "sched_attention",
                    "sched_attention_grad_workspace_bytes", "sched_attention_grad",
+                   "sched_shared_attention_workspace_bytes", "sched_shared_attention",
+                   "sched_shared_attention_grad_workspace_bytes", "sched_shared_attention_grad",
                    "sched_norm_rotate", "sched_norm_rotate_grad_workspace_bytes",
                    "sched_norm_rotate_grad", "sched_beam_workspace_bytes", "sched_beam_select",
                    "sched_beam_reorder"]
@@ -55,6 +57,17 @@ class sched_attention_desc(ctypes.Structure):
                 ("kv_heads", _I32), ("q_rows", _I64), ("k_rows", _I64), ("q_offsets", _P),
                 ("k_offsets", _P), ("k_lengths", _P), ("n_seqs", _I32), ("causal", _I32),
                 ("scale", _F)]
+
+
+class sched_shared_desc(ctypes.Structure):
+    _fields_ = [("own", sched_attention_desc), ("prefix_k", sched_heads),
+                ("prefix_v", sched_heads), ("prefix_rows", _I64), ("prefix_offsets", _P),
+                ("prefix_lengths", _P), ("group_offsets", _P), ("n_groups", _I32)]
+
+
+class sched_shared_grads(ctypes.Structure):
+    _fields_ = [(n, sched_heads) for n in ("d_out", "d_q", "d_k", "d_v", "d_prefix_k",
+                                           "d_prefix_v")]
 
 
 class sched_norm_rotate_desc(ctypes.Structure):
@@ -94,6 +107,10 @@ _ARGS = {
     "sched_attention": [_P, _P, ctypes.c_size_t, _P],
     "sched_attention_grad_workspace_bytes": [_P, _P],
     "sched_attention_grad": [_P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P],
+    "sched_shared_attention_workspace_bytes": [_P, _P],
+    "sched_shared_attention": [_P, _P, ctypes.c_size_t, _P],
+    "sched_shared_attention_grad_workspace_bytes": [_P, _P],
+    "sched_shared_attention_grad": [_P, _P, _P, ctypes.c_size_t, _P],
     "sched_norm_rotate": [_P, _P],
     "sched_norm_rotate_grad_workspace_bytes": [_P, _P],
     "sched_norm_rotate_grad": [_P, _P, _P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P],
@@ -415,6 +432,66 @@ def sched_attention_grad(q, k, v, out, lse, d_out, q_offsets, k_offsets, k_lengt
     ws, at, nbytes = c.workspace(workspace, need)
     c.done("sched_attention_grad", ctypes.byref(d), ctypes.byref(do), ctypes.byref(g[0]),
            ctypes.byref(g[1]), ctypes.byref(g[2]), at, nbytes)
+    return tuple(grads)
+
+
+def _shared_desc(c, q, k, v, prefix_k, prefix_v, out, lse, q_offsets, k_offsets, prefix_offsets,
+                 group_offsets, k_lengths, prefix_lengths, causal, scale):
+    own = _attention_desc(c, q, k, v, out, lse, q_offsets, k_offsets, k_lengths, causal, scale)
+    if prefix_k.dim() != 3 or prefix_k.shape[0] != prefix_v.shape[0]:
+        _refuse(-2, c.where + ": the prefix' keys and values are rows x heads x dim")
+    kv, dim, groups = own.kv_heads, own.head_dim, group_offsets.numel() - 1
+    return sched_shared_desc(
+        own, _heads(c, prefix_k, q.dtype, kv, dim), _heads(c, prefix_v, q.dtype, kv, dim),
+        prefix_k.shape[0], c.vector(prefix_offsets, _INT32, groups + 1),
+        None if prefix_lengths is None else c.vector(prefix_lengths, _INT32, groups),
+        c.vector(group_offsets, _INT32), groups)
+
+
+def sched_shared_attention(q, k, v, prefix_k, prefix_v, q_offsets, k_offsets, prefix_offsets,
+                           group_offsets, k_lengths=None, prefix_lengths=None, causal: bool = True,
+                           scale: Optional[float] = None, out=None, lse=None, workspace=None,
+                           stream=None) -> Tuple:
+    """(out, lse) as sched_attention, where the sequences group_offsets[g] ..
+    group_offsets[g+1] see the prefix rows prefix_offsets[g] ..
+    prefix_offsets[g+1] (the first prefix_lengths[g]) before their own keys."""
+    c = _Call("sched_shared_attention", q, stream)
+    if out is None:
+        out = c.new(tuple(q.shape), q.dtype)
+    if lse is None:
+        lse = c.new((q.shape[1], q.shape[0]) if q.dim() == 3 else (0,), _F32)
+    d = _shared_desc(c, q, k, v, prefix_k, prefix_v, out, lse, q_offsets, k_offsets, prefix_offsets,
+                     group_offsets, k_lengths, prefix_lengths, causal, scale)
+    need = c.bytes("sched_shared_attention_workspace_bytes", ctypes.byref(d))
+    ws, at, nbytes = c.workspace(workspace, need)
+    c.done("sched_shared_attention", ctypes.byref(d), at, nbytes)
+    return out, lse
+
+
+def sched_shared_attention_grad(q, k, v, prefix_k, prefix_v, out, lse, d_out, q_offsets, k_offsets,
+                                prefix_offsets, group_offsets, k_lengths=None, prefix_lengths=None,
+                                causal: bool = True, scale: Optional[float] = None, d_q=None,
+                                d_k=None, d_v=None, d_prefix_k=None, d_prefix_v=None,
+                                workspace=None, stream=None) -> Tuple:
+    """(d_q, d_k, d_v, d_prefix_k, d_prefix_v) from sched_shared_attention's
+    arguments and results and d_out."""
+    c = _Call("sched_shared_attention_grad", q, stream)
+    d = _shared_desc(c, q, k, v, prefix_k, prefix_v, out, lse, q_offsets, k_offsets, prefix_offsets,
+                     group_offsets, k_lengths, prefix_lengths, causal, scale)
+    likes = (q, k, v, prefix_k, prefix_v)
+    grads = []
+    for given, like in zip((d_q, d_k, d_v, d_prefix_k, d_prefix_v), likes):
+        t = c.new(tuple(like.shape), q.dtype) if given is None else given
+        if t.shape[0] != like.shape[0]:
+            _refuse(-2, c.where + ": a gradient has its tensor's rows")
+        grads.append(t)
+    if d_out.shape[0] != q.shape[0]:
+        _refuse(-2, c.where + ": d_out has a row per query")
+    g = sched_shared_grads(*(_heads(c, t, q.dtype, like.shape[1], q.shape[2])
+                             for t, like in zip((d_out, *grads), (q, *likes))))
+    need = c.bytes("sched_shared_attention_grad_workspace_bytes", ctypes.byref(d))
+    ws, at, nbytes = c.workspace(workspace, need)
+    c.done("sched_shared_attention_grad", ctypes.byref(d), ctypes.byref(g), at, nbytes)
     return tuple(grads)
 
 

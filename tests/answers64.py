@@ -5,7 +5,7 @@ import math
 
 import torch
 
-from policy64 import F, TINY, U, f32
+from policy64 import F, LEAST, TINY, U, f32
 
 
 def pairs_of(dim, turned, interleaved):
@@ -121,3 +121,75 @@ def reordered(states, parents, beams, lengths):
             n = states.shape[2] if lengths is None else max(0, int(lengths[p]))
             out[:, s, :n] = states[:, p, :n]
     return out
+
+
+class Shared:
+    """Attention over shared prefixes, sequence by sequence and head by head:
+    results, gradients and the bounds of every one."""
+
+    def __init__(self, q, k, v, pk, pv, q_off, k_off, p_off, groups, k_len, p_len, causal, scale, d_out=None):
+        scale, t = f32(scale), q.dtype
+        u, tiny = U[t], TINY[t]
+        q, k, v, pk, pv = (x.double() for x in (q, k, v, pk, pv))
+        rows, heads, dim = q.shape
+        share = heads // k.shape[1]
+        zeros = torch.zeros_like
+        self.out, self.out_b = zeros(q), zeros(q)
+        self.lse = torch.full((heads, rows), -math.inf, dtype=torch.float64)
+        self.lse_b = torch.zeros((heads, rows), dtype=torch.float64)
+        self.dq, self.dk, self.dv, self.dpk, self.dpv = map(zeros, (q, k, v, pk, pv))
+        self.dq_b, self.dk_b, self.dv_b, self.dpk_b, self.dpv_b = map(zeros, (q, k, v, pk, pv))
+        of = {b: g for g in range(len(groups) - 1) for b in range(groups[g], groups[g + 1])}
+        for b in range(len(q_off) - 1):
+            g = of[b]
+            own = k_off[b + 1] - k_off[b] if k_len is None else k_len[b]
+            pre = p_off[g + 1] - p_off[g] if p_len is None else p_len[g]
+            # Rows that a prefix key's sums run over.
+            all_rows = (q_off[groups[g + 1]] - q_off[groups[g]]) * share
+            rq, rk, rp = slice(q_off[b], q_off[b + 1]), slice(k_off[b], k_off[b] + own), slice(p_off[g], p_off[g] + pre)
+            m, n = rq.stop - rq.start, own + pre
+            if m <= 0 or n <= 0:
+                continue
+            seen = torch.ones((m, n), dtype=torch.bool)
+            if causal:
+                seen[:, pre:] = torch.arange(own)[None] <= torch.arange(m)[:, None] + (own - m)
+            for h in range(heads):
+                j = h // share
+                Q, K, V = q[rq, h], torch.cat([pk[rp, j], k[rk, j]]), torch.cat([pv[rp, j], v[rk, j]])
+                s = (Q @ K.T * scale).masked_fill(~seen, -math.inf)
+                lse = torch.logsumexp(s, 1, keepdim=True)
+                P = torch.where(seen, torch.exp(s - lse), 0.0)
+                P = torch.where(P < LEAST, 0.0, torch.nan_to_num(P))
+                out = P @ V
+                # A score's error: D + 8 roundings of terms of its products, and
+                # those of the exponent and the sum.
+                size = s.nan_to_num(0, 0, 0).abs()
+                ds = F * ((dim + 16) * (Q.abs() @ K.abs().T * scale) + 4 * size + n / 16 + 64)
+                ds = 2 * ds.amax(1, keepdim=True)
+                self.out[rq, h], self.lse[h, rq] = out, lse[:, 0]
+                self.out_b[rq, h] = (u + ds) * (P @ V.abs()) + u * out.abs()
+                self.out_b[rq, h] += tiny * (1 + n * V.abs().amax())
+                self.lse_b[h, rq] = ds[:, 0] + 4 * F * lse[:, 0].nan_to_num(0, 0, 0).abs()
+                if d_out is None:
+                    continue
+                dO = d_out[rq, h].double()
+                dp = 2 * ds + 4 * F * lse.nan_to_num(0, 0, 0).abs()  # probabilities from lse
+                dv = P.T @ dO
+                dv_b = ((P * (u + dp)).T @ dO.abs()) + F * (all_rows + 16) * (P.T @ dO.abs()) + \
+                    tiny * m * dO.abs().amax()
+                dP, delta = dO @ V.T, (dO * out).sum(1, keepdim=True)
+                dS = P * (dP - delta)
+                d_err = (dO.abs() * self.out_b[rq, h]).sum(1, keepdim=True)  # from the rounded out
+                s_err = P * (dp * (dP - delta).abs() + F * (dim + 16) * (dO.abs() @ V.abs().T)
+                             + d_err + F * delta.abs()) + u * dS.abs() + tiny
+                self.dq[rq, h] = dS @ K * scale
+                self.dq_b[rq, h] = (s_err + F * n * dS.abs()) @ K.abs() * scale
+                dk = dS.T @ Q * scale
+                dk_b = (s_err + F * (all_rows + 16) * dS.abs()).T @ Q.abs() * scale
+                for x, part in ((self.dv, dv), (self.dv_b, dv_b), (self.dk, dk), (self.dk_b, dk_b)):
+                    x[rk, j] += part[pre:]
+                for x, part in ((self.dpv, dv), (self.dpv_b, dv_b), (self.dpk, dk), (self.dpk_b, dk_b)):
+                    x[rp, j] += part[:pre]
+        for x, y in ((self.dq_b, self.dq), (self.dk_b, self.dk), (self.dv_b, self.dv), (self.dpk_b, self.dpk),
+                     (self.dpv_b, self.dpv)):
+            x += u * y.abs() + tiny

@@ -157,12 +157,72 @@ def test_beam_reorder(lib):
     assert rc(beams=1) == 0  # a beam alone has no other to follow
 
 
+def shared(own=None, **kw):
+    h, k = P.sched_heads(FAKE, 256, 64), P.sched_heads(FAKE, 128, 64)
+    o = dict(q=h, k=k, v=k, out=h, lse=FAKE, dtype=2, head_dim=64, q_heads=4, kv_heads=2, q_rows=6, k_rows=6,
+             q_offsets=FAKE, k_offsets=FAKE, k_lengths=0, n_seqs=3, causal=1, scale=0.1)
+    o.update(own or {})
+    a = dict(own=P.sched_attention_desc(*o.values()), prefix_k=k, prefix_v=k, prefix_rows=9, prefix_offsets=FAKE,
+             prefix_lengths=0, group_offsets=FAKE, n_groups=2)
+    a.update(kw)
+    return P.sched_shared_desc(*a.values())
+
+
+BAD_SHARED = [
+    (SIZE, dict(own=dict(head_dim=136))), (SIZE, dict(own=dict(q_heads=3))), (SIZE, dict(own=dict(n_seqs=-1))),
+    (SIZE, dict(own=dict(q_rows=1 << 31))), (SIZE, dict(n_groups=-1)), (SIZE, dict(prefix_rows=-1)),
+    (SIZE, dict(prefix_rows=1 << 31)), (SIZE, dict(n_groups=1 << 24)), (SIZE, dict(prefix_rows=(1 << 31) - 1024)),
+    (VALUE, dict(own=dict(dtype=0))), (VALUE, dict(own=dict(scale=-1.0))), (VALUE, dict(own=dict(causal=2))),
+    (VALUE, dict(own=dict(out=P.sched_heads(FAKE, 256, 32)))), (VALUE, dict(prefix_k=P.sched_heads(FAKE + 8, 128, 64))),
+    (VALUE, dict(prefix_v=P.sched_heads(FAKE, 132, 64))), (NULL, dict(prefix_k=P.sched_heads(0, 128, 64))),
+    (NULL, dict(own=dict(q_offsets=0))), (NULL, dict(own=dict(lse=0))), (NULL, dict(prefix_offsets=0)),
+    (NULL, dict(group_offsets=0)), (NULL, dict(own=dict(n_seqs=0, q_rows=0, q_offsets=0)))]
+
+
+def test_shared_attention(lib):
+    assert lib.sched_shared_attention(None, FAKE, 0, 0) == NULL
+    need = ctypes.c_size_t()
+    assert lib.sched_shared_attention_workspace_bytes(R(shared()), None) == NULL
+    for code, bad in BAD_SHARED:
+        assert lib.sched_shared_attention(R(shared(**bad)), FAKE, 1 << 40, 0) == code, bad
+        if code == SIZE:
+            assert lib.sched_shared_attention_workspace_bytes(R(shared(**bad)), R(need)) == SIZE
+    assert lib.sched_shared_attention_workspace_bytes(R(shared()), R(need)) == 0 and need.value > 0
+    for ws, size in ((0, need.value), (FAKE + 8, need.value), (FAKE, need.value - 1)):
+        assert lib.sched_shared_attention(R(shared()), ws, size, 0) == WORKSPACE
+    # Nothing to do is no error, and starts nothing.
+    assert lib.sched_shared_attention(R(shared(n_groups=0, prefix_offsets=0, group_offsets=0)), 0, 0, 0) == 0
+
+
+def test_shared_attention_grad(lib):
+    need = ctypes.c_size_t()
+    assert lib.sched_shared_attention_grad_workspace_bytes(R(shared()), R(need)) == 0 and need.value > 0
+    h, k = P.sched_heads(FAKE, 256, 64), P.sched_heads(FAKE, 128, 64)
+
+    def rc(ws=FAKE, size=1 << 40, desc=None, **kw):
+        g = dict(d_out=h, d_q=h, d_k=k, d_v=k, d_prefix_k=k, d_prefix_v=k)
+        g.update(kw)
+        return lib.sched_shared_attention_grad(R(desc or shared()), R(P.sched_shared_grads(*g.values())), ws, size, 0)
+    for code, bad in BAD_SHARED:
+        assert rc(desc=shared(**bad)) == code, bad
+    for name in ("d_out", "d_q", "d_k", "d_v", "d_prefix_k", "d_prefix_v"):
+        assert rc(**{name: P.sched_heads(0, 256, 64)}) == NULL, name
+        assert rc(**{name: P.sched_heads(FAKE, 256, 60)}) == VALUE, name
+        if name != "d_out":
+            assert rc(**{name: P.sched_heads(FAKE, 256, 32)}) == VALUE, name  # heads that overlap
+    for ws, size in ((0, need.value), (FAKE + 8, need.value), (FAKE, need.value - 1)):
+        assert rc(ws=ws, size=size) == WORKSPACE
+    assert lib.sched_shared_attention_grad(R(shared()), None, FAKE, 1 << 40, 0) == NULL
+
+
 def test_binding_refuses_tensors_of_the_host():
     torch = pytest.importorskip("torch")
     x, t = torch.zeros(4, 2, 16), torch.zeros(4, dtype=torch.int64)
     for call in (lambda: S.sched_norm_rotate(x, x, t, None), lambda: S.sched_beam_select(x[0], x[0, 0], 2),
                  lambda: S.sched_norm_rotate_grad(x, x, x, x, t, None),
-                 lambda: S.sched_beam_reorder(x, t.int(), 2)):
+                 lambda: S.sched_beam_reorder(x, t.int(), 2),
+                 lambda: S.sched_shared_attention(x, x, x, x, x, t, t, t, t),
+                 lambda: S.sched_shared_attention_grad(x, x, x, x, x, x, x, x, t, t, t, t)):
         with pytest.raises(S.SchedError) as e:
             call()
         assert e.value.name == "SCHED_E_VALUE"

@@ -368,6 +368,209 @@ def test_beams_keep_their_states():
                 assert states[0, s, :i + 1].tolist() == states[1, s, :i + 1].tolist() == path
 
 
+# --- shared prefixes -----------------------------------------------------------
+
+HALVES = [torch.float16, torch.bfloat16]
+
+
+def offsets(lengths):
+    at = [0]
+    for x in lengths:
+        at.append(at[-1] + x)
+    return at
+
+
+def check_shared(g, dtype, hq, hk, dim, prefixes, samples, queries, keys=None, slots=None, p_slots=None,
+                 causal=True, scale=None, grad=True, size=1.0):
+    """prefixes: lengths of the groups' prefixes; samples: sequences of each
+    group; queries and keys: of each sequence; slots: rows that caches own."""
+    keys = queries if keys is None else keys
+    own_rows, pre_rows = slots or keys, p_slots or prefixes
+    q_off, k_off, p_off, groups = (offsets(x) for x in (queries, own_rows, pre_rows, samples))
+    q = randn(g, q_off[-1], hq, dim, dtype=dtype) * size
+    k, v = randn(g, k_off[-1], hk, dim, dtype=dtype), randn(g, k_off[-1], hk, dim, dtype=dtype)
+    pk, pv = randn(g, p_off[-1], hk, dim, dtype=dtype), randn(g, p_off[-1], hk, dim, dtype=dtype)
+    for x, off, used in ((k, k_off, keys), (v, k_off, keys), (pk, p_off, prefixes), (pv, p_off, prefixes)):
+        for a, b, n in zip(off, off[1:], used):  # behind a length: anything
+            x[a + n:b] = math.nan if x is k or x is pk else math.inf
+    do = randn(g, q_off[-1], hq, dim, dtype=dtype)
+    k_len, p_len = keys if slots else None, prefixes if p_slots else None
+    want = R.Shared(q, k, v, pk, pv, q_off, k_off, p_off, groups, k_len, p_len, causal,
+                    1 / math.sqrt(dim) if scale is None else scale, do if grad else None)
+    args = [x.cuda() for x in (q, k, v, pk, pv)]
+    where = [i32(x) for x in (q_off, k_off, p_off, groups)]
+    how = dict(k_lengths=None if k_len is None else i32(k_len), causal=causal, scale=scale,
+               prefix_lengths=None if p_len is None else i32(p_len))
+    out, lse = S.sched_shared_attention(*args, *where, **how)
+    close(out, want.out, want.out_b, "out")
+    close(lse, want.lse, want.lse_b, "lse")
+    if not grad:
+        return
+    got = S.sched_shared_attention_grad(*args, out, lse, do.cuda(), *where, **how)
+    for x, name in zip(got, ("dq", "dk", "dv", "dpk", "dpv")):
+        close(x, getattr(want, name), getattr(want, name + "_b"), name)
+    again = S.sched_shared_attention_grad(*args, out, lse, do.cuda(), *where, **how)
+    for a, b in zip(got, again):
+        assert torch.equal(a, b)  # one order of sums
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("hq,hk,dim", [(1, 1, 8), (4, 2, 32), (3, 3, 40), (8, 1, 64), (6, 2, 80), (8, 8, 128), (5, 1, 120)])
+def test_shared_attention(dtype, hq, hk, dim):
+    g = gen(hq * 100 + dim)
+    check_shared(g, dtype, hq, hk, dim, [1], [1], [1])
+    check_shared(g, dtype, hq, hk, dim, [70, 3, 129], [2, 3, 1], [14, 14, 1, 40, 2, 33])
+    check_shared(g, dtype, hq, hk, dim, [64, 5], [4, 2], [3, 0, 65, 1, 64, 130], causal=False)
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+def test_groups_sequences_and_prefixes_without_rows(dtype):
+    g = gen(17)
+    check_shared(g, dtype, 4, 2, 64, [0, 9, 0, 40, 5], [2, 0, 1, 3, 0], [5, 0, 3, 0, 0, 20])
+    check_shared(g, dtype, 2, 2, 32, [0], [3], [0, 0, 4])
+    check_shared(g, dtype, 2, 2, 32, [30, 0], [0, 2], [0, 0])
+    # Own keys fewer or more than queries: rows that see the prefix alone, or nothing.
+    check_shared(g, dtype, 4, 1, 64, [9, 0], [2, 3], [5, 70, 6, 7, 3], [0, 3, 9, 2, 80])
+    check_shared(g, dtype, 4, 1, 64, [9, 0], [2, 3], [5, 70, 6, 7, 3], [0, 3, 0, 2, 80], causal=False)
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("prefixes", [[63], [64], [65], [127, 128], [300]])
+def test_prefixes_that_end_around_a_tile(dtype, prefixes):
+    g = gen(prefixes[0])
+    n = len(prefixes)
+    check_shared(g, dtype, 4, 2, 64, prefixes, [5] * n, [13, 1, 64, 50, 0] * n)
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("hq,hk,dim", [(2, 1, 32), (8, 2, 64), (32, 8, 128), (16, 1, 128)])
+def test_single_tokens_over_caches(dtype, hq, hk, dim):
+    g = gen(hq + dim)
+    for samples in ([1], [3, 1], [20, 0, 9], [70]):
+        n = sum(samples)
+        keys = [(7 * i * i + 3) % 150 for i in range(n)]
+        keys[0] = 0
+        prefixes = [(501 * i + 77) % 900 for i in range(len(samples))]
+        check_shared(g, dtype, hq, hk, dim, prefixes, samples, [1] * n, keys, slots=[150] * n,
+                     p_slots=[900] * len(samples), grad=False)
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+def test_shares_of_long_keys(dtype):
+    """Prefixes and own keys that several blocks share, and their backward pass."""
+    g = gen(91)
+    check_shared(g, dtype, 4, 2, 64, [3000, 1111], [2, 2], [1, 2, 1, 3], [900, 1500, 1, 700], slots=[1500] * 4)
+    check_shared(g, dtype, 2, 1, 128, [5000], [3], [20, 1, 33])
+    check_shared(g, dtype, 8, 1, 64, [700], [2], [300, 200])
+
+
+def test_tokens_behind_a_cache():
+    """Some new tokens of each sequence, more than a wave's rows, over slots."""
+    g = gen(14)
+    check_shared(g, torch.bfloat16, 8, 2, 64, [40, 90, 7], [9, 4, 8], [40] * 21,
+                 [40 + 11 * i % 70 for i in range(21)], slots=[111] * 21, p_slots=[100, 90, 64])
+
+
+def test_many_short_sequences_and_many_empty_ones():
+    g = gen(41)
+    queries = [i % 3 for i in range(300)]
+    check_shared(g, torch.bfloat16, 4, 2, 32, [21, 40], [180, 120], queries)
+    queries = [0] * 170
+    queries[3], queries[101], queries[169] = 5, 9, 2
+    check_shared(g, torch.float16, 4, 2, 32, [21, 40], [100, 70], queries)
+    check_shared(g, torch.bfloat16, 2, 2, 32, [11] * 90, [1] * 90, [i % 4 for i in range(90)])
+
+
+def test_scores_of_any_size():
+    g = gen(19)
+    check_shared(g, torch.bfloat16, 4, 2, 64, [100], [4], [30, 20, 7, 60], size=12.0)
+    check_shared(g, torch.float16, 4, 2, 64, [100], [4], [30, 20, 7, 60], scale=1.0)
+    check_shared(g, torch.float16, 2, 2, 64, [100], [2], [30, 20], scale=1e-4)
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+def test_a_shared_prefix_is_a_repeated_one(dtype):
+    """Against sched_attention of sequences that each hold the prefix: out within
+    two roundings; a prefix key's gradient is the sum over its copies."""
+    g = gen(66)
+    p, n, m, hq, hk, dim = 200, 6, 31, 8, 2, 64
+    x = randn(g, n * m, hq + 2 * hk, dim, dtype=dtype).cuda()
+    pre = randn(g, p, 2 * hk, dim, dtype=dtype).cuda()
+    do = randn(g, n * m, hq, dim, dtype=dtype).cuda()
+    q, k, v = x[:, :hq], x[:, hq:hq + hk], x[:, hq + hk:]
+    q_off, p_off, groups = i32(offsets([m] * n)), i32([0, p]), i32([0, n])
+    args = (q, k, v, pre[:, :hk], pre[:, hk:])
+    out, lse = S.sched_shared_attention(*args, q_off, q_off, p_off, groups)
+    got = S.sched_shared_attention_grad(*args, out, lse, do, q_off, q_off, p_off, groups)
+    whole = torch.cat([torch.cat([pre, x[i * m:(i + 1) * m, hq:]]) for i in range(n)])
+    k_off = i32(offsets([p + m] * n))
+    out2, lse2 = S.sched_attention(q, whole[:, :hk], whole[:, hk:], q_off, k_off)
+    d = S.sched_attention_grad(q, whole[:, :hk], whole[:, hk:], out2, lse2, do, q_off, k_off)
+    u = R.U[dtype]
+    for a, b in ((out, out2), (got[0], d[0])):
+        assert float((a.double() - b.double()).norm() / b.double().norm()) < 2 * u
+    for a, b in ((got[3], d[1]), (got[4], d[2])):
+        b = b.double().view(n, p + m, hk, dim)[:, :p].sum(0)
+        assert float((a.double() - b).norm() / b.norm()) < 2 * u
+    for a, b in ((got[1], d[1]), (got[2], d[2])):
+        b = b.double().view(n, p + m, hk, dim)[:, p:].reshape(n * m, hk, dim)
+        assert float((a.double() - b).norm() / b.norm()) < 2 * u
+
+
+def test_rows_outside_the_groups_stay():
+    """Rows behind the last sequence and prefix, on both paths."""
+    g = gen(23)
+    for lengths, queries in ((None, [3, 5, 4]), ([1, 9, 6], [1, 1, 1])):
+        keys = [9, 9, 9] if lengths else queries
+        q_off, k_off, p_off, groups = offsets(queries), offsets(keys), [0, 20, 33], [0, 2, 3]
+        q = randn(g, q_off[-1] + 7, 4, 32, dtype=torch.bfloat16).cuda()
+        k, v = (randn(g, k_off[-1] + 70, 2, 32, dtype=torch.bfloat16).cuda() for _ in range(2))
+        pk, pv = (randn(g, 33 + 90, 2, 32, dtype=torch.bfloat16).cuda() for _ in range(2))
+        where = [i32(x) for x in (q_off, k_off, p_off, groups)]
+        n = None if lengths is None else i32(lengths)
+        out, lse = torch.full_like(q, 7), torch.full((4, q.shape[0]), 7.0, device="cuda")
+        S.sched_shared_attention(q, k, v, pk, pv, *where, k_lengths=n, out=out, lse=lse)
+        assert bool((out[q_off[-1]:] == 7).all()) and bool((lse[:, q_off[-1]:] == 7).all())
+        assert not bool((out[:q_off[-1]] == 7).all(2).any())
+        grads = [torch.full_like(x, 7) for x in (q, k, v, pk, pv)]
+        S.sched_shared_attention_grad(q, k, v, pk, pv, out, lse, q, *where, k_lengths=n, d_q=grads[0],
+                                      d_k=grads[1], d_v=grads[2], d_prefix_k=grads[3], d_prefix_v=grads[4])
+        for x, end in zip(grads, (q_off[-1], k_off[-1], k_off[-1], 33, 33)):
+            assert bool((x[end:] == 7).all()) and not bool((x[:end] == 7).all(2).any())
+
+
+def test_shared_attention_grad_against_differences():
+    """Along random directions, in 64 bits, at a size that bf16 holds exactly."""
+    g = gen(5)
+    q_off, p_off, groups, do = [0, 6, 10], [0, 9], [0, 2], randn(g, 10, 2, 16, dtype=torch.bfloat16)
+    x = [randn(g, n, h, 16, dtype=torch.bfloat16) for n, h in ((10, 2), (10, 1), (10, 1), (9, 1), (9, 1))]
+    step = [randn(g, *t.shape) for t in x]
+    d = [t.cuda() for t in x]
+    where = [i32(t) for t in (q_off, q_off, p_off, groups)]
+    out, lse = S.sched_shared_attention(*d, *where)
+    got = S.sched_shared_attention_grad(*d, out, lse, do.cuda(), *where)
+
+    def loss(h):
+        y = [t.double() + h * s for t, s in zip(x, step)]
+        total = 0.0
+        for b in range(2):
+            r = slice(q_off[b], q_off[b + 1])
+            m = r.stop - r.start
+            for head in range(2):
+                k, v = torch.cat([y[3][:, 0], y[1][r, 0]]), torch.cat([y[4][:, 0], y[2][r, 0]])
+                a = y[0][r, head] @ k.T * R.f32(0.25)
+                a[:, 9:][torch.arange(m)[None] > torch.arange(m)[:, None]] = -math.inf
+                total += float((torch.softmax(a, 1) @ v * do[r, head].double()).sum())
+        return total
+
+    slope = (loss(1e-5) - loss(-1e-5)) / 2e-5
+    parts = [(a.cpu().double() * s).sum() for a, s in zip(got, step)]
+    size = math.sqrt(sum(float((a.cpu().double() * s).square().sum()) for a, s in zip(got, step)))
+    # Every gradient is off by up to three roundings of 2^-8 of itself and of what
+    # cancels in it (of the same size), with random signs: 4 sigma of it.
+    assert abs(slope - float(sum(parts))) < 4 * 3 * 2.0 ** -8 * size
+
+
 # --- streams, graphs, workspaces -------------------------------------------------
 
 
@@ -382,15 +585,23 @@ def test_on_another_stream():
     logits, scores = randn(g, 8, 9001).cuda(), (-torch.rand(8, generator=g)).cuda()
     states = randn(g, 2, 8, 30, 16).cuda()
     x, p, f = randn(g, 50, 4, 32).cuda(), torch.arange(50, device="cuda"), torch.rand(16, generator=g).cuda()
+    h = randn(g, 40, 4, 32, dtype=torch.bfloat16).cuda()
+    where = [i32(t) for t in ([0, 20, 40], [0, 20, 40], [0, 40], [0, 2])]
+
+    def attend(**kw):
+        out, lse = S.sched_shared_attention(h, h, h, h, h, *where, **kw)
+        return (out, lse, *S.sched_shared_attention_grad(h, h, h, h, h, out, lse, h, *where, **kw))
+
     here = states.clone()
-    want = beam_step(logits, scores, here), S.sched_norm_rotate(x, x, p, f)
+    want = beam_step(logits, scores, here), S.sched_norm_rotate(x, x, p, f), attend()
     stream = torch.cuda.Stream()
     stream.wait_stream(torch.cuda.current_stream())
     there = states.clone()
     stream.wait_stream(torch.cuda.current_stream())
-    got = beam_step(logits, scores, there, stream=stream), S.sched_norm_rotate(x, x, p, f, stream=stream)
+    got = (beam_step(logits, scores, there, stream=stream), S.sched_norm_rotate(x, x, p, f, stream=stream),
+           attend(stream=stream))
     torch.cuda.current_stream().wait_stream(stream)
-    for a, b in zip((*want[0], *want[1], here), (*got[0], *got[1], there)):
+    for a, b in zip((*want[0], *want[1], *want[2], here), (*got[0], *got[1], *got[2], there)):
         assert torch.equal(a, b)
 
 
@@ -401,11 +612,18 @@ def test_captured_in_a_graph():
               randn(g, 20, 6, 32).cuda()) for _ in range(4)]
     logits, scores, states, x = (t.clone() for t in draws[0])
     pos, f, w = torch.arange(20, device="cuda"), torch.rand(16, generator=g).cuda(), torch.ones(32, device="cuda")
+    where = [i32(t) for t in ([0, 8, 20], [0, 8, 20], [0, 20], [0, 2])]
+    lengths = i32([8, 5])
 
     def run(logits, scores, states, x):
         out = beam_step(logits, scores, states)
         q, k = S.sched_norm_rotate(x[:, :4], x[:, 4:], pos, f, w, w)
-        return (*out, q, k, *S.sched_norm_rotate_grad(x[:, :4], x[:, 4:], q, k, pos, f, w, w))
+        h, v = x[:, 4:].bfloat16(), q.bfloat16()
+        attended = []
+        for n in (None, lengths):  # packed, and single tokens' way
+            o, lse = S.sched_shared_attention(v, h, h, h, h, *where, k_lengths=n)
+            attended += [o, lse, *S.sched_shared_attention_grad(v, h, h, h, h, o, lse, v, *where, k_lengths=n)]
+        return (*out, q, k, *attended, *S.sched_norm_rotate_grad(x[:, :4], x[:, 4:], q, k, pos, f, w, w))
 
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
