@@ -9,6 +9,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "policy_launch.h"
 #include "tensors.h"
@@ -22,7 +23,6 @@ constexpr int kMostWidth = 128;
 constexpr int kRounds = 4;                        // of a chunk: eight logits a lane each
 constexpr int kChunk = kRounds * 8 * kWave;       // logits of a chunk
 constexpr int kMostStrips = 64;                   // of a row
-constexpr int kRoom = 10 * kMostWidth;            // of a wave's list
 constexpr uint32_t kLeast = 0x00800000u;          // the order of the lowest finite logit
 constexpr int kTokenBits = 22;                    // a row has up to 2^22 logits
 
@@ -46,10 +46,19 @@ __device__ __forceinline__ double of_order(uint64_t k) {
       (long long)(k >> 63 ? k & ~(uint64_t(1) << 63) : ~k));
 }
 
+// Lanes of the mask before this one.
 __device__ __forceinline__ int lanes_before(uint64_t mask) {
-  const int lane = int(threadIdx.x) % kWave;
-  return __popcll(mask & ((uint64_t(1) << lane) - 1));
+  return __builtin_amdgcn_mbcnt_hi(uint32_t(mask >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(mask), 0));
 }
+// The lowest bit in which the orders of a type's numbers differ by more than their
+// sign: 16-bit numbers have fewer digits.
+template <class T>
+constexpr int kLowest = sizeof(T) == 4 ? 0 : std::is_same<T, bf16>::value ? 16 : 13;
+template <class T>
+__device__ __forceinline__ uint32_t with_low_bits(uint32_t order) {
+  return order >> 31 ? order : order | ((1u << kLowest<T>) - 1);
+}
+
 // What a wave's lanes have written to LDS is read by its other lanes from here on.
 __device__ __forceinline__ void wave_order() {
   __builtin_amdgcn_wave_barrier();
@@ -60,8 +69,11 @@ struct Entry {
   uint32_t order, token;
 };
 
-// A wave's list of candidates in LDS.  cut() leaves the k best (greater orders,
-// of equal ones lower tokens), in no order.
+// A wave's list of candidates in LDS, of as many as it can come to (room_of).
+// cut() leaves the k best (greater orders, of equal ones lower tokens), in no order.
+__host__ __device__ inline int reach_of(int k) { return k + (k < 48 ? k : 48); }
+__host__ __device__ inline int room_of(int k) { return 8 * reach_of(k) + k + 2 * kWave; }
+template <class T>
 struct List {
   Entry* at;
   int n;           // entries
@@ -77,28 +89,39 @@ struct List {
 
   __device__ __forceinline__ void cut(int k) {
     if (n <= k) return;
-    constexpr int kHeld = kRoom / kWave;
-    const int lane = int(threadIdx.x) % kWave;
     wave_order();
-    Entry e[kHeld];
+    const int lane = int(threadIdx.x) % kWave;
+    constexpr int kHeld = 2;  // rounds in registers
+    if (n <= kHeld * kWave) {
+      Entry e[kHeld];
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i) {
-      e[i] = {0, ~0u};
-      if (i * kWave + lane < n) e[i] = at[i * kWave + lane];
+      for (int i = 0; i < kHeld; ++i) {
+        e[i] = {0, ~0u};
+        if (i * kWave + lane < n) e[i] = at[i * kWave + lane];
+      }
+      leave(k, kHeld, [&](int i) { return e[i]; });
+    } else {
+      const int rounds = (n + kWave - 1) / kWave;
+      leave(k, rounds, [&](int i) {
+        return i * kWave + lane < n ? at[i * kWave + lane] : Entry{0, ~0u};
+      });
     }
-    const int rounds = (n + kWave - 1) / kWave;
+  }
+
+ private:
+  template <class Get>
+  __device__ __forceinline__ void leave(int k, int rounds, Get get) {
     auto count = [&](auto in) {
       int c = 0;
-#pragma unroll
-      for (int i = 0; i < kHeld; ++i)
-        if (i < rounds) c += __popcll(__ballot(in(e[i])));
+#pragma unroll 2
+      for (int i = 0; i < rounds; ++i) c += __popcll(__ballot(in(get(i))));
       return c;
     };
     // The greatest order that k entries have or pass, bit by bit.
     uint32_t v = 0;
     int reach = n;
 #pragma unroll 1
-    for (int bit = 31; bit >= 0 && reach != k; --bit) {
+    for (int bit = 31; bit >= kLowest<T> && reach != k; --bit) {
       const uint32_t t = v | 1u << bit;
       const int c = count([&](const Entry& x) { return x.order >= t; });
       if (c >= k) {
@@ -106,6 +129,7 @@ struct List {
         reach = c;
       }
     }
+    if (reach != k) v = with_low_bits<T>(v);  // a logit's order
     // Of those that have it the lowest tokens: the least bound that leaves k.
     uint32_t upto = ~0u;
     if (reach != k) {
@@ -118,14 +142,20 @@ struct List {
       }
       upto = below;
     }
+    // In place: what is written lies before what is read next.
+    const int all = n;
     n = 0;
-    wave_order();
-#pragma unroll
-    for (int i = 0; i < kHeld; ++i)
-      if (i < rounds)
-        add(e[i].order > v || (e[i].order == v && e[i].token <= upto), e[i].order, e[i].token);
-    wave_order();
-    least = v;
+#pragma unroll 2
+    for (int i = 0; i < rounds; ++i) {
+      const int kept = n;
+      n = all;  // what get() looks at
+      const Entry e = get(i);
+      n = kept;
+      wave_order();
+      add(e.order > v || (e.order == v && e.token <= upto), e.order, e.token);
+      wave_order();
+    }
+    least = max(least, v);
   }
 };
 
@@ -133,10 +163,12 @@ struct BeamArgs {
   const char* logits;
   int64_t stride;
   int32_t rows, cols, beams, width, strips, strip_chunks, stay, lists;  // lists: of a row
+  uint32_t per_each;  // ceil(2^32 / candidates of a beam), in 32 bits: quotients of small numbers
   const float* scores;
   Tokens last;
   int64_t end_token;
-  float temperature, factor;  // log2(e) / temperature
+  double per_temperature;     // 1 / temperature
+  float factor;               // log2(e) / temperature
   Entry* entries;             // rows x lists x width; 0 orders fill what is left
   float2* sums;               // rows x strips: largest logit, sum of powers relative to it
   float* new_scores;
@@ -152,27 +184,79 @@ __device__ __forceinline__ bool present(const BeamArgs& a, int64_t row) {
   return fabsf(a.scores[row]) < INFINITY;
 }
 
+// Eight logits a lane of each of a chunk's rounds, as they are in memory; -inf
+// behind the last.
 template <class T>
-__device__ __forceinline__ void eight_logits(const T* row, int64_t at, int64_t end, float (&x)[8]) {
-  if (at + 8 <= end) {
+struct Chunk {
+  typename Vec<T>::type part[kRounds][8 / Vec<T>::kN];
+
+  __device__ __forceinline__ void fetch(const T* row, int64_t at, int64_t end) {
+    const int64_t mine = at + 8 * (int(threadIdx.x) % kWave);
+    if (at + kChunk <= end) {
 #pragma unroll
-    for (int i = 0; i < 8; i += Vec<T>::kN) {
-      const auto v = load16(row + at + i);
+      for (int r = 0; r < kRounds; ++r)
 #pragma unroll
-      for (int e = 0; e < Vec<T>::kN; ++e) x[i + e] = float(v[e]);
+        for (int i = 0; i < 8 / Vec<T>::kN; ++i)
+          part[r][i] = load16(row + mine + r * 8 * kWave + i * Vec<T>::kN);
+      return;
     }
-  } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = at + e < end ? float(row[at + e]) : -INFINITY;
+    for (int r = 0; r < kRounds; ++r)
+#pragma unroll
+      for (int i = 0; i < 8 / Vec<T>::kN; ++i) {
+        const int64_t first = mine + r * 8 * kWave + i * Vec<T>::kN;
+        if (first + Vec<T>::kN <= end) {
+          part[r][i] = load16(row + first);
+        } else {
+#pragma unroll
+          for (int e = 0; e < Vec<T>::kN; ++e)
+            part[r][i][e] = first + e < end ? row[first + e] : T(-INFINITY);
+        }
+      }
   }
-}
+  __device__ __forceinline__ float at(int r, int e) const {
+    return float(part[r][e / Vec<T>::kN][e % Vec<T>::kN]);
+  }
+};
 
 // --- strips of rows -----------------------------------------------------------
 
+// Adds what is `bound` at least, or passes it and of what is equal to it the first
+// `first`; eights: the greatest of each lane's eight.
+template <class T, bool kFirst>
+__device__ __forceinline__ void add_chunk(List<T>& list, const Chunk<T>& x, const float (&eights)[kRounds],
+                                          float bound, uint32_t token0, int first) {
+  int taken = 0;
+#pragma unroll
+  for (int r = 0; r < kRounds; ++r) {
+    if (!__ballot(eights[r] >= bound)) continue;
+    const uint32_t token = token0 + r * 8 * kWave + 8 * (int(threadIdx.x) % kWave);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float v = x.at(r, e);
+      const bool in = kFirst ? v > bound : v >= bound;
+      if (__ballot(in)) list.add(in, order_of(v), token + e);
+    }
+    if (!kFirst) continue;
+    // The first of those that are equal, in the tokens' order.
+    int nth = taken;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) nth += lanes_before(__ballot(x.at(r, e) == bound));
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float v = x.at(r, e);
+      taken += __popcll(__ballot(v == bound));
+      list.add(v == bound && nth < first, order_of(v), token + e);
+      nth += v == bound;
+    }
+  }
+}
+
 template <class T>
 __global__ __launch_bounds__(kThreads) void strips_kernel(BeamArgs a, int64_t first) {
-  __shared__ Entry lists[kWaves][kRoom];
-  const int lane = int(threadIdx.x) % kWave, wave = int(threadIdx.x) / kWave, k = a.width;
+  extern __shared__ Entry lists[];
+  const int lane = int(threadIdx.x) % kWave, k = a.width, room = room_of(k);
+  const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) / kWave);
   const int64_t unit = first + int64_t(blockIdx.x) * kWaves + wave;
   if (unit >= int64_t(a.rows) * a.strips) return;
   const int64_t row = unit / a.strips;
@@ -181,83 +265,71 @@ __global__ __launch_bounds__(kThreads) void strips_kernel(BeamArgs a, int64_t fi
   const T* const logits = reinterpret_cast<const T*>(a.logits) + row * a.stride;
   const int64_t begin = int64_t(strip) * a.strip_chunks * kChunk;
   const int64_t end = min(begin + int64_t(a.strip_chunks) * kChunk, int64_t(a.cols));
-  List list = {lists[wave], 0, 0};
+  List<T> list = {lists + wave * room, 0, 0};
   float most = -INFINITY, sum = 0.f;  // of this lane's logits
+  Chunk<T> next;
+  next.fetch(logits, begin, end);
   for (int64_t at = begin; at < end; at += kChunk) {
-    float x[kRounds][8];
-#pragma unroll
-    for (int r = 0; r < kRounds; ++r) eight_logits(logits, at + r * 8 * kWave + 8 * lane, end, x[r]);
-    // Powers relative to the largest so far; NaN and +inf end in a sum of NaN.
-    float up = most;
-#pragma unroll
-    for (int r = 0; r < kRounds; ++r)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) up = fmaxf(up, x[r][e]);
-    const float from = up == -INFINITY ? 0.f : up;
-    sum = most == -INFINITY ? sum : sum * pow2((most - from) * a.factor);  // 0, or NaN met before
-#pragma unroll
-    for (int r = 0; r < kRounds; ++r)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) sum += pow2((x[r][e] - from) * a.factor);
-    most = up;
-    // The greatest order of each lane's eight.
-    uint32_t top[kRounds];
+    const Chunk<T> x = next;
+    if (at + kChunk < end) next.fetch(logits, at + kChunk, end);
+    // The greatest of each lane's eights, and of all so far.
+    float eights[kRounds], up = most;
 #pragma unroll
     for (int r = 0; r < kRounds; ++r) {
-      float m = x[r][0];
+      eights[r] = x.at(r, 0);
 #pragma unroll
-      for (int e = 1; e < 8; ++e) m = fmaxf(m, x[r][e]);
-      top[r] = m > -INFINITY ? order_of(m) : 0u;
+      for (int e = 1; e < 8; ++e) eights[r] = fmaxf(eights[r], x.at(r, e));
+      up = fmaxf(up, eights[r]);
     }
-    uint32_t over = max(list.least, kLeast - 1);  // candidates pass it
-    int passing = 0;
+    // Powers relative to it; NaN and +inf end in a sum of NaN.
+    const float from = up == -INFINITY ? 0.f : up;
+    if (__any(up > most))
+      sum = most == -INFINITY ? sum : sum * pow2((most - from) * a.factor);  // 0, or NaN met before
+    float sums[kRounds] = {};
 #pragma unroll
-    for (int r = 0; r < kRounds; ++r) passing += __popcll(__ballot(top[r] > over));
-    if (!passing) continue;
-    if (list.n + 8 * passing > kRoom) list.cut(k);
-    uint32_t equal = 0;  // orders of which the first k are taken too
-    if (passing > k) {
-      // The k-th greatest of the eights' greatest: k logits have its order or
-      // pass it, and less than 8 k pass it.
-      uint32_t v = 0;
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+      for (int r = 0; r < kRounds; ++r) sums[r] += pow2((x.at(r, e) - from) * a.factor);
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) sum += sums[r];
+    most = up;
+    // What is taken: all that may be among the k best.  Where many eights have some, a
+    // bound that k of them reach, and not many more, is found bit by bit; a bound
+    // that more reach however far one looks is a value of many logits, of which the
+    // first k are taken.
+    uint32_t bound = max(list.least, kLeast - 1) + 1;  // what has been met k times does
+    float least = of_order(bound);                     // not count any more
+    int reach = 0;
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) reach += __popcll(__ballot(eights[r] >= least));
+    if (!reach) continue;
+    const int most_reach = reach_of(k);
+    if (reach > most_reach) {
+      uint32_t top[kRounds], v = 0;
+#pragma unroll
+      for (int r = 0; r < kRounds; ++r) top[r] = eights[r] > -INFINITY ? order_of(eights[r]) : 0u;
 #pragma unroll 1
-      for (int bit = 31; bit >= 0; --bit) {
+      for (int bit = 31; bit >= kLowest<T> && reach > most_reach; --bit) {
         const uint32_t t = v | 1u << bit;
         int c = 0;
 #pragma unroll
         for (int r = 0; r < kRounds; ++r) c += __popcll(__ballot(top[r] >= t));
-        if (c >= k) v = t;
+        if (c >= k) {
+          v = t;
+          reach = c;
+        }
       }
-      over = v;
-      equal = v;
-    }
-    int taken = 0;
-#pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
-      if (!__ballot(top[r] > over || (equal && top[r] == equal))) continue;
-      const uint32_t token = uint32_t(at + r * 8 * kWave + 8 * lane);
-      uint32_t order[8];
-      uint64_t same[8];
-      int before = 0;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        order[e] = x[r][e] > -INFINITY ? order_of(x[r][e]) : 0u;
-        list.add(order[e] > over, order[e], token + e);
-        same[e] = __ballot(equal && order[e] == equal);
-        before += lanes_before(same[e]);
-      }
-      if (!equal) continue;
-      // The first of those that are equal, in the tokens' order.
-      int nth = taken + before;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const bool mine = order[e] == equal;
-        list.add(mine && nth < k, order[e], token + e);
-        nth += mine;
-        taken += __popcll(same[e]);
+      if (reach > most_reach) v = with_low_bits<T>(v);
+      if (v >= bound) {
+        bound = v;
+        least = of_order(bound);
+        if (bound > list.least) list.least = bound;  // k logits have it or pass it
       }
     }
-    if (list.n > k && (equal || list.n > 2 * k + kWave)) list.cut(k);
+    if (list.n + 8 * min(reach, most_reach) + k > room) list.cut(k);
+    if (reach > most_reach) add_chunk<T, true>(list, x, eights, least, uint32_t(at), k);
+    else add_chunk<T, false>(list, x, eights, least, uint32_t(at), k);
+    if (list.n > 2 * k + kWave) list.cut(k);
   }
   list.cut(k);
   wave_order();
@@ -271,18 +343,19 @@ __global__ __launch_bounds__(kThreads) void strips_kernel(BeamArgs a, int64_t fi
 // A row's lists become one, where the group's together would be too many: a wave
 // each, in place.
 __global__ __launch_bounds__(kThreads) void join_lists_kernel(BeamArgs a) {
-  __shared__ Entry lists[kWaves][kRoom];
+  extern __shared__ Entry lists[];
   const int lane = int(threadIdx.x) % kWave, wave = int(threadIdx.x) / kWave, k = a.width;
+  const int room = room_of(k);
   const int64_t row = int64_t(blockIdx.x) * kWaves + wave;
   if (row >= a.rows || finished(a, row) || !present(a, row)) return;
-  List list = {lists[wave], 0, 0};
+  List<float> list = {lists + wave * room, 0, 0};
   Entry* const in = a.entries + row * a.strips * k;
   const int n = a.strips * k;
   for (int i = 0; i < n; i += kWave) {
     Entry e = {0, ~0u};
     if (i + lane < n) e = in[i + lane];
     list.add(e.order >= max(list.least, kLeast), e.order, e.token);
-    if (list.n + kWave > kRoom) list.cut(k);
+    if (list.n + kWave > room) list.cut(k);
   }
   list.cut(k);
   wave_order();
@@ -292,8 +365,9 @@ __global__ __launch_bounds__(kThreads) void join_lists_kernel(BeamArgs a) {
 // --- a group's best -------------------------------------------------------------
 
 // Sums over a block of one number per thread's wave: waves count by ballots.
+template <int kCount>
 struct Counter {
-  int (*room)[kWaves];
+  int (*room)[kCount];
   int turn;
   __device__ __forceinline__ int total(int wave_count) {
     const int wave = int(threadIdx.x) / kWave;
@@ -302,127 +376,165 @@ struct Counter {
     __syncthreads();
     int c = 0;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) c += room[turn][w];
+    for (int w = 0; w < kCount; ++w) c += room[turn][w];
     return c;
   }
 };
 
-struct Best {
-  uint64_t score[kMostWidth];
-  uint32_t place[kMostWidth];  // beam and token
-};
+constexpr int kMostRanked = 1024;  // candidates that are ranked one against the other
+enum State : int { kNone, kLive, kFinished };
 
-// A block takes a group.  kSmall: the group's logits themselves (kHeld kThreads at
-// most); else the strips' lists.
-template <class T, int kHeld, bool kSmall>
-__global__ __launch_bounds__(kThreads) void group_kernel(BeamArgs a) {
-  __shared__ double base[kMostWidth];  // of a beam: what is added to logit / temperature
-  __shared__ int counts[2][kWaves], found;
-  __shared__ Best best, sorted;
-  __shared__ int first[kMostWidth], used[kMostWidth];
-  const int group = int(blockIdx.x), t = int(threadIdx.x), lane = t % kWave;
+// A block takes a group.  kSmall: the group's logits themselves (kHeld kBlock at
+// most); else the strips' lists.  A few blocks are all there is, so that what counts
+// is how many loads wait for one another: the candidates are under way first.
+template <class T, int kBlock, int kHeld, bool kSmall>
+__global__ __launch_bounds__(kBlock) void group_kernel(BeamArgs a) {
+  __shared__ double base[kMostWidth];  // of a beam: what is added to logit / temperature, or its score
+  __shared__ int state[kMostWidth], best_rank[kMostWidth], free_slots[kMostWidth];
+  __shared__ int counts[2][kBlock / kWave], found;
+  __shared__ uint32_t bounds[kBlock / kWave];
+  __shared__ uint64_t masks[2][2], best_score[kMostRanked], sorted_score[kMostWidth];
+  __shared__ uint32_t best_place[kMostRanked], sorted_place[kMostWidth];  // beam and token
+  const int group = int(blockIdx.x), t = int(threadIdx.x), lane = t % kWave, wave = t / kWave;
   const int64_t row0 = int64_t(group) * a.beams;
   const int k = a.width;
+  const T* const logits = reinterpret_cast<const T*>(a.logits);
 
-  // Every beam's base: score - log of the sum of powers; NaN where there is none.
+  const int each = kSmall ? a.cols : a.lists * k, n = a.beams * each;
+  auto beam_of = [&](int c) { return a.per_each ? int(__umulhi(uint32_t(c), a.per_each)) : c; };
+  float x[kHeld];
+  uint32_t token[kHeld];
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    const int c = i * kBlock + t, b = beam_of(c), r = c - b * each;
+    x[i] = -INFINITY;
+    token[i] = uint32_t(r);
+    if (c >= n) continue;
+    if (kSmall) {
+      x[i] = float(logits[(row0 + b) * a.stride + r]);
+    } else {  // of a beam without logits: what the memory held, which is not used
+      const Entry e = a.entries[(row0 + b) * a.strips * k + r];
+      x[i] = e.order >= kLeast ? of_order(e.order) : -INFINITY;
+      token[i] = e.token & ((1u << kTokenBits) - 1);
+    }
+  }
+
+  // Every beam's base: score - log of the sum of powers.
   const int per_row = kSmall ? a.cols : a.strips;
   int lanes = 1;
   while (lanes < per_row && lanes < kWave) lanes *= 2;
-  for (int b = t / lanes; b < (a.beams + kThreads / lanes - 1) / (kThreads / lanes) * (kThreads / lanes);
-       b += kThreads / lanes) {
-    const int64_t row = row0 + b;
-    const bool live = b < a.beams && present(a, row) && !finished(a, row);
+  const int at_once = kBlock / lanes;
+  for (int b0 = 0; b0 < a.beams; b0 += at_once) {
+    const int b = b0 + t / lanes;
+    const int64_t row = row0 + min(b, a.beams - 1);
+    const float score = a.scores[row];
+    const bool done = finished(a, row);
     float most = -INFINITY, sum = 0.f;
-    auto power = [&](float x, float from) { return pow2((x - from) * a.factor); };
-    if (live) {
-      for (int i = t % lanes; i < per_row; i += lanes) {
-        float x, s = 1.f;
-        if (kSmall) x = float((reinterpret_cast<const T*>(a.logits) + row * a.stride)[i]);
-        else {
-          const float2 p = a.sums[row * a.strips + i];
-          x = p.x;
-          s = p.y;
-        }
-        if (kSmall ? x == -INFINITY : s == 0.f) continue;
-        const float up = fmaxf(most, x);
-        sum = (most == -INFINITY ? sum : sum * power(most, up)) + s * power(x, up);
-        most = up;
+    auto power = [&](float y, float from) { return pow2((y - from) * a.factor); };
+    for (int i = t % lanes; i < per_row; i += lanes) {
+      float y, s = 1.f;
+      if (kSmall) {
+        y = float(logits[row * a.stride + i]);
+      } else {
+        const float2 p = a.sums[row * a.strips + i];
+        y = p.x;
+        s = p.y;
       }
+      if (kSmall ? y == -INFINITY : s == 0.f) continue;
+      const float up = fmaxf(most, y);
+      sum = (most == -INFINITY ? sum : sum * power(most, up)) + s * power(y, up);
+      most = up;
     }
     for (int d = lanes / 2; d; d >>= 1) {
-      const float x = __shfl_xor(most, d), s = __shfl_xor(sum, d), up = fmaxf(most, x);
+      const float y = __shfl_xor(most, d), s = __shfl_xor(sum, d), up = fmaxf(most, y);
       sum = up == -INFINITY ? sum + s
                             : (most == -INFINITY ? sum : sum * power(most, up)) +
-                                  (x == -INFINITY ? s : s * power(x, up));
+                                  (y == -INFINITY ? s : s * power(y, up));
       most = up;
     }
     if (b < a.beams && t % lanes == 0) {
-      const double none = __longlong_as_double(0x7ff8000000000000LL);
-      const bool ok = live && sum > 0.f && sum < INFINITY && fabsf(most) < INFINITY;
-      base[b] = ok ? double(a.scores[row]) - double(most) / double(a.temperature) - log(double(sum))
-                   : none;
+      const bool there = fabsf(score) < INFINITY;
+      const bool ok = sum > 0.f && sum < INFINITY && fabsf(most) < INFINITY;
+      state[b] = !there ? kNone : done ? kFinished : ok ? kLive : kNone;
+      base[b] = done ? double(score)
+                     : double(score) - double(most) * a.per_temperature - log(double(sum));
     }
   }
   if (t == 0) found = 0;
-  if (t < kMostWidth) {
-    used[t] = 0;
-    best.score[t] = sorted.score[t] = 0;
-  }
+  if (t < kMostWidth) best_rank[t] = kMostWidth;
   __syncthreads();
 
-  // The candidates: score's order and place (beam, then token).
+  // The candidates: score's order (0: none) and place.
   uint64_t score[kHeld];
   uint32_t place[kHeld];
-  const int each = kSmall ? a.cols : a.lists * k, n = a.beams * each;
 #pragma unroll
   for (int i = 0; i < kHeld; ++i) {
-    const int c = i * kThreads + t;
-    score[i] = 0;
-    place[i] = ~0u;
-    if (c >= n) continue;
-    const int b = c / each, r = c % each;
-    const int64_t row = row0 + b;
-    if (finished(a, row)) {  // its one candidate
-      if (r == 0 && present(a, row)) {
-        score[i] = order_of(double(a.scores[row]));
-        place[i] = uint32_t(b) << kTokenBits;
-      }
-      continue;
-    }
-    float x = -INFINITY;
-    uint32_t token = uint32_t(r);
-    if (kSmall) {
-      x = float((reinterpret_cast<const T*>(a.logits) + row * a.stride)[r]);
-    } else if (present(a, row)) {
-      const Entry e = a.entries[row * a.strips * k + r];
-      if (e.order >= kLeast) {
-        x = of_order(e.order);
-        token = e.token;
-      }
-    }
-    const double s = base[b] + double(x) / double(a.temperature);
-    if (s > -INFINITY && s < INFINITY) {
-      score[i] = order_of(s);
-      place[i] = uint32_t(b) << kTokenBits | token;
-    }
+    const int c = i * kBlock + t, b = min(beam_of(c), a.beams - 1);
+    const int is = state[b];
+    const bool alone = is == kFinished;
+    double s = base[b] + (alone ? 0. : double(x[i]) * a.per_temperature);
+    const bool on = c < n && (alone ? c == b * each : is == kLive) && s > -INFINITY && s < INFINITY;
+    score[i] = on ? order_of(s) : 0;
+    place[i] = on ? uint32_t(b) << kTokenBits | (alone ? 0u : token[i]) : ~0u;
   }
 
-  // The k best: the greatest order that k of them have or pass, and of those that
-  // have it the first places.
-  Counter counter = {counts, 0};
-  auto count = [&](auto in) {
+  // What may be among the k best.  Every wave finds a bound that k of its own scores
+  // reach, and not many more, bit by bit; what reaches the greatest of them is ranked
+  // one against the other.
+  Counter<kBlock / kWave> counter = {counts, 0};
+  auto in_wave = [&](auto in) {
     int c = 0;
 #pragma unroll
     for (int i = 0; i < kHeld; ++i)
-      if (i * kThreads < n) c += __popcll(__ballot(in(score[i], place[i])));
-    return counter.total(c);
+      if (i * kBlock < n) c += __popcll(__ballot(in(score[i], place[i])));
+    return c;
   };
-  const int there = count([&](uint64_t s, uint32_t) { return s > 0; });
+  auto count = [&](auto in) { return counter.total(in_wave(in)); };
+  uint32_t least = 0;  // of the order's upper half
+  const int mine = in_wave([&](uint64_t s, uint32_t) { return s > 0; });
+  if (n > 256) {
+    if (mine > 2 * k) {
+      uint32_t hi = 0, lo = ~0u;
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i)
+        if (score[i] > 0) {
+          hi = max(hi, uint32_t(score[i] >> 32));
+          lo = min(lo, uint32_t(score[i] >> 32));
+        }
+#pragma unroll
+      for (int d = 32; d; d >>= 1) {
+        hi = max(hi, uint32_t(__shfl_xor(int(hi), d)));
+        lo = min(lo, uint32_t(__shfl_xor(int(lo), d)));
+      }
+      int bit = 31 - __clz(int(hi ^ lo));  // the bits above are all scores'
+      least = bit < 0 ? hi : hi >> bit >> 1 << bit << 1;
+      int reach = mine;
+#pragma unroll 1
+      for (; bit >= 0 && reach > 2 * k; --bit) {
+        const uint32_t bound = least | 1u << bit;
+        const int c = in_wave([&](uint64_t s, uint32_t) { return uint32_t(s >> 32) >= bound; });
+        if (c >= k) {
+          least = bound;
+          reach = c;
+        }
+      }
+    }
+    if (lane == 0) bounds[wave] = least;
+  }
+  const int there = counter.total(mine);
   uint64_t v = 1;
+  if (n > 256) {
+#pragma unroll
+    for (int w = 0; w < kBlock / kWave; ++w) least = max(least, bounds[w]);
+    v = max(uint64_t(least) << 32, uint64_t(1));
+  }
+  int reach = v == 1 ? there : count([&](uint64_t s, uint32_t) { return s >= v; });
   uint32_t upto = ~0u;
-  if (there > k) {
-    int reach = there;
+  if (reach > kMostRanked) {
+    // Many equal scores, or many results: exactly the k best, by score and place.
     v = 0;
+    reach = there;
+#pragma unroll 1
     for (int bit = 63; bit >= 0 && reach != k; --bit) {
       const uint64_t bound = v | uint64_t(1) << bit;
       const int c = count([&](uint64_t s, uint32_t) { return s >= bound; });
@@ -434,118 +546,138 @@ __global__ __launch_bounds__(kThreads) void group_kernel(BeamArgs a) {
     if (reach != k) {
       const int over = count([&](uint64_t s, uint32_t) { return s > v; });
       uint32_t below = 0;
+#pragma unroll 1
       for (int bit = 31; bit >= 0; --bit) {
         const uint32_t bound = below | 1u << bit;
         if (over + count([&](uint64_t s, uint32_t p) { return s == v && p < bound; }) < k)
           below = bound;
       }
       upto = below;
+      reach = k;
     }
   }
 #pragma unroll
   for (int i = 0; i < kHeld; ++i)
     if (score[i] > v || (score[i] == v && place[i] <= upto)) {
-      const int at = atomicAdd(&found, 1);  // in any order: they are sorted next
-      best.score[at] = score[i];
-      best.place[at] = place[i];
+      const int at = atomicAdd(&found, 1);  // in any order: they are ranked next
+      best_score[at] = score[i];
+      best_place[at] = place[i];
     }
   __syncthreads();
   const int got = min(there, k);
-  if (t < got) {
+  for (int c = t; c < reach; c += kBlock) {
+    const uint64_t s = best_score[c];
+    const uint32_t p = best_place[c];
     int rank = 0;
-    const uint64_t s = best.score[t];
-    const uint32_t p = best.place[t];
-    for (int i = 0; i < got; ++i)
-      rank += best.score[i] > s || (best.score[i] == s && best.place[i] < p);
-    sorted.score[rank] = s;
-    sorted.place[rank] = p;
+#pragma unroll 8
+    for (int i = 0; i < reach; ++i) {
+      const uint64_t other = best_score[i];
+      const uint32_t at = best_place[i];
+      rank += int(other > s) | (int(other == s) & int(at < p));
+    }
+    if (rank < k) {
+      sorted_score[rank] = s;
+      sorted_place[rank] = p;
+    }
   }
   __syncthreads();
 
+  // Rank t's slot.
   int slot = t;
+  const uint32_t at = t < got ? sorted_place[t] : 0;
+  const int beam = int(at >> kTokenBits);
   if (a.stay) {
-    const int beam = t < got ? int(sorted.place[t] >> kTokenBits) : -1;
-    bool mine = t < got;  // the beam's best continuation
-    for (int i = 0; i < min(t, got) && mine; ++i)
-      mine = int(sorted.place[i] >> kTokenBits) != beam;
-    if (mine) used[beam] = 1;
-    if (t < k) first[t] = mine;
+    if (t < got) atomicMin(&best_rank[beam], t);
     __syncthreads();
-    slot = beam;
-    if (t < k && !mine) {
-      int nth = 0;  // of those without a slot
-      for (int i = 0; i < t; ++i) nth += !first[i];
-      slot = 0;
-      for (int free = -1;; ++slot) {
-        free += !used[slot];
-        if (free == nth) break;
+    const bool kept = t < got && best_rank[beam] == t;  // the beam's best continuation
+    const bool moves = t < k && !kept, open = t < k && best_rank[t] == kMostWidth;
+    if (wave < 2) {
+      const uint64_t a0 = __ballot(moves), a1 = __ballot(open);
+      if (lane == 0) {
+        masks[0][wave] = a0;
+        masks[1][wave] = a1;
       }
     }
+    __syncthreads();
+    if (wave < 2) {  // as many ranks move as slots are left
+      auto nth = [&](int which) {
+        return lanes_before(masks[which][wave]) + (wave ? __popcll(masks[which][0]) : 0);
+      };
+      if (open) free_slots[nth(1)] = t;
+      slot = kept ? beam : nth(0);
+    }
+    __syncthreads();
+    if (moves) slot = free_slots[slot];
   }
   if (t >= k) return;
   const int64_t out = int64_t(group) * k + slot;
-  int64_t token = -1;
+  int64_t next = -1;
   int parent = -1;
   float new_score = -INFINITY;
   if (t < got) {
-    const uint32_t p = sorted.place[t];
-    parent = int(row0 + (p >> kTokenBits));
-    token = finished(a, parent) ? a.end_token : int64_t(p & ((1u << kTokenBits) - 1));
-    new_score = float(of_order(sorted.score[t]));
+    parent = int(row0 + beam);
+    next = state[beam] == kFinished ? a.end_token : int64_t(at & ((1u << kTokenBits) - 1));
+    new_score = float(of_order(sorted_score[t]));
   }
   a.new_scores[out] = new_score;
   a.parents[out] = parent;
-  if (a.wide_tokens) static_cast<int64_t*>(a.tokens)[out] = token;
-  else static_cast<int32_t*>(a.tokens)[out] = int32_t(token);
+  if (a.wide_tokens) static_cast<int64_t*>(a.tokens)[out] = next;
+  else static_cast<int32_t*>(a.tokens)[out] = int32_t(next);
 }
 
 struct Plan {
   int strips, strip_chunks, lists;
   bool small;
 };
-constexpr int kMostHeld = 64;  // candidates of a thread
+constexpr int kMostHeld = 16;  // candidates of a thread of 1024
 
 Plan plan_of(const sched_beam_desc& d) {
   Plan p = {};
   const int64_t cols = d.logits.cols, rows = d.logits.rows;
-  p.small = cols <= 4 * kWave && cols * d.beams <= 16 * kThreads;
+  p.small = cols <= 4 * kWave && cols * d.beams <= 4096;
   const int64_t chunks = (cols + kChunk - 1) / kChunk;
   // Some 4096 waves, as far as rows are long enough.
   const int64_t want = std::min<int64_t>(
       {std::max<int64_t>(1, 4096 / std::max<int64_t>(rows, 1)), chunks, int64_t(kMostStrips)});
   p.strip_chunks = int((chunks + want - 1) / want);
   p.strips = int((chunks + p.strip_chunks - 1) / p.strip_chunks);
-  p.lists = int64_t(d.beams) * p.strips * d.width > kMostHeld * kThreads ? 1 : p.strips;
+  p.lists = int64_t(d.beams) * p.strips * d.width > kMostHeld * 1024 ? 1 : p.strips;
   return p;
 }
 
-template <class T, int kHeld, bool kSmall>
+template <class T, int kBlock, int kHeld, bool kSmall>
 hipError_t group(const BeamArgs& a, int groups, hipStream_t s) {
-  hipLaunchKernelGGL((group_kernel<T, kHeld, kSmall>), dim3(unsigned(groups)), dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL((group_kernel<T, kBlock, kHeld, kSmall>), dim3(unsigned(groups)), dim3(kBlock), 0,
+                     s, a);
   return hipGetLastError();
 }
 
 template <class T>
-hipError_t select(const BeamArgs& a, const Plan& p, int groups, hipStream_t s) {
+hipError_t select(BeamArgs a, const Plan& p, int groups, hipStream_t s) {
+  const int64_t each = p.small ? a.cols : a.lists * a.width;
+  a.per_each = uint32_t(((uint64_t(1) << 32) + each - 1) / each);
   if (p.small) {
-    if (a.cols * a.beams <= 4 * kThreads) return group<T, 4, true>(a, groups, s);
-    return group<T, 16, true>(a, groups, s);
+    if (a.cols * a.beams <= 256) return group<T, 256, 1, true>(a, groups, s);
+    if (a.cols * a.beams <= 1024) return group<T, 1024, 1, true>(a, groups, s);
+    return group<T, 1024, 4, true>(a, groups, s);
   }
+  const size_t lists = size_t(kWaves) * room_of(a.width) * sizeof(Entry);
   const int64_t blocks = (int64_t(a.rows) * a.strips + kWaves - 1) / kWaves;
   for (int64_t b = 0; b < blocks; b += kMostBlocks) {
     hipLaunchKernelGGL((strips_kernel<T>), dim3(unsigned(std::min(blocks - b, kMostBlocks))),
-                       dim3(kThreads), 0, s, a, b * kWaves);
+                       dim3(kThreads), lists, s, a, b * kWaves);
     if (const hipError_t e = hipGetLastError()) return e;
   }
   if (a.lists < a.strips) {
     hipLaunchKernelGGL(join_lists_kernel, dim3(unsigned((a.rows + kWaves - 1) / kWaves)),
-                       dim3(kThreads), 0, s, a);
+                       dim3(kThreads), lists, s, a);
     if (const hipError_t e = hipGetLastError()) return e;
   }
   const int n = a.beams * a.lists * a.width;
-  if (n <= 4 * kThreads) return group<float, 4, false>(a, groups, s);
-  if (n <= 16 * kThreads) return group<float, 16, false>(a, groups, s);
-  return group<float, kMostHeld, false>(a, groups, s);
+  if (n <= 256) return group<float, 256, 1, false>(a, groups, s);
+  if (n <= 1024) return group<float, 1024, 1, false>(a, groups, s);
+  if (n <= 4096) return group<float, 1024, 4, false>(a, groups, s);
+  return group<float, 1024, kMostHeld, false>(a, groups, s);
 }
 
 size_t entry_bytes(const sched_beam_desc& d, const Plan& p) {
@@ -655,7 +787,7 @@ hipError_t launch_beam_select(const sched_beam_desc& d, void* ws, hipStream_t s)
   a.scores = d.scores;
   a.last = {d.last.data, d.last.bits == 64};
   a.end_token = d.end_token;
-  a.temperature = d.temperature;
+  a.per_temperature = 1. / double(d.temperature);
   a.factor = float(1.4426950408889634 / double(d.temperature));
   if (!p.small) {
     a.entries = static_cast<Entry*>(ws);
