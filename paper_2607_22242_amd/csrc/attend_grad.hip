@@ -83,8 +83,8 @@ __global__ __launch_bounds__(kThreads, 2) void keys_kernel(AttendArgs a, KeyPart
   auto step = [&](int r0, const T* q_tile, const T* o_tile, const Stats& stats) {
     const int r = r0 + part;
     if (r + 31 < any || r >= rows) return;
-    w.add(q_tile, o_tile, stats, rest, wave_row, part, from - r0, rows - 1 - r0,
-          r >= all && r + 31 < rows, c, places);
+    w.add(q_tile, o_tile, stats, rest, wave_row, part,
+          [&] { return RowSpan{from - r0, rows - 1 - r0}; }, r >= all && r + 31 < rows, c, places);
   };
   if (end >= begin) tiles_of.fetch(a, s, kv, rows, t, q_even, o_even, &s_even);
   for (int r0 = end; r0 >= begin; r0 -= 2 * kTile) {

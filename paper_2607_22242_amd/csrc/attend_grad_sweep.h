@@ -35,6 +35,11 @@ __device__ __forceinline__ void retreat(const AttendArgs& a, RowTile& t) {
   }
 }
 
+// Rows of a tile from one to another.
+struct RowSpan {
+  int from, upto;
+};
+
 struct Stats {
   float lse2[kTile], delta[kTile];
 };
@@ -112,11 +117,13 @@ struct KeySweep {
   Acc dk[D / 32], dv[D / 32];
   int up;  // f16: dS is held 2^up times
 
-  // Rows part .. part + 31 of a tile; the lane's key is seen by the tile's rows
-  // from `from` to `upto` (`whole`: all of the wave's are by all).
+  // Rows part .. part + 31 of a tile; the lane's key is seen by the rows of the tile
+  // that seen() names (`whole`: all of the wave's are by all).
+  template <class Seen>
   __device__ __forceinline__ void add(const T* q_tile, const T* o_tile, const Stats& stats,
-                                      const Rows<T, 64>& rest, int wave_row, int part, int from,
-                                      int upto, bool whole, float c, const Places<D>& places) {
+                                      const Rows<T, 64>& rest, int wave_row, int part,
+                                      const Seen& seen, bool whole, float c,
+                                      const Places<D>& places) {
     const Rows<T, D> qs = {q_tile, places.fresh()}, os = {o_tile, qs.places};
     typedef float Four __attribute__((ext_vector_type(4)));
     const int h4 = int(threadIdx.x) % kWave / 32 * 4;
@@ -133,10 +140,11 @@ struct KeySweep {
     for (int i = 0; i < D / 16; ++i)
       y = product(os.along(part, i), i < kHeld ? v[i] : rest.along(wave_row, i - kHeld), y);
     if (!whole) {
+      const RowSpan s = seen();
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const int r = part + c_row(i);
-        if (r < from || r > upto) x[i] = -INFINITY;
+        if (r < s.from || r > s.upto) x[i] = -INFINITY;
       }
     }
 #pragma unroll
@@ -242,13 +250,10 @@ struct RowSweep {
     }
   }
 
-  // delta of rows that see keys of the first tile only, from the probabilities
-  // as sum_j P_j dP_j: from the rounded out it is off by a rounding of out, which
-  // with few keys is as much as all other roundings together (errors of dQ and
-  // dK against exact products of 16-bit operands: 1.6 to 1.8 times before, 1.4
-  // so, which is what rounding dS and the result gives).
-  __device__ __forceinline__ void exact_delta(const T* k_tile, const T* v_tile, int last, float c,
-                                              const Places<D>& places) {
+  // Sum over a tile's keys of P_j dP_j, of this lane's half of them.
+  template <class Sees>
+  __device__ __forceinline__ float dots(const T* k_tile, const T* v_tile, int j0, const Sees& sees,
+                                        float c, const Places<D>& places) const {
     const Rows<T, D> ks = {k_tile, places.fresh()}, vs = {v_tile, ks.places};
     float sum = 0.f;
 #pragma unroll
@@ -260,10 +265,21 @@ struct RowSweep {
       for (int i = 0; i < D / 16; ++i) y = product(vs.along(32 * t, i), o[i], y);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const float s = 32 * t + c_row(i) > last ? -INFINITY : x[i];
+        const float s = sees(j0 + 32 * t + c_row(i)) ? x[i] : -INFINITY;
         sum += pow2(__builtin_fmaf(s, c, -lse2)) * y[i];
       }
     }
+    return sum;
+  }
+
+  // delta of rows that see keys of the first tile only, from the probabilities
+  // as sum_j P_j dP_j: from the rounded out it is off by a rounding of out, which
+  // with few keys is as much as all other roundings together (errors of dQ and
+  // dK against exact products of 16-bit operands: 1.6 to 1.8 times before, 1.4
+  // so, which is what rounding dS and the result gives).
+  __device__ __forceinline__ void exact_delta(const T* k_tile, const T* v_tile, int last, float c,
+                                              const Places<D>& places) {
+    const float sum = dots(k_tile, v_tile, 0, UpTo{last}, c, places);
     delta = -__builtin_ldexpf(sum + __shfl_xor(sum, 32), -up);
   }
 };

@@ -45,21 +45,32 @@ __device__ __forceinline__ Tile group_tile(const SharedArgs& s, int tile, int nu
   return tile_of([&](int g) { return first_query(s, g) * s.a.group / tile + g; }, s.n_groups, number);
 }
 
-// The sequence, among `n` from `first` on, that holds a lane's row: the last that
-// begins at or before it.  low and high: the wave's lowest and highest row.
-__device__ __forceinline__ int lane_sequence_of(const int32_t* offsets, int rows, int first, int n,
-                                                int low, int high, int row) {
+// The sequences, among `n` from `first` on, that hold a block's lowest and highest
+// row and this lane's: the last that begins at or before it.
+struct Held {
+  int low, high, mine;
+};
+__device__ __forceinline__ Held sequences_of(const int32_t* offsets, int rows, int first, int n,
+                                             int low, int high, int row) {
   const int lane = int(threadIdx.x) % kWave;
-  const int at = first + tile_of([&](int i) { return offset_at(offsets, first + i, rows); }, n, low).seq;
-  const int left = first + n - at;  // sequences from it on
+  int at = first, left = n;  // sequences from `at` on
+  if (n > kWave) {
+    at += tile_of([&](int i) { return offset_at(offsets, first + i, rows); }, n, low).seq;
+    left = first + n - at;
+  }
   const int begin = lane < left ? offset_at(offsets, at + lane, rows) : 0x7fffffff;
-  if (left > kWave && __shfl(begin, kWave - 1) <= high)  // many empty ones
-    return at + sequence_of(offsets + at, left, row);
-  int seq = 0;
+  const uint64_t behind = __ballot(begin > high);
+  if (left > kWave && !behind) {  // many empty ones
+    return {at, at + uniform(sequence_of(offsets + at, left, high)),
+            at + sequence_of(offsets + at, left, row)};
+  }
+  const uint64_t before = __ballot(begin <= low);
+  int mine = 0;
 #pragma unroll
   for (int d = kWave / 2; d; d >>= 1)
-    if (__shfl(begin, seq + d) <= row) seq += d;
-  return at + seq;
+    if (__shfl(begin, mine + d) <= row) mine += d;
+  return {at + (before ? 63 - __builtin_clzll(before) : 0),
+          at + (behind ? max(__builtin_ctzll(behind) - 1, 0) : kWave - 1), at + mine};
 }
 
 // Own keys that a query row sees, counted in all key rows.
@@ -82,27 +93,23 @@ __device__ __forceinline__ int wave_most(int x) {
   return uniform(x);
 }
 
-// The tiles of 64 keys that a block's rows meet: those of the prefix from `begin`
-// to `end`, then the own keys of the sequences seq .. last_seq, of the last one
-// those up to last_key.  Without k_lengths the sequences' keys lie one behind the
-// other and count as one; else a sequence is walked after the other.
+// The tiles of 64 own keys that a block's rows meet: of the sequences seq ..
+// last_seq, of the last one up to last_key.  Without k_lengths the sequences' keys lie
+// one behind the other and count as one; else a sequence is walked after the other.
 struct Step {
-  int own, key0, last;  // is it of the own keys; the tile's first key, the last that counts
+  int key0, last;  // the tile's first key, and the last that counts, of all key rows
   int there;
 };
 template <class T, int D>
 struct Walk {
-  typedef KeyTiles<T, D, 64, 256> Tiles;
   const SharedArgs& s;
-  const Tiles prefix;
-  Tiles own;
-  int kv, end, seq, last_seq, last_key, base, place;  // place: of the next tile, from base
+  KeyTiles<T, D, 64, 256> own;
+  int kv, seq, last_seq, last_key, base, place;  // place: of the next tile, from base
 
-  __device__ __forceinline__ Walk(const SharedArgs& s_, const Group& g, int kv_, int begin, int end_,
-                                  int first_seq, int last_seq_, int last_key_)
-      : s(s_), prefix(s_.p_k, s_.p_v, g.p0, g.keys, s_.near_p, s_.a.dim, kv_),
-        own(s_.a.k, s_.a.v, 0, 0, s_.a.near_k, s_.a.dim, kv_), kv(kv_), end(end_),
-        seq(first_seq - 1), last_seq(last_seq_), last_key(last_key_), base(0), place(begin) {}
+  __device__ __forceinline__ Walk(const SharedArgs& s_, int kv_, int first_seq, int last_seq_,
+                                  int last_key_)
+      : s(s_), own(s_.a.k, s_.a.v, 0, 0, s_.a.near_k, s_.a.dim, kv_), kv(kv_), seq(first_seq - 1),
+        last_seq(last_seq_), last_key(last_key_), base(0), place(0) {}
 
   // Own keys of the next sequence that has any.
   __device__ __forceinline__ bool enter() {
@@ -118,6 +125,7 @@ struct Walk {
       }
       if (behind <= q.k0) continue;
       base = q.k0;
+      place = 0;
       own.keys = behind - base;
       own.k = reinterpret_cast<const char*>(head_row<T>(s.a.k, base, kv));
       own.v = reinterpret_cast<const char*>(head_row<T>(s.a.v, base, kv));
@@ -127,27 +135,70 @@ struct Walk {
   }
   // The next tile, on its way to LDS.
   __device__ __forceinline__ Step next(T* k_tile, T* v_tile) {
-    if (end > 0) {
-      if (place < end) {
-        const int j0 = place;
-        prefix.fetch(j0, k_tile, v_tile, s.a.dim);
-        place += 64;
-        return {0, j0, prefix.keys - 1, 1};
-      }
-      end = 0;
-      place = 0;
-      own.keys = 0;
-    }
-    if (place >= own.keys) {
-      place = 0;
-      if (!enter()) return {0, 0, 0, 0};
-    }
+    if (place >= own.keys && !enter()) return {0, 0, 0};
     const int j0 = place;
     own.fetch(j0, k_tile, v_tile, s.a.dim);
     place += 64;
-    return {1, base + j0, base + own.keys - 1, 1};
+    return {base + j0, base + own.keys - 1, 1};
   }
 };
+
+// The tiles of a block in LDS.
+template <class T, int D>
+struct Buffers {
+  T k_even[64 * D], v_even[64 * D], k_odd[64 * D], v_odd[64 * D];
+};
+
+// A block's rows over the prefix keys begin <= j < end and then the own keys of the
+// walk (with_own), each tile under way while the one before it is worked on.
+// on_prefix(j0, k, v), on_own(step, k, v): what is done with a tile.
+template <class T, int D, class OnPrefix, class OnOwn>
+__device__ __forceinline__ void over_keys(const KeyTiles<T, D, 64, 256>& prefix, int dim, int begin,
+                                          int end, Walk<T, D>& walk, bool with_own,
+                                          Buffers<T, D>& lds, const OnPrefix& on_prefix,
+                                          const OnOwn& on_own) {
+  Step step = {0, 0, 0};
+  bool odd = false;  // where the first own tile is
+  auto first_own = [&](T* k, T* v) {
+    if (with_own) step = walk.next(k, v);
+  };
+  if (begin < end) {
+    prefix.fetch(begin, lds.k_even, lds.v_even, dim);
+    for (int j0 = begin;; j0 += 128) {
+      tiles_barrier();  // the tile is there, and nobody reads the other buffer any more
+      const bool more = j0 + 64 < end;
+      if (more) prefix.fetch(j0 + 64, lds.k_odd, lds.v_odd, dim);
+      else first_own(lds.k_odd, lds.v_odd);
+      on_prefix(j0, lds.k_even, lds.v_even);
+      if (!more) {
+        odd = true;
+        break;
+      }
+      tiles_barrier();
+      const bool again = j0 + 128 < end;
+      if (again) prefix.fetch(j0 + 128, lds.k_even, lds.v_even, dim);
+      else first_own(lds.k_even, lds.v_even);
+      on_prefix(j0 + 64, lds.k_odd, lds.v_odd);
+      if (!again) break;
+    }
+  } else {
+    first_own(lds.k_even, lds.v_even);
+  }
+  while (step.there) {
+    if (!odd) {
+      tiles_barrier();
+      const Step next = walk.next(lds.k_odd, lds.v_odd);
+      on_own(step, lds.k_even, lds.v_even);
+      if (!next.there) break;
+      step = next;
+    }
+    odd = false;
+    tiles_barrier();
+    const Step next = walk.next(lds.k_even, lds.v_even);
+    on_own(step, lds.k_odd, lds.v_odd);
+    step = next;
+  }
+}
 
 // Keys from one to another.
 struct Within {
@@ -155,7 +206,7 @@ struct Within {
   __device__ __forceinline__ bool operator()(int j) const { return j >= lo && j <= hi; }
 };
 
-// What a wave's rows see of the own keys.
+// What a wave's rows see of the own keys, and of a tile of them.
 struct Seen {
   Span mine;
   int all_lo, all_hi, any_lo, any_hi;
@@ -163,52 +214,75 @@ struct Seen {
   __device__ __forceinline__ explicit Seen(const Span& x)
       : mine(x), all_lo(wave_most(x.lo)), all_hi(wave_least(x.hi)), any_lo(wave_least(x.lo)),
         any_hi(wave_most(x.hi)) {}
+  // The most own keys that a row of the wave sees.
+  __device__ __forceinline__ int most() const { return wave_most(max(0, mine.hi - mine.lo + 1)); }
   __device__ __forceinline__ bool any(const Step& t) const {
-    return !t.own || (t.key0 <= any_hi && t.key0 + 63 >= any_lo);
+    return t.key0 <= any_hi && t.key0 + 63 >= any_lo;
   }
   __device__ __forceinline__ bool all(const Step& t) const {
-    return t.key0 + 63 <= t.last && (!t.own || (t.key0 >= all_lo && t.key0 + 63 <= all_hi));
+    return t.key0 + 63 <= min(t.last, all_hi) && t.key0 >= all_lo;
   }
   __device__ __forceinline__ Within keys(const Step& t) const {
-    return {t.own ? mine.lo : 0, t.own ? min(mine.hi, t.last) : t.last};
+    return {mine.lo, min(mine.hi, t.last)};
   }
 };
 
-// Where a block's 128 query rows lie, and what this lane's row sees; rows behind
-// the last are copies of it that nobody writes.
+// Where a block's query rows lie, and what this lane's row sees; rows behind the
+// last are copies of it that nobody writes.
 template <int kRows>
 struct RowsOf {
   Group g;
-  int first, rows, row;  // first of the tile, rows of the group, this lane's row
+  int first, rows;  // first of the tile, rows of the group
   bool there, on;
-  QueryRow me;           // query within the group
-  int query, seq, first_seq, last_seq, last_key;
+  QueryRow me;      // query within the group
+  int query, first_seq, last_seq, seq, first_key, last_key;  // keys of the tile's first and last row
   Span mine;
 
-  __device__ __forceinline__ RowsOf(const SharedArgs& s, int kv, int number, int lane_row) {
-    const Tile tile = group_tile(s, kRows, number);
+  __device__ __forceinline__ RowsOf(const SharedArgs& s, const Work& work, int tiles, int lane_row) {
+    const Tile tile = group_tile(s, kRows, tiles - 1 - work.tile);
     g = group_at(s, tile.seq);
     first = tile.index * kRows;
     rows = g.queries * s.a.group;
     there = tile.index >= 0 && first < rows;
-    if (!there) return;
-    on = first + lane_row < rows;
-    row = min(first + lane_row, rows - 1);
-    me = query_row(s.a, kv, row);
+    on = there && first + lane_row < rows;
+    me = query_row(s.a, work.kv, there ? min(first + lane_row, rows - 1) : 0);
     query = g.q0 + me.query;
+  }
+  // The rows' sequences (where there are rows).
+  __device__ __forceinline__ void find(const SharedArgs& s) {
     const int low = g.q0 + first / s.a.group;
     const int high = g.q0 + (min(first + kRows, rows) - 1) / s.a.group;
-    seq = lane_sequence_of(s.a.q_offsets, s.a.q_rows, g.seq, g.seqs, low, high, query);
-    mine = own_keys(s.a, lane_sequence(s.a, seq), query);
-    // Of the tile's first and last row, which another wave may hold.
-    first_seq = uniform(lane_sequence_of(s.a.q_offsets, s.a.q_rows, g.seq, g.seqs, low, low, low));
-    last_seq = uniform(lane_sequence_of(s.a.q_offsets, s.a.q_rows, g.seq, g.seqs, high, high, high));
-    const Seq q = sequence(s.a, last_seq);
-    const Span last = own_keys(s.a, q, high);
+    const Held held = sequences_of(s.a.q_offsets, s.a.q_rows, g.seq, g.seqs, low, high, query);
+    first_seq = uniform(held.low);
+    last_seq = uniform(held.high);
+    seq = held.mine;
+    const Seq q = lane_sequence(s.a, seq), tail = lane_sequence(s.a, last_seq);
+    first_key = uniform(offset_at(s.a.k_offsets, first_seq, s.a.k_rows));
+    mine = own_keys(s.a, q, query);
     // Sequences before the last one end within the tile: all their keys count.
-    last_key = last_seq > first_seq ? max(last.hi, q.k0 - 1) : last.hi;
+    const int last = own_keys(s.a, tail, high).hi;
+    last_key = uniform(last_seq > first_seq ? max(last, tail.k0 - 1) : last);
+  }
+  // The last key that rows of the tile see of one of its sequences.
+  __device__ __forceinline__ int last_key_of(const SharedArgs& s, int b) const {
+    if (b == last_seq) return last_key;
+    const Seq q = sequence(s.a, b);
+    return q.k0 + q.keys - 1;
   }
 };
+
+// A key that is masked for a row has weight zero, and zero times what is no number is
+// none: a sequence that holds one reaches the others of its tile.  It shows in their
+// sums, and is rare; a block that finds it takes its sequences one by one.
+template <int N>
+__device__ __forceinline__ bool no_number(const Acc (&x)[N]) {
+  float sum = 0.f;
+#pragma unroll
+  for (int d = 0; d < N; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum += x[d][i] * 0.f;
+  return sum != 0.f;  // infinities, too, give NaN here
+}
 
 inline HeadsView heads_view(const sched_heads& h) {
   return {static_cast<char*>(h.data), h.row_stride, h.head_stride};

@@ -16,42 +16,61 @@
 namespace policy {
 namespace {
 
+// One turn of a block over its rows: all of them (nth < 0), which is done unless a
+// sequence that holds what is no number has reached another's rows (true: nothing is
+// written), or those of its nth sequence (true: there is one).
 template <class T, int D>
-__global__ __launch_bounds__(kThreads, 2) void shared_kernel(SharedArgs s, int tiles) {
-  __shared__ __attribute__((aligned(16))) T k_even[kKeys * D], v_even[kKeys * D];
-  __shared__ __attribute__((aligned(16))) T k_odd[kKeys * D], v_odd[kKeys * D];
+__device__ __forceinline__ bool rows_turn(const SharedArgs& s, int block, int tiles,
+                                          Buffers<T, D>& lds, int nth) {
   const AttendArgs& a = s.a;
-  const Work work = work_of(int(blockIdx.x), tiles, a.q_heads / a.group);
-  if (work.tile >= tiles) return;
+  const bool by_one = nth >= 0;
+  const Work work = work_of(block, tiles, a.q_heads / a.group);
+  if (work.tile >= tiles) return false;
   const int lane = int(threadIdx.x) % kWave;
-  const RowsOf<kRowsOfBlock> r(s, work.kv, tiles - 1 - work.tile, 32 * wave_id() + lane % 32);
-  if (!r.there) return;
+  RowsOf<kRowsOfBlock> r(s, work, tiles, 32 * wave_id() + lane % 32);
+  if (!r.there) return false;
+  r.find(s);
+  const int alone = r.first_seq + nth;
+  if (by_one) {
+    if (alone > r.last_seq) return false;
+    tiles_barrier();  // nobody reads the last turn's tiles any more
+  }
   const Seen seen(r.mine);
   Sweep<T, D, kKeys / 32> w;
   w.start(head_row<T>(a.q, r.query, r.me.head), a.dim, r.on);
   const float c = a.scale * kLog2e;
   const Places<D> places;
-  Walk<T, D> walk(s, r.g, work.kv, 0, r.g.keys, r.first_seq, r.last_seq, r.last_key);
-  auto add = [&](const Step& t, const T* k_tile, const T* v_tile) {
-    if (seen.any(t)) w.add(k_tile, v_tile, 0, t.key0, seen.keys(t), seen.all(t), c, places);
-  };
-  Step even = walk.next(k_even, v_even), odd;
-  while (even.there) {
-    tiles_barrier();  // the tile is there, and nobody reads the other buffer any more
-    odd = walk.next(k_odd, v_odd);
-    add(even, k_even, v_even);
-    if (!odd.there) break;
-    tiles_barrier();
-    even = walk.next(k_even, v_even);
-    add(odd, k_odd, v_odd);
-  }
+  const KeyTiles<T, D, kKeys, kThreads> prefix(s.p_k, s.p_v, r.g.p0, r.g.keys, s.near_p, a.dim,
+                                               work.kv);
+  Walk<T, D> walk(s, work.kv, by_one ? alone : r.first_seq, by_one ? alone : r.last_seq,
+                  by_one ? r.last_key_of(s, alone) : r.last_key);
+  over_keys<T, D>(
+      prefix, a.dim, 0, r.g.keys, walk, true, lds,
+      [&](int j0, const T* k, const T* v) {
+        w.add(k, v, 0, j0, UpTo{r.g.keys - 1}, j0 + kKeys <= r.g.keys, c, places);
+      },
+      [&](const Step& t, const T* k, const T* v) {
+        if (seen.any(t)) w.add(k, v, 0, t.key0, seen.keys(t), seen.all(t), c, places);
+      });
+  if (!by_one && r.first_seq < r.last_seq && __syncthreads_or(r.on && no_number(w.o))) return true;
   const float sum = w.sum + __shfl_xor(w.sum, 32);
-  if (!r.on) return;
+  if (!r.on || (by_one && r.seq != alone)) return by_one;
   store_column<T, D>(head_row<T>(a.out, r.query, r.me.head), w.o, a.dim,
                      sum == 0.f ? 0.f : 1.f / sum);  // a sum of NaN stays one
   if (lane < 32)
     a.lse[int64_t(r.me.head) * a.q_rows + r.query] =
         sum == 0.f ? -INFINITY : __builtin_fmaf(w.reference(c), kLn2, ln(sum));
+  return by_one;
+}
+
+template <class T, int D>
+__global__ __launch_bounds__(kThreads, 2) void shared_kernel(SharedArgs s, int tiles) {
+  __shared__ __attribute__((aligned(16))) Buffers<T, D> lds;
+  int block = int(blockIdx.x);
+  for (int nth = -1;; ++nth) {
+    asm volatile("" : "+s"(block));  // a turn keeps nothing in registers for the next
+    if (!rows_turn<T, D>(s, block, tiles, lds, nth)) return;
+  }
 }
 
 // --- few query rows -----------------------------------------------------------

@@ -20,18 +20,19 @@ namespace {
 
 // --- dQ -------------------------------------------------------------------------
 
+// One turn of a block over its rows: all of them (nth < 0), which is done unless a
+// sequence that holds what is no number has reached another's rows (true: nothing is
+// written), or those of its nth sequence (true: there is one).
 template <class T, int D>
-__global__ __launch_bounds__(kThreads, 2) void shared_queries_kernel(SharedArgs s, RowParts p,
-                                                                     int tiles) {
-  __shared__ __attribute__((aligned(16))) T k_even[kTile * D], v_even[kTile * D];
-  __shared__ __attribute__((aligned(16))) T k_odd[kTile * D], v_odd[kTile * D];
+__device__ __forceinline__ bool rows_turn(const SharedArgs& s, const RowParts& p, int block,
+                                          int tiles, Buffers<T, D>& lds, int nth) {
   const AttendArgs& a = s.a;
-  const Work work = work_of(int(blockIdx.x), tiles, a.q_heads / a.group);
-  if (work.tile >= tiles) return;
+  const bool by_one = nth >= 0;
+  const Work work = work_of(block, tiles, a.q_heads / a.group);
+  if (work.tile >= tiles) return false;
   const int lane = int(threadIdx.x) % kWave, part = int(blockIdx.y);
-  const RowsOf<kRowsOfBlock> r(s, work.kv, tiles - 1 - work.tile, 32 * wave_id() + lane % 32);
-  if (!r.there) return;
-  const Seen seen(r.mine);
+  RowsOf<kRowsOfBlock> r(s, work, tiles, 32 * wave_id() + lane % 32);
+  if (!r.there) return false;
   // This block's share of the prefix; the last one has the own keys too.
   const int share = ((r.g.keys + kTile - 1) / kTile + p.parts - 1) / p.parts * kTile;
   const int begin = min(part * share, r.g.keys), end = min(begin + share, r.g.keys);
@@ -46,6 +47,10 @@ __global__ __launch_bounds__(kThreads, 2) void shared_queries_kernel(SharedArgs 
   }
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) w.dq[i] = Acc(0.f);
+  r.find(s);
+  const int alone = r.first_seq + nth;
+  if (by_one && (alone > r.last_seq || !with_own)) return false;
+  const Seen seen(r.mine);
   // The row's statistics, which the kernel of dK and dV reads too.
   const int64_t n = int64_t(r.me.head) * a.q_rows + r.query;
   const T* const out_row = head_row<T>(a.out, r.query, r.me.head);
@@ -59,30 +64,53 @@ __global__ __launch_bounds__(kThreads, 2) void shared_queries_kernel(SharedArgs 
   w.delta = -(sum + __shfl_xor(sum, 32));
   const float lse = r.on ? a.lse[n] : -INFINITY;
   w.lse2 = lse == -INFINITY ? INFINITY : lse * kLog2e;  // powers of rows that see nothing are 0
-  if (lane < 32 && r.on && part == 0) {
-    a.lse2[n] = w.lse2 - kLiftGrad<T>;
-    a.delta[n] = w.delta;
-  }
+  const bool mine = r.on && (!by_one || r.seq == alone);  // is the row this turn's
+  const bool first_part = lane < 32 && mine && part == 0;
+  if (first_part) a.lse2[n] = w.lse2 - kLiftGrad<T>;
   w.up = kShort<T> ? kLargest : 0;
   w.lse2 -= float(w.up);
   const float c = a.scale * kLog2e;
   const Places<D> places;
-  Walk<T, D> walk(s, r.g, work.kv, begin, begin < end ? end : 0, r.first_seq,
-                  with_own ? r.last_seq : r.first_seq - 1, r.last_key);
-  auto add = [&](const Step& t, const T* k_tile, const T* v_tile) {
-    if (seen.any(t)) w.add(k_tile, v_tile, t.key0, seen.keys(t), seen.all(t), c, places);
-  };
-  Step even = walk.next(k_even, v_even), odd;
-  while (even.there) {
-    tiles_barrier();
-    odd = walk.next(k_odd, v_odd);
-    add(even, k_even, v_even);
-    if (!odd.there) break;
-    tiles_barrier();
-    even = walk.next(k_even, v_even);
-    add(odd, k_odd, v_odd);
+  const KeyTiles<T, D, kTile, kThreads> prefix(s.p_k, s.p_v, r.g.p0, r.g.keys, s.near_p, a.dim,
+                                               work.kv);
+  const int first_seq = by_one ? alone : r.first_seq, last_seq = by_one ? alone : r.last_seq;
+  const int last_key = by_one ? r.last_key_of(s, alone) : r.last_key;
+  if (by_one) tiles_barrier();  // nobody reads the last turn's tiles any more
+  // Rows that see a tile's worth of keys at most take delta from the probabilities,
+  // as sum_j P_j dP_j: from the rounded out it is off by a rounding of out, which
+  // with few keys is as much as all other roundings together (errors of dQ and dK
+  // against 64 bits, 5 to 30 keys: 1.65 times those of rounding once, 1.4 so).
+  const bool few = r.g.keys + seen.most() <= kTile;
+  if (__syncthreads_or(few && r.last_key - r.first_key < 16 * kTile)) {
+    float dots = 0.f;
+    if (r.g.keys > 0) {  // a tile's worth at most, or no row of the block is one of them
+      prefix.fetch(0, lds.k_even, lds.v_even, a.dim);
+      tiles_barrier();
+      if (few) dots += w.dots(lds.k_even, lds.v_even, 0, UpTo{r.g.keys - 1}, c, places);
+      tiles_barrier();
+    }
+    Walk<T, D> walk(s, work.kv, first_seq, last_seq, last_key);
+    for (Step t = walk.next(lds.k_even, lds.v_even); t.there; t = walk.next(lds.k_even, lds.v_even)) {
+      tiles_barrier();
+      if (few && seen.any(t)) dots += w.dots(lds.k_even, lds.v_even, t.key0, seen.keys(t), c, places);
+      tiles_barrier();
+    }
+    if (few) w.delta = -__builtin_ldexpf(dots + __shfl_xor(dots, 32), -w.up);
   }
-  if (!r.on) return;
+  Walk<T, D> walk(s, work.kv, first_seq, last_seq, last_key);
+  over_keys<T, D>(
+      prefix, a.dim, begin, end, walk, with_own, lds,
+      [&](int j0, const T* k, const T* v) {
+        w.add(k, v, j0, UpTo{r.g.keys - 1}, j0 + kTile <= r.g.keys, c, places);
+      },
+      [&](const Step& t, const T* k, const T* v) {
+        if (seen.any(t)) w.add(k, v, t.key0, seen.keys(t), seen.all(t), c, places);
+      });
+  if (!by_one && with_own && r.first_seq < r.last_seq &&
+      __syncthreads_or(r.on && (no_number(w.dq) || w.delta * 0.f != 0.f)))
+    return true;
+  if (!mine) return by_one;
+  if (first_part) a.delta[n] = w.delta;
   if (kShort<T>) shift(w.dq, -w.up);
   if (r.g.keys == 0 && r.mine.hi < r.mine.lo) {  // a row that sees nothing, whatever it holds
 #pragma unroll
@@ -92,6 +120,18 @@ __global__ __launch_bounds__(kThreads, 2) void shared_queries_kernel(SharedArgs 
     store_column<float, D>(p.dq + row_part<D>(a, part, r.query, r.me.head), w.dq, D, a.scale);
   else
     store_column<T, D>(head_row<T>(a.d_q, r.query, r.me.head), w.dq, a.dim, a.scale);
+  return by_one;
+}
+
+template <class T, int D>
+__global__ __launch_bounds__(kThreads, 2) void shared_queries_kernel(SharedArgs s, RowParts p,
+                                                                     int tiles) {
+  __shared__ __attribute__((aligned(16))) Buffers<T, D> lds;
+  int block = int(blockIdx.x);
+  for (int nth = -1;; ++nth) {
+    asm volatile("" : "+s"(block));  // a turn keeps nothing in registers for the next
+    if (!rows_turn<T, D>(s, p, block, tiles, lds, nth)) return;
+  }
 }
 
 // Adds the parts of the groups' rows: four elements of a head a thread.
@@ -130,74 +170,88 @@ __device__ __forceinline__ int64_t prefix_part(const SharedArgs& s, int part, in
 // keys 0 .. 31 and 32 .. 63, waves 2 and 3 the odd 32; their sums meet at the end.
 // The first p_blocks blocks hold prefix keys; the others hold own keys, of one
 // sequence or several.
-template <class T, int D>
-__global__ __launch_bounds__(kThreads, 2) void shared_keys_kernel(SharedArgs s, PrefixParts p,
-                                                                  int p_tiles, int p_blocks,
-                                                                  int tiles) {
-  __shared__ __attribute__((aligned(16))) T q_even[kTile * D], o_even[kTile * D];
-  __shared__ __attribute__((aligned(16))) T q_odd[kTile * D], o_odd[kTile * D];
-  constexpr int kRest = KeySweep<T, D>::kHeld < D / 16 ? kKeysOfBlock * 64 : 8;
-  __shared__ __attribute__((aligned(16))) T v_rest[kRest];
-  __shared__ __attribute__((aligned(16))) Stats s_even, s_odd;
+// Turns are those of rows_turn, over the sequences of own keys.
+template <class T>
+struct KeyBuffers {  // arrays in LDS
+  T *q_even, *o_even, *q_odd, *o_odd, *v_rest;
+  Stats *s_even, *s_odd;
+  int *from, *upto;  // rows that see a key
+  int* seq;          // its sequence; -1: not in use, -2: another block's
+};
+template <class T, int D, bool kPrefix>
+__device__ __forceinline__ bool keys_turn(const SharedArgs& s, const PrefixParts& p, int block,
+                                          int blocks, int tiles, const KeyBuffers<T>& lds, int nth) {
   const AttendArgs& a = s.a;
-  const int kv_heads = a.q_heads / a.group;
-  const bool prefix = int(blockIdx.x) < p_blocks * p.parts;
-  const int part_of_rows = prefix ? int(blockIdx.x) / p_blocks : 0;
-  const Work work = prefix ? work_of(int(blockIdx.x) % p_blocks, p_tiles, kv_heads)
-                           : work_of(int(blockIdx.x) - p_blocks * p.parts, tiles, kv_heads);
-  if (work.tile >= (prefix ? p_tiles : tiles)) return;
+  const bool by_one = !kPrefix && nth >= 0;
+  const int part_of_rows = kPrefix ? block / blocks : 0;
+  const Work work = work_of(block - part_of_rows * blocks, tiles, a.q_heads / a.group);
+  if (work.tile >= tiles) return false;
   const int lane = int(threadIdx.x) % kWave, wave = wave_id();
   const int kv = work.kv, part = wave / 2 * 32, wave_row = wave % 2 * 32;
-  const HeadsView &ks = prefix ? s.p_k : a.k, &vs = prefix ? s.p_v : a.v;
+  const HeadsView &ks = kPrefix ? s.p_k : a.k, &vs = kPrefix ? s.p_v : a.v;
 
-  // The lane's key (a row of its tensor), the rows that see it, from .. upto of
-  // the block's `rows` rows, which begin at query q0; block_from: none of the
-  // block's keys is seen by a row before it.
-  int key, q0, rows, from, upto, block_from;
+  // The lane's key and the rows that see it: of its sequence's (its group's) `count`
+  // rows, which begin at query `query`, those from `seen` on.  What only the ends of
+  // the loop below ask for lies in LDS: registers are short.
+  int first, key, query, seen, count;
+  int in_use = 0, owned = 0;  // prefix: rows before them are, in use and at all
   bool held, on;  // is the row this block's; is it a key in use
-  if (prefix) {
+  // The block's rows, which begin at query q0; none before row block_from sees a key.
+  int q0, rows, block_from;
+  int seq = 0, low_seq = 0, high_seq = 0;  // own keys: the lane's sequence, the block's
+  if (kPrefix) {
     const Tile tile = tile_of(s.p_offsets, s.n_groups, s.p_rows, 1, kKeysOfBlock, work.tile);
     const Group g = group_at(s, tile.seq);
-    const int first = tile.index * kKeysOfBlock, j = first + wave_row + lane % 32;
-    if (tile.index < 0 || first >= g.slot) return;
+    const int at = tile.index * kKeysOfBlock, j = at + wave_row + lane % 32;
+    if (tile.index < 0 || at >= g.slot) return false;
+    first = g.p0 + at;
+    in_use = g.p0 + g.keys;
+    owned = g.p0 + g.slot;
     key = g.p0 + j;
     held = j < g.slot;
     on = j < g.keys;
-    q0 = g.q0;
-    rows = first < g.keys ? g.queries * a.group : 0;
-    from = block_from = 0;
-    upto = rows - 1;
+    query = q0 = g.q0;
+    count = rows = at < g.keys ? g.queries * a.group : 0;
+    seen = block_from = 0;
   } else {
     const int first_seq = uniform(first_sequence(s, 0));
     const int seqs = uniform(first_sequence(s, s.n_groups)) - first_seq;
-    if (seqs <= 0) return;
+    if (seqs <= 0) return false;
     const int behind = uniform(offset_at(a.k_offsets, first_seq + seqs, a.k_rows));
-    const int first =
-        uniform(offset_at(a.k_offsets, first_seq, a.k_rows)) + work.tile * kKeysOfBlock;
-    if (first >= behind) return;
+    first = uniform(offset_at(a.k_offsets, first_seq, a.k_rows)) + work.tile * kKeysOfBlock;
+    if (first >= behind) return false;
     const int last = min(first + kKeysOfBlock, behind) - 1;
     key = first + wave_row + lane % 32;
     held = key <= last;
-    const int mine = lane_sequence_of(a.k_offsets, a.k_rows, first_seq, seqs, first, last, min(key, last));
-    const Seq q = lane_sequence(a, mine);
-    const Seq head = sequence(a, uniform(lane_sequence_of(a.k_offsets, a.k_rows, first_seq, seqs, first,
-                                                          first, first)));
-    const Seq tail = sequence(a, uniform(lane_sequence_of(a.k_offsets, a.k_rows, first_seq, seqs, last,
-                                                          last, last)));
-    q0 = head.q0;
-    rows = max(0, tail.q0 + tail.queries - q0) * a.group;
-    // The first query that sees key j of a sequence; those behind it if none does.
+    const Held its = sequences_of(a.k_offsets, a.k_rows, first_seq, seqs, first, last, min(key, last));
+    seq = its.mine;
+    low_seq = uniform(its.low);
+    high_seq = uniform(its.high);
+    const Seq q = lane_sequence(a, seq), head = sequence(a, low_seq), tail = sequence(a, high_seq);
+    // The first query of a sequence that sees key j of it; `queries` if none does.
     auto seen_from = [&](const Seq& x, int j) {
-      return x.q0 - q0 + (a.causal ? min(max(0, j - (x.keys - x.queries)), x.queries) : 0);
+      return a.causal ? min(max(0, j - (x.keys - x.queries)), x.queries) : 0;
     };
     on = held && key - q.k0 < q.keys;
-    from = on ? seen_from(q, key - q.k0) * a.group : rows;
-    upto = on ? (q.q0 - q0 + q.queries) * a.group - 1 : -1;
+    query = q.q0;
+    count = q.queries * a.group;
+    seen = seen_from(q, key - q.k0) * a.group;
+    q0 = head.q0;
+    rows = max(0, tail.q0 + tail.queries - q0) * a.group;
     block_from = seen_from(head, first - head.k0) * a.group;
   }
   const float c = a.scale * kLog2e;
   const Places<D> places;
-  const Rows<T, 64> rest = {v_rest, Places<64>()};
+  const int alone = low_seq + nth;
+  if (by_one) {
+    if (alone > high_seq) return false;
+    const Seq q = sequence(a, alone);
+    q0 = q.q0;
+    rows = q.queries * a.group;
+    block_from = 0;
+    tiles_barrier();  // nobody reads the last turn's tiles any more
+  }
+  const Rows<T, 64> rest = {lds.v_rest, Places<64>()};
   KeySweep<T, D> w;
   {
     const int64_t row = on ? key : 0;
@@ -211,23 +265,37 @@ __global__ __launch_bounds__(kThreads, 2) void shared_keys_kernel(SharedArgs s, 
         w.v[i] = v;
       else if (part == 0)
         *reinterpret_cast<typename Frag<T>::type*>(
-            v_rest + at * 64 + ((2 * (i - KeySweep<T, D>::kHeld) + h) ^ turn_of<64>(at)) * 8) = v;
+            lds.v_rest + at * 64 + ((2 * (i - KeySweep<T, D>::kHeld) + h) ^ turn_of<64>(at)) * 8) = v;
+    }
+  }
+  const RowTiles<T, D> tiles_of(a);
+  // Rows that all, or any, of the wave's keys are seen by.
+  int all_from, all_upto, any_from, any_upto;
+  {
+    const bool counts = on && (!by_one || seq == alone);
+    const int from = counts ? (query - q0) * a.group + seen : rows;
+    const int upto = counts ? (query - q0) * a.group + count - 1 : -1;
+    all_from = wave_most(from);
+    all_upto = wave_least(upto);
+    any_from = wave_least(from);
+    any_upto = wave_most(upto);
+    const int at = wave_row + lane % 32;
+    if (!kPrefix && part == 0) {  // read behind the next barrier
+      lds.from[at] = from;
+      lds.upto[at] = upto;
+      lds.seq[at] = !held ? -2 : !on ? -1 : seq;
+      if (by_one && held && !on && seq != alone) lds.seq[at] = -2;
     }
   }
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) w.dk[i] = w.dv[i] = Acc(0.f);
   w.up = kLargest;
-  // Rows that all, or any, of the wave's keys are seen by; keys that are not in use
-  // are masked.
-  const int all_from = wave_most(on ? from : rows), all_upto = wave_least(on ? upto : -1);
-  const int any_from = wave_least(on ? from : rows), any_upto = wave_most(on ? upto : -1);
-  const RowTiles<T, D> tiles_of(a);
   const Seq base = {q0, 0, 0, 0, 0};
   // From the last rows to the first: blocks that run side by side read the same
   // rows at the same time.
   int begin = block_from / kTile * kTile;
   int end = block_from < rows ? (rows - 1) / kTile * kTile : -1;
-  if (prefix && p.parts > 1) {  // this block's share of the row tiles
+  if (kPrefix && p.parts > 1) {  // this block's share of the row tiles
     const int share = (max(end - begin + kTile, 0) / kTile + p.parts - 1) / p.parts;
     end -= part_of_rows * share * kTile;
     begin = max(begin, end - (share - 1) * kTile);
@@ -236,25 +304,31 @@ __global__ __launch_bounds__(kThreads, 2) void shared_keys_kernel(SharedArgs s, 
   auto step = [&](int r0, const T* q_tile, const T* o_tile, const Stats& stats) {
     const int r = r0 + part;
     if (r + 31 < any_from || r > any_upto) return;
-    w.add(q_tile, o_tile, stats, rest, wave_row, part, (on ? from : rows) - r0, (on ? upto : -1) - r0,
+    w.add(q_tile, o_tile, stats, rest, wave_row, part,
+          [&] {
+            int at = int(threadIdx.x) % 32 + wave_row;
+            asm volatile("" : "+v"(at));  // formed where it is used, not held in a register
+            if (kPrefix) return RowSpan{(first + at < in_use ? 0 : rows) - r0, rows - 1 - r0};
+            return RowSpan{lds.from[at] - r0, lds.upto[at] - r0};
+          },
           r >= all_from && r + 31 <= all_upto, c, places);
   };
-  if (end >= begin) tiles_of.fetch(a, base, kv, rows, t, q_even, o_even, &s_even);
+  if (end >= begin) tiles_of.fetch(a, base, kv, rows, t, lds.q_even, lds.o_even, lds.s_even);
   for (int r0 = end; r0 >= begin; r0 -= 2 * kTile) {
     tiles_barrier();  // the tile is there, and nobody reads the other buffer any more
     retreat(a, t);
-    if (t.r0 >= begin) tiles_of.fetch(a, base, kv, rows, t, q_odd, o_odd, &s_odd);
-    step(r0, q_even, o_even, s_even);
+    if (t.r0 >= begin) tiles_of.fetch(a, base, kv, rows, t, lds.q_odd, lds.o_odd, lds.s_odd);
+    step(r0, lds.q_even, lds.o_even, *lds.s_even);
     if (r0 - kTile < begin) break;
     tiles_barrier();
     retreat(a, t);
-    if (t.r0 >= begin) tiles_of.fetch(a, base, kv, rows, t, q_even, o_even, &s_even);
-    step(r0 - kTile, q_odd, o_odd, s_odd);
+    if (t.r0 >= begin) tiles_of.fetch(a, base, kv, rows, t, lds.q_even, lds.o_even, lds.s_even);
+    step(r0 - kTile, lds.q_odd, lds.o_odd, *lds.s_odd);
   }
   // Waves 2 and 3 hand their sums to waves 0 and 1.
-  static_assert(sizeof(q_even) == size_t(D) / 32 * 16 * kWave * sizeof(float), "a wave's sums");
-  float* const buf_k = reinterpret_cast<float*>(wave % 2 ? q_odd : q_even);
-  float* const buf_v = reinterpret_cast<float*>(wave % 2 ? o_odd : o_even);
+  static_assert(kTile * D * sizeof(T) == size_t(D) / 32 * 16 * kWave * sizeof(float), "a wave's sums");
+  float* const buf_k = reinterpret_cast<float*>(wave % 2 ? lds.q_odd : lds.q_even);
+  float* const buf_v = reinterpret_cast<float*>(wave % 2 ? lds.o_odd : lds.o_even);
   tiles_barrier();
   if (kShort<T>) {
     shift(w.dk, -w.up - int(kLiftGrad<T>));
@@ -262,20 +336,51 @@ __global__ __launch_bounds__(kThreads, 2) void shared_keys_kernel(SharedArgs s, 
   }
   if (wave >= 2) w.hand(buf_k, buf_v);
   tiles_barrier();
-  if (wave >= 2 || !held) return;
-  w.take(buf_k, buf_v);
-  if (!on) {  // also where a row that was NaN has met the tile's zeros
+  if (wave < 2) w.take(buf_k, buf_v);
+  int lane_again = int(threadIdx.x) % 32;
+  asm volatile("" : "+v"(lane_again));
+  const int row = first + wave_row + lane_again;
+  const int its = !kPrefix ? lds.seq[wave_row + lane_again] : row < in_use ? 0 : row < owned ? -1 : -2;
+  if (!kPrefix && !by_one && low_seq < high_seq &&
+      __syncthreads_or(wave < 2 && its >= 0 && (no_number(w.dk) || no_number(w.dv))))
+    return true;
+  if (wave >= 2 || its == -2 || (by_one && its >= 0 && its != alone)) return by_one;
+  if (its < 0) {  // also where a row that was NaN has met the tile's zeros
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) w.dk[i] = w.dv[i] = Acc(0.f);
   }
-  if (prefix && p.parts > 1) {
-    const int64_t at = prefix_part<D>(s, part_of_rows, kv, key);
+  if (kPrefix && p.parts > 1) {
+    const int64_t at = prefix_part<D>(s, part_of_rows, kv, row);
     store_column<float, D>(p.dk + at, w.dk, D, a.scale);
     store_column<float, D>(p.dv + at, w.dv, D, 1.f);
+  } else {
+    store_column<T, D>(head_row<T>(kPrefix ? s.d_p_k : a.d_k, row, kv), w.dk, a.dim, a.scale);
+    store_column<T, D>(head_row<T>(kPrefix ? s.d_p_v : a.d_v, row, kv), w.dv, a.dim, 1.f);
+  }
+  return by_one;
+}
+
+template <class T, int D>
+__global__ __launch_bounds__(kThreads, 2) void shared_keys_kernel(SharedArgs s, PrefixParts p,
+                                                                  int p_tiles, int p_blocks,
+                                                                  int tiles) {
+  __shared__ __attribute__((aligned(16))) T q_even[kTile * D], o_even[kTile * D];
+  __shared__ __attribute__((aligned(16))) T q_odd[kTile * D], o_odd[kTile * D];
+  constexpr int kRest = KeySweep<T, D>::kHeld < D / 16 ? kKeysOfBlock * 64 : 8;
+  __shared__ __attribute__((aligned(16))) T v_rest[kRest];
+  __shared__ __attribute__((aligned(16))) Stats s_even, s_odd;
+  __shared__ int from[kKeysOfBlock], upto[kKeysOfBlock], seq[kKeysOfBlock];
+  const KeyBuffers<T> lds = {q_even, o_even, q_odd, o_odd, v_rest, &s_even, &s_odd, from, upto, seq};
+  int block = int(blockIdx.x);
+  if (block < p_blocks * p.parts) {
+    keys_turn<T, D, true>(s, p, block, p_blocks, p_tiles, lds, -1);
     return;
   }
-  store_column<T, D>(head_row<T>(prefix ? s.d_p_k : a.d_k, key, kv), w.dk, a.dim, a.scale);
-  store_column<T, D>(head_row<T>(prefix ? s.d_p_v : a.d_v, key, kv), w.dv, a.dim, 1.f);
+  block -= p_blocks * p.parts;
+  for (int nth = -1;; ++nth) {
+    asm volatile("" : "+s"(block));
+    if (!keys_turn<T, D, false>(s, p, block, 1, tiles, lds, nth)) return;
+  }
 }
 
 // Adds the parts of the prefixes' rows: four elements of a head a thread.

@@ -539,6 +539,36 @@ def test_rows_outside_the_groups_stay():
             assert bool((x[end:] == 7).all()) and not bool((x[:end] == 7).all(2).any())
 
 
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_what_is_no_number_stays_in_its_sequence(dtype, bad):
+    """A sequence whose tensors hold NaN or infinities leaves the others of its
+    tile as they are; they share the prefix, whose gradient it reaches."""
+    g = gen(37)
+    queries = [14, 9, 20, 14, 3, 30]
+    off, p_off, groups, hq, hk, dim = offsets(queries), [0, 71, 90], [0, 4, 6], 4, 2, 64
+    x = [randn(g, off[-1], h, dim, dtype=dtype) for h in (hq, hk, hk, hq)]
+    pre = [randn(g, 90, hk, dim, dtype=dtype) for _ in range(2)]
+    where = [i32(t) for t in (off, off, p_off, groups)]
+    want = R.Shared(*x[:3], *pre, off, off, p_off, groups, None, None, True, 0.125, x[3])
+    keep = torch.ones(off[-1], dtype=torch.bool)
+    keep[off[1]:off[2]] = False
+    for i in range(4):
+        spoiled = [t.clone() for t in x]
+        spoiled[i][off[1] + 4, 0, 3] = bad
+        q, k, v, pk, pv, do = (t.cuda() for t in (*spoiled[:3], *pre, spoiled[3]))
+        out, lse = S.sched_shared_attention(q, k, v, pk, pv, *where)
+        got = out, lse.t(), *S.sched_shared_attention_grad(q, k, v, pk, pv, out, lse, do, *where)
+        for a, name in zip(got, ("out", "lse", "dq", "dk", "dv")):
+            b, bound = getattr(want, name), getattr(want, name + "_b")
+            b, bound = (t.t() if name == "lse" else t for t in (b, bound))
+            close(a[keep.cuda()], b[keep], bound[keep], (i, name))
+        shows = got[0] if i < 3 else got[2]
+        assert not bool(torch.isfinite(shows[off[1]:off[2]].float()).all())
+        for a, name in zip(got[5:], ("dpk", "dpv")):  # the other group's prefix
+            close(a[71:], getattr(want, name)[71:], getattr(want, name + "_b")[71:], (i, name))
+
+
 def test_shared_attention_grad_against_differences():
     """Along random directions, in 64 bits, at a size that bf16 holds exactly."""
     g = gen(5)
