@@ -143,10 +143,12 @@ struct Walk {
   }
 };
 
-// The tiles of a block in LDS.
-template <class T, int D>
+// The tiles of a block: arrays of their own in LDS.  (As members of one, what is read
+// of a tile would wait for the next one's loads, too: the compiler tells arrays apart,
+// not their parts.)
+template <class T>
 struct Buffers {
-  T k_even[64 * D], v_even[64 * D], k_odd[64 * D], v_odd[64 * D];
+  T *k_even, *v_even, *k_odd, *v_odd;
 };
 
 // A block's rows over the prefix keys begin <= j < end and then the own keys of the
@@ -155,7 +157,7 @@ struct Buffers {
 template <class T, int D, class OnPrefix, class OnOwn>
 __device__ __forceinline__ void over_keys(const KeyTiles<T, D, 64, 256>& prefix, int dim, int begin,
                                           int end, Walk<T, D>& walk, bool with_own,
-                                          Buffers<T, D>& lds, const OnPrefix& on_prefix,
+                                          const Buffers<T>& lds, const OnPrefix& on_prefix,
                                           const OnOwn& on_own) {
   Step step = {0, 0, 0};
   bool odd = false;  // where the first own tile is

@@ -44,12 +44,22 @@ struct Sweep {
                                       const Places<D>& places) {
     const Rows<T, D> ks = {k_tile, places.fresh()}, vs = {v_tile, ks.places};
     Acc x[kSubs];
+    scores(ks, row, x);
+    weigh(vs, row, x, j0, sees, whole, c);
+  }
+
+  // The two halves of it: products with the keys, and what follows from them.
+  __device__ __forceinline__ void scores(const Rows<T, D>& ks, int row, Acc (&x)[kSubs]) const {
 #pragma unroll
     for (int t = 0; t < kSubs; ++t) {
       x[t] = Acc(0.f);
 #pragma unroll
       for (int k = 0; k < D / 16; ++k) x[t] = product(ks.along(row + 32 * t, k), q[k], x[t]);
     }
+  }
+  template <class Sees>
+  __device__ __forceinline__ void weigh(const Rows<T, D>& vs, int row, Acc (&x)[kSubs], int j0,
+                                        const Sees& sees, bool whole, float c) {
     if (!whole) {
 #pragma unroll
       for (int t = 0; t < kSubs; ++t)

@@ -25,7 +25,7 @@ namespace {
 // written), or those of its nth sequence (true: there is one).
 template <class T, int D>
 __device__ __forceinline__ bool rows_turn(const SharedArgs& s, const RowParts& p, int block,
-                                          int tiles, Buffers<T, D>& lds, int nth) {
+                                          int tiles, const Buffers<T>& lds, int nth) {
   const AttendArgs& a = s.a;
   const bool by_one = nth >= 0;
   const Work work = work_of(block, tiles, a.q_heads / a.group);
@@ -126,7 +126,9 @@ __device__ __forceinline__ bool rows_turn(const SharedArgs& s, const RowParts& p
 template <class T, int D>
 __global__ __launch_bounds__(kThreads, 2) void shared_queries_kernel(SharedArgs s, RowParts p,
                                                                      int tiles) {
-  __shared__ __attribute__((aligned(16))) Buffers<T, D> lds;
+  __shared__ __attribute__((aligned(16))) T k_even[64 * D], v_even[64 * D];
+  __shared__ __attribute__((aligned(16))) T k_odd[64 * D], v_odd[64 * D];
+  const Buffers<T> lds = {k_even, v_even, k_odd, v_odd};
   int block = int(blockIdx.x);
   for (int nth = -1;; ++nth) {
     asm volatile("" : "+s"(block));  // a turn keeps nothing in registers for the next
