@@ -119,6 +119,7 @@ _ARGS = {
     "sched_beam_reorder": [_P, _P, _P, _I32, _P],
 }
 
+_NO_HEADS, _NOWHERE = sched_heads(), sched_tokens(None, 64, 0)  # tensors that are not there
 _F32 = _F16 = _BF16 = _INT32 = _INT64 = None  # torch's types, once it is loaded
 _torch = _types = None
 _call = {}  # the library's functions
@@ -147,7 +148,7 @@ class _Call:
     call of some microseconds is mostly what happens here, so it asks each
     tensor for as little as it needs."""
 
-    __slots__ = ("where", "device", "index", "stream", "ptr", "other")
+    __slots__ = ("where", "like", "index", "stream", "ptr", "other")
 
     def __init__(self, where: str, first, stream):
         if _torch is None:
@@ -156,7 +157,7 @@ class _Call:
         index = first.get_device() if isinstance(first, _torch.Tensor) else -1
         if index < 0 or not first.is_cuda:
             _refuse(-3, where + ": tensors are on a GPU")
-        self.index, self.device, self.stream = index, first.device, stream
+        self.index, self.like, self.stream = index, first, stream
         current = _torch._C._cuda_getCurrentRawStream(index)
         self.ptr = current if stream is None else stream.cuda_stream
         # Tensors made here belong to the call's stream, inputs to any.
@@ -170,9 +171,9 @@ class _Call:
 
     def new(self, shape, dtype):
         if not self.other:
-            return _torch.empty(shape, dtype=dtype, device=self.device)
+            return self.like.new_empty(shape, dtype=dtype)
         with _torch.cuda.stream(self.stream):
-            return _torch.empty(shape, dtype=dtype, device=self.device)
+            return self.like.new_empty(shape, dtype=dtype)
 
     def matrix(self, t) -> sched_matrix:
         self.use(t)
@@ -365,10 +366,12 @@ def sched_preference_loss(logp, ref_logp, tokens, offsets, beta: float = 0.1,
 
 
 def _heads(c: _Call, t, dtype, heads: int, dim: int) -> sched_heads:
-    c.use(t)
-    if t.dtype != dtype:
+    if c.other or t.get_device() != c.index:
+        c.use(t)
+    if t.dtype is not dtype:
         _refuse(-3, c.where + ": tensors of one type")
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim:
+    shape = t.shape
+    if len(shape) != 3 or shape[1] != heads or shape[2] != dim:
         _refuse(-2, f"{c.where}: rows x {heads} heads x {dim}")
     a, b, e = t.stride()
     if e != 1 and dim > 1:
@@ -496,26 +499,35 @@ def sched_shared_attention_grad(q, k, v, prefix_k, prefix_v, out, lse, d_out, q_
 
 
 def _rotate_desc(c, q, k, positions, frequencies, q_weight, k_weight, places, out_rows, norm, eps,
-                 interleaved):
+                 interleaved, outs=None):
+    """outs: (v or None, q_out, k_out, v_out or None) of the forward pass."""
     if q.dim() != 3 or k.dim() != 3 or k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2]:
         _refuse(-2, c.where + ": q and k are rows x heads x dim")
     rows, heads, dim = q.shape
+    kv, dtype = k.shape[1], q.dtype
     turned = 2 * frequencies.numel() if frequencies is not None else 0
-    d = sched_norm_rotate_desc()
-    d.q, d.k = _heads(c, q, q.dtype, heads, dim), _heads(c, k, q.dtype, k.shape[1], dim)
-    d.dtype, d.head_dim, d.q_heads, d.kv_heads = _types.get(q.dtype, -1), dim, heads, k.shape[1]
-    d.rows, d.out_rows = rows, rows if places is None else out_rows
-    d.positions = c.tokens(positions)
+    to = _NOWHERE
     if places is not None:
-        d.places = c.tokens(places)
+        to = c.tokens(places)
         if rows == 0:  # an empty tensor has no address
-            d.places = sched_tokens(256, d.places.bits, d.places.n)
-    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-        if w is not None:
-            setattr(d, name, c.vector(w, _F32, dim))
-    d.frequencies = c.vector(frequencies, _F32) if turned else None
-    d.turned, d.interleaved, d.norm, d.eps = turned, int(interleaved), int(norm), eps
-    return d
+            to = sched_tokens(256, to.bits, to.n)
+    else:
+        out_rows = rows
+    v = q_out = k_out = v_out = _NO_HEADS
+    if outs is not None:
+        if outs[1].shape[0] != rows or outs[2].shape[0] != out_rows:
+            _refuse(-2, c.where + ": outputs have a row per input row")
+        q_out, k_out = _heads(c, outs[1], dtype, heads, dim), _heads(c, outs[2], dtype, kv, dim)
+        if outs[0] is not None:
+            if outs[0].shape[0] != rows or outs[3].shape[0] != out_rows:
+                _refuse(-2, c.where + ": v has k's rows")
+            v, v_out = _heads(c, outs[0], dtype, kv, dim), _heads(c, outs[3], dtype, kv, dim)
+    return sched_norm_rotate_desc(
+        _heads(c, q, dtype, heads, dim), _heads(c, k, dtype, kv, dim), v, q_out, k_out, v_out,
+        _types.get(dtype, -1), dim, heads, kv, rows, out_rows, c.tokens(positions), to,
+        None if q_weight is None else c.vector(q_weight, _F32, dim),
+        None if k_weight is None else c.vector(k_weight, _F32, dim),
+        c.vector(frequencies, _F32) if turned else None, turned, int(interleaved), int(norm), eps)
 
 
 def sched_norm_rotate(q, k, positions, frequencies, q_weight=None, k_weight=None, v=None,
@@ -532,18 +544,10 @@ def sched_norm_rotate(q, k, positions, frequencies, q_weight=None, k_weight=None
         q_out = c.new(tuple(q.shape), q.dtype)
     if k_out is None:
         k_out = c.new(tuple(k.shape), q.dtype)
+    if v is not None and v_out is None:
+        v_out = c.new(tuple(v.shape), q.dtype)
     d = _rotate_desc(c, q, k, positions, frequencies, q_weight, k_weight, places, k_out.shape[0], norm,
-                     eps, interleaved)
-    kv, dim = d.kv_heads, d.head_dim
-    d.q_out, d.k_out = _heads(c, q_out, q.dtype, d.q_heads, dim), _heads(c, k_out, q.dtype, kv, dim)
-    if q_out.shape[0] != d.rows or k_out.shape[0] != d.out_rows:
-        _refuse(-2, c.where + ": outputs have a row per input row")
-    if v is not None:
-        if v_out is None:
-            v_out = c.new(tuple(v.shape), q.dtype)
-        d.v, d.v_out = _heads(c, v, q.dtype, kv, dim), _heads(c, v_out, q.dtype, kv, dim)
-        if v.shape[0] != d.rows or v_out.shape[0] != d.out_rows:
-            _refuse(-2, c.where + ": v has k's rows")
+                     eps, interleaved, (v, q_out, k_out, v_out))
     c.done("sched_norm_rotate", ctypes.byref(d))
     return (q_out, k_out) if v is None else (q_out, k_out, v_out)
 
@@ -604,7 +608,7 @@ def sched_beam_select(logits, scores, beams: int, width: Optional[int] = None, l
     if t.n != n:
         _refuse(-2, f"{c.where}: {n} tokens, not {t.n}")
     d = sched_beam_desc(m, c.vector(scores, _F32, m.rows),
-                        sched_tokens(None, 64, 0) if last is None else c.tokens(last), end_token,
+                        _NOWHERE if last is None else c.tokens(last), end_token,
                         groups, beams, width, int(stay), temperature, c.vector(new_scores, _F32, n),
                         c.vector(parents, _INT32, n), t.data, t.bits)
     need = c.bytes("sched_beam_workspace_bytes", ctypes.byref(d))
