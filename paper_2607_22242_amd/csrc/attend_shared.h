@@ -40,9 +40,40 @@ __device__ __forceinline__ Group group_at(const SharedArgs& s, int g) {
   return x;
 }
 
-// Tiles of `tile` query rows of the groups, numbered as tile_of has it.
-__device__ __forceinline__ Tile group_tile(const SharedArgs& s, int tile, int number) {
-  return tile_of([&](int g) { return first_query(s, g) * s.a.group / tile + g; }, s.n_groups, number);
+// The tile of a number, and its group: tiles of `tile` query rows of the groups, or
+// (kPrefix) of their prefix rows, numbered as tile_of has it.  Up to 63 groups are
+// asked for all that there is to know of them at once: loads that wait for one another
+// are most of a small call's time.
+struct GroupTile {
+  int index;
+  Group g;
+};
+template <bool kPrefix>
+__device__ __forceinline__ GroupTile group_tile(const SharedArgs& s, int tile, int number) {
+  if (s.n_groups >= kWave) {
+    const Tile t =
+        kPrefix ? tile_of(s.p_offsets, s.n_groups, s.p_rows, 1, tile, number)
+                : tile_of([&](int g) { return first_query(s, g) * s.a.group / tile + g; }, s.n_groups,
+                          number);
+    return {t.index, group_at(s, t.seq)};
+  }
+  const int lane = int(threadIdx.x) % kWave, at = min(lane, s.n_groups);
+  const int length = s.p_lengths && lane < s.n_groups ? s.p_lengths[lane] : 0x7fffffff;
+  const int p0 = offset_at(s.p_offsets, at, s.p_rows), seq = first_sequence(s, at);
+  const int q0 = offset_at(s.a.q_offsets, seq, s.a.q_rows);
+  const int begin = (kPrefix ? p0 / tile : q0 * s.a.group / tile) + at;
+  const uint64_t before = __ballot(lane < s.n_groups && begin <= number);
+  const int g = before ? 63 - __builtin_clzll(before) : 0;
+  auto of = [](int x, int from) { return __builtin_amdgcn_readlane(x, from); };
+  Group x;
+  x.seq = of(seq, g);
+  x.seqs = max(0, of(seq, g + 1) - x.seq);
+  x.p0 = of(p0, g);
+  x.slot = max(0, of(p0, g + 1) - x.p0);
+  x.keys = min(x.slot, max(0, of(length, g)));
+  x.q0 = of(q0, g);
+  x.queries = max(0, of(q0, g + 1) - x.q0);
+  return {number - of(begin, g), x};
 }
 
 // The sequences, among `n` from `first` on, that hold a block's lowest and highest
@@ -151,8 +182,9 @@ struct Buffers {
   T *k_even, *v_even, *k_odd, *v_odd;
 };
 
-// A block's rows over the prefix keys begin <= j < end and then the own keys of the
-// walk (with_own), each tile under way while the one before it is worked on.
+// A block's rows over the prefix keys begin <= j < end (their first tile is under way
+// in the even arrays) and then the own keys of the walk (with_own), each tile under way
+// while the one before it is worked on.
 // on_prefix(j0, k, v), on_own(step, k, v): what is done with a tile.
 template <class T, int D, class OnPrefix, class OnOwn>
 __device__ __forceinline__ void over_keys(const KeyTiles<T, D, 64, 256>& prefix, int dim, int begin,
@@ -165,7 +197,6 @@ __device__ __forceinline__ void over_keys(const KeyTiles<T, D, 64, 256>& prefix,
     if (with_own) step = walk.next(k, v);
   };
   if (begin < end) {
-    prefix.fetch(begin, lds.k_even, lds.v_even, dim);
     for (int j0 = begin;; j0 += 128) {
       tiles_barrier();  // the tile is there, and nobody reads the other buffer any more
       const bool more = j0 + 64 < end;
@@ -241,8 +272,8 @@ struct RowsOf {
   Span mine;
 
   __device__ __forceinline__ RowsOf(const SharedArgs& s, const Work& work, int tiles, int lane_row) {
-    const Tile tile = group_tile(s, kRows, tiles - 1 - work.tile);
-    g = group_at(s, tile.seq);
+    const GroupTile tile = group_tile<false>(s, kRows, tiles - 1 - work.tile);
+    g = tile.g;
     first = tile.index * kRows;
     rows = g.queries * s.a.group;
     there = tile.index >= 0 && first < rows;

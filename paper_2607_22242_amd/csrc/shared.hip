@@ -29,19 +29,18 @@ __device__ __forceinline__ bool rows_turn(const SharedArgs& s, int block, int ti
   const int lane = int(threadIdx.x) % kWave;
   RowsOf<kRowsOfBlock> r(s, work, tiles, 32 * wave_id() + lane % 32);
   if (!r.there) return false;
-  r.find(s);
-  const int alone = r.first_seq + nth;
-  if (by_one) {
-    if (alone > r.last_seq) return false;
-    tiles_barrier();  // nobody reads the last turn's tiles any more
-  }
-  const Seen seen(r.mine);
-  Sweep<T, D, kKeys / 32> w;
-  w.start(head_row<T>(a.q, r.query, r.me.head), a.dim, r.on);
-  const float c = a.scale * kLog2e;
-  const Places<D> places;
   const KeyTiles<T, D, kKeys, kThreads> prefix(s.p_k, s.p_v, r.g.p0, r.g.keys, s.near_p, a.dim,
                                                work.kv);
+  Sweep<T, D, kKeys / 32> w;
+  if (by_one) tiles_barrier();  // nobody reads the last turn's tiles any more
+  if (r.g.keys > 0) prefix.fetch(0, lds.k_even, lds.v_even, a.dim);
+  w.start(head_row<T>(a.q, r.query, r.me.head), a.dim, r.on);
+  r.find(s);
+  const int alone = r.first_seq + nth;
+  if (by_one && alone > r.last_seq) return false;
+  const Seen seen(r.mine);
+  const float c = a.scale * kLog2e;
+  const Places<D> places;
   Walk<T, D> walk(s, work.kv, by_one ? alone : r.first_seq, by_one ? alone : r.last_seq,
                   by_one ? r.last_key_of(s, alone) : r.last_key);
   over_keys<T, D>(
@@ -172,8 +171,8 @@ __device__ __forceinline__ void share_together(const SharedArgs& s, const Split&
                                                int unit, int kv, const Buffers<T>& lds) {
   const AttendArgs& a = s.a;
   const int split = unit / n.p_tiles, lane = int(threadIdx.x) % kWave;
-  const Tile tile = group_tile(s, kRowsOfBlock, unit % n.p_tiles);
-  const Group g = group_at(s, tile.seq);
+  const GroupTile tile = group_tile<false>(s, kRowsOfBlock, unit % n.p_tiles);
+  const Group& g = tile.g;
   const int first = tile.index * kRowsOfBlock, rows = g.queries * a.group;
   if (tile.index < 0 || first >= rows) return;
   const int r = first + wave_id() * 32 + lane % 32;

@@ -97,6 +97,7 @@ __device__ __forceinline__ bool rows_turn(const SharedArgs& s, const RowParts& p
     }
     if (few) w.delta = -__builtin_ldexpf(dots + __shfl_xor(dots, 32), -w.up);
   }
+  if (begin < end) prefix.fetch(begin, lds.k_even, lds.v_even, a.dim);
   Walk<T, D> walk(s, work.kv, first_seq, last_seq, last_key);
   over_keys<T, D>(
       prefix, a.dim, begin, end, walk, with_own, lds,
@@ -202,8 +203,8 @@ __device__ __forceinline__ bool keys_turn(const SharedArgs& s, const PrefixParts
   int q0, rows, block_from;
   int seq = 0, low_seq = 0, high_seq = 0;  // own keys: the lane's sequence, the block's
   if (kPrefix) {
-    const Tile tile = tile_of(s.p_offsets, s.n_groups, s.p_rows, 1, kKeysOfBlock, work.tile);
-    const Group g = group_at(s, tile.seq);
+    const GroupTile tile = group_tile<true>(s, kKeysOfBlock, work.tile);
+    const Group& g = tile.g;
     const int at = tile.index * kKeysOfBlock, j = at + wave_row + lane % 32;
     if (tile.index < 0 || at >= g.slot) return false;
     first = g.p0 + at;
