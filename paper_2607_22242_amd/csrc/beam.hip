@@ -379,6 +379,12 @@ struct Counter {
     for (int w = 0; w < kCount; ++w) c += room[turn][w];
     return c;
   }
+  // Of the last total, what the waves before this one counted.
+  __device__ __forceinline__ int before() const {
+    int c = 0;
+    for (int w = 0; w < int(threadIdx.x) / kWave; ++w) c += room[turn][w];
+    return c;
+  }
 };
 
 constexpr int kMostRanked = 1024;  // candidates that are ranked one against the other
@@ -391,7 +397,7 @@ template <class T, int kBlock, int kHeld, bool kSmall>
 __global__ __launch_bounds__(kBlock) void group_kernel(BeamArgs a) {
   __shared__ double base[kMostWidth];  // of a beam: what is added to logit / temperature, or its score
   __shared__ int state[kMostWidth], best_rank[kMostWidth], free_slots[kMostWidth];
-  __shared__ int counts[2][kBlock / kWave], found;
+  __shared__ int counts[2][kBlock / kWave];
   __shared__ uint32_t bounds[kBlock / kWave];
   __shared__ uint64_t masks[2][2], best_score[kMostRanked], sorted_score[kMostWidth];
   __shared__ uint32_t best_place[kMostRanked], sorted_place[kMostWidth];  // beam and token
@@ -460,7 +466,6 @@ __global__ __launch_bounds__(kBlock) void group_kernel(BeamArgs a) {
                      : double(score) - double(most) * a.per_temperature - log(double(sum));
     }
   }
-  if (t == 0) found = 0;
   if (t < kMostWidth) best_rank[t] = kMostWidth;
   __syncthreads();
 
@@ -528,7 +533,7 @@ __global__ __launch_bounds__(kBlock) void group_kernel(BeamArgs a) {
     for (int w = 0; w < kBlock / kWave; ++w) least = max(least, bounds[w]);
     v = max(uint64_t(least) << 32, uint64_t(1));
   }
-  int reach = v == 1 ? there : count([&](uint64_t s, uint32_t) { return s >= v; });
+  int reach = count([&](uint64_t s, uint32_t) { return s >= v; });
   uint32_t upto = ~0u;
   if (reach > kMostRanked) {
     // Many equal scores, or many results: exactly the k best, by score and place.
@@ -555,14 +560,19 @@ __global__ __launch_bounds__(kBlock) void group_kernel(BeamArgs a) {
       upto = below;
       reach = k;
     }
+    count([&](uint64_t s, uint32_t p) { return s > v || (s == v && p <= upto); });
   }
+  int at_best = counter.before();
 #pragma unroll
-  for (int i = 0; i < kHeld; ++i)
-    if (score[i] > v || (score[i] == v && place[i] <= upto)) {
-      const int at = atomicAdd(&found, 1);  // in any order: they are ranked next
-      best_score[at] = score[i];
-      best_place[at] = place[i];
+  for (int i = 0; i < kHeld; ++i) {
+    const bool in = score[i] > v || (score[i] == v && place[i] <= upto);
+    const uint64_t mask = __ballot(in);
+    if (in) {
+      best_score[at_best + lanes_before(mask)] = score[i];
+      best_place[at_best + lanes_before(mask)] = place[i];
     }
+    at_best += __popcll(mask);
+  }
   __syncthreads();
   const int got = min(there, k);
   for (int c = t; c < reach; c += kBlock) {
@@ -688,11 +698,11 @@ size_t entry_bytes(const sched_beam_desc& d, const Plan& p) {
 
 struct StateArgs {
   char* data;
-  int64_t units, rows;  // of a row, of a slot
-  int64_t outer_stride, slot_stride, row_stride;
+  int64_t rows, outer_stride, slot_stride, row_stride;
   const int32_t *parents, *lengths;
-  int32_t beams, groups, shift;  // a block has 2^shift places
-  int64_t chunks;
+  uint32_t units, per_unit;  // of a row; ceil(2^32 / units)
+  int32_t beams, shift;      // a block has 2^shift places
+  int32_t first_slot;        // parents count from the slot so many before data's
 };
 typedef uint32_t Quad __attribute__((ext_vector_type(4)));
 constexpr int kStateHeld = 16;  // units that a thread moves at once
@@ -700,20 +710,18 @@ constexpr int kStateHeld = 16;  // units that a thread moves at once
 // A block moves some places (units of 16 bytes or less) of all slots of a group:
 // it reads every slot that is followed before it writes any.
 template <class U>
-__global__ __launch_bounds__(kThreads) void reorder_kernel(StateArgs a, int64_t first) {
+__global__ __launch_bounds__(kThreads) void reorder_kernel(StateArgs a, int64_t chunk0) {
   __shared__ int from[kMostWidth], to[kMostWidth], length[kMostWidth], moves;
-  const int64_t block = first + int64_t(blockIdx.x);
-  const int64_t chunk = block % a.chunks, rest = block / a.chunks;
-  const int64_t slot0 = rest % a.groups * a.beams;
-  const int64_t begin = chunk << a.shift, row = begin / a.units;  // the chunk's first place
-  const uint32_t units = uint32_t(a.units), unit = uint32_t(begin - row * a.units);
-  char* const data = a.data + rest / a.groups * a.outer_stride + slot0 * a.slot_stride +
-                     row * a.row_stride;
   const int t = int(threadIdx.x), size = 1 << a.shift;
+  const int64_t slot0 = int64_t(blockIdx.y) * a.beams;
+  const int64_t begin = (chunk0 + blockIdx.x) << a.shift;  // the chunk's first place
+  const int64_t row = begin >> 32 ? begin / a.units : uint32_t(begin) / a.units;
+  const uint32_t unit = uint32_t(begin - row * a.units);
+  char* const data = a.data + blockIdx.z * a.outer_stride + slot0 * a.slot_stride + row * a.row_stride;
   if (t == 0) moves = 0;
   __syncthreads();
   if (t < a.beams) {
-    const int64_t p = a.parents[slot0 + t];
+    const int64_t p = int64_t(a.parents[slot0 + t]) - a.first_slot;
     if (p >= slot0 && p < slot0 + a.beams && p != slot0 + t) {
       const int64_t rows = a.lengths ? min(a.rows, int64_t(max(a.lengths[p], 0))) : a.rows;
       if (rows * a.units > begin) {
@@ -729,9 +737,11 @@ __global__ __launch_bounds__(kThreads) void reorder_kernel(StateArgs a, int64_t 
   if (work == 0) return;
   U held[kStateHeld];
   auto place = [&](int i, int slot) {
+    // Less than 2 rows where rows have 4,096 units or more, else less than 2^13 units.
     const uint32_t at = unit + uint32_t(i & (size - 1));
-    return reinterpret_cast<U*>(data + slot * a.slot_stride + int64_t(at / units) * a.row_stride) +
-           at % units;
+    const uint32_t r = a.units >= 4096 ? at >= a.units : a.per_unit ? __umulhi(at, a.per_unit) : at;
+    return reinterpret_cast<U*>(data + slot * a.slot_stride + int64_t(r) * a.row_stride) +
+           (at - r * a.units);
   };
 #pragma unroll
   for (int n = 0; n < kStateHeld; ++n) {
@@ -749,16 +759,28 @@ __global__ __launch_bounds__(kThreads) void reorder_kernel(StateArgs a, int64_t 
 
 template <class U>
 hipError_t reorder(const sched_states& x, StateArgs a, hipStream_t s) {
-  a.units = x.row_bytes / int64_t(sizeof(U));
+  a.units = uint32_t(x.row_bytes / int64_t(sizeof(U)));
+  a.per_unit = uint32_t(((uint64_t(1) << 32) + a.units - 1) / a.units);
   a.shift = 12;
   while ((kStateHeld * kThreads >> a.shift) < a.beams) --a.shift;
-  a.chunks = (a.units * x.rows + (1 << a.shift) - 1) >> a.shift;
-  const int64_t blocks = a.chunks * a.groups * x.outer;
-  for (int64_t b = 0; b < blocks; b += kMostBlocks) {
-    hipLaunchKernelGGL((reorder_kernel<U>), dim3(unsigned(std::min(blocks - b, kMostBlocks))),
-                       dim3(kThreads), 0, s, a, b);
-    if (const hipError_t e = hipGetLastError()) return e;
-  }
+  const int64_t chunks = (int64_t(a.units) * x.rows + (1 << a.shift) - 1) >> a.shift;
+  const int64_t groups = x.slots / a.beams;
+  constexpr int64_t kMostY = 65535;  // of a grid's second and third side
+  const int32_t* const parents = a.parents;
+  const int32_t* const lengths = a.lengths;
+  for (int64_t z = 0; z < x.outer; z += kMostY)
+    for (int64_t y = 0; y < groups; y += kMostY)
+      for (int64_t c = 0; c < chunks; c += kMostBlocks) {
+        // A part's groups are counted from its first.
+        a.data = static_cast<char*>(x.data) + z * x.outer_stride + y * a.beams * x.slot_stride;
+        a.parents = parents + y * a.beams;
+        a.lengths = lengths ? lengths + y * a.beams : nullptr;
+        a.first_slot = int32_t(y * a.beams);
+        const dim3 grid(unsigned(std::min(chunks - c, kMostBlocks)), unsigned(std::min(groups - y, kMostY)),
+                        unsigned(std::min(x.outer - z, kMostY)));
+        hipLaunchKernelGGL((reorder_kernel<U>), grid, dim3(kThreads), 0, s, a, c);
+        if (const hipError_t e = hipGetLastError()) return e;
+      }
   return hipSuccess;
 }
 
@@ -814,7 +836,6 @@ hipError_t launch_beam_reorder(const sched_states& x, const int32_t* parents, co
   a.parents = parents;
   a.lengths = lengths;
   a.beams = beams;
-  a.groups = int32_t(x.slots / beams);
   const uint64_t all = reinterpret_cast<uintptr_t>(x.data) | uint64_t(x.row_bytes) |
                        uint64_t(x.outer > 1 ? x.outer_stride : 0) | uint64_t(x.slot_stride) |
                        uint64_t(x.rows > 1 ? x.row_stride : 0);
