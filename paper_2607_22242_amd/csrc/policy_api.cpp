@@ -435,6 +435,11 @@ int sched_beam_select(const sched_beam_desc* d, void* d_workspace, size_t ws_byt
   if (d->end_token < -1 || (d->token_bits == 32 && d->end_token > INT32_MAX)) return SCHED_E_VALUE;
   if (int e = check_temperature(d->temperature)) return e;
   if (d->n_groups > 0 && (!d->scores || !d->new_scores || !d->parents)) return SCHED_E_NULL;
+  // In place a group's results take the place of its own beams, which it alone reads.
+  if (d->n_groups > 0 && ((d->new_scores == d->scores && d->width != d->beams) ||
+                          (d->last.data && d->tokens == d->last.data &&
+                           (d->width != d->beams || d->token_bits != d->last.bits))))
+    return SCHED_E_VALUE;
   if (int e = check_workspace(d_workspace, ws_bytes, beam_bytes(*d))) return e;
   return done(launch_beam_select(*d, d_workspace, stream_of(hip_stream)));
 }

@@ -121,7 +121,10 @@ def test_beam_select(lib):
     for bad in (dict(stay=2), dict(temperature=0.0), dict(temperature=math.nan), dict(temperature=3e-39),
                 dict(token_bits=16), dict(end_token=-2), dict(end_token=1 << 31, token_bits=32),
                 dict(last=tokens(12, 8)), dict(logits=matrix(dtype=5)), dict(logits=matrix(data=FAKE + 2)),
-                dict(tokens=FAKE + 4)):
+                dict(tokens=FAKE + 4),
+                # In place where a group has as many results as beams.
+                dict(width=3, stay=0, tokens=FAKE * 2), dict(width=3, stay=0, new_scores=FAKE * 2),
+                dict(token_bits=32)):
         assert rc(**bad) == VALUE, bad
     for bad in (dict(logits=matrix(data=0)), dict(scores=0), dict(new_scores=0), dict(parents=0), dict(tokens=0)):
         assert rc(**bad) == NULL, bad

@@ -265,6 +265,19 @@ def test_equal_scores_go_to_the_first(dtype, vocab, beams, width):
         assert torch.equal(got[1].cpu().long(), want[1]) and torch.equal(got[2].cpu(), want[2])
 
 
+@pytest.mark.parametrize("vocab", [40, 5003])
+@pytest.mark.parametrize("stay", [False, True])
+def test_beams_in_place(vocab, stay):
+    g = gen(vocab)
+    logits, scores = randn(g, 24, vocab).cuda(), randn(g, 24).cuda()
+    last = torch.randint(0, 5, (24,), generator=g).cuda()
+    want = S.sched_beam_select(logits, scores, 6, last=last, end_token=2, stay=stay)
+    got = S.sched_beam_select(logits, scores, 6, last=last, end_token=2, stay=stay, new_scores=scores, tokens=last)
+    assert got[0] is scores and got[2] is last
+    for x, y in zip(got, want):
+        assert torch.equal(x, y)
+
+
 def test_zeros_of_both_signs_are_equal():
     x = torch.tensor([[-0.0, 0.0, -0.0, -1.0]])
     got = S.sched_beam_select(x.cuda(), torch.zeros(1).cuda(), 1, 4)
@@ -672,3 +685,95 @@ def test_captured_in_a_graph():
         torch.cuda.synchronize()
         for a, b in zip((*got, states), (*want, eager[2])):
             assert torch.equal(a, b)
+
+
+# --- far rows ------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("step", [(1 << 23) + 8, (1 << 24) + 8])
+def test_rows_far_apart(step):
+    """Offsets that pass 32 bits, at distances that a tile's lanes can add up and at
+    others: the same bits as rows next to each other."""
+    g = gen(30)
+    dim, kv, rows = 64, 2, 264
+    whole = torch.empty((rows - 1) * step + 2 * kv * dim, dtype=torch.bfloat16, device="cuda")
+    far = whole.as_strided((rows, 2 * kv, dim), (step, dim, 1))
+    near = randn(g, rows, 2 * kv, dim, dtype=torch.bfloat16).cuda()
+    far.copy_(near)
+    q = randn(g, 60, 4, dim, dtype=torch.bfloat16).cuda()
+
+    def run(x, grads, **kw):
+        pre, own = x[:200], x[200:]
+        where = [i32(t) for t in ([0, 25, 60], [0, 30, 64], [0, 200], [0, 2])]
+        args = (q, own[:, :kv], own[:, kv:], pre[:, :kv], pre[:, kv:])
+        out, lse = S.sched_shared_attention(*args, *where, **kw)
+        to = {} if grads is None else dict(d_k=grads[200:, :kv], d_v=grads[200:, kv:],
+                                           d_prefix_k=grads[:200, :kv], d_prefix_v=grads[:200, kv:])
+        return out, lse, *S.sched_shared_attention_grad(*args, out, lse, q, *where, **kw, **to)
+
+    for lengths in (None, i32([30, 17])):
+        want = run(near, None, k_lengths=lengths)
+        for a, b in zip(want, run(far, None, k_lengths=lengths)):
+            assert torch.equal(a, b)
+    far.zero_()
+    got = run(near, far)
+    for a, b in zip(run(near, None), got):
+        assert torch.equal(a, b)
+    # Rows of a cache as far apart, and the gradient from there.
+    pos, freq = torch.arange(rows, device="cuda"), torch.rand(32, generator=g).cuda()
+    places = torch.randperm(rows, generator=g).cuda()
+    k, v = near[:, :kv], near[:, kv:]
+    a = S.sched_norm_rotate(k, k, pos, freq, v=v)
+    b = S.sched_norm_rotate(k, k, pos, freq, v=v, places=places, k_out=far[:, :kv], v_out=far[:, kv:])
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1][places]) and torch.equal(a[2], b[2][places])
+    a = S.sched_norm_rotate_grad(k, k, k, far[:, :kv][places], pos, freq)
+    b = S.sched_norm_rotate_grad(k, k, k, far[:, :kv], pos, freq, places=places)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_states_of_more_than_4_gib():
+    n = (1 << 30) + 24  # of 4 bytes
+    x = torch.arange(n, dtype=torch.int32, device="cuda")
+    states = torch.stack([x, x * 3, x * 5]).view(1, 3, 8, -1)
+    S.sched_beam_reorder(states, i32([2, 0, 1]), 3)
+    for i, f in enumerate((5, 1, 3)):
+        assert torch.equal(states[0, i].view(-1), x * f)
+
+
+def test_beam_select_of_the_longest_rows():
+    g = gen(31)
+    vocab = 1 << 22
+    logits, scores = torch.randn((3, vocab), generator=g).cuda() * 3, torch.tensor([-1.0, -2.0, -1.5]).cuda()
+    logits[0, -1], logits[1, -1] = 19.0, 21.0
+    z = torch.log_softmax(logits.double(), 1) + scores.double()[:, None]
+    best = z.view(-1).topk(7)
+    assert float((best.values[:-1] - best.values[1:]).min()) > 1e-5
+    got = S.sched_beam_select(logits, scores, 3, 6)
+    assert torch.equal(got[1].long(), best.indices[:-1] // vocab)
+    assert torch.equal(got[2], best.indices[:-1] % vocab)
+
+
+def test_calls_at_once():
+    """The same calls on two streams at a time, with workspaces of their own."""
+    g = gen(32)
+    logits = [randn(g, 16, 30011).cuda() for _ in range(2)]
+    scores = torch.zeros(16, device="cuda")
+    h = [randn(g, 900, 4, 64, dtype=torch.bfloat16).cuda() for _ in range(2)]
+    where = [i32(t) for t in ([0, 400, 900], [0, 400, 900], [0, 900], [0, 2])]
+
+    def run(i, **kw):
+        a = (h[i],) * 5
+        out, lse = S.sched_shared_attention(*a, *where, **kw)
+        return (*S.sched_beam_select(logits[i], scores, 8, **kw), out, lse,
+                *S.sched_shared_attention_grad(*a, out, lse, h[i], *where, **kw))
+
+    want = [run(0), run(1)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    got = [[run(i, stream=streams[i]) for i in range(2)] for _ in range(3)]
+    torch.cuda.synchronize()
+    for pair in got:
+        for a, b in zip(pair, want):
+            for x, y in zip(a, b):
+                assert torch.equal(x, y)
