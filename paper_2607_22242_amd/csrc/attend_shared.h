@@ -125,8 +125,9 @@ __device__ __forceinline__ int wave_most(int x) {
 }
 
 // The tiles of 64 own keys that a block's rows meet: of the sequences seq ..
-// last_seq, of the last one up to last_key.  Without k_lengths the sequences' keys lie
-// one behind the other and count as one; else a sequence is walked after the other.
+// last_seq, from first_key on and of the last one up to last_key.  Without k_lengths
+// the sequences' keys lie one behind the other and count as one, and nothing more has
+// to be known of them; else a sequence is walked after the other.
 struct Step {
   int key0, last;  // the tile's first key, and the last that counts, of all key rows
   int there;
@@ -138,28 +139,29 @@ struct Walk {
   int kv, seq, last_seq, last_key, base, place;  // place: of the next tile, from base
 
   __device__ __forceinline__ Walk(const SharedArgs& s_, int kv_, int first_seq, int last_seq_,
-                                  int last_key_)
+                                  int first_key, int last_key_)
       : s(s_), own(s_.a.k, s_.a.v, 0, 0, s_.a.near_k, s_.a.dim, kv_), kv(kv_), seq(first_seq - 1),
-        last_seq(last_seq_), last_key(last_key_), base(0), place(0) {}
+        last_seq(last_seq_), last_key(last_key_), base(0), place(0) {
+    if (s.a.k_lengths) return;
+    seq = last_seq;
+    go_to(first_key, last_key + 1);
+  }
 
+  __device__ __forceinline__ void go_to(int from, int behind) {
+    base = from;
+    place = 0;
+    own.keys = behind - base;
+    own.k = reinterpret_cast<const char*>(head_row<T>(s.a.k, base, kv));
+    own.v = reinterpret_cast<const char*>(head_row<T>(s.a.v, base, kv));
+  }
   // Own keys of the next sequence that has any.
   __device__ __forceinline__ bool enter() {
     while (++seq <= last_seq) {
       const Seq q = sequence(s.a, seq);
       int behind = q.k0 + q.keys;
-      if (s.a.k_lengths) {
-        if (seq == last_seq) behind = min(behind, last_key + 1);
-        if (q.queries == 0) continue;
-      } else {
-        behind = last_key + 1;
-        seq = last_seq;
-      }
-      if (behind <= q.k0) continue;
-      base = q.k0;
-      place = 0;
-      own.keys = behind - base;
-      own.k = reinterpret_cast<const char*>(head_row<T>(s.a.k, base, kv));
-      own.v = reinterpret_cast<const char*>(head_row<T>(s.a.v, base, kv));
+      if (seq == last_seq) behind = min(behind, last_key + 1);
+      if (q.queries == 0 || behind <= q.k0) continue;
+      go_to(q.k0, behind);
       return true;
     }
     return false;
@@ -296,7 +298,10 @@ struct RowsOf {
     const int last = own_keys(s.a, tail, high).hi;
     last_key = uniform(last_seq > first_seq ? max(last, tail.k0 - 1) : last);
   }
-  // The last key that rows of the tile see of one of its sequences.
+  // The first and the last key that rows of the tile see of one of its sequences.
+  __device__ __forceinline__ int first_key_of(const SharedArgs& s, int b) const {
+    return uniform(offset_at(s.a.k_offsets, b, s.a.k_rows));
+  }
   __device__ __forceinline__ int last_key_of(const SharedArgs& s, int b) const {
     if (b == last_seq) return last_key;
     const Seq q = sequence(s.a, b);

@@ -42,6 +42,7 @@ __device__ __forceinline__ bool rows_turn(const SharedArgs& s, int block, int ti
   const float c = a.scale * kLog2e;
   const Places<D> places;
   Walk<T, D> walk(s, work.kv, by_one ? alone : r.first_seq, by_one ? alone : r.last_seq,
+                  by_one ? r.first_key_of(s, alone) : r.first_key,
                   by_one ? r.last_key_of(s, alone) : r.last_key);
   over_keys<T, D>(
       prefix, a.dim, 0, r.g.keys, walk, true, lds,

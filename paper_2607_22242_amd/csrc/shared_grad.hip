@@ -74,6 +74,7 @@ __device__ __forceinline__ bool rows_turn(const SharedArgs& s, const RowParts& p
   const KeyTiles<T, D, kTile, kThreads> prefix(s.p_k, s.p_v, r.g.p0, r.g.keys, s.near_p, a.dim,
                                                work.kv);
   const int first_seq = by_one ? alone : r.first_seq, last_seq = by_one ? alone : r.last_seq;
+  const int first_key = by_one ? r.first_key_of(s, alone) : r.first_key;
   const int last_key = by_one ? r.last_key_of(s, alone) : r.last_key;
   if (by_one) tiles_barrier();  // nobody reads the last turn's tiles any more
   // Rows that see a tile's worth of keys at most take delta from the probabilities,
@@ -89,7 +90,7 @@ __device__ __forceinline__ bool rows_turn(const SharedArgs& s, const RowParts& p
       if (few) dots += w.dots(lds.k_even, lds.v_even, 0, UpTo{r.g.keys - 1}, c, places);
       tiles_barrier();
     }
-    Walk<T, D> walk(s, work.kv, first_seq, last_seq, last_key);
+    Walk<T, D> walk(s, work.kv, first_seq, last_seq, first_key, last_key);
     for (Step t = walk.next(lds.k_even, lds.v_even); t.there; t = walk.next(lds.k_even, lds.v_even)) {
       tiles_barrier();
       if (few && seen.any(t)) dots += w.dots(lds.k_even, lds.v_even, t.key0, seen.keys(t), c, places);
@@ -98,7 +99,7 @@ __device__ __forceinline__ bool rows_turn(const SharedArgs& s, const RowParts& p
     if (few) w.delta = -__builtin_ldexpf(dots + __shfl_xor(dots, 32), -w.up);
   }
   if (begin < end) prefix.fetch(begin, lds.k_even, lds.v_even, a.dim);
-  Walk<T, D> walk(s, work.kv, first_seq, last_seq, last_key);
+  Walk<T, D> walk(s, work.kv, first_seq, last_seq, first_key, last_key);
   over_keys<T, D>(
       prefix, a.dim, begin, end, walk, with_own, lds,
       [&](int j0, const T* k, const T* v) {
@@ -124,8 +125,16 @@ __device__ __forceinline__ bool rows_turn(const SharedArgs& s, const RowParts& p
   return by_one;
 }
 
+// Heads of up to 64 elements leave room for three blocks on a unit, not two, if some
+// registers that hardly anything asks for go to memory: over 16 answers of 300 tokens
+// to each of 4 prompts of 2,000, 16 heads of 64, dQ 343 -> 308 us and dK and dV 452 ->
+// 443 (f16: 366 -> 328, 490 -> 512); over 13 times 64 answers of 14 tokens, 4 heads of
+// 32, 19 -> 20.6 and 22.5 -> 19.5.
+template <int D>
+constexpr int kBlocksOfUnit = D == 64 ? 3 : 2;
+
 template <class T, int D>
-__global__ __launch_bounds__(kThreads, 2) void shared_queries_kernel(SharedArgs s, RowParts p,
+__global__ __launch_bounds__(kThreads, kBlocksOfUnit<D>) void shared_queries_kernel(SharedArgs s, RowParts p,
                                                                      int tiles) {
   __shared__ __attribute__((aligned(16))) T k_even[64 * D], v_even[64 * D];
   __shared__ __attribute__((aligned(16))) T k_odd[64 * D], v_odd[64 * D];
@@ -364,7 +373,7 @@ __device__ __forceinline__ bool keys_turn(const SharedArgs& s, const PrefixParts
 }
 
 template <class T, int D>
-__global__ __launch_bounds__(kThreads, 2) void shared_keys_kernel(SharedArgs s, PrefixParts p,
+__global__ __launch_bounds__(kThreads, kBlocksOfUnit<D>) void shared_keys_kernel(SharedArgs s, PrefixParts p,
                                                                   int p_tiles, int p_blocks,
                                                                   int tiles) {
   __shared__ __attribute__((aligned(16))) T q_even[kTile * D], o_even[kTile * D];

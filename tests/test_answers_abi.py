@@ -229,3 +229,22 @@ def test_binding_refuses_tensors_of_the_host():
         with pytest.raises(S.SchedError) as e:
             call()
         assert e.value.name == "SCHED_E_VALUE"
+
+
+@pytest.mark.parametrize("kind", [P.sched_heads, P.sched_attention_desc, P.sched_shared_desc, P.sched_shared_grads,
+                                  P.sched_norm_rotate_desc, P.sched_beam_desc])
+def test_values_packed_at_once_are_the_structure(kind):
+    values = []
+
+    def fill(kind):
+        made = kind()
+        for name, of in kind._fields_:
+            if issubclass(of, ctypes.Structure):
+                setattr(made, name, fill(of))
+            else:
+                values.append(len(values) + 1.5 if of is ctypes.c_float else 7 * len(values) + 3)
+                setattr(made, name, values[-1])
+        return made
+
+    whole = fill(kind)
+    assert P._packer(kind)(*values) == bytes(whole)
