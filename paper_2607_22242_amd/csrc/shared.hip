@@ -92,6 +92,7 @@ constexpr int kWaves = kThreads / kWave;
 struct Shares {
   int p_tiles, p_splits;  // together: tiles of 128 rows of the groups, shares of the prefix
   int o_tiles, o_splits;  // apart: tiles of 32 rows of the sequences, shares of their own keys
+  int p_first;            // those of the prefix come first, else both kinds in turn
   int units;              // of kv_heads blocks each, of both kinds
 };
 
@@ -264,10 +265,11 @@ __global__ __launch_bounds__(kThreads, 2) void shares_kernel(SharedArgs s, Split
   const Buffers<T> lds = {k_even, v_even, k_odd, v_odd};
   const int kv_heads = s.a.q_heads / s.a.group;
   const int unit = int(blockIdx.x) / kv_heads, kv = int(blockIdx.x) % kv_heads;
-  // Both kinds in turn, as often as there are of each.
+  // Those of the prefix are spread over all units, as many as there are, or over the first.
   const int p_units = n.p_tiles * n.p_splits;
-  const int together = int(int64_t(unit) * p_units / n.units);
-  if (int(int64_t(unit + 1) * p_units / n.units) > together) {
+  const int spread = n.p_first ? p_units : n.units;
+  const int together = int(int64_t(min(unit, spread)) * p_units / spread);
+  if (unit < spread && int(int64_t(unit + 1) * p_units / spread) > together) {
     share_together<T, D>(s, p, n, together, kv, lds);
     return;
   }
@@ -355,8 +357,14 @@ Plan plan_of(const sched_shared_desc& x) {
   p.split = (d.k_lengths && rows / d.n_seqs <= 32) || blocks < 128;
   if (!p.split) return p;
   // Shares of the prefix for some 448 blocks, so that the card's 512 places take own
-  // keys beside them (2 groups of 96 rows, 16,000 keys: 42 us so, 50 with 512 of them);
-  // of own keys for 1,024 waves; none of less than 256 and 128 keys on average.
+  // keys beside them; of own keys for 2,048 waves (2 groups of 4 sequences, 64 heads, 8
+  // key heads, prompts of 1,000 to 2,000, 1,000 to 4,000 own keys: 31 us, 39 with 1,024;
+  // 4 sequences of 10,000 to 30,000 own keys: 88, 96); none of less than 256 and 128
+  // keys on average.  A group's rows that are one wave's leave the prefix bound by
+  // memory, too, and its blocks, the longest, come first (prompts of 20,000 to 32,000,
+  // up to 2,000 own keys: 73 us, 80 in turn); more rows compute, and memory is kept busy
+  // by own keys beside them (8 groups of 64 sequences: 147 us in turn, 155 one after the
+  // other; one group of 16 with a prompt of 31,000: 61 and 68).
   Shares& n = p.n;
   n.p_tiles = int(tile_count(rows, x.n_groups, kRowsOfBlock));
   n.o_tiles = int(tile_count(rows, d.n_seqs, 32));
@@ -367,8 +375,9 @@ Plan plan_of(const sched_shared_desc& x) {
   const int64_t of_group = (rows / x.n_groups + kRowsOfBlock - 1) / kRowsOfBlock;
   n.p_splits = splits(x.n_groups * std::max<int64_t>(of_group, 1) * d.kv_heads, 448,
                       x.prefix_rows / x.n_groups, 256);
-  n.o_splits = splits(n.o_tiles * int64_t(d.kv_heads), 1024, d.k_rows / d.n_seqs, 128);
+  n.o_splits = splits(n.o_tiles * int64_t(d.kv_heads), 2048, d.k_rows / d.n_seqs, 128);
   n.units = n.p_tiles * n.p_splits + (n.o_tiles * n.o_splits + kWaves - 1) / kWaves;
+  n.p_first = rows / x.n_groups <= 32;
   p.parts = n.p_splits + n.o_splits;
   return p;
 }
