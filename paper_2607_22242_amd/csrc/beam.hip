@@ -387,7 +387,7 @@ struct Counter {
   }
 };
 
-constexpr int kMostRanked = 1024;  // candidates that are ranked one against the other
+constexpr int kMostRanked = 256;  // candidates that are ranked one against the other
 enum State : int { kNone, kLive, kFinished };
 
 // A block takes a group.  kSmall: the group's logits themselves (kHeld kBlock at
@@ -398,7 +398,7 @@ __global__ __launch_bounds__(kBlock) void group_kernel(BeamArgs a) {
   __shared__ double base[kMostWidth];  // of a beam: what is added to logit / temperature, or its score
   __shared__ int state[kMostWidth], best_rank[kMostWidth], free_slots[kMostWidth];
   __shared__ int counts[2][kBlock / kWave];
-  __shared__ uint32_t bounds[kBlock / kWave];
+  __shared__ uint32_t bounds[3][kBlock / kWave];
   __shared__ uint64_t masks[2][2], best_score[kMostRanked], sorted_score[kMostWidth];
   __shared__ uint32_t best_place[kMostRanked], sorted_place[kMostWidth];  // beam and token
   const int group = int(blockIdx.x), t = int(threadIdx.x), lane = t % kWave, wave = t / kWave;
@@ -484,8 +484,8 @@ __global__ __launch_bounds__(kBlock) void group_kernel(BeamArgs a) {
   }
 
   // What may be among the k best.  Every wave finds a bound that k of its own scores
-  // reach, and not many more, bit by bit; what reaches the greatest of them is ranked
-  // one against the other.
+  // reach, and not many more, bit by bit; where what reaches the greatest of them is still
+  // many the waves go on together, and the rest is ranked one against the other.
   Counter<kBlock / kWave> counter = {counts, 0};
   auto in_wave = [&](auto in) {
     int c = 0;
@@ -497,20 +497,21 @@ __global__ __launch_bounds__(kBlock) void group_kernel(BeamArgs a) {
   auto count = [&](auto in) { return counter.total(in_wave(in)); };
   uint32_t least = 0;  // of the order's upper half
   const int mine = in_wave([&](uint64_t s, uint32_t) { return s > 0; });
-  if (n > 256) {
-    if (mine > 2 * k) {
-      uint32_t hi = 0, lo = ~0u;
+  if (n > kMostRanked) {
+    uint32_t hi = 0, lo = ~0u;
 #pragma unroll
-      for (int i = 0; i < kHeld; ++i)
-        if (score[i] > 0) {
-          hi = max(hi, uint32_t(score[i] >> 32));
-          lo = min(lo, uint32_t(score[i] >> 32));
-        }
-#pragma unroll
-      for (int d = 32; d; d >>= 1) {
-        hi = max(hi, uint32_t(__shfl_xor(int(hi), d)));
-        lo = min(lo, uint32_t(__shfl_xor(int(lo), d)));
+    for (int i = 0; i < kHeld; ++i)
+      if (score[i] > 0) {
+        hi = max(hi, uint32_t(score[i] >> 32));
+        lo = min(lo, uint32_t(score[i] >> 32));
       }
+#pragma unroll
+    for (int d = 32; d; d >>= 1) {
+      hi = max(hi, uint32_t(__shfl_xor(int(hi), d)));
+      lo = min(lo, uint32_t(__shfl_xor(int(lo), d)));
+    }
+    least = mine ? lo : 0;
+    if (mine > 2 * k) {
       int bit = 31 - __clz(int(hi ^ lo));  // the bits above are all scores'
       least = bit < 0 ? hi : hi >> bit >> 1 << bit << 1;
       int reach = mine;
@@ -524,19 +525,45 @@ __global__ __launch_bounds__(kBlock) void group_kernel(BeamArgs a) {
         }
       }
     }
-    if (lane == 0) bounds[wave] = least;
+    if (lane == 0) {
+      bounds[0][wave] = mine >= k ? least : 0;
+      bounds[1][wave] = mine ? lo : ~0u;
+      bounds[2][wave] = hi;
+    }
   }
   const int there = counter.total(mine);
   uint64_t v = 1;
-  if (n > 256) {
+  uint32_t low = ~0u, high = 0;  // of all scores
+  if (n > kMostRanked) {
+    least = 0;
 #pragma unroll
-    for (int w = 0; w < kBlock / kWave; ++w) least = max(least, bounds[w]);
+    for (int w = 0; w < kBlock / kWave; ++w) {
+      least = max(least, bounds[0][w]);
+      low = min(low, bounds[1][w]);
+      high = max(high, bounds[2][w]);
+    }
     v = max(uint64_t(least) << 32, uint64_t(1));
   }
   int reach = count([&](uint64_t s, uint32_t) { return s >= v; });
+  if (reach > kMostRanked) {  // the waves together, in the same way
+    low = max(low, least);
+    int bit = 31 - __clz(int(high ^ low));
+    least = bit < 0 ? high : high >> bit >> 1 << bit << 1;
+#pragma unroll 1
+    for (; bit >= 0 && reach > kMostRanked; --bit) {
+      const uint32_t bound = least | 1u << bit;
+      const int c = count([&](uint64_t s, uint32_t) { return uint32_t(s >> 32) >= bound; });
+      if (c >= k) {
+        least = bound;
+        reach = c;
+      }
+    }
+    v = max(uint64_t(least) << 32, v);
+    reach = count([&](uint64_t s, uint32_t) { return s >= v; });
+  }
   uint32_t upto = ~0u;
   if (reach > kMostRanked) {
-    // Many equal scores, or many results: exactly the k best, by score and place.
+    // Many equal scores: exactly the k best, by score and place.
     v = 0;
     reach = there;
 #pragma unroll 1
@@ -575,17 +602,23 @@ __global__ __launch_bounds__(kBlock) void group_kernel(BeamArgs a) {
   }
   __syncthreads();
   const int got = min(there, k);
-  for (int c = t; c < reach; c += kBlock) {
+  {
+    constexpr int kSides = kBlock / kMostRanked;  // threads that rank one
+    const int c = t / kSides;
     const uint64_t s = best_score[c];
     const uint32_t p = best_place[c];
     int rank = 0;
+    if (c < reach) {
 #pragma unroll 8
-    for (int i = 0; i < reach; ++i) {
-      const uint64_t other = best_score[i];
-      const uint32_t at = best_place[i];
-      rank += int(other > s) | (int(other == s) & int(at < p));
+      for (int i = t % kSides; i < reach; i += kSides) {
+        const uint64_t other = best_score[i];
+        const uint32_t at = best_place[i];
+        rank += int(other > s) | (int(other == s) & int(at < p));
+      }
     }
-    if (rank < k) {
+#pragma unroll
+    for (int d = 1; d < kSides; d *= 2) rank += __shfl_xor(rank, d);
+    if (c < reach && t % kSides == 0 && rank < k) {
       sorted_score[rank] = s;
       sorted_place[rank] = p;
     }
@@ -644,9 +677,13 @@ constexpr int kMostHeld = 16;  // candidates of a thread of 1024
 Plan plan_of(const sched_beam_desc& d) {
   Plan p = {};
   const int64_t cols = d.logits.cols, rows = d.logits.rows;
+  // The group's block reads the logits itself where they are few: 13 groups of 16 beams,
+  // 128 logits 13.2 us, 17.3 by strips; of 64 beams, 16 logits 14.1 and 21.5; of 32 beams,
+  // 128 logits 19.0 and 16.7; of 8 beams, 400 logits, which it does not, 14.2 and 12.8.
   p.small = cols <= 4 * kWave && cols * d.beams <= 4096;
   const int64_t chunks = (cols + kChunk - 1) / kChunk;
-  // Some 4096 waves, as far as rows are long enough.
+  // Some 4096 waves, as far as rows are long enough (256 rows of 131,072, with the groups'
+  // blocks: 47 us; 2,048 waves 49, 8,192 58).
   const int64_t want = std::min<int64_t>(
       {std::max<int64_t>(1, 4096 / std::max<int64_t>(rows, 1)), chunks, int64_t(kMostStrips)});
   p.strip_chunks = int((chunks + want - 1) / want);
@@ -662,12 +699,20 @@ hipError_t group(const BeamArgs& a, int groups, hipStream_t s) {
   return hipGetLastError();
 }
 
+// Blocks of 256 threads for a group of up to 256 candidates, where there is a group for
+// every unit at least or hardly anything to rank; else of 1024, four of which rank one
+// candidate (13 groups of 192: 6.8 us, 8.9 with 256; of 12: 5.0 and 4.4; 1,024 groups of
+// 128: 20.5 and 8.9).
+bool narrow(int candidates, int groups) {
+  return candidates <= 256 && (candidates <= 64 || groups > 256);
+}
+
 template <class T>
 hipError_t select(BeamArgs a, const Plan& p, int groups, hipStream_t s) {
   const int64_t each = p.small ? a.cols : a.lists * a.width;
   a.per_each = uint32_t(((uint64_t(1) << 32) + each - 1) / each);
   if (p.small) {
-    if (a.cols * a.beams <= 256) return group<T, 256, 1, true>(a, groups, s);
+    if (narrow(a.cols * a.beams, groups)) return group<T, 256, 1, true>(a, groups, s);
     if (a.cols * a.beams <= 1024) return group<T, 1024, 1, true>(a, groups, s);
     return group<T, 1024, 4, true>(a, groups, s);
   }
@@ -684,7 +729,7 @@ hipError_t select(BeamArgs a, const Plan& p, int groups, hipStream_t s) {
     if (const hipError_t e = hipGetLastError()) return e;
   }
   const int n = a.beams * a.lists * a.width;
-  if (n <= 256) return group<float, 256, 1, false>(a, groups, s);
+  if (narrow(n, groups)) return group<float, 256, 1, false>(a, groups, s);
   if (n <= 1024) return group<float, 1024, 1, false>(a, groups, s);
   if (n <= 4096) return group<float, 1024, 4, false>(a, groups, s);
   return group<float, 1024, kMostHeld, false>(a, groups, s);
