@@ -5,7 +5,12 @@
 // best logits (a continuation that is not among its strip's best is not among
 // the group's) and what the sum of powers needs; a block per group then gives
 // the strips' best their scores and takes the best of those.  Bound by the
-// logits' bytes where rows are long.
+// logits' bytes where rows are long, and by what waits for one another in a
+// group's block where they are short.  16 groups of 16 beams, 131,072 logits in
+// bfloat16: strips 29 us (67 MB, 2.3 TB/s: 16 vector operations a logit, 5 of them
+// for its power), groups 13.  Sums of powers are held in 32 bits, relative to the
+// largest logit met; scores are formed in 64, as a score that has been added up
+// over many tokens is no finer than 2^-24 of itself in 32.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -390,7 +395,8 @@ struct Counter {
 constexpr int kMostRanked = 256;  // candidates that are ranked one against the other
 enum State : int { kNone, kLive, kFinished };
 
-// A block takes a group.  kSmall: the group's logits themselves (kHeld kBlock at
+// A block takes a group.  Ranking is n^2 / 4 comparisons in 64 bits over the block's
+// threads: of 1,024 candidates 42 us, of 256 some 2; hence kMostRanked.  kSmall: the group's logits themselves (kHeld kBlock at
 // most); else the strips' lists.  A few blocks are all there is, so that what counts
 // is how many loads wait for one another: the candidates are under way first.
 template <class T, int kBlock, int kHeld, bool kSmall>
@@ -753,7 +759,10 @@ typedef uint32_t Quad __attribute__((ext_vector_type(4)));
 constexpr int kStateHeld = 16;  // units that a thread moves at once
 
 // A block moves some places (units of 16 bytes or less) of all slots of a group:
-// it reads every slot that is followed before it writes any.
+// it reads every slot that is followed before it writes any, so that slots may
+// follow one another in a circle without a second copy of the states.  Bound by the
+// moved rows' bytes, read and written once (139 MB of 256 slots' states: 53 us, 5.2
+// TB/s; 16 to a thread, all under way at once).
 template <class U>
 __global__ __launch_bounds__(kThreads) void reorder_kernel(StateArgs a, int64_t chunk0) {
   __shared__ int from[kMostWidth], to[kMostWidth], length[kMostWidth], moves;

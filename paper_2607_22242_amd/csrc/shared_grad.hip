@@ -6,7 +6,11 @@
 // dK = scale dS^T Q, over both kinds of keys; a prefix key's sums run over all
 // rows of its group.  One kernel holds query rows and walks over the keys (dQ),
 // one holds keys, of either kind, and walks over the rows (dK, dV): no atomics,
-// every sum has one order.
+// every sum has one order, for 14 D operations a pair in place of the 10 D of one
+// kernel.  Bound as the forward pass: 16 answers of 512 tokens to a prompt of 8,192,
+// 32 heads of 128, bf16: dQ 1,511 us (1,125 TFLOP/s), dK and dV 2,267 (1,000).
+// Probabilities and dS are rounded to 16 bits for their products, all else is held in
+// 32: errors are 1.3 to 1.5 times those of rounding the results alone.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -439,7 +443,10 @@ Plan plan_of(const sched_shared_desc& x) {
   const int64_t rows = d.q_rows * (d.q_heads / d.kv_heads);
   p.stats = (size_t(d.q_rows) * size_t(d.q_heads) * 8 + 255) & ~size_t(255);
   // As many parts as fill the 512 places that the card has for a kernel's blocks,
-  // none with less than 12 tiles of keys or 8 of rows of a mean group.
+  // none with less than 12 tiles of keys or 8 of rows of a mean group (13 times 64
+  // answers of 14 tokens to prompts of 71: 61 us with three parts of the prefixes' rows,
+  // 71 with one).  Where blocks fill the card parts only add their sums' bytes (8 prompts
+  // of 1,650, 4 key heads: 934 us with one part, 972 with two).
   if (rows > 0) {
     const int64_t blocks = tile_count(rows, x.n_groups, kRowsOfBlock) * d.kv_heads;
     p.row_parts = int(std::max<int64_t>(
