@@ -96,8 +96,8 @@ constexpr int kWaves = kThreads / kWave;
 struct Shares {
   int p_tiles, p_splits;  // together: tiles of 128 rows of the groups, shares of the prefix
   int o_tiles, o_splits;  // apart: tiles of 32 rows of the sequences, shares of their own keys
-  int p_first;            // those of the prefix come first, else both kinds in turn
-  int units;              // of kv_heads blocks each, of both kinds
+  int units, spread;      // of kv_heads blocks each, of both kinds; the first `spread` have
+                          // those of the prefix, evenly
 };
 
 // Tiles of one wave, as KeyTiles has them.
@@ -269,11 +269,9 @@ __global__ __launch_bounds__(kThreads, 2) void shares_kernel(SharedArgs s, Split
   const Buffers<T> lds = {k_even, v_even, k_odd, v_odd};
   const int kv_heads = s.a.q_heads / s.a.group;
   const int unit = int(blockIdx.x) / kv_heads, kv = int(blockIdx.x) % kv_heads;
-  // Those of the prefix are spread over all units, as many as there are, or over the first.
   const int p_units = n.p_tiles * n.p_splits;
-  const int spread = n.p_first ? p_units : n.units;
-  const int together = int(int64_t(min(unit, spread)) * p_units / spread);
-  if (unit < spread && int(int64_t(unit + 1) * p_units / spread) > together) {
+  const int together = int(int64_t(min(unit, n.spread)) * p_units / n.spread);
+  if (unit < n.spread && int(int64_t(unit + 1) * p_units / n.spread) > together) {
     share_together<T, D>(s, p, n, together, kv, lds);
     return;
   }
@@ -371,8 +369,9 @@ Plan plan_of(const sched_shared_desc& x) {
   // keys on average.  A group's rows that are one wave's leave the prefix bound by
   // memory, too, and its blocks, the longest, come first (prompts of 20,000 to 32,000,
   // up to 2,000 own keys: 73 us, 80 in turn); more rows compute, and memory is kept busy
-  // by own keys beside them (8 groups of 64 sequences: 147 us in turn, 155 one after the
-  // other; one group of 16 with a prompt of 31,000: 61 and 68).
+  // by own keys beside them, all but the last quarter of which go in turn with them (8
+  // groups of 64 sequences: 142 us, 147.5 if all do, 155 one after the other; one group
+  // of 16 with a prompt of 31,000: 58.5, 61 and 68).
   Shares& n = p.n;
   n.p_tiles = int(tile_count(rows, x.n_groups, kRowsOfBlock));
   n.o_tiles = int(tile_count(rows, d.n_seqs, 32));
@@ -385,7 +384,8 @@ Plan plan_of(const sched_shared_desc& x) {
                       x.prefix_rows / x.n_groups, 256);
   n.o_splits = splits(n.o_tiles * int64_t(d.kv_heads), 2048, d.k_rows / d.n_seqs, 128);
   n.units = n.p_tiles * n.p_splits + (n.o_tiles * n.o_splits + kWaves - 1) / kWaves;
-  n.p_first = rows / x.n_groups <= 32;
+  const int p_units = n.p_tiles * n.p_splits;
+  n.spread = rows / x.n_groups <= 32 ? p_units : n.units - (n.units - p_units) / 4;
   p.parts = n.p_splits + n.o_splits;
   return p;
 }
