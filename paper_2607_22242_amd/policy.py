@@ -641,8 +641,8 @@ def sched_beam_select(logits, scores, beams: int, width: Optional[int] = None, l
     c = _Call("sched_beam_select", logits, stream)
     m = c.matrix(logits)
     width = beams if width is None else width
-    if beams < 1 or width < 1 or m.rows % beams:
-        _refuse(-2, c.where + ": a row per beam")
+    if not (1 <= beams <= 128 and 1 <= width <= 128) or m.rows % beams:
+        _refuse(-2, c.where + ": a row per beam, 1 to 128 beams and results")
     groups = m.rows // beams
     n = groups * width
     if new_scores is None:

@@ -777,3 +777,16 @@ def test_calls_at_once():
         for a, b in zip(pair, want):
             for x, y in zip(a, b):
                 assert torch.equal(x, y)
+
+
+def test_numbers_that_no_type_holds():
+    x, s, h = torch.zeros((4, 9), device="cuda"), torch.zeros(4, device="cuda"), torch.zeros((4, 2, 8), device="cuda")
+    at = torch.arange(4, device="cuda")
+    for call in (lambda: S.sched_beam_select(x, s, 2, end_token=1 << 70), lambda: S.sched_beam_select(x, s, 2, 1 << 40),
+                 lambda: S.sched_beam_select(x, s, 2, temperature=1e300), lambda: S.sched_norm_rotate(h, h, at, None, eps=1e39),
+                 lambda: S.sched_norm_rotate(h, h, at, None, norm=1 << 32)):
+        with pytest.raises(S.SchedError):
+            call()
+    b = h.bfloat16()
+    with pytest.raises(S.SchedError):
+        S.sched_attention(b, b, b, i32([0, 4]), i32([0, 4]), scale=1e300)
