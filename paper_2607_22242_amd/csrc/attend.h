@@ -38,7 +38,7 @@ __device__ __forceinline__ Acc product(Frag<f16>::type a, Frag<f16>::type b, Acc
 // Probabilities and dS are rounded to the operands' 16 bits for their products:
 // in 32 bits those would run at a sixteenth of the rate.  The error of a result
 // against 64 bits is 1.4 times that of one rounding of it (f16 and bf16, 2,048 and
-// 4,096 tokens).  f16 is normal from 2^-14 to 2^16 only, with steps of 2^-24 below:
+// 4,096 tokens); with what the rounding leaves in a second product (kFine) once.  f16 is normal from 2^-14 to 2^16 only, with steps of 2^-24 below:
 // there both are multiplied with powers of two, which results are divided by.
 // kLift: of the forward pass' powers, 2^8 at most: what is lost of 65,536 keys
 // stays below 2^-16 of the largest value.  kLiftGrad: of the backward pass'
@@ -387,6 +387,19 @@ __device__ __forceinline__ typename Frag<T>::type narrow(const Acc& x, int s) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] = T(x[8 * s + e]);
   return v;
+}
+
+// What narrow() has left of it; nothing of what is not finite.
+template <class T>
+__device__ __forceinline__ typename Frag<T>::type rest_of(const Acc& x, int s,
+                                                          const typename Frag<T>::type& v) {
+  typename Frag<T>::type r;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float d = x[8 * s + e] - float(v[e]);
+    r[e] = T(fabsf(d) < INFINITY ? d : 0.f);
+  }
+  return r;
 }
 
 // Values of f16 of one row or key (a lane's and those of the lane 32 on) that pass

@@ -110,7 +110,7 @@ struct RowTiles {
 // (D / 32 tiles each) and the keys and values take most of the 256 registers
 // that leave two waves on a unit; of 128 elements the values' upper half stays
 // in LDS for that.
-template <class T, int D>
+template <class T, int D, bool kFine = false>
 struct KeySweep {
   static constexpr int kHeld = D == 128 ? D / 32 : D / 16;  // pieces of the values in registers
   typename Frag<T>::type k[D / 16], v[kHeld];
@@ -169,6 +169,13 @@ struct KeySweep {
       for (int d = 0; d < D / 32; ++d) dv[d] = product(os.across(part + 16 * p, d), pb, dv[d]);
 #pragma unroll
       for (int d = 0; d < D / 32; ++d) dk[d] = product(qs.across(part + 16 * p, d), db, dk[d]);
+      if (kFine) {
+        const auto p_rest = rest_of<T>(x, p, pb), d_rest = rest_of<T>(y, p, db);
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d) dv[d] = product(os.across(part + 16 * p, d), p_rest, dv[d]);
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d) dk[d] = product(qs.across(part + 16 * p, d), d_rest, dk[d]);
+      }
     }
   }
 
@@ -208,7 +215,7 @@ __device__ __forceinline__ int64_t key_part(const AttendArgs& a, int part, int k
 
 // 32 query rows of a wave (lane l has row l % 32): the lanes' columns are query
 // rows, their values run along the keys.
-template <class T, int D>
+template <class T, int D, bool kFine = false>
 struct RowSweep {
   typename Frag<T>::type q[D / 16], o[D / 16];
   Acc dq[D / 32];
@@ -246,6 +253,12 @@ struct RowSweep {
         const auto b = narrow<T>(y, p);
 #pragma unroll
         for (int d = 0; d < D / 32; ++d) dq[d] = product(ks.across(32 * t + 16 * p, d), b, dq[d]);
+        if (kFine) {
+          const auto rest = rest_of<T>(y, p, b);
+#pragma unroll
+          for (int d = 0; d < D / 32; ++d)
+            dq[d] = product(ks.across(32 * t + 16 * p, d), rest, dq[d]);
+        }
       }
     }
   }

@@ -15,7 +15,7 @@ constexpr float kSlack = 8.f;
 
 // A wave's 32 query rows (lane l has row l % 32) and what has been added up
 // over the keys so far, 32 kSubs of them at a time.
-template <class T, int D, int kSubs>
+template <class T, int D, int kSubs, bool kFine = false>
 struct Sweep {
   typename Frag<T>::type q[D / 16];
   Acc o[D / 32];
@@ -94,9 +94,14 @@ struct Sweep {
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
         const auto b = narrow<T>(x[t], p);
+        typename Frag<T>::type rest;
+        if (kFine) rest = rest_of<T>(x[t], p, b);
 #pragma unroll
-        for (int d = 0; d < D / 32; ++d)
-          o[d] = product(vs.across(row + 32 * t + 16 * p, d), b, o[d]);
+        for (int d = 0; d < D / 32; ++d) {
+          const auto v = vs.across(row + 32 * t + 16 * p, d);
+          o[d] = product(v, b, o[d]);
+          if (kFine) o[d] = product(v, rest, o[d]);
+        }
       }
   }
 };

@@ -23,7 +23,7 @@ namespace {
 // One turn of a block over its rows: all of them (nth < 0), which is done unless a
 // sequence that holds what is no number has reached another's rows (true: nothing is
 // written), or those of its nth sequence (true: there is one).
-template <class T, int D>
+template <class T, int D, bool kFine>
 __device__ __forceinline__ bool rows_turn(const SharedArgs& s, int block, int tiles,
                                           const Buffers<T>& lds, int nth) {
   const AttendArgs& a = s.a;
@@ -35,7 +35,7 @@ __device__ __forceinline__ bool rows_turn(const SharedArgs& s, int block, int ti
   if (!r.there) return false;
   const KeyTiles<T, D, kKeys, kThreads> prefix(s.p_k, s.p_v, r.g.p0, r.g.keys, s.near_p, a.dim,
                                                work.kv);
-  Sweep<T, D, kKeys / 32> w;
+  Sweep<T, D, kKeys / 32, kFine> w;
   if (by_one) tiles_barrier();  // nobody reads the last turn's tiles any more
   if (r.g.keys > 0) prefix.fetch(0, lds.k_even, lds.v_even, a.dim);
   w.start(head_row<T>(a.q, r.query, r.me.head), a.dim, r.on);
@@ -67,7 +67,7 @@ __device__ __forceinline__ bool rows_turn(const SharedArgs& s, int block, int ti
   return by_one;
 }
 
-template <class T, int D>
+template <class T, int D, bool kFine>
 __global__ __launch_bounds__(kThreads, 2) void shared_kernel(SharedArgs s, int tiles) {
   __shared__ __attribute__((aligned(16))) T k_even[64 * D], v_even[64 * D];
   __shared__ __attribute__((aligned(16))) T k_odd[64 * D], v_odd[64 * D];
@@ -75,7 +75,7 @@ __global__ __launch_bounds__(kThreads, 2) void shared_kernel(SharedArgs s, int t
   int block = int(blockIdx.x);
   for (int nth = -1;; ++nth) {
     asm volatile("" : "+s"(block));  // a turn keeps nothing in registers for the next
-    if (!rows_turn<T, D>(s, block, tiles, lds, nth)) return;
+    if (!rows_turn<T, D, kFine>(s, block, tiles, lds, nth)) return;
   }
 }
 
@@ -147,9 +147,9 @@ __device__ __forceinline__ void wait_for_reads() {
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 }
 
-template <class T, int D, int kSubs>
+template <class T, int D, int kSubs, bool kFine>
 __device__ __forceinline__ void store_part(const AttendArgs& a, const Split& p,
-                                           const Sweep<T, D, kSubs>& w, int64_t row, int head,
+                                           const Sweep<T, D, kSubs, kFine>& w, int64_t row, int head,
                                            int part, bool on, float c) {
   const float sum = w.sum + __shfl_xor(w.sum, 32);
   if (!on) return;
@@ -172,7 +172,7 @@ __device__ __forceinline__ int prefix_share(const SharedArgs& s, int splits) {
   return ((wave_most(most) + kKeys - 1) / kKeys + splits - 1) / splits * kKeys;
 }
 
-template <class T, int D>
+template <class T, int D, bool kFine>
 __device__ __forceinline__ void share_together(const SharedArgs& s, const Split& p, const Shares& n,
                                                int unit, int kv, const Buffers<T>& lds) {
   const AttendArgs& a = s.a;
@@ -188,7 +188,7 @@ __device__ __forceinline__ void share_together(const SharedArgs& s, const Split&
   const int begin = min(split * share, g.keys), end = min(begin + share, g.keys);
   const float c = a.scale * kLog2e;
   const Places<D> places;
-  Sweep<T, D, kKeys / 32> w;
+  Sweep<T, D, kKeys / 32, kFine> w;
   w.start(head_row<T>(a.q, g.q0 + me.query, me.head), a.dim, on);
   const KeyTiles<T, D, kKeys, kThreads> tiles_of(s.p_k, s.p_v, g.p0, g.keys, s.near_p, a.dim, kv);
   const bool any = first + wave_id() * 32 < rows;  // other waves bring tiles only
@@ -208,7 +208,7 @@ __device__ __forceinline__ void share_together(const SharedArgs& s, const Split&
   store_part<T, D>(a, p, w, g.q0 + me.query, me.head, split, on, c);
 }
 
-template <class T, int D>
+template <class T, int D, bool kFine>
 __device__ __forceinline__ void share_apart(const SharedArgs& s, const Split& p, const Shares& n,
                                             int unit, int kv, T* k_tile, T* v_tile) {
   const AttendArgs& a = s.a;
@@ -235,7 +235,7 @@ __device__ __forceinline__ void share_apart(const SharedArgs& s, const Split& p,
   }
   const bool on = first + lane % 32 < rows;
   const QueryRow me = query_row(a, kv, on ? first + lane % 32 : first);
-  Sweep<T, D, 1> w;
+  Sweep<T, D, 1, kFine> w;
   w.start(head_row<T>(a.q, q.q0 + me.query, me.head), a.dim, on);
   const float c = a.scale * kLog2e;
   const Places<D> places;
@@ -262,7 +262,7 @@ __device__ __forceinline__ void share_apart(const SharedArgs& s, const Split& p,
   store_part<T, D>(a, p, w, q.q0 + me.query, me.head, n.p_splits + split, on, c);
 }
 
-template <class T, int D>
+template <class T, int D, bool kFine>
 __global__ __launch_bounds__(kThreads, 2) void shares_kernel(SharedArgs s, Split p, Shares n) {
   __shared__ __attribute__((aligned(16))) T k_even[64 * D], v_even[64 * D];
   __shared__ __attribute__((aligned(16))) T k_odd[64 * D], v_odd[64 * D];
@@ -272,7 +272,7 @@ __global__ __launch_bounds__(kThreads, 2) void shares_kernel(SharedArgs s, Split
   const int p_units = n.p_tiles * n.p_splits;
   const int together = int(int64_t(min(unit, n.spread)) * p_units / n.spread);
   if (unit < n.spread && int(int64_t(unit + 1) * p_units / n.spread) > together) {
-    share_together<T, D>(s, p, n, together, kv, lds);
+    share_together<T, D, kFine>(s, p, n, together, kv, lds);
     return;
   }
   const int wave = wave_id();
@@ -280,8 +280,8 @@ __global__ __launch_bounds__(kThreads, 2) void shares_kernel(SharedArgs s, Split
   const int its = int(apart / kv_heads), its_kv = int(apart % kv_heads);
   // Keys and values in arrays that the compiler tells apart (Buffers).
   const int at = wave % 2 * kStream * D;
-  if (wave < 2) share_apart<T, D>(s, p, n, its, its_kv, k_even + at, v_even + at);
-  else share_apart<T, D>(s, p, n, its, its_kv, k_odd + at, v_odd + at);
+  if (wave < 2) share_apart<T, D, kFine>(s, p, n, its, its_kv, k_even + at, v_even + at);
+  else share_apart<T, D, kFine>(s, p, n, its, its_kv, k_odd + at, v_odd + at);
 }
 
 // Joins the parts of rows of the groups' sequences (others have none): a wave per row
@@ -394,17 +394,17 @@ size_t part_count(const sched_shared_desc& x, const Plan& p) {
   return size_t(x.own.q_rows) * size_t(x.own.q_heads) * size_t(p.parts);
 }
 
-template <class T, int D>
+template <class T, int D, bool kFine>
 hipError_t shared(const SharedArgs& s, const Plan& n, void* ws, size_t parts, hipStream_t stream) {
   const int kv_heads = s.a.q_heads / s.a.group;
   if (!n.split) {
     const int64_t tiles = tile_count(int64_t(s.a.q_rows) * s.a.group, s.n_groups, kRowsOfBlock);
-    hipLaunchKernelGGL((shared_kernel<T, D>), dim3(unsigned(work_blocks(tiles, kv_heads))),
+    hipLaunchKernelGGL((shared_kernel<T, D, kFine>), dim3(unsigned(work_blocks(tiles, kv_heads))),
                        dim3(kThreads), 0, stream, s, int(tiles));
     return hipGetLastError();
   }
   const Split p = {static_cast<float*>(ws), static_cast<float*>(ws) + parts * D, n.parts};
-  hipLaunchKernelGGL((shares_kernel<T, D>), dim3(unsigned(n.n.units) * unsigned(kv_heads)),
+  hipLaunchKernelGGL((shares_kernel<T, D, kFine>), dim3(unsigned(n.n.units) * unsigned(kv_heads)),
                      dim3(kThreads), 0, stream, s, p, n.n);
   hipError_t e = hipGetLastError();
   const int64_t joins = (int64_t(s.a.q_rows) * s.a.q_heads + kWaves - 1) / kWaves;
@@ -443,10 +443,16 @@ hipError_t launch_shared(const sched_shared_desc& x, void* ws, hipStream_t strea
   if (x.n_groups == 0 || x.own.n_seqs == 0 || x.own.q_rows == 0) return hipSuccess;
   const SharedArgs s = shared_args(x);
   const size_t parts = part_count(x, p);
-  const bool wide = x.own.head_dim > 64;
-  if (x.own.dtype == SCHED_F16)
-    return wide ? shared<f16, 128>(s, p, ws, parts, stream) : shared<f16, 64>(s, p, ws, parts, stream);
-  return wide ? shared<bf16, 128>(s, p, ws, parts, stream) : shared<bf16, 64>(s, p, ws, parts, stream);
+  auto run = [&](auto fine) {
+    constexpr bool kFine = decltype(fine)::value;
+    const bool wide = x.own.head_dim > 64;
+    if (x.own.dtype == SCHED_F16)
+      return wide ? shared<f16, 128, kFine>(s, p, ws, parts, stream)
+                  : shared<f16, 64, kFine>(s, p, ws, parts, stream);
+    return wide ? shared<bf16, 128, kFine>(s, p, ws, parts, stream)
+                : shared<bf16, 64, kFine>(s, p, ws, parts, stream);
+  };
+  return is_small(x) ? run(std::true_type()) : run(std::false_type());
 }
 
 }  // namespace policy

@@ -27,7 +27,7 @@ namespace {
 // One turn of a block over its rows: all of them (nth < 0), which is done unless a
 // sequence that holds what is no number has reached another's rows (true: nothing is
 // written), or those of its nth sequence (true: there is one).
-template <class T, int D>
+template <class T, int D, bool kFine>
 __device__ __forceinline__ bool rows_turn(const SharedArgs& s, const RowParts& p, int block,
                                           int tiles, const Buffers<T>& lds, int nth) {
   const AttendArgs& a = s.a;
@@ -42,7 +42,7 @@ __device__ __forceinline__ bool rows_turn(const SharedArgs& s, const RowParts& p
   const int begin = min(part * share, r.g.keys), end = min(begin + share, r.g.keys);
   const bool with_own = part == p.parts - 1;
 
-  RowSweep<T, D> w;
+  RowSweep<T, D, kFine> w;
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) {
     const int d = 16 * i + 8 * (lane / 32);
@@ -134,11 +134,11 @@ __device__ __forceinline__ bool rows_turn(const SharedArgs& s, const RowParts& p
 // to each of 4 prompts of 2,000, 16 heads of 64, dQ 343 -> 308 us and dK and dV 452 ->
 // 443 (f16: 366 -> 328, 490 -> 512); over 13 times 64 answers of 14 tokens, 4 heads of
 // 32, 19 -> 20.6 and 22.5 -> 19.5.
-template <int D>
-constexpr int kBlocksOfUnit = D == 64 ? 3 : 2;
+template <int D, bool kFine>
+constexpr int kBlocksOfUnit = D == 64 && !kFine ? 3 : 2;
 
-template <class T, int D>
-__global__ __launch_bounds__(kThreads, kBlocksOfUnit<D>) void shared_queries_kernel(SharedArgs s, RowParts p,
+template <class T, int D, bool kFine>
+__global__ __launch_bounds__(kThreads, (kBlocksOfUnit<D, kFine>)) void shared_queries_kernel(SharedArgs s, RowParts p,
                                                                      int tiles) {
   __shared__ __attribute__((aligned(16))) T k_even[64 * D], v_even[64 * D];
   __shared__ __attribute__((aligned(16))) T k_odd[64 * D], v_odd[64 * D];
@@ -146,7 +146,7 @@ __global__ __launch_bounds__(kThreads, kBlocksOfUnit<D>) void shared_queries_ker
   int block = int(blockIdx.x);
   for (int nth = -1;; ++nth) {
     asm volatile("" : "+s"(block));  // a turn keeps nothing in registers for the next
-    if (!rows_turn<T, D>(s, p, block, tiles, lds, nth)) return;
+    if (!rows_turn<T, D, kFine>(s, p, block, tiles, lds, nth)) return;
   }
 }
 
@@ -194,7 +194,7 @@ struct KeyBuffers {  // arrays in LDS
   int *from, *upto;  // rows that see a key
   int* seq;          // its sequence; -1: not in use, -2: another block's
 };
-template <class T, int D, bool kPrefix>
+template <class T, int D, bool kPrefix, bool kFine>
 __device__ __forceinline__ bool keys_turn(const SharedArgs& s, const PrefixParts& p, int block,
                                           int blocks, int tiles, const KeyBuffers<T>& lds, int nth) {
   const AttendArgs& a = s.a;
@@ -268,7 +268,7 @@ __device__ __forceinline__ bool keys_turn(const SharedArgs& s, const PrefixParts
     tiles_barrier();  // nobody reads the last turn's tiles any more
   }
   const Rows<T, 64> rest = {lds.v_rest, Places<64>()};
-  KeySweep<T, D> w;
+  KeySweep<T, D, kFine> w;
   {
     const int64_t row = on ? key : 0;
     const T *k_row = head_row<T>(ks, row, kv), *v_row = head_row<T>(vs, row, kv);
@@ -376,8 +376,8 @@ __device__ __forceinline__ bool keys_turn(const SharedArgs& s, const PrefixParts
   return by_one;
 }
 
-template <class T, int D>
-__global__ __launch_bounds__(kThreads, kBlocksOfUnit<D>) void shared_keys_kernel(SharedArgs s, PrefixParts p,
+template <class T, int D, bool kFinePrefix, bool kFine>
+__global__ __launch_bounds__(kThreads, (kBlocksOfUnit<D, kFinePrefix>)) void shared_keys_kernel(SharedArgs s, PrefixParts p,
                                                                   int p_tiles, int p_blocks,
                                                                   int tiles) {
   __shared__ __attribute__((aligned(16))) T q_even[kTile * D], o_even[kTile * D];
@@ -389,13 +389,13 @@ __global__ __launch_bounds__(kThreads, kBlocksOfUnit<D>) void shared_keys_kernel
   const KeyBuffers<T> lds = {q_even, o_even, q_odd, o_odd, v_rest, &s_even, &s_odd, from, upto, seq};
   int block = int(blockIdx.x);
   if (block < p_blocks * p.parts) {
-    keys_turn<T, D, true>(s, p, block, p_blocks, p_tiles, lds, -1);
+    keys_turn<T, D, true, kFinePrefix>(s, p, block, p_blocks, p_tiles, lds, -1);
     return;
   }
   block -= p_blocks * p.parts;
   for (int nth = -1;; ++nth) {
     asm volatile("" : "+s"(block));
-    if (!keys_turn<T, D, false>(s, p, block, 1, tiles, lds, nth)) return;
+    if (!keys_turn<T, D, false, kFine>(s, p, block, 1, tiles, lds, nth)) return;
   }
 }
 
@@ -431,14 +431,23 @@ __global__ __launch_bounds__(kThreads) void add_prefix_kernel(SharedArgs s, Pref
 // --- launches -----------------------------------------------------------------------
 
 struct Plan {
+  bool fine_rows, fine_prefix, fine_own;  // second products (kFine): for dQ; for dK and dV
   int row_parts, prefix_parts;
   size_t stats, row_values, prefix_values;  // bytes; values of dQ, and of dK or dV
 };
 
 Plan plan_of(const sched_shared_desc& x) {
   const sched_attention_desc& d = x.own;
-  Plan p = {1, 1, 0, 0, 0};
+  Plan p = {false, false, false, 1, 1, 0, 0, 0};
   if (x.n_groups == 0) return p;
+  // Also for dQ where rows see few keys, so that a rounded delta is much of what is
+  // left of a difference (13 times 64 answers of 14 tokens, 71 + 14 keys, 4 heads of 32:
+  // dQ is 1.04 times as far off as one rounding, 1.49 without, in 21.7 us, 20.4
+  // without), and for prefixes of a tile, a part of a call's keys that counts little.
+  // All of it takes that call's 60 us to 68; its 2^22 pairs are none of a small one.
+  p.fine_own = is_small(x);
+  p.fine_rows = p.fine_own || mean_keys(x) <= 128;
+  p.fine_prefix = p.fine_own || x.prefix_rows / x.n_groups <= kKeysOfBlock;
   const size_t width = d.head_dim > 64 ? 128 : 64;
   const int64_t rows = d.q_rows * (d.q_heads / d.kv_heads);
   p.stats = (size_t(d.q_rows) * size_t(d.q_heads) * 8 + 255) & ~size_t(255);
@@ -472,8 +481,8 @@ hipError_t shared_grad(const SharedArgs& s, const Plan& n, float* parts, hipStre
     const RowParts r = {parts, n.row_parts};
     const int64_t tiles = tile_count(int64_t(s.a.q_rows) * s.a.group, s.n_groups, kRowsOfBlock);
     const dim3 grid(unsigned(work_blocks(tiles, kv_heads)), unsigned(r.parts));
-    hipLaunchKernelGGL((shared_queries_kernel<T, D>), grid, dim3(kThreads), 0, stream, s, r,
-                       int(tiles));
+    const auto kernel = n.fine_rows ? shared_queries_kernel<T, D, true> : shared_queries_kernel<T, D, false>;
+    hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, s, r, int(tiles));
     e = hipGetLastError();
     const int64_t adds = (int64_t(s.a.q_rows) * s.a.q_heads * (D / 4) + kThreads - 1) / kThreads;
     for (int64_t b = 0; r.parts > 1 && b < adds && e == hipSuccess; b += kMostBlocks) {
@@ -488,8 +497,11 @@ hipError_t shared_grad(const SharedArgs& s, const Plan& n, float* parts, hipStre
   const int64_t o_tiles = s.a.n_seqs > 0 ? (int64_t(s.a.k_rows) + kKeysOfBlock - 1) / kKeysOfBlock : 0;
   const int64_t p_blocks = work_blocks(p_tiles, kv_heads), o_blocks = work_blocks(o_tiles, kv_heads);
   if (p_blocks + o_blocks == 0) return hipSuccess;
-  hipLaunchKernelGGL((shared_keys_kernel<T, D>), dim3(unsigned(p_blocks * p.parts + o_blocks)),
-                     dim3(kThreads), 0, stream, s, p, int(p_tiles), int(p_blocks), int(o_tiles));
+  const auto kernel = n.fine_own      ? shared_keys_kernel<T, D, true, true>
+                      : n.fine_prefix ? shared_keys_kernel<T, D, true, false>
+                                      : shared_keys_kernel<T, D, false, false>;
+  hipLaunchKernelGGL(kernel, dim3(unsigned(p_blocks * p.parts + o_blocks)), dim3(kThreads), 0, stream,
+                     s, p, int(p_tiles), int(p_blocks), int(o_tiles));
   e = hipGetLastError();
   const int64_t adds = (int64_t(s.p_rows) * kv_heads * (D / 4) + kThreads - 1) / kThreads;
   for (int64_t b = 0; p.parts > 1 && b < adds && e == hipSuccess; b += kMostBlocks) {

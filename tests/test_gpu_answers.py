@@ -790,3 +790,26 @@ def test_numbers_that_no_type_holds():
     b = h.bfloat16()
     with pytest.raises(S.SchedError):
         S.sched_attention(b, b, b, i32([0, 4]), i32([0, 4]), scale=1e300)
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("hq,hk,dim,prefixes,samples,lo,hi", [(32, 4, 16, [1, 2, 2, 1], 3, 6, 31), (8, 2, 64, [40, 9], 5, 1, 20),
+                                                             (4, 1, 128, [30], 8, 14, 14)])
+def test_small_calls_are_rounded_once(dtype, hq, hk, dim, prefixes, samples, lo, hi):
+    """Of rows that see up to 64 keys.  Probabilities and dS are known to 2^-16 of
+    themselves or better and all else to 2^-20, where a result's rounding is 2^-9 or
+    2^-12 of it: in norm nothing beside it."""
+    g = gen(dim)
+    lengths = torch.randint(lo, hi + 1, (len(prefixes) * samples,), generator=g).tolist()
+    off, p_off, groups = offsets(lengths), offsets(prefixes), offsets([samples] * len(prefixes))
+    q, do = (randn(g, off[-1], hq, dim, dtype=dtype) for _ in range(2))
+    k, v = (randn(g, off[-1], hk, dim, dtype=dtype) for _ in range(2))
+    pk, pv = (randn(g, p_off[-1], hk, dim, dtype=dtype) for _ in range(2))
+    want = R.Shared(q, k, v, pk, pv, off, off, p_off, groups, None, None, True, 1 / math.sqrt(dim), do)
+    args, where = [x.cuda() for x in (q, k, v, pk, pv)], [i32(x) for x in (off, off, p_off, groups)]
+    out, lse = S.sched_shared_attention(*args, *where)
+    grads = S.sched_shared_attention_grad(*args, out, lse, do.cuda(), *where)
+    for x, name in zip((out, *grads), ("out", "dq", "dk", "dv", "dpk", "dpv")):
+        y = getattr(want, name)
+        once = float((y.to(dtype).double() - y).norm())
+        assert float((x.cpu().double() - y).norm()) < 1.1 * once, name
