@@ -138,8 +138,8 @@ template <int D, bool kFine>
 constexpr int kBlocksOfUnit = D == 64 && !kFine ? 3 : 2;
 
 template <class T, int D, bool kFine>
-__global__ __launch_bounds__(kThreads, (kBlocksOfUnit<D, kFine>)) void shared_queries_kernel(SharedArgs s, RowParts p,
-                                                                     int tiles) {
+__global__ __launch_bounds__(kThreads, (kBlocksOfUnit<D, kFine>)) void shared_queries_kernel(
+    SharedArgs s, RowParts p, int tiles) {
   __shared__ __attribute__((aligned(16))) T k_even[64 * D], v_even[64 * D];
   __shared__ __attribute__((aligned(16))) T k_odd[64 * D], v_odd[64 * D];
   const Buffers<T> lds = {k_even, v_even, k_odd, v_odd};
@@ -377,9 +377,8 @@ __device__ __forceinline__ bool keys_turn(const SharedArgs& s, const PrefixParts
 }
 
 template <class T, int D, bool kFinePrefix, bool kFine>
-__global__ __launch_bounds__(kThreads, (kBlocksOfUnit<D, kFinePrefix>)) void shared_keys_kernel(SharedArgs s, PrefixParts p,
-                                                                  int p_tiles, int p_blocks,
-                                                                  int tiles) {
+__global__ __launch_bounds__(kThreads, (kBlocksOfUnit<D, kFinePrefix || kFine>)) void shared_keys_kernel(
+    SharedArgs s, PrefixParts p, int p_tiles, int p_blocks, int tiles) {
   __shared__ __attribute__((aligned(16))) T q_even[kTile * D], o_even[kTile * D];
   __shared__ __attribute__((aligned(16))) T q_odd[kTile * D], o_odd[kTile * D];
   constexpr int kRest = KeySweep<T, D>::kHeld < D / 16 ? kKeysOfBlock * 64 : 8;
@@ -440,16 +439,20 @@ Plan plan_of(const sched_shared_desc& x) {
   const sched_attention_desc& d = x.own;
   Plan p = {false, false, false, 1, 1, 0, 0, 0};
   if (x.n_groups == 0) return p;
-  // Also for dQ where rows see few keys, so that a rounded delta is much of what is
-  // left of a difference (13 times 64 answers of 14 tokens, 71 + 14 keys, 4 heads of 32:
-  // dQ is 1.04 times as far off as one rounding, 1.49 without, in 21.7 us, 20.4
-  // without), and for prefixes of a tile, a part of a call's keys that counts little.
-  // All of it takes that call's 60 us to 68; its 2^22 pairs are none of a small one.
-  p.fine_own = is_small(x);
-  p.fine_rows = p.fine_own || mean_keys(x) <= 128;
-  p.fine_prefix = p.fine_own || x.prefix_rows / x.n_groups <= kKeysOfBlock;
   const size_t width = d.head_dim > 64 ? 128 : 64;
   const int64_t rows = d.q_rows * (d.q_heads / d.kv_heads);
+  // Also for dQ where a rounded delta is much of what is left of a difference: of heads
+  // of up to 48 elements (16: 1.15 times as far off as one rounding, 1.52 without; 32: 1.47
+  // without; 32 answers of 20 to 100 tokens to each of 4 prompts of 300, 16 heads of 48: 51
+  // us, 43 without), and where rows see few keys (13 times 64 answers of 14 tokens, 71 + 14 keys:
+  // 1.06, 1.49 without, in 22 us, 20.4 without); for prefixes of a tile, and own keys
+  // whose sums have few terms, parts of a call that count little, whose errors are
+  // those of few numbers.  All of it takes the answers' 60 us to 68: 2^22 pairs are not
+  // a small call's.
+  const bool small = is_small(x);
+  p.fine_rows = small || d.head_dim <= 48 || mean_keys(x) <= 128;
+  p.fine_prefix = small || x.prefix_rows / x.n_groups <= kKeysOfBlock;
+  p.fine_own = small || rows <= 16 * int64_t(d.n_seqs);
   p.stats = (size_t(d.q_rows) * size_t(d.q_heads) * 8 + 255) & ~size_t(255);
   // As many parts as fill the 512 places that the card has for a kernel's blocks,
   // none with less than 12 tiles of keys or 8 of rows of a mean group (13 times 64
@@ -497,9 +500,10 @@ hipError_t shared_grad(const SharedArgs& s, const Plan& n, float* parts, hipStre
   const int64_t o_tiles = s.a.n_seqs > 0 ? (int64_t(s.a.k_rows) + kKeysOfBlock - 1) / kKeysOfBlock : 0;
   const int64_t p_blocks = work_blocks(p_tiles, kv_heads), o_blocks = work_blocks(o_tiles, kv_heads);
   if (p_blocks + o_blocks == 0) return hipSuccess;
-  const auto kernel = n.fine_own      ? shared_keys_kernel<T, D, true, true>
-                      : n.fine_prefix ? shared_keys_kernel<T, D, true, false>
-                                      : shared_keys_kernel<T, D, false, false>;
+  const auto kernel = n.fine_prefix ? n.fine_own ? shared_keys_kernel<T, D, true, true>
+                                                 : shared_keys_kernel<T, D, true, false>
+                      : n.fine_own  ? shared_keys_kernel<T, D, false, true>
+                                    : shared_keys_kernel<T, D, false, false>;
   hipLaunchKernelGGL(kernel, dim3(unsigned(p_blocks * p.parts + o_blocks)), dim3(kThreads), 0, stream,
                      s, p, int(p_tiles), int(p_blocks), int(o_tiles));
   e = hipGetLastError();
