@@ -96,29 +96,39 @@ struct List {
     if (n <= k) return;
     wave_order();
     const int lane = int(threadIdx.x) % kWave;
-    constexpr int kHeld = 2;  // rounds in registers
-    if (n <= kHeld * kWave) {
-      Entry e[kHeld];
-#pragma unroll
-      for (int i = 0; i < kHeld; ++i) {
-        e[i] = {0, ~0u};
-        if (i * kWave + lane < n) e[i] = at[i * kWave + lane];
-      }
-      leave(k, kHeld, [&](int i) { return e[i]; });
+    if (n <= 2 * kWave) {
+      held<2>(k);
+    } else if (n <= 4 * kWave) {
+      held<4>(k);
+    } else if (n <= 8 * kWave) {
+      held<8>(k);
+    } else if (n <= 16 * kWave) {
+      held<16>(k);
     } else {
       const int rounds = (n + kWave - 1) / kWave;
-      leave(k, rounds, [&](int i) {
+      leave<2>(k, rounds, [&](int i) {
         return i * kWave + lane < n ? at[i * kWave + lane] : Entry{0, ~0u};
       });
     }
   }
 
  private:
-  template <class Get>
+  template <int kHeld>  // entries in registers: what waits for LDS takes ten times as long
+  __device__ __forceinline__ void held(int k) {
+    const int lane = int(threadIdx.x) % kWave;
+    Entry e[kHeld];
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      e[i] = {0, ~0u};
+      if (i * kWave + lane < n) e[i] = at[i * kWave + lane];
+    }
+    leave<kHeld>(k, kHeld, [&](int i) { return e[i]; });
+  }
+  template <int kUnroll, class Get>
   __device__ __forceinline__ void leave(int k, int rounds, Get get) {
     auto count = [&](auto in) {
       int c = 0;
-#pragma unroll 2
+#pragma unroll kUnroll
       for (int i = 0; i < rounds; ++i) c += __popcll(__ballot(in(get(i))));
       return c;
     };
@@ -150,7 +160,7 @@ struct List {
     // In place: what is written lies before what is read next.
     const int all = n;
     n = 0;
-#pragma unroll 2
+#pragma unroll kUnroll
     for (int i = 0; i < rounds; ++i) {
       const int kept = n;
       n = all;  // what get() looks at
