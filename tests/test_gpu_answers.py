@@ -813,3 +813,54 @@ def test_small_calls_are_rounded_once(dtype, hq, hk, dim, prefixes, samples, lo,
         y = getattr(want, name)
         once = float((y.to(dtype).double() - y).norm())
         assert float((x.cpu().double() - y).norm()) < 1.1 * once, name
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("hq,hk,dim", [(8, 2, 64), (8, 1, 128), (9, 3, 120)])
+def test_calls_that_are_not_small(dtype, hq, hk, dim):
+    """More than 2^21 pairs of a row and a key: products of rounded operands alone."""
+    g = gen(hq + dim)
+    check_shared(g, dtype, hq, hk, dim, [400, 333], [3, 3], [100, 130, 77, 120, 99, 110])
+    check_shared(g, dtype, hq, hk, dim, [900], [5], [70, 0, 64, 129, 1], [100, 20, 64, 200, 30],
+                 slots=[200] * 5, p_slots=[1000], causal=False)
+    check_shared(g, dtype, 32, 8, dim, [1500, 1300], [20, 35], [1] * 55, [(31 * i) % 400 for i in range(55)],
+                 slots=[400] * 55, p_slots=[1600] * 2, grad=False)
+    # Of few rows to a sequence, of short prefixes, and of few keys.
+    check_shared(g, dtype, 16, 8, dim, [1000], [100], [1, 2] * 50)
+    check_shared(g, dtype, 8, 2, dim, [40], [6], [200] * 6)
+    check_shared(g, dtype, 16, 4, dim, [90], [60], [20] * 60)
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_what_is_no_number_stays_in_its_sequence_of_larger_calls(dtype, bad):
+    g = gen(38)
+    queries = [(5 * i) % 31 for i in range(40)]
+    off, p_off, groups, hq, hk, dim = offsets(queries), [0, 700, 1120], [0, 25, 40], 16, 8, 64
+    x = [randn(g, off[-1], h, dim, dtype=dtype) for h in (hq, hk, hk, hq)]
+    pre = [randn(g, 1120, hk, dim, dtype=dtype) for _ in range(2)]
+    where = [i32(t) for t in (off, off, p_off, groups)]
+    want = R.Shared(*x[:3], *pre, off, off, p_off, groups, None, None, True, 0.125, x[3])
+    keep = torch.ones(off[-1], dtype=torch.bool)
+    keep[off[11]:off[12]] = False
+    for i in range(4):
+        spoiled = [t.clone() for t in x]
+        spoiled[i][off[11] + 4, 0, 3] = bad
+        q, k, v, pk, pv, do = (t.cuda() for t in (*spoiled[:3], *pre, spoiled[3]))
+        out, lse = S.sched_shared_attention(q, k, v, pk, pv, *where)
+        got = out, lse.t(), *S.sched_shared_attention_grad(q, k, v, pk, pv, out, lse, do, *where)
+        for a, name in zip(got, ("out", "lse", "dq", "dk", "dv")):
+            b, bound = getattr(want, name), getattr(want, name + "_b")
+            b, bound = (t.t() if name == "lse" else t for t in (b, bound))
+            close(a[keep.cuda()], b[keep], bound[keep], (i, name))
+        for a, name in zip(got[5:], ("dpk", "dpv")):  # the other group's prefix
+            close(a[700:], getattr(want, name)[700:], getattr(want, name + "_b")[700:], (i, name))
+
+
+def test_beam_select_of_many_groups_and_of_short_strips():
+    check_beams(gen(60), 300, 4, 4, 20, torch.float32, stay=True)
+    check_beams(gen(61), 300, 2, 2, 700, torch.float32)
+    check_beams(gen(62), 2, 40, 40, 6300, torch.float32, stay=True)
+    check_beams(gen(63), 3, 5, 100, 300, torch.float32)
+    check_beams(gen(64), 1, 2, 128, 1500, torch.float32)
+    check_beams(gen(65), 2, 16, 16, 64, torch.float32)
