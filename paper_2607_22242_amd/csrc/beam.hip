@@ -113,7 +113,9 @@ struct List {
   }
 
  private:
-  template <int kHeld>  // entries in registers: what waits for LDS takes ten times as long
+  // Entries in registers (2 groups of 40 beams of 12,709 logits: strips 13 us, 32 if what
+  // is more than 128 entries is counted in LDS).
+  template <int kHeld>
   __device__ __forceinline__ void held(int k) {
     const int lane = int(threadIdx.x) % kWave;
     Entry e[kHeld];
@@ -405,10 +407,11 @@ struct Counter {
 constexpr int kMostRanked = 256;  // candidates that are ranked one against the other
 enum State : int { kNone, kLive, kFinished };
 
-// A block takes a group.  Ranking is n^2 / 4 comparisons in 64 bits over the block's
-// threads: of 1,024 candidates 42 us, of 256 some 2; hence kMostRanked.  kSmall: the group's logits themselves (kHeld kBlock at
+// A block takes a group.  kSmall: the group's logits themselves (kHeld kBlock at
 // most); else the strips' lists.  A few blocks are all there is, so that what counts
-// is how many loads wait for one another: the candidates are under way first.
+// is how many loads wait for one another: the candidates are under way first.  Ranking
+// is n^2 comparisons in 64 bits over the block's threads: of 1,024 candidates 42 us, of
+// 256 some 2; hence kMostRanked.
 template <class T, int kBlock, int kHeld, bool kSmall>
 __global__ __launch_bounds__(kBlock) void group_kernel(BeamArgs a) {
   __shared__ double base[kMostWidth];  // of a beam: what is added to logit / temperature, or its score
