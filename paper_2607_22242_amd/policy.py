@@ -143,9 +143,9 @@ def _packer(kind):
     return struct.Struct(form + "x" * (ctypes.sizeof(kind) - at)).pack
 
 
-_pack_heads, _pack_attention, _pack_shared, _pack_grads, _pack_rotate, _pack_beam = map(
-    _packer, (sched_heads, sched_attention_desc, sched_shared_desc, sched_shared_grads,
-              sched_norm_rotate_desc, sched_beam_desc))
+(_pack_heads, _pack_attention, _pack_shared, _pack_grads, _pack_rotate, _pack_beam,
+ _pack_states) = map(_packer, (sched_heads, sched_attention_desc, sched_shared_desc, sched_shared_grads,
+                               sched_norm_rotate_desc, sched_beam_desc, sched_states))
 _F32 = _F16 = _BF16 = _INT32 = _INT64 = None  # torch's types, once it is loaded
 _torch = _types = None
 _call = {}  # the library's functions
@@ -208,8 +208,9 @@ class _Call:
         with _torch.cuda.stream(self.stream):
             return _torch.empty_like(t, memory_format=_torch.contiguous_format)
 
-    def matrix(self, t) -> sched_matrix:
-        self.use(t)
+    def matrix_values(self, t) -> Tuple:
+        if self.other or t.get_device() != self.index:
+            self.use(t)
         kind = _types.get(t.dtype)
         if kind is None:
             _refuse(-3, self.where + ": float32, float16 or bfloat16")
@@ -220,7 +221,10 @@ class _Call:
         if step != 1 and cols > 1:
             _refuse(-3, self.where + ": the elements of a row are next to each other")
         stride = stride if rows > 1 else max(stride, cols)
-        return sched_matrix(t.data_ptr(), kind, rows, cols, stride)
+        return t.data_ptr(), kind, rows, cols, stride
+
+    def matrix(self, t) -> sched_matrix:
+        return sched_matrix(*self.matrix_values(t))
 
     def token_values(self, t) -> Tuple:
         if self.other or t.get_device() != self.index:
@@ -639,11 +643,11 @@ def sched_beam_select(logits, scores, beams: int, width: Optional[int] = None, l
     beam that ends in end_token is finished.  stay: a beam's best continuation
     keeps its slot; otherwise results are ordered by score."""
     c = _Call("sched_beam_select", logits, stream)
-    m = c.matrix(logits)
-    width = beams if width is None else width
-    if not (1 <= beams <= 128 and 1 <= width <= 128) or m.rows % beams:
+    m = c.matrix_values(logits)
+    rows, width = m[2], beams if width is None else width
+    if not (1 <= beams <= 128 and 1 <= width <= 128) or rows % beams:
         _refuse(-2, c.where + ": a row per beam, 1 to 128 beams and results")
-    groups = m.rows // beams
+    groups = rows // beams
     n = groups * width
     if new_scores is None:
         new_scores = c.new((n,), _F32)
@@ -655,7 +659,7 @@ def sched_beam_select(logits, scores, beams: int, width: Optional[int] = None, l
     if count != n:
         _refuse(-2, f"{c.where}: {n} tokens, not {count}")
     d = c.packed(_pack_beam, (
-        m.data or 0, m.dtype, m.rows, m.cols, m.stride, c.vector(scores, _F32, m.rows),
+        *m, c.vector(scores, _F32, rows),
         *(_NOWHERE if last is None else c.token_values(last)), end_token, groups, beams, width,
         int(stay), temperature, c.vector(new_scores, _F32, n), c.vector(parents, _INT32, n), at, bits))
     need = c.bytes("sched_beam_workspace_bytes", d)
@@ -670,16 +674,16 @@ def sched_beam_reorder(states, parents, beams: int, lengths=None, stream=None):
     parents[s] of its group of `beams`, in place; returns states."""
     c = _Call("sched_beam_reorder", states, stream)
     c.use(states)
-    if states.dim() < 3:
-        _refuse(-2, c.where + ": states are outer x slots x rows x ...")
-    size, row = states.element_size(), 1
-    for n, step in zip(reversed(states.shape[3:]), reversed(states.stride()[3:])):
-        if n != 1 and step != row:
+    if states.dim() < 3 or not 1 <= beams <= 128:
+        _refuse(-2, c.where + ": states are outer x slots x rows x ..., 1 to 128 beams")
+    size, row, shape, steps = states.element_size(), 1, states.shape, states.stride()
+    for i in range(len(shape) - 1, 2, -1):
+        if shape[i] != 1 and steps[i] != row:
             _refuse(-3, c.where + ": the elements of a row are next to each other")
-        row *= n
-    outer, slots, rows = states.shape[:3]
-    a, b, e = (x * size for x in states.stride()[:3])
-    d = sched_states(states.data_ptr(), outer, slots, rows, row * size, a, b, e)
-    c.done("sched_beam_reorder", ctypes.byref(d), c.vector(parents, _INT32, slots),
+        row *= shape[i]
+    slots = shape[1]
+    d = c.packed(_pack_states, (states.data_ptr(), shape[0], slots, shape[2], row * size, steps[0] * size,
+                                steps[1] * size, steps[2] * size))
+    c.done("sched_beam_reorder", d, c.vector(parents, _INT32, slots),
            None if lengths is None else c.vector(lengths, _INT32, slots), beams)
     return states

@@ -232,7 +232,7 @@ def test_binding_refuses_tensors_of_the_host():
 
 
 @pytest.mark.parametrize("kind", [P.sched_heads, P.sched_attention_desc, P.sched_shared_desc, P.sched_shared_grads,
-                                  P.sched_norm_rotate_desc, P.sched_beam_desc])
+                                  P.sched_norm_rotate_desc, P.sched_beam_desc, P.sched_states])
 def test_values_packed_at_once_are_the_structure(kind):
     values = []
 

@@ -784,7 +784,8 @@ def test_numbers_that_no_type_holds():
     at = torch.arange(4, device="cuda")
     for call in (lambda: S.sched_beam_select(x, s, 2, end_token=1 << 70), lambda: S.sched_beam_select(x, s, 2, 1 << 40),
                  lambda: S.sched_beam_select(x, s, 2, temperature=1e300), lambda: S.sched_norm_rotate(h, h, at, None, eps=1e39),
-                 lambda: S.sched_norm_rotate(h, h, at, None, norm=1 << 32)):
+                 lambda: S.sched_norm_rotate(h, h, at, None, norm=1 << 32),
+                 lambda: S.sched_beam_reorder(h[None], at.int(), (1 << 32) + 2)):
         with pytest.raises(S.SchedError):
             call()
     b = h.bfloat16()
