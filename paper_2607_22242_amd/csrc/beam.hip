@@ -414,7 +414,10 @@ enum State : int { kNone, kLive, kFinished };
 // 256 some 2; hence kMostRanked.
 template <class T, int kBlock, int kHeld, bool kSmall>
 __global__ __launch_bounds__(kBlock) void group_kernel(BeamArgs a) {
-  __shared__ double base[kMostWidth];  // of a beam: what is added to logit / temperature, or its score
+  // Of a beam: its greatest logit, and what is added to (logit - greatest) / temperature,
+  // or its score.
+  __shared__ float greatest[kMostWidth];
+  __shared__ double base[kMostWidth];
   __shared__ int state[kMostWidth], best_rank[kMostWidth], free_slots[kMostWidth];
   __shared__ int counts[2][kBlock / kWave];
   __shared__ uint32_t bounds[3][kBlock / kWave];
@@ -444,7 +447,7 @@ __global__ __launch_bounds__(kBlock) void group_kernel(BeamArgs a) {
     }
   }
 
-  // Every beam's base: score - log of the sum of powers.
+  // Every beam's greatest logit, and its base: score - log of the sum of powers.
   const int per_row = kSmall ? a.cols : a.strips;
   int lanes = 1;
   while (lanes < per_row && lanes < kWave) lanes *= 2;
@@ -481,8 +484,8 @@ __global__ __launch_bounds__(kBlock) void group_kernel(BeamArgs a) {
       const bool there = fabsf(score) < INFINITY;
       const bool ok = sum > 0.f && sum < INFINITY && fabsf(most) < INFINITY;
       state[b] = !there ? kNone : done ? kFinished : ok ? kLive : kNone;
-      base[b] = done ? double(score)
-                     : double(score) - double(most) * a.per_temperature - log(double(sum));
+      greatest[b] = most;
+      base[b] = done ? double(score) : double(score) - log(double(sum));
     }
   }
   if (t < kMostWidth) best_rank[t] = kMostWidth;
@@ -496,7 +499,9 @@ __global__ __launch_bounds__(kBlock) void group_kernel(BeamArgs a) {
     const int c = i * kBlock + t, b = min(beam_of(c), a.beams - 1);
     const int is = state[b];
     const bool alone = is == kFinished;
-    double s = base[b] + (alone ? 0. : double(x[i]) * a.per_temperature);
+    // The greatest is taken away first: added to it, what is far below (a score beside a
+    // row of a type's lowest number) would be lost.
+    const double s = base[b] + (alone ? 0. : (double(x[i]) - double(greatest[b])) * a.per_temperature);
     const bool on = c < n && (alone ? c == b * each : is == kLive) && s > -INFINITY && s < INFINITY;
     score[i] = on ? order_of(s) : 0;
     place[i] = on ? uint32_t(b) << kTokenBits | (alone ? 0u : token[i]) : ~0u;

@@ -1,0 +1,112 @@
+"""The operators that serve many answers to one prompt, at the ends of their
+ranges: logits far from zero, what is no number beside what is."""
+import math
+import os
+import sys
+
+import pytest
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
+from answers64 import beam_results  # noqa: E402
+from policy64 import F, close, f32  # noqa: E402
+
+import paper_2607_22242_amd as S  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def randn(g, *shape, dtype=torch.float32):
+    return torch.randn(shape, generator=g).to(dtype)
+
+
+# --- beams far from zero ---------------------------------------------------------
+
+
+def candidates(logits, scores, beams, temperature):
+    """Per group a list of (score, beam, token), best first, equal ones by beam and
+    token.  A row's greatest logit is taken away first, so that what all logits of a
+    row have in common never meets the score; a greatest logit that is not finite
+    leaves no candidate."""
+    groups = [[] for _ in range(logits.shape[0] // beams)]
+    for i, row in enumerate(logits.double()):
+        start, most = float(scores[i]), float(row.max())
+        if not math.isfinite(start) or not math.isfinite(most):
+            continue
+        z = (row - most) / f32(temperature)
+        base = start - math.log(float(torch.exp(z).sum()))
+        groups[i // beams] += [(base + x, i % beams, t) for t, x in enumerate(z.tolist()) if x > -math.inf]
+    for found in groups:
+        found.sort(key=lambda c: (-c[0], c[1], c[2]))
+    return groups
+
+
+def check_far_beams(logits, scores, beams, width, temperature, stay=False):
+    groups = candidates(logits, scores, beams, temperature)
+    for found in groups:
+        # Beams that 64-bit scores tell apart by a lot, whatever the sums' errors.
+        for a, b in zip(found[:width], found[1:width + 1]):
+            assert a[1] == b[1] or a[0] == b[0] or a[0] - b[0] > 1e-4 + 1e-12 * abs(a[0]), "input"
+    want = beam_results(groups, beams, width, stay)
+    got = S.sched_beam_select(logits.cuda(), scores.cuda(), beams, width, temperature=temperature, stay=stay)
+    assert torch.equal(got[1].cpu().long(), want[1]), "parents"
+    assert torch.equal(got[2].cpu(), want[2]), "tokens"
+    # A power with exponent -a is off by 2^-24 (2 a + 2) of itself, and the powers' sum
+    # of a's by less than log2(n) of theirs; a lane adds n / 64 of them and the
+    # reference moves; the result is rounded.  Nothing grows with what a row's logits
+    # have in common.
+    n = logits.shape[1]
+    close(got[0], want[0], F * (16 * math.log2(n + 1) + n / 64 + 64 + want[0].nan_to_num(0, 0, 0).abs()), "scores")
+
+
+FAR_ROWS = [3, 256, 700, 5003]  # a group's own reading of logits, and strips of rows
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("vocab", FAR_ROWS)
+def test_beams_of_the_lowest_logits(dtype, vocab):
+    """A row whose tokens are all masked with the type's lowest number has equal
+    log-probabilities, not the best ones."""
+    beams = 4
+    logits = (randn(gen(vocab), 2 * beams, vocab) * 2).to(dtype)
+    scores = torch.linspace(-4, -4.5, 2 * beams)
+    logits[1] = torch.finfo(dtype).min       # among ordinary beams
+    logits[beams:] = torch.finfo(dtype).min  # a group of such rows
+    logits[beams + 2, vocab // 2] = 1.0      # and one with a single token left
+    for stay in (False, True):
+        check_far_beams(logits, scores, beams, beams, 1.0, stay)
+
+
+@pytest.mark.parametrize("dtype,offset", [(torch.float32, 1e20), (torch.float32, -1e20), (torch.float32, 3e38),
+                                          (torch.bfloat16, 1e20), (torch.bfloat16, -3e38), (torch.float16, 6e4)])
+@pytest.mark.parametrize("vocab", FAR_ROWS)
+def test_beams_of_rows_with_an_offset(dtype, offset, vocab):
+    """Logits whose steps, at that distance from zero, are far more than 1, and one value
+    all over: scores are what the beams had, less the logarithm of how many there are."""
+    g = gen(vocab + 1)
+    beams = 5
+    logits = torch.full((beams, vocab), offset).to(dtype)
+    logits[0] = randn(g, vocab).to(dtype)
+    up = torch.rand((2, vocab), generator=g) < 0.3  # a step or two above it
+    logits[2:4] = torch.where(up, logits[2:4] * (1 + 4 * torch.finfo(dtype).eps), logits[2:4]).to(dtype)
+    logits[2:4][torch.isinf(logits[2:4])] = offset
+    scores = torch.tensor([-6.0, -5.0, -4.5, -5.7, -3.9])
+    check_far_beams(logits, scores, beams, beams, 1.0)
+    check_far_beams(logits, scores, beams, beams, 0.7, stay=True)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("temperature", [1e-12, 1e-20, 1e-30])
+@pytest.mark.parametrize("vocab", FAR_ROWS)
+def test_beams_at_the_lowest_temperatures(dtype, temperature, vocab):
+    """Every beam's best token goes on with the score that the beam had."""
+    beams = 6
+    logits = randn(gen(vocab + 2), beams, vocab).to(dtype)
+    logits[:, vocab // 3] = torch.arange(beams).to(dtype) + 8
+    scores = torch.tensor([-6.0, -5.0, -4.5, -5.7, -3.9, -4.1])
+    check_far_beams(logits, scores, beams, beams, temperature)
+    check_far_beams(logits, scores, beams, beams, temperature, stay=True)
