@@ -278,8 +278,9 @@ struct RowSweep {
       for (int i = 0; i < D / 16; ++i) y = product(vs.along(32 * t, i), o[i], y);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const float s = sees(j0 + 32 * t + c_row(i)) ? x[i] : -INFINITY;
-        sum += pow2(__builtin_fmaf(s, c, -lse2)) * y[i];
+        // What is not seen may be no number, times a power of 0 too.
+        const float d = pow2(__builtin_fmaf(x[i], c, -lse2)) * y[i];
+        sum += sees(j0 + 32 * t + c_row(i)) ? d : 0.f;
       }
     }
     return sum;

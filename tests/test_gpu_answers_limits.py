@@ -8,8 +8,9 @@ import pytest
 import torch
 
 sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
-from answers64 import beam_results  # noqa: E402
+from answers64 import Shared, beam_results  # noqa: E402
 from policy64 import F, close, f32  # noqa: E402
+from test_gpu_answers import check_shared, i32, offsets  # noqa: E402
 
 import paper_2607_22242_amd as S  # noqa: E402
 
@@ -110,3 +111,52 @@ def test_beams_at_the_lowest_temperatures(dtype, temperature, vocab):
     scores = torch.tensor([-6.0, -5.0, -4.5, -5.7, -3.9, -4.1])
     check_far_beams(logits, scores, beams, beams, temperature)
     check_far_beams(logits, scores, beams, beams, temperature, stay=True)
+
+
+# --- shared prefixes of very unequal lengths -----------------------------------------
+
+HALVES = [torch.float16, torch.bfloat16]
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("prefixes", [[4000, 10], [3000, 0], [10, 5000]])
+def test_short_answers_behind_unequal_prefixes(dtype, prefixes):
+    """Blocks share the long prefix' keys, and the other group's rows see a tile of
+    keys at most."""
+    check_shared(gen(prefixes[0]), dtype, 4, 2, 64, prefixes, [4, 4], [10, 9, 12, 10, 10, 1, 10, 8])
+    check_shared(gen(prefixes[1]), dtype, 4, 2, 128, prefixes, [4, 4], [10] * 8, [10, 40, 0, 9, 10, 7, 30, 10],
+                 slots=[40] * 8, p_slots=[5000, 5000])
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("prefixes", [[4000, 10], [0, 4000]])
+def test_what_is_no_number_stays_in_its_sequence_where_blocks_share_prefixes(dtype, bad, prefixes):
+    """Each of the blocks that share a group's prefix forms its rows' delta for itself."""
+    g = gen(39)
+    queries, hq, hk, dim = [10, 9, 12, 10, 10, 4, 10, 8], 4, 2, 64
+    off, p_off, groups = offsets(queries), offsets(prefixes), [0, 4, 8]
+    short = 4 if prefixes[0] > prefixes[1] else 0  # the first sequence of the short prefix
+    x = [randn(g, off[-1], h, dim, dtype=dtype) for h in (hq, hk, hk, hq)]
+    pre = [randn(g, p_off[-1], hk, dim, dtype=dtype) for _ in range(2)]
+    where = [i32(t) for t in (off, off, p_off, groups)]
+    want = Shared(*x[:3], *pre, off, off, p_off, groups, None, None, True, 0.125, x[3])
+    there = torch.arange(p_off[-1])
+    for spoiled in (short + 2, (short + 5) % 8):  # of either group
+        keep = torch.ones(off[-1], dtype=torch.bool)
+        keep[off[spoiled]:off[spoiled + 1]] = False
+        its = 0 if spoiled < 4 else 1
+        others = (there < p_off[its]) | (there >= p_off[its + 1])
+        for i in range(4):
+            y = [t.clone() for t in x]
+            y[i][off[spoiled] + 3, 0, 3] = bad
+            q, k, v, pk, pv, do = (t.cuda() for t in (*y[:3], *pre, y[3]))
+            out, lse = S.sched_shared_attention(q, k, v, pk, pv, *where)
+            got = out, lse.t(), *S.sched_shared_attention_grad(q, k, v, pk, pv, out, lse, do, *where)
+            for a, name in zip(got, ("out", "lse", "dq", "dk", "dv")):
+                b, bound = getattr(want, name), getattr(want, name + "_b")
+                b, bound = (t.t() if name == "lse" else t for t in (b, bound))
+                close(a[keep.cuda()], b[keep], bound[keep], (spoiled, i, name))
+            for a, name in zip(got[5:], ("dpk", "dpv")):  # the other group's prefix
+                close(a[others.cuda()], getattr(want, name)[others], getattr(want, name + "_b")[others],
+                      (spoiled, i, name))
