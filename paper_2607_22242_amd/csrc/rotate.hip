@@ -124,8 +124,10 @@ __device__ __forceinline__ void turn(const RotateArgs& a, const float* cos, cons
     for (int e = 0; e < 4; ++e) {
       const float c = cos[j + e], s = kBack ? -sin[j + e] : sin[j + e];
       const float u = x[2 * e], v = x[2 * e + 1];
-      x[2 * e] = u * c - v * s;
-      x[2 * e + 1] = u * s + v * c;
+      if (j + e < a.pairs) {  // by no angle a neighbour's infinity would still come in
+        x[2 * e] = u * c - v * s;
+        x[2 * e + 1] = u * s + v * c;
+      }
     }
   } else if (kPairs == kLanes) {
     const int apart = a.pairs / 8;

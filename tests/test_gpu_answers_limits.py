@@ -160,3 +160,34 @@ def test_what_is_no_number_stays_in_its_sequence_where_blocks_share_prefixes(dty
             for a, name in zip(got[5:], ("dpk", "dpv")):  # the other group's prefix
                 close(a[others.cuda()], getattr(want, name)[others], getattr(want, name + "_b")[others],
                       (spoiled, i, name))
+
+
+# --- elements that are not turned -----------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("interleaved,dim,turned", [(True, 16, 6), (True, 64, 2), (True, 128, 64), (False, 64, 32),
+                                                    (False, 40, 20), (True, 24, 0)])
+def test_elements_that_are_not_turned_stay(dtype, interleaved, dim, turned):
+    """Whatever their neighbours hold, infinities and NaN among them; what is turned
+    does not meet them."""
+    g = gen(dim + turned)
+    x, pos = randn(g, 11, 5, dim, dtype=dtype), torch.arange(11).cuda()
+    freq = torch.rand(turned // 2, generator=g).cuda() if turned else None
+    how = dict(norm=False, interleaved=interleaved)
+    odd = x.clone()
+    for i, e in enumerate(range(turned, dim, 3)):
+        odd[i % 11, i % 5, e] = (math.inf, -math.inf, math.nan)[i % 3]
+
+    def run(t):
+        t = t.cuda()
+        forward = S.sched_norm_rotate(t[:, :3], t[:, 3:], pos, freq, **how)
+        back = S.sched_norm_rotate_grad(t[:, :3], t[:, 3:], t[:, :3], t[:, 3:], pos, freq, **how)[:2]
+        return [torch.cat(y, 1).cpu() for y in (forward, back)]
+
+    for a, b in zip(run(x), run(odd)):
+        assert torch.equal(a[..., :turned], b[..., :turned])
+        for got, want in ((a, x), (b, odd)):
+            got, want = got[..., turned:].float(), want[..., turned:].float()
+            assert torch.equal(torch.isnan(got), torch.isnan(want))
+            assert torch.equal(torch.nan_to_num(got, 7.0), torch.nan_to_num(want, 7.0))
