@@ -378,7 +378,9 @@ int sched_norm_rotate(const sched_norm_rotate_desc* d, void* hip_stream) {
     if (int e = check_heads(d->v_out, d->out_rows, heads, dim, true)) return e;
   }
   // In place is the same rows and heads; a row that goes to another's place is not.
-  if (!in_step(d->q, d->q_out) || !in_step(d->k, d->k_out) || (values && !in_step(d->v, d->v_out)))
+  // Without rows tensors have no memory, and one address.
+  if (d->rows > 0 && (!in_step(d->q, d->q_out) || !in_step(d->k, d->k_out) ||
+                      (values && !in_step(d->v, d->v_out))))
     return SCHED_E_VALUE;
   if (placed && d->rows > 0 &&
       (d->k.data == d->k_out.data || (values && d->v.data == d->v_out.data)))
@@ -405,9 +407,9 @@ int sched_norm_rotate_grad(const sched_norm_rotate_desc* d, const sched_heads* d
   if (int e = check_heads(*d_q, d->rows, d->q_heads, dim, true)) return e;
   if (int e = check_heads(*d_k, d->rows, d->kv_heads, dim, true)) return e;
   if (!d->norm && (d_q_weight || d_k_weight)) return SCHED_E_VALUE;
-  if (!in_step(*d_q, d->q) || !in_step(*d_q, *d_q_out) || !in_step(*d_k, d->k) ||
-      !in_step(*d_k, *d_k_out) ||
-      (d->places.data && d->rows > 0 && d_k->data == d_k_out->data))
+  if (d->rows > 0 &&
+      (!in_step(*d_q, d->q) || !in_step(*d_q, *d_q_out) || !in_step(*d_k, d->k) ||
+       !in_step(*d_k, *d_k_out) || (d->places.data && d_k->data == d_k_out->data)))
     return SCHED_E_VALUE;
   if (d_q_weight || d_k_weight)
     if (int e = check_workspace(d_workspace, ws_bytes, norm_rotate_grad_bytes(*d))) return e;

@@ -248,3 +248,18 @@ def test_values_packed_at_once_are_the_structure(kind):
 
     whole = fill(kind)
     assert P._packer(kind)(*values) == bytes(whole)
+
+
+def test_norm_rotate_of_no_rows(lib):
+    """Equal addresses, of tensors without memory among them, are the same memory
+    only where there are rows in it."""
+    for data in (0, FAKE):
+        at = dict(rows=0, out_rows=0, positions=tokens(0, data=0), q=heads(data, 256), k=heads(data, 256),
+                  v=heads(data, 256), q_out=heads(data), k_out=heads(data, 64), v_out=heads(data, 64))
+        grads = [heads(data), heads(data, 64), heads(data, 512), heads(data, 192)]
+        assert lib.sched_norm_rotate(R(rotate(**at)), 0) == 0
+        assert lib.sched_norm_rotate_grad(R(rotate(**at)), *map(R, grads), 0, 0, 0, 0, 0) == 0
+        if data:  # no row goes to a place of a cache
+            at.update(places=tokens(0), out_rows=9)
+            assert lib.sched_norm_rotate(R(rotate(**at)), 0) == 0
+            assert lib.sched_norm_rotate_grad(R(rotate(**at)), *map(R, grads), 0, 0, 0, 0, 0) == 0

@@ -191,3 +191,31 @@ def test_elements_that_are_not_turned_stay(dtype, interleaved, dim, turned):
             got, want = got[..., turned:].float(), want[..., turned:].float()
             assert torch.equal(torch.isnan(got), torch.isnan(want))
             assert torch.equal(torch.nan_to_num(got, 7.0), torch.nan_to_num(want, 7.0))
+
+
+# --- batches without rows -------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_no_rows_of_a_joint_projection(dtype):
+    """Slices of a projection of no rows, with results of their own: tensors without
+    memory are not the same memory."""
+    hq, hk, dim = 4, 2, 32
+    x = torch.empty((0, hq + 2 * hk, dim), dtype=dtype, device="cuda")
+    q, k, v = x[:, :hq], x[:, hq:hq + hk], x[:, hq + hk:]
+    p, f = torch.empty(0, dtype=torch.int64, device="cuda"), torch.ones(dim // 2, device="cuda")
+    w = torch.ones(dim, device="cuda")
+    for t in S.sched_norm_rotate(q, k, p, f, w, w, v=v):
+        assert t.shape[0] == 0 and t.dtype == dtype
+    out = torch.empty_like(x)
+    S.sched_norm_rotate(q, k, p, f, w, w, v=v, q_out=out[:, :hq], k_out=out[:, hq:hq + hk], v_out=out[:, hq + hk:])
+    cache = torch.ones((2, 4, hk, dim), dtype=dtype, device="cuda")
+    S.sched_norm_rotate(q, k, p, f, w, w, v=v, places=p, k_out=cache[0], v_out=cache[1])
+    assert bool((cache == 1).all())
+    d_q, d_k = (torch.empty((0, h, dim), dtype=dtype, device="cuda") for h in (hq, hk))
+    for places, d_k_out in ((None, d_k), (p, cache[0])):
+        got = S.sched_norm_rotate_grad(q, k, d_q, d_k_out, p, f, w, w, places=places)
+        assert got[0].shape == (0, hq, dim) and got[1].shape == (0, hk, dim)
+        assert not bool(got[2].any()) and not bool(got[3].any())
+    d = torch.empty_like(x)
+    S.sched_norm_rotate_grad(q, k, d_q, d_k, p, f, d_q=d[:, :hq], d_k=d[:, hq:hq + hk])
