@@ -255,7 +255,8 @@ int sched_shared_attention_grad(const sched_shared_desc *desc, const sched_share
  * values.  q_out may be q itself, and without places k_out k itself; outputs
  * overlap no input otherwise.  head_dim: a multiple of 8 up to 256.  turned:
  * even, up to head_dim (0: norms alone).  Weights are 32-bit (null: ones; with
- * norm = 0 they have to be).  eps >= 0. */
+ * norm = 0 they have to be).  eps >= 0.  Squares are added up in 32 bits, which
+ * elements of up to 10^18 in magnitude stay within. */
 typedef struct {
     sched_heads q, k, v;             /* rows x q_heads (kv_heads) x head_dim */
     sched_heads q_out, k_out, v_out; /* q_out has `rows` rows, the others out_rows */
@@ -297,7 +298,8 @@ int sched_norm_rotate_grad(const sched_norm_rotate_desc *desc, const sched_heads
  * few states move: a beam's best continuation keeps the beam's slot, the others,
  * best first, take the slots that are left, from the lowest.  A result has its
  * new score, its parent's row and its token; where there are fewer candidates
- * than `width` the others' scores are -inf and parents and tokens -1.
+ * than `width` the others' scores are -inf and parents and tokens -1.  (A score
+ * below what 32 bits hold becomes -inf, too, and keeps its parent and token.)
  * Where width = beams new_scores may be scores and tokens last.data (of one
  * width of tokens); outputs overlap no input otherwise.
  * beams and width: 1 to 128.  logits: up to 2^22 columns.  temperature as above. */

@@ -116,7 +116,7 @@ struct UpTo {
 struct Split {
   float* sums;     // a part: D of a row's sums and, behind all of them,
   float* weights;  // reference (to the base 2) and sum of powers
-  int parts;       // of a row: two per split
+  int parts;       // of a row
 };
 __device__ __forceinline__ int64_t part_of(const AttendArgs& a, const Split& p, int64_t row,
                                            int head, int part) {

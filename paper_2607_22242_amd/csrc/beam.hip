@@ -7,7 +7,7 @@
 // the strips' best their scores and takes the best of those.  Bound by the
 // logits' bytes where rows are long, and by what waits for one another in a
 // group's block where they are short.  16 groups of 16 beams, 131,072 logits in
-// bfloat16: strips 29 us (67 MB, 2.3 TB/s: 16 vector operations a logit, 5 of them
+// bfloat16: strips 31 us (67 MB, 2.2 TB/s: 16 vector operations a logit, 5 of them
 // for its power), groups 13.  Sums of powers are held in 32 bits, relative to the
 // largest logit met; scores are formed in 64, as a score that has been added up
 // over many tokens is no finer than 2^-24 of itself in 32.
@@ -707,7 +707,7 @@ Plan plan_of(const sched_beam_desc& d) {
   p.small = cols <= 4 * kWave && cols * d.beams <= 4096;
   const int64_t chunks = (cols + kChunk - 1) / kChunk;
   // Some 4096 waves, as far as rows are long enough (256 rows of 131,072, with the groups'
-  // blocks: 47 us; 2,048 waves 49, 8,192 58).
+  // blocks: 2,048 waves take 4 % longer, 8,192 23 %).
   const int64_t want = std::min<int64_t>(
       {std::max<int64_t>(1, 4096 / std::max<int64_t>(rows, 1)), chunks, int64_t(kMostStrips)});
   p.strip_chunks = int((chunks + want - 1) / want);
@@ -779,7 +779,7 @@ constexpr int kStateHeld = 16;  // units that a thread moves at once
 // A block moves some places (units of 16 bytes or less) of all slots of a group:
 // it reads every slot that is followed before it writes any, so that slots may
 // follow one another in a circle without a second copy of the states.  Bound by the
-// moved rows' bytes, read and written once (139 MB of 256 slots' states: 53 us, 5.2
+// moved rows' bytes, read and written once (141 MB of 256 slots' states: 55 us, 5.1
 // TB/s; 16 to a thread, all under way at once).
 template <class U>
 __global__ __launch_bounds__(kThreads) void reorder_kernel(StateArgs a, int64_t chunk0) {

@@ -4,7 +4,7 @@
 // R(-p f) dy: dw = sum g o (r x), u = g o w, dx = r (u - (r x) mean(u o (r x))).
 // Some 8 and 16 operations per element in and out: bound by memory.  65,536 tokens
 // of 32 and 8 heads of 128 in bfloat16: forward 270 us (1.34 GB, 5.0 TB/s), backward
-// 475 (2.01 GB, 4.2 TB/s; a copy reaches 4.9).
+// 470 (2.01 GB, 4.3 TB/s; a copy reaches 4.9).
 //
 // A head is held by a power of two of lanes, eight elements each, so that its sums
 // are a few shuffles.  A block takes some rows: it forms their cosines and sines
@@ -172,7 +172,7 @@ __device__ __forceinline__ void weights_of(const float* w, int piece, bool on, E
 
 // The lane groups take the heads of the block's rows in turn, one at a time: the units'
 // many waves keep enough of them on their way (65,536 tokens of 32 and 8 heads of 128:
-// 1.34 GB in 282 us; two heads at once 296, four 312, eight 345).
+// two heads at once take 5 % longer, four 11 %, eight 22 %).
 template <class T, int kPairs, int kGroup>
 __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a) {
   constexpr int kGroups = kThreads / kGroup;
@@ -344,13 +344,13 @@ __global__ __launch_bounds__(1024) void add_weights_kernel(const float* parts, i
 }
 
 // Rows of a block: enough blocks for the card first (forward and backward of 1,001
-// tokens: 25.6 us with one row, 32.6 with four), then as many as share the angles (65,536
-// tokens: 705 us with eight rows, 709 with four, 746 with two, 887 with one).
+// tokens: four rows take 27 % longer than one), then as many as share the angles (65,536
+// tokens: four rows take 1 % longer than eight, two 6 %, one 26 %).
 int rows_of_block(int64_t rows) {
   return int(std::min<int64_t>(kMostRows, std::max<int64_t>(1, rows / 1024)));
 }
-// Blocks of the backward pass (65,536 tokens, both passes: 705 us with 1,024, 860 with
-// 512, 708 with 2,048).
+// Blocks of the backward pass (65,536 tokens, both passes: 512 take 22 % longer than
+// 1,024, 2,048 as long).
 int grad_blocks(int64_t rows) {
   const int64_t chunks = (rows + rows_of_block(rows) - 1) / rows_of_block(rows);
   return int(std::min<int64_t>(chunks, 1024));

@@ -7,7 +7,7 @@
 // over both kinds of keys, so that a prefix key is read once for 128 rows: bound by
 // matrix instructions and the exponentials between them, at the clock that the card's
 // power leaves (16 answers of 512 tokens to a prompt of 8,192, 32 heads of 128, bf16:
-// 1,130 us, 1,003 TFLOP/s; halving what is read from LDS would save 5 % of it).  With
+// 1,119 us, 1,013 TFLOP/s; halving what is read from LDS would save 5 % of it).  With
 // few the keys are shared by blocks: bound by the bytes of the keys and values.
 #include <hip/hip_runtime.h>
 

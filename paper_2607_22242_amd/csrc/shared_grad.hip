@@ -8,7 +8,7 @@
 // one holds keys, of either kind, and walks over the rows (dK, dV): no atomics,
 // every sum has one order, for 14 D operations a pair in place of the 10 D of one
 // kernel.  Bound as the forward pass: 16 answers of 512 tokens to a prompt of 8,192,
-// 32 heads of 128, bf16: dQ 1,511 us (1,125 TFLOP/s), dK and dV 2,267 (1,000).
+// 32 heads of 128, bf16: dQ 1,490 us (1,141 TFLOP/s), dK and dV 2,232 (1,016).
 // Probabilities and dS are rounded to 16 bits for their products, all else is held in
 // 32: errors are 1.4 to 1.5 times those of rounding the results alone, or, with second
 // products (kFine), 1.0 to 1.15 times.
