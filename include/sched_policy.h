@@ -299,7 +299,9 @@ int sched_norm_rotate_grad(const sched_norm_rotate_desc *desc, const sched_heads
  * best first, take the slots that are left, from the lowest.  A result has its
  * new score, its parent's row and its token; where there are fewer candidates
  * than `width` the others' scores are -inf and parents and tokens -1.  (A score
- * below what 32 bits hold becomes -inf, too, and keeps its parent and token.)
+ * below what 32 bits hold becomes -inf, too, and keeps its parent and token.  Of a
+ * beam's tokens that 64 bits do not tell apart, as at temperatures from 1e15 on,
+ * which ones are taken may go by their logits.)
  * Where width = beams new_scores may be scores and tokens last.data (of one
  * width of tokens); outputs overlap no input otherwise.
  * beams and width: 1 to 128.  logits: up to 2^22 columns.  temperature as above. */
